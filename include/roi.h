@@ -279,6 +279,90 @@ int roi_cat_mask_bwd(const uint16_t* grad_W_masked, const uint16_t* W, const flo
                      hipStream_t stream);
 
 /*
+ * The linear layer around a masked weight, in 8 bits.  Rows of activations
+ * (or of weights) are held as int8 with one fp32 scale each: the tokens' rows
+ * are the left operand of the layer's product and, kept until the backward,
+ * the checkpoint its weight gradient reads; the weights' rows are those of a
+ * masked weight (roi_mask_fwd, roi_mask_export), dense or 2:4-compressed.
+ *
+ * Conventions beside the shared ones above:
+ *  - x [tokens, cols], weight [rows, cols], y [tokens, rows]; any sizes >= 0
+ *    with rows and cols below 2^22 and tokens below 2^31.  Rows of a length
+ *    that is no multiple of 16 bytes are read by slower loads.
+ *  - An empty tensor's pointer may be NULL.  A sum over nothing is 0.
+ *  - workspace: device memory of at least the bytes that the matching
+ *    *_workspace call returns (it may be NULL where that is 0), 16-byte
+ *    aligned, overlapping nothing; its contents need no preparation and are
+ *    undefined afterwards.  Calls that may run at the same time need one each.
+ *  - Results do not depend on the order in which blocks run: the same inputs
+ *    give the same bits.
+ */
+typedef enum { ROI_BF16 = 0, ROI_FP32 = 1 } roi_dtype;
+
+/*
+ * roi_quantize_rows -- symmetric int8 rows with one scale each, by a fixed
+ * sequence of IEEE fp32 operations, so that the integers are reproducible:
+ *   amax = max_c |x[c]|, scale = max(fl(amax / 127), 2^-126),
+ *   inv  = fl(127 fl(1 / amax)), or 2^126 where scale is 2^-126,
+ *   q[c] = rint(fl(x[c] inv))            (ties to even; -127 .. 127).
+ * A row of zeros gets q = 0.  A row that holds a NaN or an infinity gets
+ * q = 0 and scale = NaN, so that everything computed from that row is NaN.
+ *  x     bf16 or fp32 [rows, cols] (read; dtype says which)
+ *  q     int8 [rows, cols]         (written)
+ *  scale fp32 [rows]               (written)
+ * rows and cols here are those of x (below 2^31).
+ */
+int roi_quantize_rows(const void* x, int dtype, int64_t rows, int64_t cols, int8_t* q,
+                      float* scale, hipStream_t stream);
+/*
+ * roi_dequantize_rows -- x[r, c] = q[r, c] scale[r], one fp32 product, rounded
+ * to nearest where x is bf16.  Arguments as above, q and scale read, x written.
+ */
+int roi_dequantize_rows(const int8_t* q, const float* scale, int64_t rows, int64_t cols, void* x,
+                        int dtype, hipStream_t stream);
+
+/*
+ * roi_linear_i8 -- y[t, r] = xs[t] ws[r] sum_c xq[t, c] wq[r, c] (+ bias[r]).
+ * The sum is exact in int32 (cols <= 131071, so that no int8 values can
+ * overflow it); then fl(fl(sum ws) xs), the bias added, in fp32, and one
+ * rounding to y's type.
+ *  xq    int8 [tokens, cols], xs fp32 [tokens]  (roi_quantize_rows)
+ *  wq    int8 [rows, cols], or with meta int8 [rows, cols / 2]: the two kept
+ *        values of every group of four in increasing index order (the rows of
+ *        roi_mask_export's values at 2:4, quantized)
+ *  meta  NULL, or roi_mask_export's 2:4 metadata uint32 [rows * cols / 32];
+ *        needs cols % 32 == 0 (a row's words are its own)
+ *  ws    fp32 [rows]
+ *  bias  bf16 [rows] or NULL
+ *  y     bf16 or fp32 [tokens, rows] (written; dtype says which)
+ */
+int64_t roi_linear_i8_workspace(int64_t tokens, int64_t rows, int64_t cols, int packed);
+int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uint32_t* meta,
+                  const float* ws, const uint16_t* bias, int64_t tokens, int64_t rows,
+                  int64_t cols, void* y, int dtype, void* workspace, int64_t workspace_bytes,
+                  hipStream_t stream);
+
+/*
+ * The gradients of that product, straight through its rounding.
+ * roi_linear_i8_grad_weight: grad_w[r, c] = sum_t grad_y[t, r] xs[t] xq[t, c],
+ * the dL/dW_masked that roi_mask_bwd takes, from the checkpoint (xq, xs).
+ * roi_linear_i8_grad_input:  grad_x[t, c] = sum_r grad_y[t, r] ws[r] wq[r, c]
+ * (wq dense).  The scaled int8 operand is rounded once to bf16 (the type of
+ * the other operand and of the result, and what the bf16 matrix cores take);
+ * products and sums are fp32, and the result is rounded to bf16.
+ *  grad_y bf16 [tokens, rows] (read)
+ *  grad_w bf16 [rows, cols], grad_x bf16 [tokens, cols] (overwritten)
+ */
+int64_t roi_linear_i8_grad_weight_workspace(int64_t tokens, int64_t rows, int64_t cols);
+int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* xq, const float* xs,
+                              int64_t tokens, int64_t rows, int64_t cols, uint16_t* grad_w,
+                              void* workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t roi_linear_i8_grad_input_workspace(int64_t tokens, int64_t rows, int64_t cols);
+int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq, const float* ws,
+                             int64_t tokens, int64_t rows, int64_t cols, uint16_t* grad_x,
+                             void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/*
  * roi_gumbel_noise -- the noise of `count` consecutive elements starting at
  * global index elem_offset (elem_offset % 4 == 0): the raw Philox words
  * and/or g = -L(-L(u)) (Algorithm 1).  Either output may be NULL, not both.

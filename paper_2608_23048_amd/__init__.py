@@ -110,6 +110,20 @@ def lib() -> ctypes.CDLL:
         L.roi_fast_noise_from_words.restype = _int
         L.roi_stream_copy.argtypes = [_vp, _vp, _i64, _vp]
         L.roi_stream_copy.restype = _int
+        L.roi_quantize_rows.argtypes = [_vp, _int, _i64, _i64, _vp, _vp, _vp]
+        L.roi_quantize_rows.restype = _int
+        L.roi_dequantize_rows.argtypes = [_vp, _vp, _i64, _i64, _vp, _int, _vp]
+        L.roi_dequantize_rows.restype = _int
+        L.roi_linear_i8_workspace.argtypes = [_i64, _i64, _i64, _int]
+        L.roi_linear_i8_workspace.restype = _i64
+        L.roi_linear_i8.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _int,
+                                    _vp, _i64, _vp]
+        L.roi_linear_i8.restype = _int
+        for name in ("roi_linear_i8_grad_weight", "roi_linear_i8_grad_input"):
+            getattr(L, name + "_workspace").argtypes = [_i64, _i64, _i64]
+            getattr(L, name + "_workspace").restype = _i64
+            getattr(L, name).argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp]
+            getattr(L, name).restype = _int
         L.roi_anneal.argtypes = [_f32, _f32, _i64, _i64]
         L.roi_anneal.restype = _f32
         L.roi_status_string.argtypes = [_int]
@@ -431,6 +445,189 @@ def mask_bwd_grouped(tensors, n: int, m: int, tau: float = 1.0, lam: float = 1.0
     _raise_on(lib().roi_mask_bwd_grouped(ctypes.addressof(arr), len(outs), n, m, tau, lam, seed,
                                          step, stream))
     return outs
+
+
+# ------------------------------------------- the 8-bit linear layer around a mask
+ROI_BF16, ROI_FP32 = 0, 1
+
+
+def _dtype_code(dtype, name="dtype"):
+    torch = _torch
+    if dtype is torch.bfloat16:
+        return ROI_BF16
+    if dtype is torch.float32:
+        return ROI_FP32
+    raise TypeError(f"{name} must be torch.bfloat16 or torch.float32, got {dtype}")
+
+
+def _check_sized(t, dtype, name, shape, device):
+    """_check_tensor, and the shape and the device that the other arguments imply."""
+    _check_tensor(t, dtype, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _call(t, fn, *args):
+    """fn(*args, stream) on t's device and its current stream."""
+    torch, index = _torch, t.get_device()
+    if index == torch.cuda.current_device():
+        _raise_on(fn(*args, _stream(t)))
+    else:
+        with torch.cuda.device(index):
+            _raise_on(fn(*args, _stream(t)))
+
+
+def _workspace(given, need, device):
+    """(pointer, bytes) of a call's workspace; allocated when none is given."""
+    torch = _torch
+    if need < 0:
+        _raise_on(ROI_E_UNSUPPORTED)
+    if given is None:
+        given = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        return given, _ptr(given), need
+    _check_tensor(given, torch.uint8, "workspace")
+    if given.device != device:
+        raise ValueError(f"workspace is on {given.device}, expected {device}")
+    return given, _ptr(given), given.numel()
+
+
+def quantize_rows(x, out=None):
+    """int8 rows with one fp32 scale each: x bf16 or fp32 [rows, cols] (1-D: one
+    row) -> (q int8 like x, scale fp32 [rows]), x ~ q scale[:, None], |q| <= 127.
+    Tokens' rows are linear_i8's operand and the checkpoint its weight gradient
+    reads; weights' rows (of a masked weight, or the 2:4 export's values viewed
+    as [rows, cols / 2]) are its other operand.  A row with a NaN or an infinity
+    gets q = 0 and scale NaN.  ``out``: (q, scale), preallocated."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a torch.Tensor")
+    code = _dtype_code(x.dtype, "x")
+    _check_tensor(x, x.dtype, "x")
+    rows, cols = _shape2d(x)
+    if out is None:
+        q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+        scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    else:
+        q, scale = out
+        _check_sized(q, torch.int8, "q", x.shape, x.device)
+        _check_sized(scale, torch.float32, "scale", (rows,), x.device)
+    _call(x, lib().roi_quantize_rows, _ptr(x), code, rows, cols, _ptr(q), _ptr(scale))
+    return q, scale
+
+
+def dequantize_rows(q, scale, dtype=None, out=None):
+    """x = q scale[:, None] in ``dtype`` (bf16, the default, or fp32): restores
+    quantize_rows' rows where the backward of another operation needs them."""
+    torch = _torch or _load_torch()
+    _check_tensor(q, torch.int8, "q")
+    rows, cols = _shape2d(q)
+    _check_sized(scale, torch.float32, "scale", (rows,), q.device)
+    dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
+    code = _dtype_code(dtype)
+    if out is None:
+        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    else:
+        _check_sized(out, dtype, "out", q.shape, q.device)
+    _call(q, lib().roi_dequantize_rows, _ptr(q), _ptr(scale), rows, cols, _ptr(out), code)
+    return out
+
+
+def linear_i8(xq, xs, wq, ws, meta=None, bias=None, dtype=None, out=None, workspace=None):
+    """y[t, r] = xs[t] ws[r] sum_c xq[t, c] wq[r, c] (+ bias[r]), the sum exact.
+
+    xq int8 [tokens, cols], xs fp32 [tokens]; wq int8 [rows, cols], ws fp32
+    [rows]; or 2:4-compressed: wq int8 [rows, cols / 2] (quantize_rows of
+    mask_export's values as [rows, cols / 2]) with its ``meta``, cols % 32 == 0.
+    bias bf16 [rows].  y [tokens, rows] in ``dtype`` (bf16, the default, or
+    fp32).  ``workspace``: a uint8 tensor of linear_i8_workspace bytes."""
+    torch = _torch or _load_torch()
+    _check_tensor(xq, torch.int8, "xq")
+    _check_tensor(wq, torch.int8, "wq")
+    if xq.dim() != 2 or wq.dim() != 2:
+        raise ValueError("xq and wq must be 2-D")
+    (tokens, cols), rows, dev = xq.shape, wq.shape[0], xq.device
+    _check_sized(xs, torch.float32, "xs", (tokens,), dev)
+    _check_sized(ws, torch.float32, "ws", (rows,), dev)
+    if meta is None:
+        _check_sized(wq, torch.int8, "wq", (rows, cols), dev)
+    else:
+        if cols % 32:
+            raise ValueError(f"2:4 weights need cols % 32 == 0 (got {cols})")
+        _check_sized(wq, torch.int8, "wq", (rows, cols // 2), dev)
+        _check_sized(meta, torch.int32, "meta", (rows * cols // 32,), dev)
+    if bias is not None:
+        _check_sized(bias, torch.bfloat16, "bias", (rows,), dev)
+    dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
+    code = _dtype_code(dtype)
+    if out is None:
+        out = torch.empty((tokens, rows), dtype=dtype, device=dev)
+    else:
+        _check_sized(out, dtype, "out", (tokens, rows), dev)
+    L = lib()
+    _keep, ws_ptr, ws_bytes = _workspace(
+        workspace, L.roi_linear_i8_workspace(tokens, rows, cols, meta is not None), dev)
+    _call(xq, L.roi_linear_i8, _ptr(xq), _ptr(xs), _ptr(wq), _ptr(meta), _ptr(ws), _ptr(bias),
+          tokens, rows, cols, _ptr(out), code, ws_ptr, ws_bytes)
+    return out
+
+
+def linear_i8_workspace(tokens: int, rows: int, cols: int, packed: bool = False) -> int:
+    """Bytes of linear_i8's workspace (packed: 2:4-compressed weights)."""
+    return _workspace_bytes(lib().roi_linear_i8_workspace(tokens, rows, cols, packed))
+
+
+def _workspace_bytes(n):
+    if n < 0:
+        _raise_on(ROI_E_INVAL)
+    return int(n)
+
+
+def _grad_i8(name, grad_y, q, scale, by_tokens, out, workspace):
+    torch = _torch or _load_torch()
+    _check_tensor(grad_y, torch.bfloat16, "grad_y")
+    qname, sname = ("xq", "xs") if by_tokens else ("wq", "ws")
+    _check_tensor(q, torch.int8, qname)
+    if grad_y.dim() != 2 or q.dim() != 2:
+        raise ValueError(f"grad_y and {qname} must be 2-D")
+    (tokens, rows), cols, dev = grad_y.shape, q.shape[1], grad_y.device
+    summed, kept = (tokens, rows) if by_tokens else (rows, tokens)
+    _check_sized(q, torch.int8, qname, (summed, cols), dev)
+    _check_sized(scale, torch.float32, sname, (summed,), dev)
+    if out is None:
+        out = torch.empty((kept, cols), dtype=torch.bfloat16, device=dev)
+    else:
+        _check_sized(out, torch.bfloat16, "out", (kept, cols), dev)
+    L = lib()
+    _keep, ws_ptr, ws_bytes = _workspace(
+        workspace, getattr(L, name + "_workspace")(tokens, rows, cols), dev)
+    _call(grad_y, getattr(L, name), _ptr(grad_y), _ptr(q), _ptr(scale), tokens, rows, cols,
+          _ptr(out), ws_ptr, ws_bytes)
+    return out
+
+
+def linear_i8_grad_weight(grad_y, xq, xs, out=None, workspace=None):
+    """dL/dW (bf16 [rows, cols], mask_bwd's grad_W_masked) of a linear layer from
+    dL/dy (bf16 [tokens, rows]) and the 8-bit checkpoint of its input:
+    sum_t grad_y[t, r] xs[t] xq[t, c]."""
+    return _grad_i8("roi_linear_i8_grad_weight", grad_y, xq, xs, True, out, workspace)
+
+
+def linear_i8_grad_input(grad_y, wq, ws, out=None, workspace=None):
+    """dL/dx (bf16 [tokens, cols]) of a linear layer with int8 weight rows:
+    sum_r grad_y[t, r] ws[r] wq[r, c]."""
+    return _grad_i8("roi_linear_i8_grad_input", grad_y, wq, ws, False, out, workspace)
+
+
+def linear_i8_grad_weight_workspace(tokens: int, rows: int, cols: int) -> int:
+    """Bytes of linear_i8_grad_weight's workspace."""
+    return _workspace_bytes(lib().roi_linear_i8_grad_weight_workspace(tokens, rows, cols))
+
+
+def linear_i8_grad_input_workspace(tokens: int, rows: int, cols: int) -> int:
+    """Bytes of linear_i8_grad_input's workspace."""
+    return _workspace_bytes(lib().roi_linear_i8_grad_input_workspace(tokens, rows, cols))
 
 
 def gumbel_noise(count: int, seed: int = 0, step: int = 0, elem_offset: int = 0, device="cuda",

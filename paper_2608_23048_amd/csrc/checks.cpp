@@ -252,4 +252,134 @@ int validate_cat(bool fwd, const uint16_t* W, const float* alpha, const uint16_t
     return ok();
 }
 
+namespace {
+
+struct Buffer {
+    const void* p;
+    size_t n;
+    bool out;
+};
+
+// Present, aligned, and no output over anything else (an empty buffer's
+// pointer is not looked at).
+int check_buffers(const Buffer* b, int count)
+{
+    for (int i = 0; i < count; ++i) {
+        if (b[i].n == 0) continue;
+        if (!b[i].p) return fail(ROI_E_INVAL, "a required pointer is NULL");
+        if (!aligned16(b[i].p)) return fail(ROI_E_INVAL, "device pointers must be 16-byte aligned");
+    }
+    for (int i = 0; i < count; ++i)
+        for (int j = i + 1; j < count; ++j)
+            if ((b[i].out || b[j].out) && overlap(b[i].p, b[i].n, b[j].p, b[j].n))
+                return fail(ROI_E_INVAL, "an output overlaps another input or output");
+    return ROI_OK;
+}
+
+int check_workspace(const void* workspace, int64_t bytes, int64_t need)
+{
+    if (bytes < 0) return fail(ROI_E_INVAL, "workspace_bytes must be >= 0");
+    if (bytes < need)
+        return fail(ROI_E_INVAL, "the workspace has %lld bytes, %lld are needed", (long long)bytes,
+                    (long long)need);
+    if (need > 0 && !workspace) return fail(ROI_E_INVAL, "the workspace must not be NULL");
+    return ROI_OK;
+}
+
+int check_dtype(int dtype)
+{
+    if (dtype != ROI_BF16 && dtype != ROI_FP32)
+        return fail(ROI_E_INVAL, "dtype must be ROI_BF16 or ROI_FP32 (got %d)", dtype);
+    return ROI_OK;
+}
+
+} // namespace
+
+int validate_rows_i8(const void* x, int dtype, const int8_t* q, const float* scale, int64_t rows,
+                     int64_t cols, bool x_out, bool* todo)
+{
+    *todo = false;
+    if (int st = check_dtype(dtype)) return st;
+    if (rows < 0 || cols < 0)
+        return fail(ROI_E_INVAL, "rows (%lld) and cols (%lld) must be >= 0", (long long)rows,
+                    (long long)cols);
+    if (rows >= kMaxTokens || cols >= kMaxTokens)
+        return fail(ROI_E_UNSUPPORTED, "rows and cols must be below 2^31");
+    const size_t n = (size_t)rows * (size_t)cols; // below 2^62
+    const Buffer b[] = {{x, n * (dtype == ROI_FP32 ? 4 : 2), x_out},
+                        {q, n, !x_out},
+                        {scale, (size_t)rows * 4, !x_out}};
+    if (int st = check_buffers(b, 3)) return st;
+    *todo = x_out ? n > 0 : rows > 0;
+    return ok();
+}
+
+int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols)
+{
+    if (tokens < 0 || rows < 0 || cols < 0)
+        return fail(ROI_E_INVAL, "tokens (%lld), rows (%lld) and cols (%lld) must be >= 0",
+                    (long long)tokens, (long long)rows, (long long)cols);
+    if (tokens >= kMaxTokens || rows >= kMaxLinearDim || cols >= kMaxLinearDim)
+        return fail(ROI_E_UNSUPPORTED, "tokens must be below 2^31, rows and cols below 2^22");
+    return ROI_OK;
+}
+
+Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step)
+{
+    Cut c{};
+    c.tile = 128;
+    c.tm = (m + c.tile - 1) / c.tile;
+    c.tn = (n + c.tile - 1) / c.tile;
+    c.steps = (k + step - 1) / step;
+    c.splits = 1;
+    return c;
+}
+
+int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uint32_t* meta,
+                       const float* ws, const uint16_t* bias, int64_t tokens, int64_t rows,
+                       int64_t cols, const void* y, int dtype, const void* workspace,
+                       int64_t workspace_bytes, int64_t need, bool* todo)
+{
+    *todo = false;
+    if (int st = check_dtype(dtype)) return st;
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    if (cols > kMaxI8Sum)
+        return fail(ROI_E_UNSUPPORTED, "cols (%lld) must be at most %lld for an exact int32 sum",
+                    (long long)cols, (long long)kMaxI8Sum);
+    if (meta && cols % 32 != 0)
+        return fail(ROI_E_INVAL, "2:4 weights need cols %% 32 == 0 (got %lld)", (long long)cols);
+    if (int st = check_workspace(workspace, workspace_bytes, need)) return st;
+    const size_t t = (size_t)tokens, r = (size_t)rows, c = (size_t)cols;
+    const Buffer b[] = {{xq, t * c, false},
+                        {xs, t * 4, false},
+                        {wq, meta ? r * (c / 2) : r * c, false},
+                        {meta, meta ? r * (c / 32) * 4 : 0, false},
+                        {ws, r * 4, false},
+                        {bias, bias ? r * 2 : 0, false},
+                        {y, t * r * (dtype == ROI_FP32 ? 4 : 2), true},
+                        {workspace, (size_t)need, true}};
+    if (int st = check_buffers(b, 8)) return st;
+    *todo = tokens > 0 && rows > 0;
+    return ok();
+}
+
+int validate_grad_i8(const uint16_t* grad_y, const int8_t* q, const float* scale, int64_t krows,
+                     int64_t tokens, int64_t rows, int64_t cols, const uint16_t* out,
+                     int64_t out_rows, const void* workspace, int64_t workspace_bytes,
+                     int64_t need, bool* todo)
+{
+    *todo = false;
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    if (int st = check_workspace(workspace, workspace_bytes, need)) return st;
+    const size_t c = (size_t)cols;
+    const Buffer b[] = {{grad_y, (size_t)tokens * (size_t)rows * 2, false},
+                        {q, (size_t)krows * c, false},
+                        {scale, (size_t)krows * 4, false},
+                        {out, (size_t)out_rows * c * 2, true},
+                        {workspace, (size_t)need, true}};
+    if (int st = check_buffers(b, 5)) return st;
+    *todo = out_rows > 0 && cols > 0;
+    return ok();
+}
+
 } // namespace roi

@@ -91,6 +91,42 @@ int validate_cat(bool fwd, const uint16_t* W, const float* alpha, const uint16_t
                  const uint16_t* W_masked, const float* S, const uint8_t* choice,
                  const float* dalpha, int64_t* ngroups, int* C);
 
+// One int8-rows call (roi_quantize_rows, roi_dequantize_rows).  x_out: x is the
+// output.  *todo is false when there is nothing to write.
+int validate_rows_i8(const void* x, int dtype, const int8_t* q, const float* scale, int64_t rows,
+                     int64_t cols, bool x_out, bool* todo);
+
+// The largest product and gradient sizes, and the longest exact int32 sum of
+// products of two int8 values (131071 * 2^14 < 2^31).
+constexpr int64_t kMaxLinearDim = (int64_t)1 << 22;
+constexpr int64_t kMaxTokens = (int64_t)1 << 31;
+constexpr int64_t kMaxI8Sum = 131071;
+
+// How a product of m x n outputs over k steps is cut: tiles of one size and
+// parts of the sum per tile (partial sums pass through the workspace when
+// there is more than one).
+struct Cut {
+    int tile;           // output rows and columns of a tile
+    int64_t tm, tn;     // tiles
+    int splits;         // parts of the sum
+    int64_t steps;      // steps of the whole sum
+    int64_t bytes;      // workspace
+};
+Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step);
+
+// Sizes of a linear call: ROI_OK, or why the call is refused.
+int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols);
+int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uint32_t* meta,
+                       const float* ws, const uint16_t* bias, int64_t tokens, int64_t rows,
+                       int64_t cols, const void* y, int dtype, const void* workspace,
+                       int64_t workspace_bytes, int64_t need, bool* todo);
+// q [krows, cols] and scale [krows] beside grad_y [tokens, rows]; out has
+// out_rows rows of cols.
+int validate_grad_i8(const uint16_t* grad_y, const int8_t* q, const float* scale, int64_t krows,
+                     int64_t tokens, int64_t rows, int64_t cols, const uint16_t* out,
+                     int64_t out_rows, const void* workspace, int64_t workspace_bytes,
+                     int64_t need, bool* todo);
+
 // Calls launch(first, count, elem0) for consecutive pieces of [0, items) --
 // items of `per_item` elements starting at global element elem_offset -- so
 // that within a piece every Philox block index (element / 4) has the same high

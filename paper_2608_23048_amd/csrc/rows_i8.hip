@@ -1,0 +1,271 @@
+// rows_i8.hip -- gfx950 kernels of the int8 rows: quantize_rows and
+// dequantize_rows.
+//
+// scale = max(fl(amax / 127), 2^-126), inv = fl(127 fl(1 / amax)) (2^126 at that
+// floor), q = rint(fl(x inv)): the two divisions are one per row and IEEE, the
+// per-element work is a product, a rounding and a pack.  Both kernels are bound
+// by HBM: 3 bytes an element from bf16 (5 from fp32), once each.  The row is
+// read once: it stays in the registers of the waves that own it between the
+// maximum and the rounding.
+#include <hip/hip_runtime.h>
+
+#include "host.hpp"
+#include "rows.hpp"
+#include "roi.h"
+
+namespace roi {
+namespace {
+
+constexpr float kScaleFloor = 0x1p-126f;
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// Eight consecutive elements of a row, as loaded.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+    uint32_t w[4];
+    __device__ __forceinline__ float get(int i) const
+    {
+        return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    }
+    __device__ __forceinline__ void set(int i, uint16_t v)
+    {
+        w[i / 2] = i & 1 ? (w[i / 2] & 0xFFFFu) | ((uint32_t)v << 16)
+                         : (w[i / 2] & 0xFFFF0000u) | v;
+    }
+};
+template <>
+struct Eight<uint32_t> {
+    uint32_t w[8];
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
+    __device__ __forceinline__ void set(int i, uint32_t v) { w[i] = v; }
+};
+
+// Elements 8 c .. 8 c + 7 of a row of `cols`, zeros past its end.
+template <typename T>
+__device__ __forceinline__ Eight<T> load_eight(const T* row, int64_t c, int64_t cols)
+{
+    Eight<T> e{};
+    const int64_t k = 8 * c;
+    if (k + 8 <= cols) {
+        e = load_any<Eight<T>>(row + k);
+    } else if (k < cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < cols) e.set(i, row[k + i]);
+    }
+    return e;
+}
+
+// The largest magnitude as fp32 bits: magnitudes of floats order as integers,
+// infinities and NaN above every number.
+template <typename T>
+__device__ __forceinline__ uint32_t max_bits(const Eight<T>& e, uint32_t m)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __float_as_uint(e.get(i)) & 0x7FFFFFFFu;
+        m = b > m ? b : m;
+    }
+    return m;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_quantized(const Eight<T>& e, float inv, bool finite,
+                                                int8_t* row, int64_t c, int64_t cols)
+{
+    uint32_t p[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int v = finite ? (int)__builtin_rintf(e.get(i) * inv) : 0;
+        p[i / 4] |= (uint32_t)(v & 0xFF) << (8 * (i % 4));
+    }
+    const int64_t k = 8 * c;
+    if (k + 8 <= cols) {
+        store_any(row + k, Pair{p[0], p[1]});
+    } else if (k < cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < cols) row[k + i] = (int8_t)(p[i / 4] >> (8 * (i % 4)));
+    }
+}
+
+// A row over kWaves waves (a block holds 4 / kWaves rows when kWaves <= 4),
+// each lane holding kChunks groups of eight in registers; kChunks == 0: a row
+// longer than that, read twice.
+template <typename T, int kWaves, int kChunks>
+__global__ __launch_bounds__(kWaves > 4 ? 64 * kWaves : 256) void quantize_rows_kernel(
+    const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols)
+{
+    constexpr int kRowsPerBlock = kWaves > 4 ? 1 : 4 / kWaves;
+    constexpr int kLanes = 64 * kWaves;
+    __shared__ uint32_t part[kWaves > 4 ? kWaves : 4];
+    const int wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x % kLanes;
+    const int64_t r = (int64_t)blockIdx.x * kRowsPerBlock + threadIdx.x / kLanes;
+    const bool live = r < rows;
+    const T* row = x + (live ? r : 0) * cols;
+    int8_t* out = q + (live ? r : 0) * cols;
+    const int64_t chunks = live ? (cols + 7) / 8 : 0;
+
+    constexpr int kHeld = kChunks > 0 ? kChunks : 1;
+    Eight<T> held[kHeld];
+    uint32_t m = 0;
+    if constexpr (kChunks > 0) {
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int64_t c = lane + (int64_t)j * kLanes;
+            held[j] = c < chunks ? load_eight(row, c, cols) : Eight<T>{};
+        }
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) m = max_bits(held[j], m);
+    } else {
+        for (int64_t c = lane; c < chunks; c += kLanes) m = max_bits(load_eight(row, c, cols), m);
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) {
+        const uint32_t o = (uint32_t)__shfl_xor((int)m, d);
+        m = o > m ? o : m;
+    }
+    if constexpr (kWaves > 1) {
+        if ((threadIdx.x & 63) == 0) part[wave] = m;
+        __syncthreads();
+        const int first = wave - wave % kWaves;
+#pragma unroll
+        for (int j = 0; j < kWaves; ++j) m = part[first + j] > m ? part[first + j] : m;
+    }
+    if (!live) return;
+
+    const float amax = __uint_as_float(m);
+    const bool finite = m < kInfBits;
+    const float s = amax / 127.0f;
+    const bool low = !(s > kScaleFloor);
+    const float inv = low ? 0x1p126f : 127.0f * (1.0f / amax);
+    if (lane == 0) scale[r] = finite ? (low ? kScaleFloor : s) : __uint_as_float(0x7FC00000u);
+    if constexpr (kChunks > 0) {
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int64_t c = lane + (int64_t)j * kLanes;
+            if (c < chunks) store_quantized(held[j], inv, finite, out, c, cols);
+        }
+    } else {
+        for (int64_t c = lane; c < chunks; c += kLanes)
+            store_quantized(load_eight(row, c, cols), inv, finite, out, c, cols);
+    }
+}
+
+// One wave per 1024 elements of a row, 16 a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void dequantize_rows_kernel(const int8_t* q, const float* scale,
+                                                              T* x, int64_t rows, int64_t cols,
+                                                              int64_t per_row)
+{
+    const int64_t waves = rows * per_row;
+    const int lane = threadIdx.x & 63;
+    for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < waves;
+         w += (int64_t)gridDim.x * 4) {
+        const int64_t r = w / per_row, k = ((w % per_row) * 64 + lane) * 16;
+        const float s = scale[r];
+        const int8_t* in = q + r * cols;
+        T* out = x + r * cols;
+        if (k + 16 <= cols) {
+            const Quad v = load_any<Quad>(in + k);
+            float f[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f[i] = (float)(int8_t)(v.w[i / 4] >> (8 * (i % 4))) * s;
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    Quad o;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        o.w[i] = bf16x2_rne(f[8 * h + 2 * i], f[8 * h + 2 * i + 1]);
+                    store_any(out + k + 8 * h, o);
+                }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    Quad o;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o.w[i] = __float_as_uint(f[4 * h + i]);
+                    store_any(out + k + 4 * h, o);
+                }
+            }
+        } else {
+            for (int64_t i = k; i < cols; ++i) {
+                const float f = (float)in[i] * s;
+                if constexpr (sizeof(T) == 2)
+                    out[i] = (uint16_t)bf16x2_rne(f, 0.0f);
+                else
+                    out[i] = f;
+            }
+        }
+    }
+}
+
+template <typename T, int kWaves, int kChunks>
+void launch_quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols,
+                     hipStream_t stream)
+{
+    constexpr int kThreads = kWaves > 4 ? 64 * kWaves : 256;
+    constexpr int kRowsPerBlock = kWaves > 4 ? 1 : 4 / kWaves;
+    // a launch has fewer than 2^32 threads; longer inputs take several
+    const int64_t most = (int64_t)(0xFFFFFFFFu / kThreads) * kRowsPerBlock;
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = rows - r < most ? rows - r : most;
+        hipLaunchKernelGGL((quantize_rows_kernel<T, kWaves, kChunks>),
+                           dim3((unsigned)((n + kRowsPerBlock - 1) / kRowsPerBlock)),
+                           dim3(kThreads), 0, stream, x + r * cols, q + r * cols, scale + r, n,
+                           cols);
+    }
+}
+
+template <typename T>
+void quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols, hipStream_t stream)
+{
+    if (cols <= 64 * 8 * 4)
+        launch_quantize<T, 1, 4>(x, q, scale, rows, cols, stream);
+    else if (cols <= 256 * 8 * 4)
+        launch_quantize<T, 4, 4>(x, q, scale, rows, cols, stream);
+    else if (cols <= 1024 * 8 * 4)
+        launch_quantize<T, 16, 4>(x, q, scale, rows, cols, stream);
+    else
+        launch_quantize<T, 16, 0>(x, q, scale, rows, cols, stream);
+}
+
+} // namespace
+} // namespace roi
+
+using namespace roi;
+
+extern "C" int roi_quantize_rows(const void* x, int dtype, int64_t rows, int64_t cols, int8_t* q,
+                                 float* scale, hipStream_t stream)
+{
+    bool todo;
+    if (int st = validate_rows_i8(x, dtype, q, scale, rows, cols, false, &todo)) return st;
+    if (!todo) return ok();
+    if (dtype == ROI_BF16)
+        quantize(static_cast<const uint16_t*>(x), q, scale, rows, cols, stream);
+    else
+        quantize(static_cast<const uint32_t*>(x), q, scale, rows, cols, stream);
+    return launch_status("roi_quantize_rows");
+}
+
+extern "C" int roi_dequantize_rows(const int8_t* q, const float* scale, int64_t rows, int64_t cols,
+                                   void* x, int dtype, hipStream_t stream)
+{
+    bool todo;
+    if (int st = validate_rows_i8(x, dtype, q, scale, rows, cols, true, &todo)) return st;
+    if (!todo) return ok();
+    const int64_t per_row = (cols + 1023) / 1024;
+    const int64_t blocks = (rows * per_row + 3) / 4; // below 2^31 * 2^21
+    const dim3 grid((unsigned)(blocks < 0xFFFFFF ? blocks : 0xFFFFFF));
+    if (dtype == ROI_BF16)
+        hipLaunchKernelGGL((dequantize_rows_kernel<uint16_t>), grid, dim3(256), 0, stream, q, scale,
+                           static_cast<uint16_t*>(x), rows, cols, per_row);
+    else
+        hipLaunchKernelGGL((dequantize_rows_kernel<float>), grid, dim3(256), 0, stream, q, scale,
+                           static_cast<float*>(x), rows, cols, per_row);
+    return launch_status("roi_dequantize_rows");
+}
