@@ -303,7 +303,7 @@ int validate_rows_i8(const void* x, int dtype, const int8_t* q, const float* sca
     if (rows < 0 || cols < 0)
         return fail(ROI_E_INVAL, "rows (%lld) and cols (%lld) must be >= 0", (long long)rows,
                     (long long)cols);
-    if (rows >= kMaxTokens || cols >= kMaxTokens)
+    if (rows >= kMaxRowsI8 || cols >= kMaxRowsI8)
         return fail(ROI_E_UNSUPPORTED, "rows and cols must be below 2^31");
     const size_t n = (size_t)rows * (size_t)cols; // below 2^62
     const Buffer b[] = {{x, n * (dtype == ROI_FP32 ? 4 : 2), x_out},
@@ -320,14 +320,14 @@ int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols)
         return fail(ROI_E_INVAL, "tokens (%lld), rows (%lld) and cols (%lld) must be >= 0",
                     (long long)tokens, (long long)rows, (long long)cols);
     if (tokens >= kMaxTokens || rows >= kMaxLinearDim || cols >= kMaxLinearDim)
-        return fail(ROI_E_UNSUPPORTED, "tokens must be below 2^31, rows and cols below 2^22");
+        return fail(ROI_E_UNSUPPORTED, "tokens must be below 2^30, rows and cols below 2^22");
     return ROI_OK;
 }
 
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step)
 {
     Cut c{};
-    c.tile = 128;
+    c.tile = m > 1024 && n > 1024 ? 256 : 128;
     c.tm = (m + c.tile - 1) / c.tile;
     c.tn = (n + c.tile - 1) / c.tile;
     c.steps = (k + step - 1) / step;

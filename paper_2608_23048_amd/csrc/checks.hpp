@@ -96,10 +96,12 @@ int validate_cat(bool fwd, const uint16_t* W, const float* alpha, const uint16_t
 int validate_rows_i8(const void* x, int dtype, const int8_t* q, const float* scale, int64_t rows,
                      int64_t cols, bool x_out, bool* todo);
 
-// The largest product and gradient sizes, and the longest exact int32 sum of
+// The longest int8 row and the most of them; the largest product and gradient
+// sizes (kernels count tokens, rows and columns in 32 bits); and the longest exact int32 sum of
 // products of two int8 values (131071 * 2^14 < 2^31).
+constexpr int64_t kMaxRowsI8 = (int64_t)1 << 31;
 constexpr int64_t kMaxLinearDim = (int64_t)1 << 22;
-constexpr int64_t kMaxTokens = (int64_t)1 << 31;
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 constexpr int64_t kMaxI8Sum = 131071;
 
 // How a product of m x n outputs over k steps is cut: tiles of one size and

@@ -16,6 +16,8 @@
 //     four values at row i / 4, columns 4 (i % 4) ..; lane i gets column i.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "host.hpp"
 #include "mm.hpp"
 #include "roi.h"
@@ -26,11 +28,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kTile = 128;   // of out, in d and in c
-constexpr int kThreads = 256;
-constexpr int kSum = 64;     // sum indices a step
-constexpr int kTileBytes = kTile * kRowBytes;
-static_assert(kTileBytes == kSum * kTile * 2, "both layouts of dy take the same LDS");
+constexpr int kSum = 64; // sum indices a step
 
 struct Word {
     uint32_t w[1];
@@ -42,100 +40,177 @@ struct GradArgs {
     const float* scale;
     uint16_t* out;
     float* partial; // fp32 [splits, D, cols]
-    int64_t K, D, cols;
+    int K, D, cols;
     uint32_t td, tc, splits;
-    int64_t steps;
+    int steps;
 };
 
-// dy's tile of the step at sum index k0 into LDS.  kSumRows: [64 k][128 d], the
-// 16-byte chunk j of row k at place j ^ 2 (k & 3), so that the four rows that a
-// group of 16 lanes reads together lie in different banks.  Otherwise [128 d]
-// k-rows (mm.hpp).  What lies past K or D is zero or repeats the last row.
-template <bool kSumRows, bool kWhole>
-__device__ __forceinline__ void stage_dy(const GradArgs& a, int64_t k0, int64_t d0,
-                                         ROI_LDS uint8_t* dst)
-{
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t width = kSumRows ? a.D : a.K; // of a row of dy, in elements
-    const uint8_t* base = reinterpret_cast<const uint8_t*>(a.dy) +
-                          2 * (kSumRows ? k0 * width + d0 : d0 * width + k0);
+// dy's tile of a step in LDS.  kSumRows: [64 k][kTile d], the 16-byte chunk j of
+// row k at place j ^ 2 (k & 3), so that the four rows that a group of 16 lanes
+// reads together lie in different banks.  Otherwise [kTile d] k-rows (mm.hpp).
+// What lies past K is zero; past D, zero or the last row again.
+template <int kTile, bool kSumRows, bool kWhole>
+struct DyTile {
+    static constexpr int kThreads = Tile<kTile>::kThreads;
+    static constexpr int kLoads = kTile * kRowBytes / (16 * kThreads);
+    static constexpr int kAcrossRow = kSumRows ? kTile / 8 : 8; // chunks of a row
+    const uint8_t* base; // of row 0, column d0 (kSumRows), or of row d0
+    int K, D, d0;
+    uint32_t at;  // byte offset of load 0 from base
+    int from[4];  // where read() starts, by block of 16 columns (mod 4)
+
+    __device__ __forceinline__ DyTile(const GradArgs& a, int d0_)
+        : base(reinterpret_cast<const uint8_t*>(a.dy) + 2 * (kSumRows ? d0_ : (int64_t)d0_ * a.K)),
+          K(a.K), D(a.D), d0(d0_)
+    {
+        at = 2 * ((uint32_t)row(0) * width() + 8 * chunk());
+        if (kSumRows && 8 * chunk() >= D - d0) at = kNowhere;
+        const int lane = threadIdx.x & 63, g = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < kTileBytes / (16 * kThreads); ++i) {
-        const int place = i * kThreads + threadIdx.x;
-        int row, chunk;
-        if constexpr (kSumRows) {
-            row = place / (kTile / 8);
-            chunk = (place % (kTile / 8)) ^ (2 * (row & 3));
-        } else {
-            row = place / 8;
-            chunk = (place % 8) ^ (row & 7);
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (kSumRows) {
+                const int r = 8 * g + ((lane & 15) >> 2);
+                from[j] = r * (2 * kTile) + (2 * (j ^ (r & 3)) + ((lane & 3) >> 1)) * 16 +
+                          (lane & 1) * 8;
+            } else {
+                from[j] = (16 * j + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
+            }
         }
-        const int64_t rows_left = kSumRows ? a.K - k0 : a.D - d0;
-        const int64_t at = (kSumRows ? d0 : k0) + 8 * chunk; // first element's index in its row
-        // a row past the end: zeros where it is summed over, else any row
-        const int64_t rr = row < rows_left ? row : rows_left - 1;
-        const bool live = (!kSumRows || row < rows_left) && at < width;
+    }
+    // Row and chunk of this thread's load i (the chunk is the same for all: the
+    // rows differ by a multiple of eight).
+    __device__ __forceinline__ static int row(int i)
+    {
+        return (i * kThreads + (int)threadIdx.x) / kAcrossRow;
+    }
+    __device__ __forceinline__ static int chunk()
+    {
+        return (threadIdx.x % kAcrossRow) ^ (kSumRows ? 2 * (row(0) & 3) : row(0) & 7);
+    }
+    // Elements of a row of dy.
+    __device__ __forceinline__ uint32_t width() const { return kSumRows ? D : K; }
+    // Load i of the step at sum index k0.
+    __device__ __forceinline__ void stage(int i, int k0, ROI_LDS uint8_t* dst) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint8_t* p = base + 2 * (kSumRows ? (int64_t)k0 * D : k0);
+        const bool live = row(i) < (kSumRows ? K - k0 : D - d0) &&
+                          (kSumRows || 8 * chunk() < K - k0);
         if constexpr (kWhole) {
-            load_to_lds(buffer_at(base), live ? (uint32_t)(2 * (rr * width + 8 * chunk)) : kNowhere,
+            load_to_lds(buffer_at(p), live ? at : kNowhere, 2 * (i * kThreads / kAcrossRow) * width(),
                         dst + (i * kThreads + wave * 64) * 16);
         } else {
-            const uint8_t* p = base + 2 * (rr * width - (kSumRows ? d0 : k0));
-            lds_write(dst + place * 16, live ? load_row<Quad>(p, 2 * at, 2 * width) : Quad{});
+            Quad v{};
+            if (live && at != kNowhere) {
+                const int64_t k = (kSumRows ? d0 : k0) + 8 * chunk(); // within dy's row
+                v = load_row<Quad>(p + 2 * ((int64_t)row(i) * width() - (kSumRows ? d0 : k0)), 2 * k,
+                                   2 * (int64_t)width());
+            }
+            lds_write(dst + (i * kThreads + threadIdx.x) * 16, v);
         }
     }
-}
-
-// The int8 tile of a step: thread `item` takes eight sum indices of four
-// columns, and writes each column's eight values as one 16-byte chunk of that
-// column's k-row.  Chunk j of row c lies at place j ^ ((c ^ c / 4) & 7): any
-// eight lanes that write (c = 4 lane + i) or read (consecutive c) meet eight
-// different places.
-__device__ __forceinline__ int q_place(int c, int chunk)
-{
-    return c * kRowBytes + (chunk ^ ((c ^ (c >> 2)) & 7)) * 16;
-}
-
-struct QTile {
-    uint32_t v[8];
-    float s[8];
+    // The 16 columns d of block `block` (its number mod 4 is j), sum indices
+    // 32 h + 8 g .. + 7.
+    __device__ __forceinline__ bf16x8 read(const ROI_LDS uint8_t* src, int block, int j, int h) const
+    {
+        if constexpr (kSumRows) {
+            typedef short i16x8 __attribute__((ext_vector_type(8)));
+            const ROI_LDS uint8_t* p = src + from[j] + block / 4 * 128 + h * 32 * (2 * kTile);
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ROI_LDS i16x4*)p);
+            const i16x4 hi =
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((ROI_LDS i16x4*)(p + 4 * (2 * kTile)));
+            const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(bf16x8, both);
+        } else { // chunk 4 + g is 64 bytes away: the places' third bit flips
+            return lds_read<bf16x8>(src + block / 4 * 64 * kRowBytes + 16 * j * kRowBytes +
+                                    (from[0] ^ (64 * h)));
+        }
+    }
 };
 
-template <bool kWhole>
-__device__ __forceinline__ QTile load_q(const GradArgs& a, int64_t k0, int64_t c0)
-{
-    const int oct = threadIdx.x / (kTile / 4), group = threadIdx.x % (kTile / 4);
-    const int64_t c = c0 + 4 * group;
-    QTile t;
-    const uint8_t* base = reinterpret_cast<const uint8_t*>(a.q) + k0 * a.cols + c0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int row = 8 * oct + j;
-        const bool live = k0 + row < a.K && c < a.cols;
-        t.s[j] = live ? a.scale[k0 + row] : 0.0f;
-        if constexpr (kWhole)
-            t.v[j] = __builtin_amdgcn_raw_buffer_load_b32(
-                buffer_at(base), live ? (uint32_t)(row * a.cols + 4 * group) : kNowhere, 0, 0);
-        else
-            t.v[j] = live ? load_row<Word>(base + row * a.cols - c0, c, a.cols).w[0] : 0;
-    }
-    return t;
-}
+// The int8 tile of a step: an item is eight sum indices of four columns, whose
+// values are scaled, rounded to bf16, and written as one 16-byte chunk of each
+// column's k-row.  Chunk j of row c lies at place j ^ ((c ^ c / 4) & 7): any
+// eight lanes that write (c = 4 lane + b) or read (consecutive c) meet eight
+// different places.  A step's 64 scales are one load, lane k's the k-th.
+template <int kTile, bool kWhole>
+struct QTile {
+    static constexpr int kItems = kTile * 2 / Tile<kTile>::kThreads;
+    static_assert(kItems == 1, "one item a thread");
+    static constexpr bool kOneOct = kTile / 4 == 64; // all of a wave's items have the same sum indices
+    const uint8_t* base; // of row 0, column c0
+    const float* scale;
+    int K, left;         // columns from this thread's first on
+    uint32_t cols;
+    int to, from;        // where write() and read() start
+    uint32_t v[8], s;
 
-__device__ __forceinline__ void write_q(const QTile& t, ROI_LDS uint8_t* dst)
-{
-    const int oct = threadIdx.x / (kTile / 4), group = threadIdx.x % (kTile / 4);
+    __device__ __forceinline__ QTile(const GradArgs& a, int c0)
+        : base(reinterpret_cast<const uint8_t*>(a.q) + c0), scale(a.scale), K(a.K),
+          left(a.cols - c0 - 4 * group()), cols(a.cols)
+    {
+        const int lane = threadIdx.x & 63;
+        to = place(4 * group(), oct());
+        from = place(lane & 15, lane >> 4);
+    }
+    __device__ __forceinline__ static int oct()
+    {
+        const int o = threadIdx.x / (kTile / 4);
+        return kOneOct ? __builtin_amdgcn_readfirstlane(o) : o;
+    }
+    __device__ __forceinline__ static int group() { return threadIdx.x % (kTile / 4); }
+    __device__ __forceinline__ static int place(int c, int chunk)
+    {
+        return c * kRowBytes + (chunk ^ ((c ^ (c >> 2)) & 7)) * 16;
+    }
+
+    __device__ __forceinline__ void load(int k0)
+    {
+        const int lane = threadIdx.x & 63;
+        s = __builtin_amdgcn_raw_buffer_load_b32(buffer_at(scale + k0),
+                                                 lane < K - k0 ? 4 * lane : kNowhere, 0, 0);
+        const uint8_t* p = base + (int64_t)k0 * cols;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < 8; ++j) {
+            // a row past the end is the last again, times a scale of zero
+            const int row = least(8 * oct() + j, K - k0 - 1);
+            if constexpr (kWhole && kOneOct)
+                v[j] = __builtin_amdgcn_raw_buffer_load_b32(
+                    buffer_at(p), left > 0 ? 4 * group() : kNowhere, row * (int)cols, 0);
+            else if constexpr (kWhole)
+                v[j] = __builtin_amdgcn_raw_buffer_load_b32(
+                    buffer_at(p), left > 0 && row >= 0 ? row * cols + 4 * group() : kNowhere, 0, 0);
+            else
+                v[j] = left > 0 && row >= 0
+                           ? load_row<Word>(p + (int64_t)row * cols + 4 * group(), 0, left).w[0]
+                           : 0;
+        }
+    }
+    // Column b.
+    __device__ __forceinline__ void write(int b, ROI_LDS uint8_t* dst) const
+    {
         float f[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = (float)(int8_t)(t.v[j] >> (8 * i)) * t.s[j];
-        lds_write(dst + q_place(4 * group + i, oct),
+        for (int j = 0; j < 8; ++j) {
+            const int k = 8 * oct() + j;
+            const int sk = kOneOct ? __builtin_amdgcn_readlane((int)s, k) : __shfl((int)s, k);
+            f[j] = (float)(int8_t)(v[j] >> (8 * b)) * __uint_as_float(sk);
+        }
+        // the place of column b is that of column 0 with its low bits flipped by b
+        lds_write(dst + (to ^ (16 * b)) + b * kRowBytes,
                   Quad{bf16x2_rne(f[0], f[1]), bf16x2_rne(f[2], f[3]), bf16x2_rne(f[4], f[5]),
                        bf16x2_rne(f[6], f[7])});
     }
-}
+    // The 16 columns of block `block` (its number is even or odd as i), sum
+    // indices 32 h + 8 g .. + 7: chunk 4 h + g, and the place's third bit flips
+    // with h and with each block.
+    __device__ __forceinline__ bf16x8 read(const ROI_LDS uint8_t* src, int block, int i, int h) const
+    {
+        return lds_read<bf16x8>(src + block * 16 * kRowBytes + (from ^ (64 * ((i + h) & 1))));
+    }
+};
 
-__device__ __forceinline__ void store4(const GradArgs& a, int64_t d, int64_t c, f32x4 v)
+__device__ __forceinline__ void store4(const GradArgs& a, int64_t d, int c, f32x4 v)
 {
     uint16_t* p = a.out + d * a.cols + c;
     if (c + 4 <= a.cols) {
@@ -147,97 +222,117 @@ __device__ __forceinline__ void store4(const GradArgs& a, int64_t d, int64_t c, 
     }
 }
 
-template <bool kSumRows, bool kWhole>
-__global__ __launch_bounds__(kThreads) void grad_tile_kernel(GradArgs a)
+template <int kTile, bool kSumRows, bool kWhole>
+__global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradArgs a)
 {
+    constexpr int kTileBytes = kTile * kRowBytes;
+    static_assert(kTileBytes == kSum * kTile * 2, "both layouts of dy take the same LDS");
+    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    static_assert(kJ == 4 && kI % 2 == 0, "DyTile::read and QTile::read");
+    using Dy = DyTile<kTile, kSumRows, kWhole>;
+    using Q = QTile<kTile, kWhole>;
+    static_assert(Dy::kLoads <= kI && kI >= 4, "a part a row");
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0][0];
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wc = (wave >> 1) * 64, wd = (wave & 1) * 64;
-    uint32_t td, tc;
+    // first block of 16 of this wave along c and d
+    const int bc = wave / Tile<kTile>::kAcross * kI, bd = wave % Tile<kTile>::kAcross * kJ;
+    int td, tc;
     tile_at(xcd_order(blockIdx.x, a.td * a.tc), a.td, a.tc, 8, td, tc);
-    const int64_t d0 = (int64_t)td * kTile, c0 = (int64_t)tc * kTile;
+    const int d0 = td * kTile, c0 = tc * kTile;
 
-    f32x4 acc[4][4] = {};
-    if (a.steps > 0) {
-        stage_dy<kSumRows, kWhole>(a, 0, d0, base + kTileBytes);
-        write_q(load_q<kWhole>(a, 0, c0), base);
-    }
-    __syncthreads();
-    for (int64_t s = 0; s < a.steps; ++s) {
-        ROI_LDS uint8_t* cur = base + (s & 1) * 2 * kTileBytes;
-        ROI_LDS uint8_t* nxt = base + (~s & 1) * 2 * kTileBytes;
-        const bool more = s + 1 < a.steps;
-        QTile next{};
-        if (more) {
-            stage_dy<kSumRows, kWhole>(a, (s + 1) * kSum, d0, nxt + kTileBytes);
-            next = load_q<kWhole>(a, (s + 1) * kSum, c0);
-        }
-        ROI_LDS uint8_t* dyt = cur + kTileBytes;
+    f32x4 acc[kI][kJ] = {};
+    const Dy dy(a, d0);
+    Q q(a, c0);
+    // As in linear_i8.hip: a half step's products beside the reads of the next,
+    // one barrier a step.  The int8 tile of step s + 2 is in registers by then.
+    auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
+    struct Half {
+        bf16x8 q[kI], y[kJ];
+    };
+    // the products of a half, beside the reads of half h of step s and (load)
+    // the tiles of step s + 1, as whose int8 part q is written; past the sum's
+    // end all of that is zeros and unused
+    auto half = [&](const Half& f, int s, int h, Half& next, auto load) {
+        ROI_LDS uint8_t* src = buffer(s);
+        ROI_LDS uint8_t* dst = buffer(s + 1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            bf16x8 q[4], y[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                q[i] = lds_read<bf16x8>(cur + q_place(wc + 16 * i + (lane & 15), 4 * h + g));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (kSumRows) {
-                    typedef short i16x8 __attribute__((ext_vector_type(8)));
-                    const int row = 32 * h + 8 * g + ((lane & 15) >> 2);
-                    const int chunk = (wd + 16 * j) / 8 + ((lane & 3) >> 1);
-                    ROI_LDS uint8_t* p = dyt + row * (2 * kTile) +
-                                         (chunk ^ (2 * (row & 3))) * 16 + (lane & 1) * 8;
-                    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ROI_LDS i16x4*)p);
-                    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (ROI_LDS i16x4*)(p + 4 * (2 * kTile)));
-                    const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    y[j] = __builtin_bit_cast(bf16x8, both);
-                } else {
-                    y[j] = lds_read<bf16x8>(dyt + (wd + 16 * j + (lane & 15)) * kRowBytes +
-                                            ((4 * h + g) ^ (lane & 7)) * 16);
-                }
+        for (int i = 0; i < kI; ++i) {
+            if (i < kJ) next.y[i] = dy.read(src + kTileBytes, bd + i, i, h);
+            next.q[i] = q.read(src, bc + i, i, h);
+            if constexpr (decltype(load)::value) {
+                if (i < Dy::kLoads) dy.stage(i, (s + 1) * kSum, dst + kTileBytes);
+                if (i % (kI / 4) == 0) q.write(i / (kI / 4), dst);
+                if (i == kI - 1) q.load((s + 2) * kSum);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] =
-                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[i], y[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < kJ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.q[i], f.y[j], acc[i][j], 0, 0, 0);
+            keep_order();
         }
-        if (more) write_q(next, nxt);
-        __syncthreads();
+    };
+    if (a.steps > 0) {
+        Half lo, hi;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int i = 0; i < Dy::kLoads; ++i) dy.stage(i, s * kSum, buffer(s) + kTileBytes);
+            q.load(s * kSum);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) q.write(b, buffer(s));
+        }
+        q.load(2 * kSum);
+        loads_barrier();
+#pragma unroll
+        for (int i = 0; i < kI; ++i) lo.q[i] = q.read(buffer(0), bc + i, i, 0);
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) lo.y[j] = dy.read(buffer(0) + kTileBytes, bd + j, j, 0);
+        for (int s = 0; s < a.steps; ++s) {
+            half(lo, s, 1, hi, std::false_type{});
+            loads_barrier();
+            half(hi, s + 1, 0, lo, std::true_type{});
+        }
+        loads_barrier();
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t d = d0 + wd + 16 * j + (lane & 15);
+    for (int j = 0; j < kJ; ++j) {
+        const int d = d0 + 16 * (bd + j) + (lane & 15);
         if (d >= a.D) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t c = c0 + wc + 16 * i + 4 * g;
+        for (int i = 0; i < kI; ++i) {
+            const int c = c0 + 16 * (bc + i) + 4 * g;
             if (c < a.cols) store4(a, d, c, acc[i][j]);
         }
     }
+}
+
+template <int kTile, bool kSumRows>
+void launch_tiles(const GradArgs& a, hipStream_t stream)
+{
+    const dim3 grid(a.td * a.tc), block(Tile<kTile>::kThreads);
+    // 16-byte chunks of dy's rows and 4-byte words of q's that end with the row
+    const bool whole = (kSumRows ? a.D : a.K) % 8 == 0 && a.cols % 4 == 0;
+    if (whole)
+        hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows, false>), grid, block, 0, stream, a);
 }
 
 template <bool kSumRows>
 int launch(GradArgs a, const char* what, hipStream_t stream)
 {
     const Cut c = cut_product(a.D, a.cols, a.K, kSum);
-    if (c.tm * c.tn > (int64_t)(0xFFFFFFFFu / kThreads))
+    if (c.tm * c.tn > (int64_t)(0xFFFFFFFFu / Tile<256>::kThreads))
         return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
     a.td = (uint32_t)c.tm;
     a.tc = (uint32_t)c.tn;
     a.splits = 1;
-    a.steps = c.steps;
-    const dim3 grid((unsigned)(c.tm * c.tn));
-    // 16-byte chunks of dy's rows and 4-byte words of q's that end with the row
-    const bool whole = (kSumRows ? a.D : a.K) % 8 == 0 && a.cols % 4 == 0;
-    if (whole)
-        hipLaunchKernelGGL((grad_tile_kernel<kSumRows, true>), grid, dim3(kThreads), 0, stream, a);
+    a.steps = (int)c.steps;
+    if (c.tile == 256)
+        launch_tiles<256, kSumRows>(a, stream);
     else
-        hipLaunchKernelGGL((grad_tile_kernel<kSumRows, false>), grid, dim3(kThreads), 0, stream, a);
+        launch_tiles<128, kSumRows>(a, stream);
     return launch_status(what);
 }
 
@@ -273,8 +368,8 @@ extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* x
                                   workspace, workspace_bytes, 0, &todo))
         return st;
     if (!todo) return ok();
-    const GradArgs a{grad_y, xq, xs, grad_w, static_cast<float*>(workspace), tokens, rows, cols,
-                     0, 0, 1, 0};
+    const GradArgs a{grad_y, xq, xs, grad_w, static_cast<float*>(workspace), (int)tokens, (int)rows,
+                     (int)cols, 0, 0, 1, 0};
     return launch<true>(a, "roi_linear_i8_grad_weight", stream);
 }
 
@@ -288,7 +383,7 @@ extern "C" int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq
                                   workspace, workspace_bytes, 0, &todo))
         return st;
     if (!todo) return ok();
-    const GradArgs a{grad_y, wq, ws, grad_x, static_cast<float*>(workspace), rows, tokens, cols,
-                     0, 0, 1, 0};
+    const GradArgs a{grad_y, wq, ws, grad_x, static_cast<float*>(workspace), (int)rows, (int)tokens,
+                     (int)cols, 0, 0, 1, 0};
     return launch<false>(a, "roi_linear_i8_grad_input", stream);
 }

@@ -14,6 +14,8 @@
 //     columns 16 g .. 16 g + 15 and 64 + 16 g .. 64 + 16 g + 15; result as above.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "host.hpp"
 #include "mm.hpp"
 #include "roi.h"
@@ -30,25 +32,28 @@ struct LinearArgs {
     const uint16_t* bias;
     void* y;
     int* partial; // int32 [splits, tokens, rows]
-    int64_t tokens, rows, cols;
+    int tokens, rows, cols;
     uint32_t tm, tn, splits; // tiles along the rows and the tokens, parts of the sum
-    int64_t steps;
+    int steps;
 };
 
-// Four results of token t, rows r .. r + 3, from their exact sums.  The scale
-// of the weight comes first: sum ws stays far from overflow for any weight.
+// Four results from their exact sums.  The scale of the weight comes first: sum
+// ws stays far from overflow for any weight.  Without a bias -0 is added, which
+// changes nothing.
+__device__ __forceinline__ f32x4 finish4(i32x4 sum, const float (&ws)[4], const float (&add)[4],
+                                         float xs)
+{
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)sum[i] * ws[i] * xs + add[i];
+    return v;
+}
+
+// Rows r .. r + 3 of token t (those that y has).
 template <typename Out>
-__device__ __forceinline__ void finish4(const LinearArgs& a, int64_t t, int64_t r, i32x4 sum)
+__device__ __forceinline__ void store4(const LinearArgs& a, int64_t t, int r, f32x4 v)
 {
     Out* y = static_cast<Out*>(a.y) + t * a.rows + r;
-    const float xs = a.xs[t];
-    float v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t ri = r + i < a.rows ? r + i : a.rows - 1;
-        v[i] = (float)sum[i] * a.ws[ri] * xs;
-        if (a.bias) v[i] += bf16_bits_to_float(a.bias[ri]);
-    }
     if (r + 4 <= a.rows) {
         if constexpr (sizeof(Out) == 2)
             store_any(y, Pair{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])});
@@ -77,7 +82,7 @@ constexpr int kFewWaves = 8;
 // Operand chunk `k` .. k + 15 of a row of `len` bytes; kGuard: it may pass the
 // row's end, where the values are zero.
 template <bool kGuard>
-__device__ __forceinline__ i32x4 chunk16(const int8_t* row, int64_t k, int64_t len)
+__device__ __forceinline__ i32x4 chunk16(const int8_t* row, int k, int len)
 {
     const uint8_t* p = reinterpret_cast<const uint8_t*>(row);
     const Quad v = kGuard ? load_row<Quad>(p, k, len) : load_any<Quad>(p + k);
@@ -89,13 +94,13 @@ __device__ __forceinline__ i32x4 chunk16(const int8_t* row, int64_t k, int64_t l
 // within the step is free, as long as both operands follow it.
 template <int kTok, bool kPacked, bool kGuard>
 __device__ __forceinline__ void few_step(const int8_t* wrow, const uint32_t* mrow,
-                                         const int8_t* const (&xrow)[kTok], int64_t k, int64_t cols,
+                                         const int8_t* const (&xrow)[kTok], int k, int cols,
                                          int g, i32x4 (&acc)[kTok])
 {
     if constexpr (!kPacked) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t c = k + 32 * g + 16 * h;
+            const int c = k + 32 * g + 16 * h;
             const i32x4 w = chunk16<kGuard>(wrow, c, cols);
 #pragma unroll
             for (int j = 0; j < kTok; ++j)
@@ -108,10 +113,10 @@ __device__ __forceinline__ void few_step(const int8_t* wrow, const uint32_t* mro
         // 64 (g / 2) + 32 h + 16 (g % 2) and 16 at 128 further on
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t c = k + 64 * g + 32 * h;
+            const int c = k + 64 * g + 32 * h;
             const i32x4 w = chunk16<kGuard>(wrow, c / 2, cols / 2);
             const int idx = !kGuard || c < cols ? (int)mrow[c / 32] : 0x44444444;
-            const int64_t b = k + 64 * (g / 2) + 32 * h + 16 * (g % 2);
+            const int b = k + 64 * (g / 2) + 32 * h + 16 * (g % 2);
 #pragma unroll
             for (int j = 0; j < kTok; ++j) {
                 const i32x4 lo = chunk16<kGuard>(xrow[j], b, cols);
@@ -130,21 +135,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
     __shared__ i32x4 part[kFewWaves][kTok][64];
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t r0 = (int64_t)(blockIdx.x % a.tm) * 16;
-    const int64_t t0 = (int64_t)(blockIdx.x / a.tm) * (16 * kTok);
+    const int r0 = blockIdx.x % a.tm * 16, t0 = blockIdx.x / a.tm * (16 * kTok);
     // rows and tokens past the end repeat the last one; their results are dropped
-    const int64_t r = r0 + (lane & 15) < a.rows ? r0 + (lane & 15) : a.rows - 1;
+    const int64_t r = least(r0 + (lane & 15), a.rows - 1);
     const int8_t* wrow = a.w + r * (kPacked ? a.cols / 2 : a.cols);
     const uint32_t* mrow = kPacked ? a.meta + r * (a.cols / 32) : nullptr;
     const int8_t* xrow[kTok];
 #pragma unroll
     for (int j = 0; j < kTok; ++j) {
-        const int64_t t = t0 + 16 * j + (lane & 15);
-        xrow[j] = a.x + (t < a.tokens ? t : a.tokens - 1) * a.cols;
+        xrow[j] = a.x + (int64_t)least(t0 + 16 * j + (lane & 15), a.tokens - 1) * a.cols;
     }
     i32x4 acc[kTok] = {};
-    const int64_t whole = a.cols / kStep;
-    int64_t s = wave;
+    const int whole = a.cols / kStep;
+    int s = wave;
     for (; s + 3 * kFewWaves < whole; s += 4 * kFewWaves)
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -152,7 +155,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
                                            acc);
     for (; s < whole; s += kFewWaves)
         few_step<kTok, kPacked, false>(wrow, mrow, xrow, s * kStep, a.cols, g, acc);
-    if (whole * kStep < a.cols && wave == (int)(whole % kFewWaves))
+    if (whole * kStep < a.cols && wave == whole % kFewWaves)
         few_step<kTok, kPacked, true>(wrow, mrow, xrow, whole * kStep, a.cols, g, acc);
 #pragma unroll
     for (int j = 0; j < kTok; ++j) part[wave][j][lane] = acc[j];
@@ -161,96 +164,155 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
         i32x4 sum = {};
 #pragma unroll
         for (int v = 0; v < kFewWaves; ++v) sum += part[v][j][lane];
-        const int64_t t = t0 + 16 * j + (lane & 15), ro = r0 + 4 * g;
-        if (t < a.tokens && ro < a.rows) finish4<Out>(a, t, ro, sum);
+        const int t = t0 + 16 * j + (lane & 15), ro = r0 + 4 * g;
+        if (t >= a.tokens || ro >= a.rows) continue;
+        float ws[4], add[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int rc = least(ro + e, a.rows - 1);
+            ws[e] = a.ws[rc];
+            add[e] = a.bias ? bf16_bits_to_float(a.bias[rc]) : -0.0f;
+        }
+        store4<Out>(a, t, ro, finish4(sum, ws, add, a.xs[t]));
     }
 }
 
 // --------------------------------------------------------------- many tokens
-// A block of 4 waves makes a 128 x 128 tile, each wave 64 x 64, over steps of
-// 128 columns.  Two LDS buffers: the next step's tiles load while this one's
-// are multiplied.
-constexpr int kTile = 128;
-constexpr int kThreads = 256;
-constexpr int kTileBytes = kTile * kRowBytes;
+// A block makes one tile (mm.hpp) over steps of 128 columns, in two LDS buffers.
+// A wave multiplies half a step's operands while it reads the next half's, row
+// by row: past a row's products its registers take the next half's row.  One
+// barrier a step, between the halves: past it every wave holds all it needs of
+// this step's buffer, which takes the step after the next, and the next step's
+// buffer, loading for a whole step, is complete.
 
-// The 128-byte k-rows row0 .. row0 + 127 of an operand of `n` rows of `len`
-// bytes, from byte k on, into LDS.  kWhole: rows are whole 16-byte chunks.
-template <bool kWhole>
-__device__ __forceinline__ void stage(const int8_t* p, int64_t row0, int64_t n, int64_t len,
-                                      int64_t k, ROI_LDS uint8_t* dst)
-{
-    const uint8_t* base = reinterpret_cast<const uint8_t*>(p) + row0 * len;
-    const int64_t left = n - row0;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-    for (int i = 0; i < kTileBytes / (16 * kThreads); ++i) {
-        const int place = i * kThreads + threadIdx.x;
-        const int row = place / 8, chunk = (place % 8) ^ (row & 7);
-        const int64_t rr = row < left ? row : left - 1; // rows past the end repeat the last
-        const int64_t b = k + 16 * chunk;
-        if constexpr (kWhole) {
-            load_to_lds(buffer_at(base), b < len ? (uint32_t)(rr * len + b) : kNowhere,
-                        dst + (i * kThreads + wave * 64) * 16);
-        } else {
-            lds_write(dst + place * 16, load_row<Quad>(base + rr * len, b, len));
-        }
+// The k-rows row0 .. of an operand of `n` rows of `len` bytes that this thread
+// brings to LDS.  kWhole: rows are whole 16-byte chunks.
+template <int kTile, bool kWhole>
+struct KRows {
+    static constexpr int kThreads = Tile<kTile>::kThreads;
+    static constexpr int kLoads = kTile * kRowBytes / (16 * kThreads);
+    const uint8_t* base;
+    int left, len; // rows from row0 on, and their bytes
+    uint32_t at;   // byte offset of load 0 from base
+
+    __device__ __forceinline__ KRows(const int8_t* p, int row0, int n, int len_)
+        : base(reinterpret_cast<const uint8_t*>(p) + (int64_t)row0 * len_), left(n - row0),
+          len(len_), at((uint32_t)row(0) * len_ + 16 * chunk())
+    {
     }
-}
+    // Row and chunk of this thread's load i (the chunk is the same for all: the
+    // rows differ by a multiple of eight).
+    __device__ __forceinline__ static int row(int i) { return (i * kThreads + (int)threadIdx.x) / 8; }
+    __device__ __forceinline__ static int chunk() { return (threadIdx.x % 8) ^ (row(0) & 7); }
+    // Load i of bytes k .. k + 127 of the rows; zeros past the end.
+    __device__ __forceinline__ void stage(int i, int k, ROI_LDS uint8_t* dst) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const bool live = row(i) < left && k + 16 * chunk() < len;
+        if constexpr (kWhole)
+            load_to_lds(buffer_at(base + k), live ? at : kNowhere, i * (kThreads / 8) * len,
+                        dst + (i * kThreads + wave * 64) * 16);
+        else
+            lds_write(dst + (i * kThreads + threadIdx.x) * 16,
+                      live ? load_row<Quad>(base + (int64_t)row(i) * len, k + 16 * chunk(), len)
+                           : Quad{});
+    }
+};
 
-template <bool kWhole, typename Out>
-__global__ __launch_bounds__(kThreads) void linear_tile_kernel(LinearArgs a)
+template <int kTile, bool kWhole, typename Out>
+__global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(LinearArgs a)
 {
+    constexpr int kTileBytes = kTile * kRowBytes;
+    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0][0];
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = (wave >> 1) * 64, wn = (wave & 1) * 64;
-    uint32_t tm, tn;
+    const int wm = wave / Tile<kTile>::kAcross * 16 * kI, wn = wave % Tile<kTile>::kAcross * 16 * kJ;
+    int tm, tn;
     tile_at(xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, tm, tn);
-    const int64_t r0 = (int64_t)tm * kTile, t0 = (int64_t)tn * kTile;
+    const int r0 = tm * kTile, t0 = tn * kTile;
 
-    i32x4 acc[4][4] = {};
+    i32x4 acc[kI][kJ] = {};
+    const KRows<kTile, kWhole> wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
+    constexpr int kLoads = KRows<kTile, kWhole>::kLoads;
+    auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
+    // loads `first` .. of step s, of the 2 kLoads that bring both tiles
+    auto stage = [&](int s, int first, int count) {
+        for (int i = first; i < first + count; ++i)
+            if (i < kLoads)
+                wrows.stage(i, s * kRowBytes, buffer(s));
+            else
+                xrows.stage(i - kLoads, s * kRowBytes, buffer(s) + kTileBytes);
+    };
+    struct Half {
+        i32x4 w[kI], x[kJ];
+    };
+    auto read_w = [&](int s, int h, Half& f, int i) {
+        f.w[i] = lds_read<i32x4>(buffer(s) + (wm + 16 * i + (lane & 15)) * kRowBytes +
+                                 ((4 * h + g) ^ (lane & 7)) * 16);
+    };
+    auto read_x = [&](int s, int h, Half& f, int j) {
+        f.x[j] = lds_read<i32x4>(buffer(s) + kTileBytes + (wn + 16 * j + (lane & 15)) * kRowBytes +
+                                 ((4 * h + g) ^ (lane & 7)) * 16);
+    };
+    // the products of a half, beside the reads of half h of step s and (kLoad)
+    // the loads of step s + 1: past the sum's end these bring zeros and those
+    // read them, and neither is used
+    auto half = [&](const Half& f, int s, int h, Half& next, auto load) {
+        constexpr int kPart = 2 * kLoads / kI;
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
+            if (i < kJ) read_x(s, h, next, i);
+            read_w(s, h, next, i);
+            if (decltype(load)::value) stage(s + 1, i * kPart, kPart);
+#pragma unroll
+            for (int j = 0; j < kJ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.w[i], f.x[j], acc[i][j], 0, 0, 0);
+            keep_order();
+        }
+    };
+    static_assert(2 * kLoads % kI == 0, "loads are spread over the rows");
     if (a.steps > 0) {
-        stage<kWhole>(a.w, r0, a.rows, a.cols, 0, base);
-        stage<kWhole>(a.x, t0, a.tokens, a.cols, 0, base + kTileBytes);
+        Half lo, hi;
+        stage(0, 0, 2 * kLoads);
+        stage(1, 0, 2 * kLoads);
+        loads_barrier();
+#pragma unroll
+        for (int i = 0; i < kI; ++i) read_w(0, 0, lo, i);
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) read_x(0, 0, lo, j);
+        for (int s = 0; s < a.steps; ++s) {
+            half(lo, s, 1, hi, std::false_type{});
+            loads_barrier();
+            half(hi, s + 1, 0, lo, std::true_type{});
+        }
+        loads_barrier();
     }
-    __syncthreads();
-    for (int64_t s = 0; s < a.steps; ++s) {
-        ROI_LDS uint8_t* cur = base + (s & 1) * 2 * kTileBytes;
-        ROI_LDS uint8_t* nxt = base + (~s & 1) * 2 * kTileBytes;
-        if (s + 1 < a.steps) {
-            stage<kWhole>(a.w, r0, a.rows, a.cols, (s + 1) * kRowBytes, nxt);
-            stage<kWhole>(a.x, t0, a.tokens, a.cols, (s + 1) * kRowBytes, nxt + kTileBytes);
+    // every scale before the first store, which might overwrite one for all the
+    // compiler knows
+    float ws[kI][4], add[kI][4], xs[kJ];
+#pragma unroll
+    for (int i = 0; i < kI; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = r0 + wm + 16 * i + 4 * g + e, rc = least(r, a.rows - 1);
+            ws[i][e] = a.ws[rc];
+            add[i][e] = a.bias ? bf16_bits_to_float(a.bias[rc]) : -0.0f;
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int place = ((4 * h + g) ^ (lane & 7)) * 16;
-            i32x4 w[4], x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = lds_read<i32x4>(cur + (wm + 16 * i + (lane & 15)) * kRowBytes + place);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                x[i] = lds_read<i32x4>(cur + kTileBytes +
-                                       (wn + 16 * i + (lane & 15)) * kRowBytes + place);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] =
-                        __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
-        }
-        __syncthreads();
+    for (int j = 0; j < kJ; ++j) {
+        const int t = t0 + wn + 16 * j + (lane & 15);
+        xs[j] = a.xs[least(t, a.tokens - 1)];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t t = t0 + wn + 16 * j + (lane & 15);
+    for (int j = 0; j < kJ; ++j) {
+        const int t = t0 + wn + 16 * j + (lane & 15);
         if (t >= a.tokens) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t r = r0 + wm + 16 * i + 4 * g;
-            if (r < a.rows) finish4<Out>(a, t, r, acc[i][j]);
+        for (int i = 0; i < kI; ++i) {
+            const int r = r0 + wm + 16 * i + 4 * g;
+            if (r < a.rows) store4<Out>(a, t, r, finish4(acc[i][j], ws[i], add[i], xs[j]));
         }
     }
 }
@@ -258,12 +320,22 @@ __global__ __launch_bounds__(kThreads) void linear_tile_kernel(LinearArgs a)
 // Blocks of one launch: fewer than 2^32 threads.
 bool fits(int64_t blocks, int threads) { return blocks <= (int64_t)(0xFFFFFFFFu / (uint32_t)threads); }
 
+template <int kTile, typename Out>
+void launch_tiles(const LinearArgs& a, hipStream_t stream)
+{
+    const dim3 grid(a.tm * a.tn), block(Tile<kTile>::kThreads);
+    if (a.cols % 16 == 0)
+        hipLaunchKernelGGL((linear_tile_kernel<kTile, true, Out>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((linear_tile_kernel<kTile, false, Out>), grid, block, 0, stream, a);
+}
+
 template <typename Out>
 int launch(LinearArgs a, hipStream_t stream)
 {
     if (a.tokens <= 64 || a.meta) {
         const int tok = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-        const int64_t tm = (a.rows + 15) / 16, tn = (a.tokens + 16 * tok - 1) / (16 * tok);
+        const int64_t tm = (a.rows + 15) / 16, tn = ((int64_t)a.tokens + 16 * tok - 1) / (16 * tok);
         if (!fits(tm * tn, 64 * kFewWaves))
             return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
         a.tm = (uint32_t)tm;
@@ -280,17 +352,16 @@ int launch(LinearArgs a, hipStream_t stream)
         return launch_status("roi_linear_i8");
     }
     const Cut c = cut_product(a.rows, a.tokens, a.cols, kRowBytes);
-    if (!fits(c.tm * c.tn, kThreads))
+    if (!fits(c.tm * c.tn, Tile<256>::kThreads))
         return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
     a.tm = (uint32_t)c.tm;
     a.tn = (uint32_t)c.tn;
     a.splits = 1;
-    a.steps = c.steps;
-    const dim3 grid((unsigned)(c.tm * c.tn));
-    if (a.cols % 16 == 0)
-        hipLaunchKernelGGL((linear_tile_kernel<true, Out>), grid, dim3(kThreads), 0, stream, a);
+    a.steps = (int)c.steps;
+    if (c.tile == 256)
+        launch_tiles<256, Out>(a, stream);
     else
-        hipLaunchKernelGGL((linear_tile_kernel<false, Out>), grid, dim3(kThreads), 0, stream, a);
+        launch_tiles<128, Out>(a, stream);
     return launch_status("roi_linear_i8");
 }
 
@@ -316,7 +387,7 @@ extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq
                                     workspace, workspace_bytes, 0, &todo))
         return st;
     if (!todo) return ok();
-    LinearArgs a{xq, xs, wq, meta, ws, bias, y, static_cast<int*>(workspace), tokens, rows, cols,
-                 0, 0, 1, 0};
+    LinearArgs a{xq, xs, wq, meta, ws, bias, y, static_cast<int*>(workspace), (int)tokens, (int)rows,
+                 (int)cols, 0, 0, 1, 0};
     return dtype == ROI_BF16 ? launch<uint16_t>(a, stream) : launch<float>(a, stream);
 }

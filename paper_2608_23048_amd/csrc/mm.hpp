@@ -25,6 +25,20 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kRowBytes = 128; // of a k-row in LDS
 
+// Blocks of a product: a square tile over kWaves waves, two by kAcross, each
+// with kI x kJ results of 16 x 16.
+template <int kTile>
+struct Tile {
+    static constexpr int kWaves = kTile == 256 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kAcross = kWaves / 2;
+    static constexpr int kI = kTile / 32, kJ = kTile / (16 * kAcross);
+};
+
+// Keeps the compiler from moving instructions across: the loops below are laid
+// out by hand.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // A byte offset that no buffer below reaches: a load from there gives zeros.
 constexpr uint32_t kNowhere = 0x80000000u;
 
@@ -35,12 +49,24 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p)
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7FFFFFFF, 0x00020000);
 }
 
-// 16 bytes a lane from the buffer into LDS, lane l's at dst + 16 l (dst is the
-// same for the wave).
+// 16 bytes a lane from the buffer into LDS, lane l's at dst + 16 l (dst and
+// `more`, a further offset, are the same for the wave).
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t offset,
-                                            ROI_LDS uint8_t* dst)
+                                            uint32_t more, ROI_LDS uint8_t* dst)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (ROI_LDS void*)dst, 16, (int)offset, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (ROI_LDS void*)dst, 16, (int)offset, (int)more, 0,
+                                             0);
+}
+
+__device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
+
+// A barrier past which what every wave has loaded to LDS is there: the barrier
+// itself waits for a wave's LDS operations only, and loads to LDS are counted
+// with the loads from memory.
+__device__ __forceinline__ void loads_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
 }
 
 template <typename V>
@@ -64,13 +90,13 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t b, uint32_t n)
 // Tile t of tm x tn, in bands of `band` tile rows, so that the tiles in flight
 // on an XCD form a block of few rows and columns.
 __device__ __forceinline__ void tile_at(uint32_t t, uint32_t tm, uint32_t tn, uint32_t band,
-                                        uint32_t& m, uint32_t& n)
+                                        int& m, int& n)
 {
     const uint32_t first = t / (band * tn) * band;
     const uint32_t height = tm - first < band ? tm - first : band;
     const uint32_t in = t - first * tn;
-    m = first + in % height;
-    n = in / height;
+    m = (int)(first + in % height);
+    n = (int)(in / height);
 }
 
 } // namespace roi
