@@ -324,15 +324,58 @@ int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols)
     return ROI_OK;
 }
 
-Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step)
+namespace {
+
+constexpr int64_t kUnits = 256;           // compute units of an MI355X
+constexpr int64_t kMostSplits = 64;
+constexpr double kPartBytesPerUs = 2.5e6; // a part is written and read again
+constexpr double kSumLaunchUs = 4;
+
+// One tile size: the tiles of whole rounds over the units are whole.  The last
+// round's are cut if they fill half of it or less, so that all units have a
+// part.  *us: what the call is expected to take.
+Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double step_us,
+              double rest_us, double* us)
 {
     Cut c{};
-    c.tile = m > 1024 && n > 1024 ? 256 : 128;
-    c.tm = (m + c.tile - 1) / c.tile;
-    c.tn = (n + c.tile - 1) / c.tile;
+    c.tile = tile;
+    c.tm = (m + tile - 1) / tile;
+    c.tn = (n + tile - 1) / tile;
     c.steps = (k + step - 1) / step;
+    const int64_t tiles = c.tm * c.tn, slots = kUnits * (tile == 256 ? 1 : 2);
+    const double whole = (double)c.steps * step_us + rest_us;
+    const int64_t rest = tiles % slots;
+    c.full = tiles;
     c.splits = 1;
+    *us = (double)((tiles + slots - 1) / slots) * whole;
+    // a part of a sum has four steps at least
+    const int64_t splits =
+        rest ? std::min(std::min(slots / rest, c.steps / 4), kMostSplits) : 1;
+    if (splits > 1) {
+        const double part_bytes = (double)(rest * splits) * tile * tile * 4;
+        const double cut = (double)(tiles / slots) * whole +
+                           (double)((c.steps + splits - 1) / splits) * step_us + rest_us +
+                           part_bytes / kPartBytesPerUs + kSumLaunchUs;
+        if (cut < *us) {
+            *us = cut;
+            c.full = tiles - rest;
+            c.splits = splits;
+            c.bytes = rest * splits * tile * tile * 4;
+        }
+    }
+    // a launch has fewer than 2^32 threads
+    c.fits = (c.full + rest * c.splits) * (tile == 256 ? 512 : 256) < ((int64_t)1 << 32);
     return c;
+}
+
+} // namespace
+
+Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost)
+{
+    double us256, us128;
+    const Cut big = cut_tiles(m, n, k, step, 256, cost.step256, cost.rest256, &us256);
+    const Cut small = cut_tiles(m, n, k, step, 128, cost.step128, cost.rest128, &us128);
+    return us128 < us256 && small.fits ? small : big;
 }
 
 int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uint32_t* meta,

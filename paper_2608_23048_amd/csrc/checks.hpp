@@ -104,17 +104,26 @@ constexpr int64_t kMaxLinearDim = (int64_t)1 << 22;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 constexpr int64_t kMaxI8Sum = 131071;
 
-// How a product of m x n outputs over k steps is cut: tiles of one size and
-// parts of the sum per tile (partial sums pass through the workspace when
-// there is more than one).
+// How a product of m x n results over a sum of k is cut: square tiles, of which
+// the first `full` are whole and the sums of the others are cut into `splits`
+// parts, which pass through the workspace as 32-bit values.
 struct Cut {
-    int tile;           // output rows and columns of a tile
-    int64_t tm, tn;     // tiles
-    int splits;         // parts of the sum
-    int64_t steps;      // steps of the whole sum
-    int64_t bytes;      // workspace
+    int tile;
+    int64_t tm, tn, full;
+    int64_t splits;
+    int64_t steps; // of the whole sum
+    int64_t bytes; // of workspace
+    bool fits;     // fewer blocks than a launch takes
 };
-Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step);
+// Times of the tiled kernels in microseconds: a step of a 256-tile on every
+// compute unit, of two 128-tiles on every unit, and what a tile costs beside
+// its steps.
+struct TileCost {
+    double step256, rest256, step128, rest128;
+};
+constexpr TileCost kLinearCost = {1.36, 12, 0.80, 9};
+constexpr TileCost kGradCost = {1.70, 14, 1.60, 10};
+Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost);
 
 // Sizes of a linear call: ROI_OK, or why the call is refused.
 int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols);

@@ -39,15 +39,14 @@ struct GradArgs {
     const int8_t* q;
     const float* scale;
     uint16_t* out;
-    float* partial; // fp32 [splits, D, cols]
+    float* partial; // fp32 parts of tiles (part_at)
     int K, D, cols;
-    uint32_t td, tc, splits;
-    int steps;
+    Grid grid; // tiles along d and c
 };
 
 // dy's tile of a step in LDS.  kSumRows: [64 k][kTile d], the 16-byte chunk j of
-// row k at place j ^ 2 (k & 3), so that the four rows that a group of 16 lanes
-// reads together lie in different banks.  Otherwise [kTile d] k-rows (mm.hpp).
+// row k at place j ^ 2 (k & 3) ^ (k & 8), so that the rows that 32 lanes read
+// together (four of each of two groups of 16) lie in different banks.  Otherwise [kTile d] k-rows (mm.hpp).
 // What lies past K is zero; past D, zero or the last row again.
 template <int kTile, bool kSumRows, bool kWhole>
 struct DyTile {
@@ -57,35 +56,39 @@ struct DyTile {
     const uint8_t* base; // of row 0, column d0 (kSumRows), or of row d0
     int K, D, d0;
     uint32_t at;  // byte offset of load 0 from base
-    int from[4];  // where read() starts, by block of 16 columns (mod 4)
+    int from[kSumRows ? 4 : 1]; // where read() starts, by block of 16 columns
 
-    __device__ __forceinline__ DyTile(const GradArgs& a, int d0_)
+    // block: the wave's first of 16 columns
+    __device__ __forceinline__ DyTile(const GradArgs& a, int d0_, int block)
         : base(reinterpret_cast<const uint8_t*>(a.dy) + 2 * (kSumRows ? d0_ : (int64_t)d0_ * a.K)),
           K(a.K), D(a.D), d0(d0_)
     {
         at = 2 * ((uint32_t)row(0) * width() + 8 * chunk());
         if (kSumRows && 8 * chunk() >= D - d0) at = kNowhere;
         const int lane = threadIdx.x & 63, g = lane >> 4;
+        if constexpr (kSumRows) {
+            const int r = 8 * g + ((lane & 15) >> 2);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (kSumRows) {
-                const int r = 8 * g + ((lane & 15) >> 2);
-                from[j] = r * (2 * kTile) + (2 * (j ^ (r & 3)) + ((lane & 3) >> 1)) * 16 +
-                          (lane & 1) * 8;
-            } else {
-                from[j] = (16 * j + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
-            }
+            for (int j = 0; j < 4; ++j)
+                from[j] = r * (2 * kTile) + (lane & 1) * 8 +
+                          ((2 * (block + j) + ((lane & 3) >> 1)) ^ spread(r)) * 16;
+        } else {
+            from[0] = (16 * block + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
         }
     }
+    __device__ __forceinline__ static int spread(int row)
+    {
+        return kSumRows ? (2 * (row & 3)) ^ (row & 8) : row & 7;
+    }
     // Row and chunk of this thread's load i (the chunk is the same for all: the
-    // rows differ by a multiple of eight).
+    // rows differ by a multiple of sixteen).
     __device__ __forceinline__ static int row(int i)
     {
         return (i * kThreads + (int)threadIdx.x) / kAcrossRow;
     }
     __device__ __forceinline__ static int chunk()
     {
-        return (threadIdx.x % kAcrossRow) ^ (kSumRows ? 2 * (row(0) & 3) : row(0) & 7);
+        return (threadIdx.x % kAcrossRow) ^ spread(row(0));
     }
     // Elements of a row of dy.
     __device__ __forceinline__ uint32_t width() const { return kSumRows ? D : K; }
@@ -97,8 +100,9 @@ struct DyTile {
         const bool live = row(i) < (kSumRows ? K - k0 : D - d0) &&
                           (kSumRows || 8 * chunk() < K - k0);
         if constexpr (kWhole) {
-            load_to_lds(buffer_at(p), live ? at : kNowhere, 2 * (i * kThreads / kAcrossRow) * width(),
-                        dst + (i * kThreads + wave * 64) * 16);
+            load_to_lds<kSumRows>(buffer_at(p), live ? at : kNowhere,
+                                  2 * (i * kThreads / kAcrossRow) * width(),
+                                  dst + (i * kThreads + wave * 64) * 16);
         } else {
             Quad v{};
             if (live && at != kNowhere) {
@@ -109,21 +113,19 @@ struct DyTile {
             lds_write(dst + (i * kThreads + threadIdx.x) * 16, v);
         }
     }
-    // The 16 columns d of block `block` (its number mod 4 is j), sum indices
-    // 32 h + 8 g .. + 7.
-    __device__ __forceinline__ bf16x8 read(const ROI_LDS uint8_t* src, int block, int j, int h) const
+    // The 16 columns d of the wave's block j, sum indices 32 h + 8 g .. + 7.
+    __device__ __forceinline__ bf16x8 read(const ROI_LDS uint8_t* src, int j, int h) const
     {
         if constexpr (kSumRows) {
             typedef short i16x8 __attribute__((ext_vector_type(8)));
-            const ROI_LDS uint8_t* p = src + from[j] + block / 4 * 128 + h * 32 * (2 * kTile);
+            const ROI_LDS uint8_t* p = src + from[j] + h * 32 * (2 * kTile);
             const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ROI_LDS i16x4*)p);
             const i16x4 hi =
                 __builtin_amdgcn_ds_read_tr16_b64_v4i16((ROI_LDS i16x4*)(p + 4 * (2 * kTile)));
             const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(bf16x8, both);
         } else { // chunk 4 + g is 64 bytes away: the places' third bit flips
-            return lds_read<bf16x8>(src + block / 4 * 64 * kRowBytes + 16 * j * kRowBytes +
-                                    (from[0] ^ (64 * h)));
+            return lds_read<bf16x8>(src + 16 * j * kRowBytes + (from[0] ^ (64 * h)));
         }
     }
 };
@@ -210,18 +212,11 @@ struct QTile {
     }
 };
 
-__device__ __forceinline__ void store4(const GradArgs& a, int64_t d, int c, f32x4 v)
-{
-    uint16_t* p = a.out + d * a.cols + c;
-    if (c + 4 <= a.cols) {
-        store_any(p, Pair{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])});
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (c + i < a.cols) p[i] = (uint16_t)bf16x2_rne(v[i], 0.0f);
-    }
-}
-
+// As in linear_i8.hip, a half step's products stand beside the reads of the
+// next, with one barrier a step.  LDS holds the int8 operand's bf16 tiles of two
+// steps and dy's of three: what is loaded to LDS in one step is awaited two
+// steps later.  The int8 tile of step s + 3 goes to registers in step s and to
+// LDS, scaled, in step s + 1.
 template <int kTile, bool kSumRows, bool kWhole>
 __global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradArgs a)
 {
@@ -232,39 +227,41 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradAr
     using Dy = DyTile<kTile, kSumRows, kWhole>;
     using Q = QTile<kTile, kWhole>;
     static_assert(Dy::kLoads <= kI && kI >= 4, "a part a row");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];
-    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0][0];
+    using Out = RowsOut<kI, 8>;
+    static_assert(Tile<kTile>::kWaves * 16 * kJ * Out::kRow <= 5 * kTileBytes, "results pass LDS");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[5][kTileBytes];
+    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0];
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // first block of 16 of this wave along c and d
     const int bc = wave / Tile<kTile>::kAcross * kI, bd = wave % Tile<kTile>::kAcross * kJ;
-    int td, tc;
-    tile_at(xcd_order(blockIdx.x, a.td * a.tc), a.td, a.tc, 8, td, tc);
-    const int d0 = td * kTile, c0 = tc * kTile;
+    const Piece piece = piece_of(a.grid, blockIdx.x);
+    const int d0 = piece.m * kTile, c0 = piece.n * kTile;
+    const int k0 = piece.first * kSum;
 
     f32x4 acc[kI][kJ] = {};
-    const Dy dy(a, d0);
+    const Dy dy(a, d0, bd);
     Q q(a, c0);
-    // As in linear_i8.hip: a half step's products beside the reads of the next,
-    // one barrier a step.  The int8 tile of step s + 2 is in registers by then.
-    auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
     struct Half {
         bf16x8 q[kI], y[kJ];
     };
-    // the products of a half, beside the reads of half h of step s and (load)
-    // the tiles of step s + 1, as whose int8 part q is written; past the sum's
-    // end all of that is zeros and unused
-    auto half = [&](const Half& f, int s, int h, Half& next, auto load) {
-        ROI_LDS uint8_t* src = buffer(s);
-        ROI_LDS uint8_t* dst = buffer(s + 1);
+    // the products of a half, beside the reads of half h of the step whose tiles
+    // are at qs and ys; kLoad: also q, loaded, is written to qd and loaded for
+    // sum index k, for which dy goes to yd.  Past the end of the sum or of this
+    // part all of that is in bounds or zeros, and unused.
+    auto half = [&](const Half& f, ROI_LDS uint8_t* qs, ROI_LDS uint8_t* ys, int h, Half& next,
+                    auto load, ROI_LDS uint8_t* qd, ROI_LDS uint8_t* yd, int k) {
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
-            if (i < kJ) next.y[i] = dy.read(src + kTileBytes, bd + i, i, h);
-            next.q[i] = q.read(src, bc + i, i, h);
+            if (i < kJ) next.y[i] = dy.read(ys, i, h);
+            next.q[i] = q.read(qs, bc + i, i, h);
             if constexpr (decltype(load)::value) {
-                if (i < Dy::kLoads) dy.stage(i, (s + 1) * kSum, dst + kTileBytes);
-                if (i % (kI / 4) == 0) q.write(i / (kI / 4), dst);
-                if (i == kI - 1) q.load((s + 2) * kSum);
+                if (i < 4) q.write(i, qd);
+                if (i == (kI > 4 ? 4 : 3)) q.load(k);
+                if (i == kI - 1) {
+#pragma unroll
+                    for (int l = 0; l < Dy::kLoads; ++l) dy.stage(l, k, yd);
+                }
             }
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
@@ -272,37 +269,100 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradAr
             keep_order();
         }
     };
-    if (a.steps > 0) {
+    if (piece.count > 0) {
         Half lo, hi;
+        ROI_LDS uint8_t *q0 = base, *q1 = base + kTileBytes; // of this step and the next
+        ROI_LDS uint8_t *y0 = base + 2 * kTileBytes, *y1 = y0 + kTileBytes, *y2 = y1 + kTileBytes;
+        {
+            Q second = q;
+            q.load(k0);
+            second.load(k0 + kSum);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+            for (int i = 0; i < Dy::kLoads; ++i) dy.stage(i, k0, y0);
 #pragma unroll
-            for (int i = 0; i < Dy::kLoads; ++i) dy.stage(i, s * kSum, buffer(s) + kTileBytes);
-            q.load(s * kSum);
+            for (int i = 0; i < Dy::kLoads; ++i) dy.stage(i, k0 + kSum, y1);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) q.write(b, buffer(s));
+            for (int b = 0; b < 4; ++b) q.write(b, q0);
+            q.load(k0 + 2 * kSum);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) second.write(b, q1);
         }
-        q.load(2 * kSum);
-        loads_barrier();
+        keep_order();
 #pragma unroll
-        for (int i = 0; i < kI; ++i) lo.q[i] = q.read(buffer(0), bc + i, i, 0);
+        for (int i = 0; i < Dy::kLoads; ++i) dy.stage(i, k0 + 2 * kSum, y2);
+        loads_barrier<Dy::kLoads>();
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) lo.y[j] = dy.read(buffer(0) + kTileBytes, bd + j, j, 0);
-        for (int s = 0; s < a.steps; ++s) {
-            half(lo, s, 1, hi, std::false_type{});
-            loads_barrier();
-            half(hi, s + 1, 0, lo, std::true_type{});
+        for (int i = 0; i < kI; ++i) lo.q[i] = q.read(q0, bc + i, i, 0);
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) lo.y[j] = dy.read(y0, j, 0);
+        for (int s = 0; s < piece.count; ++s) {
+            half(lo, q0, y0, 1, hi, std::false_type{}, q0, y0, 0);
+            loads_barrier<Dy::kLoads>();
+            half(hi, q1, y1, 0, lo, std::true_type{}, q0, y0, k0 + (s + 3) * kSum);
+            ROI_LDS uint8_t* const t = q0;
+            q0 = q1;
+            q1 = t;
+            ROI_LDS uint8_t* const u = y0;
+            y0 = y1;
+            y1 = y2;
+            y2 = u;
         }
         loads_barrier();
     }
+    if (piece.part >= 0) {
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) {
-        const int d = d0 + 16 * (bd + j) + (lane & 15);
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+            for (int j = 0; j < kJ; ++j)
+                *reinterpret_cast<f32x4*>(a.partial + part_at<kTile>(piece.part, wave, i, j, lane)) =
+                    acc[i][j];
+        return;
+    }
+    ROI_LDS uint8_t* mine = base + wave * (16 * kJ * Out::kRow);
+#pragma unroll
+    for (int j = 0; j < kJ; ++j)
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+            *reinterpret_cast<ROI_LDS u32x2*>(Out::at(mine, 16 * j + (lane & 15), i, g)) =
+                u32x2{bf16x2_rne(acc[i][j][0], acc[i][j][1]), bf16x2_rne(acc[i][j][2], acc[i][j][3])};
+#pragma unroll
+    for (int n = 0; n < 16 * kJ / Out::kAtOnce; ++n) {
+        int row, chunk;
+        const Quad v = Out::get(mine, n, row, chunk);
+        const int d = d0 + 16 * bd + row, c = c0 + 16 * bc + 8 * chunk;
+        if (d < a.D) store_chunk(a.out + (int64_t)d * a.cols, c, a.cols, v);
+    }
+}
+
+// The sums of the tiles that were cut: one wave for the 16 x 64 results that a
+// wave of the tile's kernel held at one i, the parts in their order.
+template <int kTile>
+__global__ __launch_bounds__(64) void grad_sum_kernel(GradArgs a)
+{
+    using T = Tile<kTile>;
+    const int lane = threadIdx.x, g = lane >> 4;
+    const int i = blockIdx.x % T::kI, wave = blockIdx.x / T::kI % T::kWaves;
+    const uint32_t tile = blockIdx.x / (T::kI * T::kWaves);
+    const Piece piece = tile_piece(a.grid, a.grid.full + tile);
+    f32x4 sum[T::kJ] = {};
+    for (uint32_t p = 0; p < a.grid.splits; ++p)
+#pragma unroll
+        for (int j = 0; j < T::kJ; ++j)
+            sum[j] += *reinterpret_cast<const f32x4*>(
+                a.partial + part_at<kTile>((int64_t)tile * a.grid.splits + p, wave, i, j, lane));
+    const int c = piece.n * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * g;
+#pragma unroll
+    for (int j = 0; j < T::kJ; ++j) {
+        const int d = piece.m * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
         if (d >= a.D) continue;
+        uint16_t* p = a.out + (int64_t)d * a.cols + c;
+        const Pair v{bf16x2_rne(sum[j][0], sum[j][1]), bf16x2_rne(sum[j][2], sum[j][3])};
+        if (c + 4 <= a.cols) {
+            store_any(p, v);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kI; ++i) {
-            const int c = c0 + 16 * (bc + i) + 4 * g;
-            if (c < a.cols) store4(a, d, c, acc[i][j]);
+            for (int e = 0; e < 4; ++e)
+                if (c + e < a.cols) p[e] = (uint16_t)(v.w[e / 2] >> (16 * (e % 2)));
         }
     }
 }
@@ -310,25 +370,24 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradAr
 template <int kTile, bool kSumRows>
 void launch_tiles(const GradArgs& a, hipStream_t stream)
 {
-    const dim3 grid(a.td * a.tc), block(Tile<kTile>::kThreads);
+    using T = Tile<kTile>;
+    const dim3 grid(a.grid.blocks()), block(T::kThreads);
     // 16-byte chunks of dy's rows and 4-byte words of q's that end with the row
     const bool whole = (kSumRows ? a.D : a.K) % 8 == 0 && a.cols % 4 == 0;
     if (whole)
         hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows, true>), grid, block, 0, stream, a);
     else
         hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows, false>), grid, block, 0, stream, a);
+    if (a.grid.rest() > 0)
+        hipLaunchKernelGGL((grad_sum_kernel<kTile>), dim3(a.grid.rest() * T::kI * T::kWaves), dim3(64),
+                           0, stream, a);
 }
 
 template <bool kSumRows>
-int launch(GradArgs a, const char* what, hipStream_t stream)
+int launch(GradArgs a, const Cut& c, const char* what, hipStream_t stream)
 {
-    const Cut c = cut_product(a.D, a.cols, a.K, kSum);
-    if (c.tm * c.tn > (int64_t)(0xFFFFFFFFu / Tile<256>::kThreads))
-        return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
-    a.td = (uint32_t)c.tm;
-    a.tc = (uint32_t)c.tn;
-    a.splits = 1;
-    a.steps = (int)c.steps;
+    if (!c.fits) return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
+    a.grid = Grid{(uint32_t)c.tm, (uint32_t)c.tn, (uint32_t)c.full, (uint32_t)c.splits, (int)c.steps};
     if (c.tile == 256)
         launch_tiles<256, kSumRows>(a, stream);
     else
@@ -336,11 +395,13 @@ int launch(GradArgs a, const char* what, hipStream_t stream)
     return launch_status(what);
 }
 
-int64_t workspace(int64_t tokens, int64_t rows, int64_t cols)
+Cut cut_weight(int64_t tokens, int64_t rows, int64_t cols)
 {
-    if (check_linear_sizes(tokens, rows, cols)) return -1;
-    ok();
-    return 0;
+    return cut_product(rows, cols, tokens, kSum, kGradCost);
+}
+Cut cut_input(int64_t tokens, int64_t rows, int64_t cols)
+{
+    return cut_product(tokens, cols, rows, kSum, kGradCost);
 }
 
 } // namespace
@@ -350,12 +411,16 @@ using namespace roi;
 
 extern "C" int64_t roi_linear_i8_grad_weight_workspace(int64_t tokens, int64_t rows, int64_t cols)
 {
-    return workspace(tokens, rows, cols);
+    if (check_linear_sizes(tokens, rows, cols)) return -1;
+    ok();
+    return cut_weight(tokens, rows, cols).bytes;
 }
 
 extern "C" int64_t roi_linear_i8_grad_input_workspace(int64_t tokens, int64_t rows, int64_t cols)
 {
-    return workspace(tokens, rows, cols);
+    if (check_linear_sizes(tokens, rows, cols)) return -1;
+    ok();
+    return cut_input(tokens, rows, cols).bytes;
 }
 
 extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* xq, const float* xs,
@@ -364,13 +429,15 @@ extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* x
                                          hipStream_t stream)
 {
     bool todo;
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    const Cut c = cut_weight(tokens, rows, cols);
     if (int st = validate_grad_i8(grad_y, xq, xs, tokens, tokens, rows, cols, grad_w, rows,
-                                  workspace, workspace_bytes, 0, &todo))
+                                  workspace, workspace_bytes, c.bytes, &todo))
         return st;
     if (!todo) return ok();
     const GradArgs a{grad_y, xq, xs, grad_w, static_cast<float*>(workspace), (int)tokens, (int)rows,
-                     (int)cols, 0, 0, 1, 0};
-    return launch<true>(a, "roi_linear_i8_grad_weight", stream);
+                     (int)cols, {}};
+    return launch<true>(a, c, "roi_linear_i8_grad_weight", stream);
 }
 
 extern "C" int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq, const float* ws,
@@ -379,11 +446,13 @@ extern "C" int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq
                                         hipStream_t stream)
 {
     bool todo;
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    const Cut c = cut_input(tokens, rows, cols);
     if (int st = validate_grad_i8(grad_y, wq, ws, rows, tokens, rows, cols, grad_x, tokens,
-                                  workspace, workspace_bytes, 0, &todo))
+                                  workspace, workspace_bytes, c.bytes, &todo))
         return st;
     if (!todo) return ok();
     const GradArgs a{grad_y, wq, ws, grad_x, static_cast<float*>(workspace), (int)rows, (int)tokens,
-                     (int)cols, 0, 0, 1, 0};
-    return launch<false>(a, "roi_linear_i8_grad_input", stream);
+                     (int)cols, {}};
+    return launch<false>(a, c, "roi_linear_i8_grad_input", stream);
 }

@@ -31,15 +31,26 @@ struct LinearArgs {
     const float* ws;
     const uint16_t* bias;
     void* y;
-    int* partial; // int32 [splits, tokens, rows]
+    int* partial; // int32 parts of tiles (part_at)
     int tokens, rows, cols;
-    uint32_t tm, tn, splits; // tiles along the rows and the tokens, parts of the sum
-    int steps;
+    Grid grid; // tiles along the rows and the tokens (few tokens: grid.tm alone)
 };
 
+// The scales of rows r .. r + 3, and what is added to their results: without a
+// bias -0, which changes nothing.
+__device__ __forceinline__ void row_scales(const LinearArgs& a, int r, float (&ws)[4],
+                                           float (&add)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int rc = least(r + e, a.rows - 1);
+        ws[e] = a.ws[rc];
+        add[e] = a.bias ? bf16_bits_to_float(a.bias[rc]) : -0.0f;
+    }
+}
+
 // Four results from their exact sums.  The scale of the weight comes first: sum
-// ws stays far from overflow for any weight.  Without a bias -0 is added, which
-// changes nothing.
+// ws stays far from overflow for any weight.
 __device__ __forceinline__ f32x4 finish4(i32x4 sum, const float (&ws)[4], const float (&add)[4],
                                          float xs)
 {
@@ -135,7 +146,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
     __shared__ i32x4 part[kFewWaves][kTok][64];
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r0 = blockIdx.x % a.tm * 16, t0 = blockIdx.x / a.tm * (16 * kTok);
+    const int r0 = blockIdx.x % a.grid.tm * 16, t0 = blockIdx.x / a.grid.tm * (16 * kTok);
     // rows and tokens past the end repeat the last one; their results are dropped
     const int64_t r = least(r0 + (lane & 15), a.rows - 1);
     const int8_t* wrow = a.w + r * (kPacked ? a.cols / 2 : a.cols);
@@ -167,12 +178,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
         const int t = t0 + 16 * j + (lane & 15), ro = r0 + 4 * g;
         if (t >= a.tokens || ro >= a.rows) continue;
         float ws[4], add[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int rc = least(ro + e, a.rows - 1);
-            ws[e] = a.ws[rc];
-            add[e] = a.bias ? bf16_bits_to_float(a.bias[rc]) : -0.0f;
-        }
+        row_scales(a, ro, ws, add);
         store4<Out>(a, t, ro, finish4(sum, ws, add, a.xs[t]));
     }
 }
@@ -210,7 +216,7 @@ struct KRows {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const bool live = row(i) < left && k + 16 * chunk() < len;
         if constexpr (kWhole)
-            load_to_lds(buffer_at(base + k), live ? at : kNowhere, i * (kThreads / 8) * len,
+            load_to_lds<false>(buffer_at(base + k), live ? at : kNowhere, i * (kThreads / 8) * len,
                         dst + (i * kThreads + wave * 64) * 16);
         else
             lds_write(dst + (i * kThreads + threadIdx.x) * 16,
@@ -229,9 +235,8 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(Line
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / Tile<kTile>::kAcross * 16 * kI, wn = wave % Tile<kTile>::kAcross * 16 * kJ;
-    int tm, tn;
-    tile_at(xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, 8, tm, tn);
-    const int r0 = tm * kTile, t0 = tn * kTile;
+    const Piece piece = piece_of(a.grid, blockIdx.x);
+    const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x4 acc[kI][kJ] = {};
     const KRows<kTile, kWhole> wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
@@ -241,9 +246,9 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(Line
     auto stage = [&](int s, int first, int count) {
         for (int i = first; i < first + count; ++i)
             if (i < kLoads)
-                wrows.stage(i, s * kRowBytes, buffer(s));
+                wrows.stage(i, (piece.first + s) * kRowBytes, buffer(s));
             else
-                xrows.stage(i - kLoads, s * kRowBytes, buffer(s) + kTileBytes);
+                xrows.stage(i - kLoads, (piece.first + s) * kRowBytes, buffer(s) + kTileBytes);
     };
     struct Half {
         i32x4 w[kI], x[kJ];
@@ -273,7 +278,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(Line
         }
     };
     static_assert(2 * kLoads % kI == 0, "loads are spread over the rows");
-    if (a.steps > 0) {
+    if (piece.count > 0) {
         Half lo, hi;
         stage(0, 0, 2 * kLoads);
         stage(1, 0, 2 * kLoads);
@@ -282,38 +287,87 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(Line
         for (int i = 0; i < kI; ++i) read_w(0, 0, lo, i);
 #pragma unroll
         for (int j = 0; j < kJ; ++j) read_x(0, 0, lo, j);
-        for (int s = 0; s < a.steps; ++s) {
+        for (int s = 0; s < piece.count; ++s) {
             half(lo, s, 1, hi, std::false_type{});
             loads_barrier();
             half(hi, s + 1, 0, lo, std::true_type{});
         }
         loads_barrier();
     }
+    if (piece.part >= 0) {
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+            for (int j = 0; j < kJ; ++j)
+                *reinterpret_cast<i32x4*>(a.partial + part_at<kTile>(piece.part, wave, i, j, lane)) =
+                    acc[i][j];
+        return;
+    }
     // every scale before the first store, which might overwrite one for all the
     // compiler knows
     float ws[kI][4], add[kI][4], xs[kJ];
 #pragma unroll
-    for (int i = 0; i < kI; ++i)
+    for (int i = 0; i < kI; ++i) row_scales(a, r0 + wm + 16 * i + 4 * g, ws[i], add[i]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int r = r0 + wm + 16 * i + 4 * g + e, rc = least(r, a.rows - 1);
-            ws[i][e] = a.ws[rc];
-            add[i][e] = a.bias ? bf16_bits_to_float(a.bias[rc]) : -0.0f;
+    for (int j = 0; j < kJ; ++j) xs[j] = a.xs[least(t0 + wn + 16 * j + (lane & 15), a.tokens - 1)];
+    // as many blocks of 16 tokens at a time as fit this wave's LDS
+    using Rows = RowsOut<kI, 4 * sizeof(Out)>;
+    constexpr int kAtATime = 4 * kTileBytes / Tile<kTile>::kWaves / (16 * Rows::kRow) < kJ
+                                 ? 4 * kTileBytes / Tile<kTile>::kWaves / (16 * Rows::kRow)
+                                 : kJ;
+    static_assert(kAtATime >= 1 && kJ % kAtATime == 0, "results pass LDS");
+    ROI_LDS uint8_t* mine = base + wave * (kAtATime * 16 * Rows::kRow);
+#pragma unroll
+    for (int first = 0; first < kJ; first += kAtATime) {
+#pragma unroll
+        for (int j = 0; j < kAtATime; ++j)
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+                const f32x4 v = finish4(acc[i][first + j], ws[i], add[i], xs[first + j]);
+                ROI_LDS uint8_t* at = Rows::at(mine, 16 * j + (lane & 15), i, g);
+                if constexpr (sizeof(Out) == 2)
+                    *reinterpret_cast<ROI_LDS u32x2*>(at) =
+                        u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
+                else
+                    *reinterpret_cast<ROI_LDS f32x4*>(at) = v;
+            }
+#pragma unroll
+        for (int n = 0; n < 16 * kAtATime / Rows::kAtOnce; ++n) {
+            int row, chunk;
+            const Quad v = Rows::get(mine, n, row, chunk);
+            const int t = t0 + wn + 16 * first + row;
+            const int r = r0 + wm + chunk * (int)(16 / sizeof(Out));
+            using Bits = std::conditional_t<sizeof(Out) == 2, uint16_t, uint32_t>;
+            if (t < a.tokens)
+                store_chunk(static_cast<Bits*>(a.y) + (int64_t)t * a.rows, r, a.rows, v);
         }
-#pragma unroll
-    for (int j = 0; j < kJ; ++j) {
-        const int t = t0 + wn + 16 * j + (lane & 15);
-        xs[j] = a.xs[least(t, a.tokens - 1)];
     }
+}
+
+// The sums of the tiles that were cut: one wave for the 16 x 64 results that a
+// wave of the tile's kernel held at one i.
+template <int kTile, typename Out>
+__global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
+{
+    using T = Tile<kTile>;
+    const int lane = threadIdx.x, g = lane >> 4;
+    const int i = blockIdx.x % T::kI, wave = blockIdx.x / T::kI % T::kWaves;
+    const uint32_t tile = blockIdx.x / (T::kI * T::kWaves);
+    const Piece piece = tile_piece(a.grid, a.grid.full + tile);
+    i32x4 sum[T::kJ] = {};
+    for (uint32_t p = 0; p < a.grid.splits; ++p)
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) {
-        const int t = t0 + wn + 16 * j + (lane & 15);
-        if (t >= a.tokens) continue;
+        for (int j = 0; j < T::kJ; ++j)
+            sum[j] += *reinterpret_cast<const i32x4*>(
+                a.partial + part_at<kTile>((int64_t)tile * a.grid.splits + p, wave, i, j, lane));
+    const int r = piece.m * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * g;
+    if (r >= a.rows) return;
+    float ws[4], add[4];
+    row_scales(a, r, ws, add);
 #pragma unroll
-        for (int i = 0; i < kI; ++i) {
-            const int r = r0 + wm + 16 * i + 4 * g;
-            if (r < a.rows) store4<Out>(a, t, r, finish4(acc[i][j], ws[i], add[i], xs[j]));
-        }
+    for (int j = 0; j < T::kJ; ++j) {
+        const int t = piece.n * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
+        if (t < a.tokens) store4<Out>(a, t, r, finish4(sum[j], ws, add, a.xs[t]));
     }
 }
 
@@ -323,22 +377,34 @@ bool fits(int64_t blocks, int threads) { return blocks <= (int64_t)(0xFFFFFFFFu 
 template <int kTile, typename Out>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
-    const dim3 grid(a.tm * a.tn), block(Tile<kTile>::kThreads);
+    using T = Tile<kTile>;
+    const dim3 grid(a.grid.blocks()), block(T::kThreads);
     if (a.cols % 16 == 0)
         hipLaunchKernelGGL((linear_tile_kernel<kTile, true, Out>), grid, block, 0, stream, a);
     else
         hipLaunchKernelGGL((linear_tile_kernel<kTile, false, Out>), grid, block, 0, stream, a);
+    if (a.grid.rest() > 0)
+        hipLaunchKernelGGL((linear_sum_kernel<kTile, Out>), dim3(a.grid.rest() * T::kI * T::kWaves),
+                           dim3(64), 0, stream, a);
+}
+
+// Whether the call takes the kernel for few tokens, which needs no workspace.
+bool few(int64_t tokens, bool packed) { return tokens <= 64 || packed; }
+
+Cut cut_linear(int64_t tokens, int64_t rows, int64_t cols)
+{
+    return cut_product(rows, tokens, cols, kRowBytes, kLinearCost);
 }
 
 template <typename Out>
 int launch(LinearArgs a, hipStream_t stream)
 {
-    if (a.tokens <= 64 || a.meta) {
+    if (few(a.tokens, a.meta)) {
         const int tok = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
         const int64_t tm = (a.rows + 15) / 16, tn = ((int64_t)a.tokens + 16 * tok - 1) / (16 * tok);
         if (!fits(tm * tn, 64 * kFewWaves))
             return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
-        a.tm = (uint32_t)tm;
+        a.grid.tm = (uint32_t)tm;
         const dim3 grid((unsigned)(tm * tn)), block(64 * kFewWaves);
         auto go = [&](auto dense, auto packed) {
             hipLaunchKernelGGL(a.meta ? packed : dense, grid, block, 0, stream, a);
@@ -351,13 +417,9 @@ int launch(LinearArgs a, hipStream_t stream)
             go(linear_few_kernel<4, false, Out>, linear_few_kernel<4, true, Out>);
         return launch_status("roi_linear_i8");
     }
-    const Cut c = cut_product(a.rows, a.tokens, a.cols, kRowBytes);
-    if (!fits(c.tm * c.tn, Tile<256>::kThreads))
-        return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
-    a.tm = (uint32_t)c.tm;
-    a.tn = (uint32_t)c.tn;
-    a.splits = 1;
-    a.steps = (int)c.steps;
+    const Cut c = cut_linear(a.tokens, a.rows, a.cols);
+    if (!c.fits) return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
+    a.grid = Grid{(uint32_t)c.tm, (uint32_t)c.tn, (uint32_t)c.full, (uint32_t)c.splits, (int)c.steps};
     if (c.tile == 256)
         launch_tiles<256, Out>(a, stream);
     else
@@ -374,7 +436,7 @@ extern "C" int64_t roi_linear_i8_workspace(int64_t tokens, int64_t rows, int64_t
 {
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
-    return 0;
+    return few(tokens, packed != 0) ? 0 : cut_linear(tokens, rows, cols).bytes;
 }
 
 extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq,
@@ -383,11 +445,14 @@ extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq
                              void* workspace, int64_t workspace_bytes, hipStream_t stream)
 {
     bool todo;
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    const int64_t need =
+        few(tokens, meta != nullptr) ? 0 : cut_linear(tokens, rows, cols).bytes;
     if (int st = validate_linear_i8(xq, xs, wq, meta, ws, bias, tokens, rows, cols, y, dtype,
-                                    workspace, workspace_bytes, 0, &todo))
+                                    workspace, workspace_bytes, need, &todo))
         return st;
     if (!todo) return ok();
-    LinearArgs a{xq, xs, wq, meta, ws, bias, y, static_cast<int*>(workspace), (int)tokens, (int)rows,
-                 (int)cols, 0, 0, 1, 0};
+    const LinearArgs a{xq, xs, wq, meta, ws, bias, y, static_cast<int*>(workspace), (int)tokens,
+                       (int)rows, (int)cols, {}};
     return dtype == ROI_BF16 ? launch<uint16_t>(a, stream) : launch<float>(a, stream);
 }

@@ -50,22 +50,36 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p)
 }
 
 // 16 bytes a lane from the buffer into LDS, lane l's at dst + 16 l (dst and
-// `more`, a further offset, are the same for the wave).
+// `more`, a further offset, are the same for the wave); loads_barrier() is what
+// waits for it.  kUnseen: in assembly, because the compiler has every transposing
+// LDS read wait for all loads to LDS that it knows of.  (It has no result
+// register.  The s_nop covers the wait states between a write of m0 or of a
+// scalar operand and this read.)  The compiler's own form is faster where it
+// serves: 8192^3 int8 402 us against 427.
+template <bool kUnseen>
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t offset,
                                             uint32_t more, ROI_LDS uint8_t* dst)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (ROI_LDS void*)dst, 16, (int)offset, (int)more, 0,
-                                             0);
+    if constexpr (kUnseen)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :
+                     : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src), "s"(more)
+                     : "memory");
+    else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (ROI_LDS void*)dst, 16, (int)offset, (int)more,
+                                                 0, 0);
 }
 
 __device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
 
-// A barrier past which what every wave has loaded to LDS is there: the barrier
-// itself waits for a wave's LDS operations only, and loads to LDS are counted
-// with the loads from memory.
+// A barrier past which what every wave has loaded to LDS is there, its last
+// kLater loads from memory apart: the barrier itself waits for a wave's LDS
+// operations only, and loads to LDS are counted with the loads from memory, in
+// their order.
+template <int kLater = 0>
 __device__ __forceinline__ void loads_barrier()
 {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLater) : "memory");
     __syncthreads();
 }
 
@@ -87,16 +101,92 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t b, uint32_t n)
     return x * q + (x < r ? x : r) + b / 8;
 }
 
-// Tile t of tm x tn, in bands of `band` tile rows, so that the tiles in flight
-// on an XCD form a block of few rows and columns.
-__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tm, uint32_t tn, uint32_t band,
-                                        int& m, int& n)
+// What a block does: steps first .. first + count - 1 of the sum of tile (m, n).
+// The first `full` tiles are whole; the others' sums are cut into `splits`
+// parts, of which this is number `part` (-1: a whole tile).  Blocks take the
+// tiles in bands of eight tile rows, so that the tiles in flight on an XCD form
+// a block of few rows and columns, and the parts of equal place in the sum
+// together.
+struct Grid {
+    uint32_t tm, tn, full, splits;
+    int steps;
+    __host__ __device__ uint32_t rest() const { return tm * tn - full; }
+    __host__ __device__ uint32_t blocks() const { return full + rest() * splits; }
+};
+struct Piece {
+    int m, n, first, count, part;
+};
+__device__ __forceinline__ Piece tile_piece(const Grid& g, uint32_t t)
 {
-    const uint32_t first = t / (band * tn) * band;
-    const uint32_t height = tm - first < band ? tm - first : band;
-    const uint32_t in = t - first * tn;
-    m = (int)(first + in % height);
-    n = (int)(in / height);
+    constexpr uint32_t kBand = 8;
+    const uint32_t first = t / (kBand * g.tn) * kBand;
+    const uint32_t height = g.tm - first < kBand ? g.tm - first : kBand;
+    const uint32_t in = t - first * g.tn;
+    return Piece{(int)(first + in % height), (int)(in / height), 0, g.steps, -1};
+}
+__device__ __forceinline__ Piece piece_of(const Grid& g, uint32_t block)
+{
+    if (block < g.full) return tile_piece(g, xcd_order(block, g.full));
+    const uint32_t b = xcd_order(block - g.full, g.rest() * g.splits);
+    const uint32_t i = b % g.rest(), j = b / g.rest();
+    Piece p = tile_piece(g, g.full + i);
+    p.first = (int)((int64_t)g.steps * j / g.splits);
+    p.count = (int)((int64_t)g.steps * (j + 1) / g.splits) - p.first;
+    p.part = (int)(i * g.splits + j);
+    return p;
+}
+
+// Where a wave's 16 x 16 results (i, j) of a part lie in the workspace: four
+// values a lane, in the order of the tile's threads.
+template <int kTile>
+__device__ __forceinline__ int64_t part_at(int64_t part, int wave, int i, int j, int lane)
+{
+    return part * (kTile * kTile) + (((wave * Tile<kTile>::kI + i) * Tile<kTile>::kJ + j) * 64 + lane) * 4;
+}
+
+// Results of a wave to memory, by way of its own part of LDS: a lane holds four
+// consecutive columns, and 16 lanes 16 different rows, so stored as they are
+// they would be 32-byte pieces; past LDS a wave stores whole rows.  kBytes: of
+// four results.  Chunk j of 16 bytes of row r is kept at place j ^ (r mod the
+// chunks of a row).
+template <int kI, int kBytes>
+struct RowsOut {
+    static constexpr int kChunks = kI * 4 * kBytes / 16; // of a row
+    static constexpr int kRow = kChunks * 16;
+    static constexpr int kAtOnce = 64 / kChunks;         // rows a wave stores at once
+    static_assert(kChunks >= 8 && kChunks <= 64, "rows of 128 to 1024 bytes");
+
+    // The results of block i for row `row` (of 16 lanes' rows), lane group g.
+    __device__ __forceinline__ static ROI_LDS uint8_t* at(ROI_LDS uint8_t* lds, int row, int i, int g)
+    {
+        const int byte = (4 * i + g) * kBytes;
+        return lds + row * kRow + ((byte / 16) ^ (row % kChunks)) * 16 + byte % 16;
+    }
+    // Store number n: this lane's row, its chunk, and the chunk's bytes.
+    __device__ __forceinline__ static Quad get(ROI_LDS uint8_t* lds, int n, int& row, int& chunk)
+    {
+        const int lane = threadIdx.x & 63;
+        row = n * kAtOnce + lane / kChunks;
+        chunk = lane % kChunks;
+        const u32x4 v = *reinterpret_cast<const ROI_LDS u32x4*>(
+            lds + row * kRow + (chunk ^ (row % kChunks)) * 16);
+        return Quad{v.x, v.y, v.z, v.w};
+    }
+};
+
+// Element first .. of a row that ends at `end`, from 16 bytes of T.
+template <typename T>
+__device__ __forceinline__ void store_chunk(T* row, int first, int end, const Quad& v)
+{
+    constexpr int kN = 16 / sizeof(T);
+    if (first + kN <= end) {
+        store_any(row + first, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e)
+            if (first + e < end)
+                row[first + e] = sizeof(T) == 2 ? (T)(v.w[e / 2] >> (16 * (e % 2))) : (T)v.w[e];
+    }
 }
 
 } // namespace roi
