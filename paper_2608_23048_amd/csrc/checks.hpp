@@ -122,6 +122,7 @@ struct TileCost {
     double step256, rest256, step128, rest128;
 };
 constexpr TileCost kLinearCost = {1.36, 12, 0.80, 9};
+constexpr TileCost kPackedCost = {0.80, 12, 0.60, 9};
 constexpr TileCost kGradCost = {1.70, 14, 1.60, 10};
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost);
 

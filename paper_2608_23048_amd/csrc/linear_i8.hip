@@ -191,39 +191,112 @@ __global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a
 // this step's buffer, which takes the step after the next, and the next step's
 // buffer, loading for a whole step, is complete.
 
-// The k-rows row0 .. of an operand of `n` rows of `len` bytes that this thread
-// brings to LDS.  kWhole: rows are whole 16-byte chunks.
-template <int kTile, bool kWhole>
-struct KRows {
+// Rows row0 .. of an operand of `n` rows of `len` bytes, kBytes of each, that
+// this thread brings to LDS.  Rows of 128 bytes lie as k-rows (mm.hpp); in rows
+// of 64, place j ^ spread(row) holds chunk j, so that 16 lanes reading the same
+// chunk of 16 rows cover all the LDS banks, and so do any aligned eight.
+// kWhole: rows are whole 16-byte chunks.
+template <int kTile, int kBytes, bool kWhole>
+struct Rows {
     static constexpr int kThreads = Tile<kTile>::kThreads;
-    static constexpr int kLoads = kTile * kRowBytes / (16 * kThreads);
+    static constexpr int kLoads = kTile * kBytes / (16 * kThreads);
+    static constexpr int kChunks = kBytes / 16;
     const uint8_t* base;
     int left, len; // rows from row0 on, and their bytes
     uint32_t at;   // byte offset of load 0 from base
 
-    __device__ __forceinline__ KRows(const int8_t* p, int row0, int n, int len_)
+    __device__ __forceinline__ Rows(const int8_t* p, int row0, int n, int len_)
         : base(reinterpret_cast<const uint8_t*>(p) + (int64_t)row0 * len_), left(n - row0),
           len(len_), at((uint32_t)row(0) * len_ + 16 * chunk())
     {
     }
+    __device__ __forceinline__ static int spread(int row)
+    {
+        return kChunks == 8 ? row & 7 : ((row >> 1) & 3) ^ ((row >> 3) & 1);
+    }
     // Row and chunk of this thread's load i (the chunk is the same for all: the
-    // rows differ by a multiple of eight).
-    __device__ __forceinline__ static int row(int i) { return (i * kThreads + (int)threadIdx.x) / 8; }
-    __device__ __forceinline__ static int chunk() { return (threadIdx.x % 8) ^ (row(0) & 7); }
-    // Load i of bytes k .. k + 127 of the rows; zeros past the end.
+    // rows differ by a multiple of sixteen).
+    __device__ __forceinline__ static int row(int i)
+    {
+        return (i * kThreads + (int)threadIdx.x) / kChunks;
+    }
+    __device__ __forceinline__ static int chunk() { return (threadIdx.x % kChunks) ^ spread(row(0)); }
+    // Load i of bytes k .. k + kBytes - 1 of the rows; zeros past the end.
     __device__ __forceinline__ void stage(int i, int k, ROI_LDS uint8_t* dst) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const bool live = row(i) < left && k + 16 * chunk() < len;
         if constexpr (kWhole)
-            load_to_lds<false>(buffer_at(base + k), live ? at : kNowhere, i * (kThreads / 8) * len,
-                        dst + (i * kThreads + wave * 64) * 16);
+            load_to_lds<false>(buffer_at(base + k), live ? at : kNowhere,
+                               i * (kThreads / kChunks) * len, dst + (i * kThreads + wave * 64) * 16);
         else
             lds_write(dst + (i * kThreads + threadIdx.x) * 16,
                       live ? load_row<Quad>(base + (int64_t)row(i) * len, k + 16 * chunk(), len)
                            : Quad{});
     }
 };
+
+// A tile's results from a wave's sums: a part of a cut tile as it is, else scaled
+// and through LDS (all of which is free) to y.
+template <int kTile, typename Out>
+__device__ __forceinline__ void write_tile(const LinearArgs& a, const Piece& piece,
+                                           const i32x4 (&acc)[Tile<kTile>::kI][Tile<kTile>::kJ],
+                                           ROI_LDS uint8_t* base)
+{
+    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r0 = piece.m * kTile + wave / Tile<kTile>::kAcross * 16 * kI;
+    const int t0 = piece.n * kTile + wave % Tile<kTile>::kAcross * 16 * kJ;
+    if (piece.part >= 0) {
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+            for (int j = 0; j < kJ; ++j)
+                *reinterpret_cast<i32x4*>(a.partial + part_at<kTile>(piece.part, wave, i, j, lane)) =
+                    acc[i][j];
+        return;
+    }
+    // every scale before the first store, which might overwrite one for all the
+    // compiler knows
+    float ws[kI][4], add[kI][4], xs[kJ];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) row_scales(a, r0 + 16 * i + 4 * g, ws[i], add[i]);
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) xs[j] = a.xs[least(t0 + 16 * j + (lane & 15), a.tokens - 1)];
+    // as many blocks of 16 tokens at a time as fit this wave's LDS
+    using Lines = RowsOut<kI, 4 * sizeof(Out)>;
+    constexpr int kAtATime = kTile * kRowBytes * 4 / Tile<kTile>::kWaves / (16 * Lines::kRow) < kJ
+                                 ? kTile * kRowBytes * 4 / Tile<kTile>::kWaves / (16 * Lines::kRow)
+                                 : kJ;
+    static_assert(kAtATime >= 1 && kJ % kAtATime == 0, "results pass LDS");
+    ROI_LDS uint8_t* mine = base + wave * (kAtATime * 16 * Lines::kRow);
+#pragma unroll
+    for (int first = 0; first < kJ; first += kAtATime) {
+#pragma unroll
+        for (int j = 0; j < kAtATime; ++j)
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+                const f32x4 v = finish4(acc[i][first + j], ws[i], add[i], xs[first + j]);
+                ROI_LDS uint8_t* at = Lines::at(mine, 16 * j + (lane & 15), i, g);
+                if constexpr (sizeof(Out) == 2)
+                    *reinterpret_cast<ROI_LDS u32x2*>(at) =
+                        u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
+                else
+                    *reinterpret_cast<ROI_LDS f32x4*>(at) = v;
+            }
+#pragma unroll
+        for (int n = 0; n < 16 * kAtATime / Lines::kAtOnce; ++n) {
+            int row, chunk;
+            const Quad v = Lines::get(mine, n, row, chunk);
+            const int t = t0 + 16 * first + row;
+            const int r = r0 + chunk * (int)(16 / sizeof(Out));
+            using Bits = std::conditional_t<sizeof(Out) == 2, uint16_t, uint32_t>;
+            if (t < a.tokens)
+                store_chunk(static_cast<Bits*>(a.y) + (int64_t)t * a.rows, r, a.rows, v);
+        }
+    }
+}
 
 template <int kTile, bool kWhole, typename Out>
 __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(LinearArgs a)
@@ -239,8 +312,9 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(Line
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x4 acc[kI][kJ] = {};
-    const KRows<kTile, kWhole> wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
-    constexpr int kLoads = KRows<kTile, kWhole>::kLoads;
+    using R = Rows<kTile, kRowBytes, kWhole>;
+    const R wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
+    constexpr int kLoads = R::kLoads;
     auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
     // loads `first` .. of step s, of the 2 kLoads that bring both tiles
     auto stage = [&](int s, int first, int count) {
@@ -294,54 +368,123 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(Line
         }
         loads_barrier();
     }
-    if (piece.part >= 0) {
-#pragma unroll
-        for (int i = 0; i < kI; ++i)
-#pragma unroll
-            for (int j = 0; j < kJ; ++j)
-                *reinterpret_cast<i32x4*>(a.partial + part_at<kTile>(piece.part, wave, i, j, lane)) =
-                    acc[i][j];
-        return;
-    }
-    // every scale before the first store, which might overwrite one for all the
-    // compiler knows
-    float ws[kI][4], add[kI][4], xs[kJ];
-#pragma unroll
-    for (int i = 0; i < kI; ++i) row_scales(a, r0 + wm + 16 * i + 4 * g, ws[i], add[i]);
-#pragma unroll
-    for (int j = 0; j < kJ; ++j) xs[j] = a.xs[least(t0 + wn + 16 * j + (lane & 15), a.tokens - 1)];
-    // as many blocks of 16 tokens at a time as fit this wave's LDS
-    using Rows = RowsOut<kI, 4 * sizeof(Out)>;
-    constexpr int kAtATime = 4 * kTileBytes / Tile<kTile>::kWaves / (16 * Rows::kRow) < kJ
-                                 ? 4 * kTileBytes / Tile<kTile>::kWaves / (16 * Rows::kRow)
-                                 : kJ;
-    static_assert(kAtATime >= 1 && kJ % kAtATime == 0, "results pass LDS");
-    ROI_LDS uint8_t* mine = base + wave * (kAtATime * 16 * Rows::kRow);
-#pragma unroll
-    for (int first = 0; first < kJ; first += kAtATime) {
-#pragma unroll
-        for (int j = 0; j < kAtATime; ++j)
-#pragma unroll
-            for (int i = 0; i < kI; ++i) {
-                const f32x4 v = finish4(acc[i][first + j], ws[i], add[i], xs[first + j]);
-                ROI_LDS uint8_t* at = Rows::at(mine, 16 * j + (lane & 15), i, g);
-                if constexpr (sizeof(Out) == 2)
-                    *reinterpret_cast<ROI_LDS u32x2*>(at) =
-                        u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
-                else
-                    *reinterpret_cast<ROI_LDS f32x4*>(at) = v;
+    write_tile<kTile, Out>(a, piece, acc, base);
+}
+
+// The same with 2:4 weights: a step of 128 columns is one instruction's sum, so
+// that a step's operands are read while the step before is multiplied, and a
+// step's tiles (64 bytes a weight row, its four metadata words, 128 bytes a
+// token) have two steps to arrive, in three LDS buffers.
+template <int kTile, typename Out>
+__global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_packed_kernel(LinearArgs a)
+{
+    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    constexpr int kThreads = Tile<kTile>::kThreads;
+    constexpr int kW = kTile * 64, kX = kTile * 128, kM = kTile * 16, kStage = kW + kX + kM;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[3][kStage];
+    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0];
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / Tile<kTile>::kAcross * 16 * kI, wn = wave % Tile<kTile>::kAcross * 16 * kJ;
+    const Piece piece = piece_of(a.grid, blockIdx.x);
+    const int r0 = piece.m * kTile, t0 = piece.n * kTile;
+
+    i32x4 acc[kI][kJ] = {};
+    using W = Rows<kTile, 64, true>;
+    using X = Rows<kTile, 128, true>;
+    const W wrows(a.w, r0, a.rows, a.cols / 2);
+    const X xrows(a.x, t0, a.tokens, a.cols);
+    // metadata: a word a lane, four words a row
+    constexpr int kMetaLoads = kTile * 4 / kThreads;
+    const int words = a.cols / 32, word = threadIdx.x % 4;
+    const uint32_t* meta = a.meta + (int64_t)r0 * words;
+    constexpr int kLoads = W::kLoads + X::kLoads + kMetaLoads;
+    static_assert(kLoads % kI == 0, "loads are spread over the rows");
+    auto stage = [&](int s, int first, int count, ROI_LDS uint8_t* dst) {
+        const int k = (piece.first + s) * 128;
+        for (int i = first; i < first + count; ++i) {
+            if (i < W::kLoads) {
+                wrows.stage(i, k / 2, dst);
+            } else if (i < W::kLoads + X::kLoads) {
+                xrows.stage(i - W::kLoads, k, dst + kW);
+            } else {
+                const int l = i - W::kLoads - X::kLoads;
+                const int row = (l * kThreads + (int)threadIdx.x) / 4;
+                const bool live = row < a.rows - r0 && k + 32 * word < a.cols;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    buffer_at(meta + k / 32),
+                    (ROI_LDS void*)(dst + kW + kX + (l * kThreads + wave * 64) * 4), 4,
+                    live ? 4 * (row * words + word) : (int)kNowhere, 0, 0, 0);
             }
-#pragma unroll
-        for (int n = 0; n < 16 * kAtATime / Rows::kAtOnce; ++n) {
-            int row, chunk;
-            const Quad v = Rows::get(mine, n, row, chunk);
-            const int t = t0 + wn + 16 * first + row;
-            const int r = r0 + wm + chunk * (int)(16 / sizeof(Out));
-            using Bits = std::conditional_t<sizeof(Out) == 2, uint16_t, uint32_t>;
-            if (t < a.tokens)
-                store_chunk(static_cast<Bits*>(a.y) + (int64_t)t * a.rows, r, a.rows, v);
         }
+    };
+    struct Step {
+        i32x4 w[kI];
+        int m[kI];
+        i32x8 x[kJ];
+    };
+    const int from_w = (wm + (lane & 15)) * 64 + (g ^ W::spread(lane & 15)) * 16;
+    const int from_m = kW + kX + (wm + (lane & 15)) * 16 + g * 4;
+    const int from_x = kW + (wn + (lane & 15)) * 128 + (g ^ X::spread(lane & 15)) * 16;
+    auto read_w = [&](ROI_LDS uint8_t* src, Step& f, int i) {
+        f.w[i] = lds_read<i32x4>(src + from_w + i * 16 * 64);
+        f.m[i] = lds_read<int>(src + from_m + i * 16 * 16);
+    };
+    auto read_x = [&](ROI_LDS uint8_t* src, Step& f, int j) {
+        const i32x4 lo = lds_read<i32x4>(src + from_x + j * 16 * 128);
+        const i32x4 hi = lds_read<i32x4>(src + (from_x ^ 64) + j * 16 * 128);
+        f.x[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // the products of a step, beside the reads of the next (at src) and the loads
+    // of step s, to dst; a block of tokens is read past the last product of the
+    // one before it (there are no registers for both)
+    auto step = [&](const Step& f, Step& next, ROI_LDS uint8_t* src, int s, ROI_LDS uint8_t* dst) {
+        constexpr int kPart = kLoads / kI;
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
+            read_w(src, next, i);
+            stage(s, i * kPart, kPart, dst);
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) {
+                acc[i][j] = __builtin_amdgcn_smfmac_i32_16x16x128_i8(f.w[i], f.x[j], acc[i][j],
+                                                                     f.m[i], 0, 0);
+                if (i == kI - 1) read_x(src, next, j);
+            }
+            keep_order();
+        }
+    };
+    if (piece.count > 0) {
+        ROI_LDS uint8_t *b0 = base, *b1 = base + kStage, *b2 = base + 2 * kStage;
+        Step even, odd;
+        stage(0, 0, kLoads, b0);
+        stage(1, 0, kLoads, b1);
+        stage(2, 0, kLoads, b2);
+        loads_barrier<2 * kLoads>();
+#pragma unroll
+        for (int i = 0; i < kI; ++i) read_w(b0, even, i);
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) read_x(b0, even, j);
+        // past the end of the sum or of this part, loads are in bounds or zeros,
+        // and unused
+        int s = 0;
+        for (; s + 2 <= piece.count; s += 2) {
+            loads_barrier<kLoads>();
+            step(even, odd, b1, s + 3, b0);
+            loads_barrier<kLoads>();
+            step(odd, even, b2, s + 4, b1);
+            ROI_LDS uint8_t* const t = b0;
+            b0 = b2;
+            b2 = b1;
+            b1 = t;
+        }
+        if (s < piece.count) {
+            loads_barrier<kLoads>();
+            step(even, odd, b1, s + 3, b0);
+        }
+        loads_barrier();
     }
+    static_assert(3 * kStage >= 4 * kTile * kRowBytes, "results pass LDS");
+    write_tile<kTile, Out>(a, piece, acc, base);
 }
 
 // The sums of the tiles that were cut: one wave for the 16 x 64 results that a
@@ -379,7 +522,9 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
     using T = Tile<kTile>;
     const dim3 grid(a.grid.blocks()), block(T::kThreads);
-    if (a.cols % 16 == 0)
+    if (a.meta)
+        hipLaunchKernelGGL((linear_packed_kernel<kTile, Out>), grid, block, 0, stream, a);
+    else if (a.cols % 16 == 0)
         hipLaunchKernelGGL((linear_tile_kernel<kTile, true, Out>), grid, block, 0, stream, a);
     else
         hipLaunchKernelGGL((linear_tile_kernel<kTile, false, Out>), grid, block, 0, stream, a);
@@ -389,17 +534,17 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
 }
 
 // Whether the call takes the kernel for few tokens, which needs no workspace.
-bool few(int64_t tokens, bool packed) { return tokens <= 64 || packed; }
+bool few(int64_t tokens) { return tokens <= 64; }
 
-Cut cut_linear(int64_t tokens, int64_t rows, int64_t cols)
+Cut cut_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
 {
-    return cut_product(rows, tokens, cols, kRowBytes, kLinearCost);
+    return cut_product(rows, tokens, cols, kRowBytes, packed ? kPackedCost : kLinearCost);
 }
 
 template <typename Out>
 int launch(LinearArgs a, hipStream_t stream)
 {
-    if (few(a.tokens, a.meta)) {
+    if (few(a.tokens)) {
         const int tok = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
         const int64_t tm = (a.rows + 15) / 16, tn = ((int64_t)a.tokens + 16 * tok - 1) / (16 * tok);
         if (!fits(tm * tn, 64 * kFewWaves))
@@ -417,7 +562,7 @@ int launch(LinearArgs a, hipStream_t stream)
             go(linear_few_kernel<4, false, Out>, linear_few_kernel<4, true, Out>);
         return launch_status("roi_linear_i8");
     }
-    const Cut c = cut_linear(a.tokens, a.rows, a.cols);
+    const Cut c = cut_linear(a.tokens, a.rows, a.cols, a.meta != nullptr);
     if (!c.fits) return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
     a.grid = Grid{(uint32_t)c.tm, (uint32_t)c.tn, (uint32_t)c.full, (uint32_t)c.splits, (int)c.steps};
     if (c.tile == 256)
@@ -436,7 +581,7 @@ extern "C" int64_t roi_linear_i8_workspace(int64_t tokens, int64_t rows, int64_t
 {
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
-    return few(tokens, packed != 0) ? 0 : cut_linear(tokens, rows, cols).bytes;
+    return few(tokens) ? 0 : cut_linear(tokens, rows, cols, packed != 0).bytes;
 }
 
 extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq,
@@ -447,7 +592,7 @@ extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq
     bool todo;
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
     const int64_t need =
-        few(tokens, meta != nullptr) ? 0 : cut_linear(tokens, rows, cols).bytes;
+        few(tokens) ? 0 : cut_linear(tokens, rows, cols, meta != nullptr).bytes;
     if (int st = validate_linear_i8(xq, xs, wq, meta, ws, bias, tokens, rows, cols, y, dtype,
                                     workspace, workspace_bytes, need, &todo))
         return st;

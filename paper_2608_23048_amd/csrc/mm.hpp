@@ -73,14 +73,13 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t
 __device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }
 
 // A barrier past which what every wave has loaded to LDS is there, its last
-// kLater loads from memory apart: the barrier itself waits for a wave's LDS
-// operations only, and loads to LDS are counted with the loads from memory, in
-// their order.
+// kLater loads from memory apart (loads to LDS are counted with the loads from
+// memory, in their order), and its other LDS operations are done.  Written out
+// because the compiler's barrier waits for all loads to LDS at some places.
 template <int kLater = 0>
 __device__ __forceinline__ void loads_barrier()
 {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLater) : "memory");
-    __syncthreads();
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
 }
 
 template <typename V>
@@ -116,13 +115,17 @@ struct Grid {
 struct Piece {
     int m, n, first, count, part;
 };
+// A value that is the same for the wave, in a scalar register (the divisions
+// below are done in vector ones).
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 __device__ __forceinline__ Piece tile_piece(const Grid& g, uint32_t t)
 {
     constexpr uint32_t kBand = 8;
     const uint32_t first = t / (kBand * g.tn) * kBand;
     const uint32_t height = g.tm - first < kBand ? g.tm - first : kBand;
     const uint32_t in = t - first * g.tn;
-    return Piece{(int)(first + in % height), (int)(in / height), 0, g.steps, -1};
+    return Piece{scalar((int)(first + in % height)), scalar((int)(in / height)), 0, g.steps, -1};
 }
 __device__ __forceinline__ Piece piece_of(const Grid& g, uint32_t block)
 {
@@ -130,9 +133,9 @@ __device__ __forceinline__ Piece piece_of(const Grid& g, uint32_t block)
     const uint32_t b = xcd_order(block - g.full, g.rest() * g.splits);
     const uint32_t i = b % g.rest(), j = b / g.rest();
     Piece p = tile_piece(g, g.full + i);
-    p.first = (int)((int64_t)g.steps * j / g.splits);
-    p.count = (int)((int64_t)g.steps * (j + 1) / g.splits) - p.first;
-    p.part = (int)(i * g.splits + j);
+    p.first = scalar((int)((int64_t)g.steps * j / g.splits));
+    p.count = scalar((int)((int64_t)g.steps * (j + 1) / g.splits)) - p.first;
+    p.part = scalar((int)(i * g.splits + j));
     return p;
 }
 
