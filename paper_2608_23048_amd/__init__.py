@@ -452,45 +452,49 @@ ROI_BF16, ROI_FP32 = 0, 1
 
 
 def _dtype_code(dtype, name="dtype"):
-    torch = _torch
-    if dtype is torch.bfloat16:
+    if dtype is _torch.bfloat16:
         return ROI_BF16
-    if dtype is torch.float32:
+    if dtype is _torch.float32:
         return ROI_FP32
     raise TypeError(f"{name} must be torch.bfloat16 or torch.float32, got {dtype}")
 
 
 def _check_sized(t, dtype, name, shape, device):
-    """_check_tensor, and the shape and the device that the other arguments imply."""
+    """_check_tensor, and the shape and the device index that the other arguments
+    imply."""
+    if (type(t) is _torch.Tensor and t.dtype is dtype and t.shape == shape
+            and t.get_device() == device and device >= 0 and t.is_contiguous()):
+        return
     _check_tensor(t, dtype, name)
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, expected device {device}")
 
 
-def _call(t, fn, *args):
-    """fn(*args, stream) on t's device and its current stream."""
-    torch, index = _torch, t.get_device()
-    if index == torch.cuda.current_device():
-        _raise_on(fn(*args, _stream(t)))
+def _call(device, fn, *args):
+    """fn(*args, stream) on a device and its current stream."""
+    if device == _torch._C._cuda_getDevice():
+        status = fn(*args, _raw_stream(device))
     else:
-        with torch.cuda.device(index):
-            _raise_on(fn(*args, _stream(t)))
+        with _torch.cuda.device(device):
+            status = fn(*args, _raw_stream(device))
+    if status:
+        _raise_on(status)
 
 
-def _workspace(given, need, device):
-    """(pointer, bytes) of a call's workspace; allocated when none is given."""
-    torch = _torch
-    if need < 0:
-        _raise_on(ROI_E_UNSUPPORTED)
+def _workspace(given, need, like):
+    """The workspace tensor (or None) and its bytes; allocated when none is given."""
     if given is None:
-        given = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        return given, _ptr(given), need
-    _check_tensor(given, torch.uint8, "workspace")
-    if given.device != device:
-        raise ValueError(f"workspace is on {given.device}, expected {device}")
-    return given, _ptr(given), given.numel()
+        if need > 0:
+            return _torch.empty(need, dtype=_torch.uint8, device=like.device), need
+        if need < 0:
+            _raise_on(ROI_E_UNSUPPORTED)
+        return None, 0
+    _check_tensor(given, _torch.uint8, "workspace")
+    if given.get_device() != like.get_device():
+        raise ValueError(f"workspace is on {given.device}, expected {like.device}")
+    return given, given.numel()
 
 
 def quantize_rows(x, out=None):
@@ -504,16 +508,19 @@ def quantize_rows(x, out=None):
     if not isinstance(x, torch.Tensor):
         raise TypeError("x must be a torch.Tensor")
     code = _dtype_code(x.dtype, "x")
-    _check_tensor(x, x.dtype, "x")
+    if not (x.is_cuda and x.is_contiguous()):
+        _check_tensor(x, x.dtype, "x")
     rows, cols = _shape2d(x)
+    device = x.get_device()
     if out is None:
-        q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+        q = torch.empty_like(x, dtype=torch.int8)
         scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
     else:
         q, scale = out
-        _check_sized(q, torch.int8, "q", x.shape, x.device)
-        _check_sized(scale, torch.float32, "scale", (rows,), x.device)
-    _call(x, lib().roi_quantize_rows, _ptr(x), code, rows, cols, _ptr(q), _ptr(scale))
+        _check_sized(q, torch.int8, "q", x.shape, device)
+        _check_sized(scale, torch.float32, "scale", (rows,), device)
+    _call(device, lib().roi_quantize_rows, x.data_ptr(), code, rows, cols, q.data_ptr(),
+          scale.data_ptr())
     return q, scale
 
 
@@ -523,14 +530,16 @@ def dequantize_rows(q, scale, dtype=None, out=None):
     torch = _torch or _load_torch()
     _check_tensor(q, torch.int8, "q")
     rows, cols = _shape2d(q)
-    _check_sized(scale, torch.float32, "scale", (rows,), q.device)
+    device = q.get_device()
+    _check_sized(scale, torch.float32, "scale", (rows,), device)
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
     code = _dtype_code(dtype)
     if out is None:
-        out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        out = torch.empty_like(q, dtype=dtype)
     else:
-        _check_sized(out, dtype, "out", q.shape, q.device)
-    _call(q, lib().roi_dequantize_rows, _ptr(q), _ptr(scale), rows, cols, _ptr(out), code)
+        _check_sized(out, dtype, "out", q.shape, device)
+    _call(device, lib().roi_dequantize_rows, q.data_ptr(), scale.data_ptr(), rows, cols,
+          out.data_ptr(), code)
     return out
 
 
@@ -547,29 +556,31 @@ def linear_i8(xq, xs, wq, ws, meta=None, bias=None, dtype=None, out=None, worksp
     _check_tensor(wq, torch.int8, "wq")
     if xq.dim() != 2 or wq.dim() != 2:
         raise ValueError("xq and wq must be 2-D")
-    (tokens, cols), rows, dev = xq.shape, wq.shape[0], xq.device
-    _check_sized(xs, torch.float32, "xs", (tokens,), dev)
-    _check_sized(ws, torch.float32, "ws", (rows,), dev)
-    if meta is None:
-        _check_sized(wq, torch.int8, "wq", (rows, cols), dev)
-    else:
+    (tokens, cols), (rows, held), device = xq.shape, wq.shape, xq.get_device()
+    _check_sized(xs, torch.float32, "xs", (tokens,), device)
+    _check_sized(ws, torch.float32, "ws", (rows,), device)
+    if wq.get_device() != device:
+        raise ValueError(f"wq is on {wq.device}, expected device {device}")
+    if meta is not None:
         if cols % 32:
             raise ValueError(f"2:4 weights need cols % 32 == 0 (got {cols})")
-        _check_sized(wq, torch.int8, "wq", (rows, cols // 2), dev)
-        _check_sized(meta, torch.int32, "meta", (rows * cols // 32,), dev)
+        _check_sized(meta, torch.int32, "meta", (rows * cols // 32,), device)
+    if held != (cols if meta is None else cols // 2):
+        raise ValueError(f"wq has shape {tuple(wq.shape)}, expected "
+                         f"{(rows, cols if meta is None else cols // 2)}")
     if bias is not None:
-        _check_sized(bias, torch.bfloat16, "bias", (rows,), dev)
+        _check_sized(bias, torch.bfloat16, "bias", (rows,), device)
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
     code = _dtype_code(dtype)
     if out is None:
-        out = torch.empty((tokens, rows), dtype=dtype, device=dev)
+        out = torch.empty((tokens, rows), dtype=dtype, device=xq.device)
     else:
-        _check_sized(out, dtype, "out", (tokens, rows), dev)
+        _check_sized(out, dtype, "out", (tokens, rows), device)
     L = lib()
-    _keep, ws_ptr, ws_bytes = _workspace(
-        workspace, L.roi_linear_i8_workspace(tokens, rows, cols, meta is not None), dev)
-    _call(xq, L.roi_linear_i8, _ptr(xq), _ptr(xs), _ptr(wq), _ptr(meta), _ptr(ws), _ptr(bias),
-          tokens, rows, cols, _ptr(out), code, ws_ptr, ws_bytes)
+    work, nbytes = _workspace(
+        workspace, L.roi_linear_i8_workspace(tokens, rows, cols, meta is not None), xq)
+    _call(device, L.roi_linear_i8, xq.data_ptr(), xs.data_ptr(), wq.data_ptr(), _ptr(meta),
+          ws.data_ptr(), _ptr(bias), tokens, rows, cols, out.data_ptr(), code, _ptr(work), nbytes)
     return out
 
 
@@ -591,19 +602,19 @@ def _grad_i8(name, grad_y, q, scale, by_tokens, out, workspace):
     _check_tensor(q, torch.int8, qname)
     if grad_y.dim() != 2 or q.dim() != 2:
         raise ValueError(f"grad_y and {qname} must be 2-D")
-    (tokens, rows), cols, dev = grad_y.shape, q.shape[1], grad_y.device
+    (tokens, rows), cols, device = grad_y.shape, q.shape[1], grad_y.get_device()
     summed, kept = (tokens, rows) if by_tokens else (rows, tokens)
-    _check_sized(q, torch.int8, qname, (summed, cols), dev)
-    _check_sized(scale, torch.float32, sname, (summed,), dev)
+    _check_sized(q, torch.int8, qname, (summed, cols), device)
+    _check_sized(scale, torch.float32, sname, (summed,), device)
     if out is None:
-        out = torch.empty((kept, cols), dtype=torch.bfloat16, device=dev)
+        out = torch.empty((kept, cols), dtype=torch.bfloat16, device=grad_y.device)
     else:
-        _check_sized(out, torch.bfloat16, "out", (kept, cols), dev)
+        _check_sized(out, torch.bfloat16, "out", (kept, cols), device)
     L = lib()
-    _keep, ws_ptr, ws_bytes = _workspace(
-        workspace, getattr(L, name + "_workspace")(tokens, rows, cols), dev)
-    _call(grad_y, getattr(L, name), _ptr(grad_y), _ptr(q), _ptr(scale), tokens, rows, cols,
-          _ptr(out), ws_ptr, ws_bytes)
+    work, nbytes = _workspace(workspace, getattr(L, name + "_workspace")(tokens, rows, cols),
+                              grad_y)
+    _call(device, getattr(L, name), grad_y.data_ptr(), q.data_ptr(), scale.data_ptr(), tokens,
+          rows, cols, out.data_ptr(), _ptr(work), nbytes)
     return out
 
 

@@ -333,9 +333,9 @@ constexpr double kSumLaunchUs = 4;
 
 // One tile size: the tiles of whole rounds over the units are whole.  The last
 // round's are cut if they fill half of it or less, so that all units have a
-// part.  *us: what the call is expected to take.
+// part.
 Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double step_us,
-              double rest_us, double* us)
+              double rest_us)
 {
     Cut c{};
     c.tile = tile;
@@ -347,7 +347,7 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double st
     const int64_t rest = tiles % slots;
     c.full = tiles;
     c.splits = 1;
-    *us = (double)((tiles + slots - 1) / slots) * whole;
+    c.us = (double)((tiles + slots - 1) / slots) * whole;
     // a part of a sum has four steps at least
     const int64_t splits =
         rest ? std::min(std::min(slots / rest, c.steps / 4), kMostSplits) : 1;
@@ -356,8 +356,8 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double st
         const double cut = (double)(tiles / slots) * whole +
                            (double)((c.steps + splits - 1) / splits) * step_us + rest_us +
                            part_bytes / kPartBytesPerUs + kSumLaunchUs;
-        if (cut < *us) {
-            *us = cut;
+        if (cut < c.us) {
+            c.us = cut;
             c.full = tiles - rest;
             c.splits = splits;
             c.bytes = rest * splits * tile * tile * 4;
@@ -372,10 +372,25 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double st
 
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost)
 {
-    double us256, us128;
-    const Cut big = cut_tiles(m, n, k, step, 256, cost.step256, cost.rest256, &us256);
-    const Cut small = cut_tiles(m, n, k, step, 128, cost.step128, cost.rest128, &us128);
-    return us128 < us256 && small.fits ? small : big;
+    const Cut big = cut_tiles(m, n, k, step, 256, cost.step256, cost.rest256);
+    const Cut small = cut_tiles(m, n, k, step, 128, cost.step128, cost.rest128);
+    return small.us < big.us && small.fits ? small : big;
+}
+
+// The streaming kernel takes 32 tokens at a time, each time at 7.5e6 bytes of a
+// dense weight a microsecond from the caches (6e6 at 2:4, of the dense weight it
+// stands for).  64 tokens through 3584 x 3584 take 5.6 us so and 17.5 in tiles,
+// through 18944 x 3584 25 and 29; 128 tokens 8.3 and 17.4, 44 and 30.
+LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
+{
+    LinearPlan p{};
+    p.few = tokens <= 32;
+    if (p.few) return p;
+    p.cut = cut_product(rows, tokens, cols, 128, packed ? kPackedCost : kLinearCost);
+    const double few_us = 3 + (double)((tokens + 31) / 32) * (double)rows * (double)cols /
+                                  (packed ? 6.0e6 : 7.5e6);
+    p.few = tokens <= 1024 && few_us < p.cut.us;
+    return p;
 }
 
 int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uint32_t* meta,

@@ -113,6 +113,7 @@ struct Cut {
     int64_t splits;
     int64_t steps; // of the whole sum
     int64_t bytes; // of workspace
+    double us;     // what the call is expected to take
     bool fits;     // fewer blocks than a launch takes
 };
 // Times of the tiled kernels in microseconds: a step of a 256-tile on every
@@ -121,10 +122,18 @@ struct Cut {
 struct TileCost {
     double step256, rest256, step128, rest128;
 };
-constexpr TileCost kLinearCost = {1.36, 12, 0.80, 9};
-constexpr TileCost kPackedCost = {0.80, 12, 0.60, 9};
+constexpr TileCost kLinearCost = {1.36, 12, 0.80, 6};
+constexpr TileCost kPackedCost = {0.80, 12, 0.60, 5};
 constexpr TileCost kGradCost = {1.70, 14, 1.60, 10};
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost);
+
+// The int8 product's way: with few tokens the kernel that streams the weight
+// past them (no workspace), else the tiles of `cut`.
+struct LinearPlan {
+    bool few;
+    Cut cut;
+};
+LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed);
 
 // Sizes of a linear call: ROI_OK, or why the call is refused.
 int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols);

@@ -84,102 +84,149 @@ __device__ __forceinline__ void store4(const LinearArgs& a, int64_t t, int r, f3
 }
 
 // ---------------------------------------------------------------- few tokens
-// A block owns 16 weight rows and up to 16 kTok tokens; its waves share out the
-// sum and add up their parts in LDS.  The weight is read once, straight into
-// the matrix instructions' operands: nothing of it is used twice.  Bound by the
-// weight's bytes.
-constexpr int kFewWaves = 8;
-
-// Operand chunk `k` .. k + 15 of a row of `len` bytes; kGuard: it may pass the
-// row's end, where the values are zero.
-template <bool kGuard>
-__device__ __forceinline__ i32x4 chunk16(const int8_t* row, int k, int len)
+// A block owns 16 kRow weight rows and up to kTokens (8, or a multiple of 16); its waves share out
+// the sum and add up their parts in LDS.  The weight is read once: bound by its
+// bytes.  A wave brings its steps of the sum (128 columns, 256 of a 2:4 weight)
+// to a ring of kDepth slots in LDS of its own and needs no barrier.  Through LDS,
+// because eight lanes then read 128 consecutive bytes of a row; operands loaded
+// straight to registers are 64 separate pieces of 16 bytes a load, and the
+// vector cache takes one a cycle: 14 us against NN for a token through the 2:4
+// 18944 x 3584 layer.
+template <int kWaves, int kRow, int kTokens, int kDepth, bool kPacked, bool kWhole, typename Out>
+__global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
 {
-    const uint8_t* p = reinterpret_cast<const uint8_t*>(row);
-    const Quad v = kGuard ? load_row<Quad>(p, k, len) : load_any<Quad>(p + k);
-    return i32x4{(int)v.w[0], (int)v.w[1], (int)v.w[2], (int)v.w[3]};
-}
+    constexpr int kTok = (kTokens + 15) / 16;
+    constexpr int kHalves = kPacked ? 2 : 1; // of 128 columns of x
+    constexpr int kXHalf = kTokens * 128;
+    constexpr int kW = kRow * 2048, kX = kHalves * kXHalf, kM = kPacked ? kRow * 512 : 0;
+    constexpr int kSlot = kW + kX + kM;
+    constexpr int kLoads = 2 * kRow + kTokens / 8 * kHalves + (kPacked ? 2 * kRow : 0);
+    constexpr int kColumns = 128 * kHalves;
+    static_assert(kRow * kTok * 1024 <= kDepth * kSlot, "the parts of the sum take the ring's place");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves][kDepth * kSlot];
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int wave = scalar(threadIdx.x >> 6);
+    ROI_LDS uint8_t* ring = (ROI_LDS uint8_t*)&lds[0][0] + wave * (kDepth * kSlot);
+    const int r0 = scalar(blockIdx.x % a.grid.tm) * (16 * kRow);
+    const int t0 = scalar(blockIdx.x / a.grid.tm) * kTokens;
 
-// One step of the sum: 128 columns of a dense weight, 256 of a 2:4 one.  A lane
-// reads 32 consecutive bytes of its row, as two operands; the sum's order
-// within the step is free, as long as both operands follow it.
-template <int kTok, bool kPacked, bool kGuard>
-__device__ __forceinline__ void few_step(const int8_t* wrow, const uint32_t* mrow,
-                                         const int8_t* const (&xrow)[kTok], int k, int cols,
-                                         int g, i32x4 (&acc)[kTok])
-{
-    if constexpr (!kPacked) {
+    // a load brings 128 bytes of eight rows: this lane's of the eight, its chunk
+    // of a row (kept at the place of k-rows, mm.hpp), and its metadata word
+    const int row = lane / 8, chunk = (lane % 8) ^ row, word = lane % 8;
+    const int wlen = kPacked ? a.cols / 2 : a.cols, words = a.cols / 32;
+    const uint8_t* wbase = reinterpret_cast<const uint8_t*>(a.w) + (int64_t)r0 * wlen;
+    const uint8_t* xbase = reinterpret_cast<const uint8_t*>(a.x) + (int64_t)t0 * a.cols;
+    const uint32_t* mbase = kPacked ? a.meta + (int64_t)r0 * words : nullptr;
+    auto bring = [&](const uint8_t* base, int first, int rows, int k, int len, ROI_LDS uint8_t* dst) {
+        const bool live = first + row < rows && k + 16 * chunk < len;
+        if constexpr (kWhole)
+            load_to_lds<false>(buffer_at(base + k),
+                               live ? (uint32_t)row * len + 16 * chunk : kNowhere, first * len, dst);
+        else
+            lds_write(dst + lane * 16, live ? load_row<Quad>(base + (int64_t)(first + row) * len,
+                                                             k + 16 * chunk, len)
+                                            : Quad{});
+    };
+    // step s of the sum (past its end: zeros) into a slot
+    auto stage = [&](int s, ROI_LDS uint8_t* slot) {
+        const int k = s * kColumns;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = k + 32 * g + 16 * h;
-            const i32x4 w = chunk16<kGuard>(wrow, c, cols);
+        for (int i = 0; i < 2 * kRow; ++i)
+            bring(wbase, 8 * i, a.rows - r0, k / kHalves, wlen, slot + i * 1024);
 #pragma unroll
-            for (int j = 0; j < kTok; ++j)
-                acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-                    w, chunk16<kGuard>(xrow[j], c, cols), acc[j], 0, 0, 0);
-        }
-    } else {
-        // instruction h: operand lane g holds the dense columns 64 g + 32 h ..
-        // + 31 of the step, so the second operand's lane g holds 16 columns at
-        // 64 (g / 2) + 32 h + 16 (g % 2) and 16 at 128 further on
+        for (int i = 0; i < kTokens / 8 * kHalves; ++i)
+            bring(xbase, 8 * (i / kHalves), a.tokens - t0, k + 128 * (i % kHalves), a.cols,
+                  slot + kW + (i % kHalves) * kXHalf + i / kHalves * 1024);
+        if constexpr (kPacked) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = k + 64 * g + 32 * h;
-            const i32x4 w = chunk16<kGuard>(wrow, c / 2, cols / 2);
-            const int idx = !kGuard || c < cols ? (int)mrow[c / 32] : 0x44444444;
-            const int b = k + 64 * (g / 2) + 32 * h + 16 * (g % 2);
-#pragma unroll
-            for (int j = 0; j < kTok; ++j) {
-                const i32x4 lo = chunk16<kGuard>(xrow[j], b, cols);
-                const i32x4 hi = chunk16<kGuard>(xrow[j], b + 128, cols);
-                const i32x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                acc[j] = __builtin_amdgcn_smfmac_i32_16x16x128_i8(w, x, acc[j], idx, 0, 0);
+            for (int i = 0; i < 2 * kRow; ++i) {
+                const bool live = 8 * i + row < a.rows - r0 && k + 32 * word < a.cols;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    buffer_at(mbase + k / 32), (ROI_LDS void*)(slot + kW + kX + i * 256), 4,
+                    live ? 4 * (row * words + word) : (int)kNowhere, 4 * 8 * i * words, 0, 0);
             }
         }
+    };
+    i32x4 acc[kRow][kTok] = {};
+    const int from = (lane & 15) * 128 + (g ^ (lane & 7)) * 16;
+    // of eight tokens, the second eight lanes read the first's again
+    const int from_x = (lane & (kTokens < 16 ? 7 : 15)) * 128 + (g ^ (lane & 7)) * 16;
+    auto multiply = [&](ROI_LDS uint8_t* slot) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) { // chunk 4 h + g: the place's third bit flips
+            i32x4 w[kRow];
+#pragma unroll
+            for (int i = 0; i < kRow; ++i) w[i] = lds_read<i32x4>(slot + i * 2048 + (from ^ (64 * h)));
+            if constexpr (kPacked) {
+                int m[kRow];
+                i32x8 x[kTok];
+#pragma unroll
+                for (int i = 0; i < kRow; ++i)
+                    m[i] = lds_read<int>(slot + kW + kX + i * 512 + (lane & 15) * 32 + h * 16 + g * 4);
+#pragma unroll
+                for (int j = 0; j < kTok; ++j) {
+                    ROI_LDS uint8_t* p = slot + kW + h * kXHalf + j * 2048;
+                    x[j] = __builtin_shufflevector(lds_read<i32x4>(p + from_x),
+                                                   lds_read<i32x4>(p + (from_x ^ 64)), 0, 1, 2, 3, 4, 5,
+                                                   6, 7);
+                }
+#pragma unroll
+                for (int i = 0; i < kRow; ++i)
+#pragma unroll
+                    for (int j = 0; j < kTok; ++j)
+                        acc[i][j] = __builtin_amdgcn_smfmac_i32_16x16x128_i8(w[i], x[j], acc[i][j],
+                                                                             m[i], 0, 0);
+            } else {
+                i32x4 x[kTok];
+#pragma unroll
+                for (int j = 0; j < kTok; ++j)
+                    x[j] = lds_read<i32x4>(slot + kW + j * 2048 + (from_x ^ (64 * h)));
+#pragma unroll
+                for (int i = 0; i < kRow; ++i)
+#pragma unroll
+                    for (int j = 0; j < kTok; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0,
+                                                                          0);
+            }
+        }
+    };
+    // step n of this wave is step wave + n kWaves of the sum
+    const int steps = (a.cols + kColumns - 1) / kColumns;
+    const int mine = steps > wave ? (steps - wave + kWaves - 1) / kWaves : 0;
+    if (mine > 0) {
+#pragma unroll
+        for (int n = 0; n < kDepth; ++n) stage(wave + n * kWaves, ring + n * kSlot);
+        int slot = 0;
+        for (int n = 0; n < mine; ++n) {
+            loads_wait<(kDepth - 1) * kLoads>();
+            multiply(ring + slot);
+            // the slot is read: its values are in registers before its next loads
+            keep_order();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            stage(wave + (n + kDepth) * kWaves, ring + slot);
+            slot = slot + kSlot < kDepth * kSlot ? slot + kSlot : 0;
+        }
+        loads_wait<0>();
     }
-}
-
-template <int kTok, bool kPacked, typename Out>
-__global__ __launch_bounds__(64 * kFewWaves) void linear_few_kernel(LinearArgs a)
-{
-    constexpr int kStep = kPacked ? 256 : 128;
-    __shared__ i32x4 part[kFewWaves][kTok][64];
-    const int lane = threadIdx.x & 63, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r0 = blockIdx.x % a.grid.tm * 16, t0 = blockIdx.x / a.grid.tm * (16 * kTok);
-    // rows and tokens past the end repeat the last one; their results are dropped
-    const int64_t r = least(r0 + (lane & 15), a.rows - 1);
-    const int8_t* wrow = a.w + r * (kPacked ? a.cols / 2 : a.cols);
-    const uint32_t* mrow = kPacked ? a.meta + r * (a.cols / 32) : nullptr;
-    const int8_t* xrow[kTok];
 #pragma unroll
-    for (int j = 0; j < kTok; ++j) {
-        xrow[j] = a.x + (int64_t)least(t0 + 16 * j + (lane & 15), a.tokens - 1) * a.cols;
-    }
-    i32x4 acc[kTok] = {};
-    const int whole = a.cols / kStep;
-    int s = wave;
-    for (; s + 3 * kFewWaves < whole; s += 4 * kFewWaves)
+    for (int i = 0; i < kRow; ++i)
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            few_step<kTok, kPacked, false>(wrow, mrow, xrow, (s + u * kFewWaves) * kStep, a.cols, g,
-                                           acc);
-    for (; s < whole; s += kFewWaves)
-        few_step<kTok, kPacked, false>(wrow, mrow, xrow, s * kStep, a.cols, g, acc);
-    if (whole * kStep < a.cols && wave == whole % kFewWaves)
-        few_step<kTok, kPacked, true>(wrow, mrow, xrow, whole * kStep, a.cols, g, acc);
-#pragma unroll
-    for (int j = 0; j < kTok; ++j) part[wave][j][lane] = acc[j];
+        for (int j = 0; j < kTok; ++j)
+            *reinterpret_cast<ROI_LDS i32x4*>(ring + ((i * kTok + j) * 64 + lane) * 16) = acc[i][j];
     __syncthreads();
-    for (int j = wave; j < kTok; j += kFewWaves) {
+    for (int b = wave; b < kRow * kTok; b += kWaves) {
+        const int in = 16 * (b % kTok) + (lane & 15);
+        const int t = t0 + in, r = r0 + 16 * (b / kTok) + 4 * g;
+        if (in >= kTokens || t >= a.tokens || r >= a.rows) continue;
+        float ws[4], add[4];
+        row_scales(a, r, ws, add);
+        const float xs = a.xs[t];
         i32x4 sum = {};
 #pragma unroll
-        for (int v = 0; v < kFewWaves; ++v) sum += part[v][j][lane];
-        const int t = t0 + 16 * j + (lane & 15), ro = r0 + 4 * g;
-        if (t >= a.tokens || ro >= a.rows) continue;
-        float ws[4], add[4];
-        row_scales(a, ro, ws, add);
-        store4<Out>(a, t, ro, finish4(sum, ws, add, a.xs[t]));
+        for (int v = 0; v < kWaves; ++v)
+            sum += lds_read<i32x4>((ROI_LDS uint8_t*)&lds[0][0] + v * (kDepth * kSlot) +
+                                   (b * 64 + lane) * 16);
+        store4<Out>(a, t, r, finish4(sum, ws, add, xs));
     }
 }
 
@@ -514,9 +561,6 @@ __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
     }
 }
 
-// Blocks of one launch: fewer than 2^32 threads.
-bool fits(int64_t blocks, int threads) { return blocks <= (int64_t)(0xFFFFFFFFu / (uint32_t)threads); }
-
 template <int kTile, typename Out>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
@@ -533,36 +577,43 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
                            dim3(64), 0, stream, a);
 }
 
-// Whether the call takes the kernel for few tokens, which needs no workspace.
-bool few(int64_t tokens) { return tokens <= 64; }
-
-Cut cut_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
+template <int kWaves, int kRow, int kTokens, int kDepth, bool kPacked, typename Out>
+int launch_few_as(LinearArgs a, hipStream_t stream)
 {
-    return cut_product(rows, tokens, cols, kRowBytes, packed ? kPackedCost : kLinearCost);
+    const int64_t tm = ((int64_t)a.rows + 16 * kRow - 1) / (16 * kRow);
+    const int64_t tn = ((int64_t)a.tokens + kTokens - 1) / kTokens;
+    a.grid.tm = (uint32_t)tm; // few tokens and fewer than 2^22 rows: a launch has room
+    const dim3 grid((unsigned)(tm * tn)), block(64 * kWaves);
+    if (a.cols % 16 == 0)
+        hipLaunchKernelGGL((linear_few_kernel<kWaves, kRow, kTokens, kDepth, kPacked, true, Out>), grid,
+                           block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((linear_few_kernel<kWaves, kRow, kTokens, kDepth, false, false, Out>), grid,
+                           block, 0, stream, a); // never 2:4: that has whole words
+    return launch_status("roi_linear_i8");
+}
+
+template <bool kPacked, typename Out>
+int launch_few(const LinearArgs& a, hipStream_t stream)
+{
+    if (a.tokens > 16) return launch_few_as<4, 2, 32, 2, kPacked, Out>(a, stream);
+    // With at least two blocks a compute unit a shallow ring lets more of them
+    // run at once: one token through 18944 x 3584 at 2:4 takes 11.2 us with two
+    // slots and 13.8 with three, through 3584 x 18944 13.2 and 10.5.
+    const bool many = a.rows >= 16 * 512;
+    if (a.tokens > 8)
+        return many ? launch_few_as<4, 1, 16, 2, kPacked, Out>(a, stream)
+                    : launch_few_as<4, 1, 16, 3, kPacked, Out>(a, stream);
+    return many ? launch_few_as<4, 1, 8, 2, kPacked, Out>(a, stream)
+                : launch_few_as<4, 1, 8, 3, kPacked, Out>(a, stream);
 }
 
 template <typename Out>
-int launch(LinearArgs a, hipStream_t stream)
+int launch(LinearArgs a, const LinearPlan& plan, hipStream_t stream)
 {
-    if (few(a.tokens)) {
-        const int tok = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-        const int64_t tm = (a.rows + 15) / 16, tn = ((int64_t)a.tokens + 16 * tok - 1) / (16 * tok);
-        if (!fits(tm * tn, 64 * kFewWaves))
-            return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
-        a.grid.tm = (uint32_t)tm;
-        const dim3 grid((unsigned)(tm * tn)), block(64 * kFewWaves);
-        auto go = [&](auto dense, auto packed) {
-            hipLaunchKernelGGL(a.meta ? packed : dense, grid, block, 0, stream, a);
-        };
-        if (tok == 1)
-            go(linear_few_kernel<1, false, Out>, linear_few_kernel<1, true, Out>);
-        else if (tok == 2)
-            go(linear_few_kernel<2, false, Out>, linear_few_kernel<2, true, Out>);
-        else
-            go(linear_few_kernel<4, false, Out>, linear_few_kernel<4, true, Out>);
-        return launch_status("roi_linear_i8");
-    }
-    const Cut c = cut_linear(a.tokens, a.rows, a.cols, a.meta != nullptr);
+    if (plan.few)
+        return a.meta ? launch_few<true, Out>(a, stream) : launch_few<false, Out>(a, stream);
+    const Cut& c = plan.cut;
     if (!c.fits) return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
     a.grid = Grid{(uint32_t)c.tm, (uint32_t)c.tn, (uint32_t)c.full, (uint32_t)c.splits, (int)c.steps};
     if (c.tile == 256)
@@ -581,7 +632,8 @@ extern "C" int64_t roi_linear_i8_workspace(int64_t tokens, int64_t rows, int64_t
 {
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
-    return few(tokens) ? 0 : cut_linear(tokens, rows, cols, packed != 0).bytes;
+    const LinearPlan plan = plan_linear(tokens, rows, cols, packed != 0);
+    return plan.few ? 0 : plan.cut.bytes;
 }
 
 extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq,
@@ -591,13 +643,12 @@ extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq
 {
     bool todo;
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
-    const int64_t need =
-        few(tokens) ? 0 : cut_linear(tokens, rows, cols, meta != nullptr).bytes;
+    const LinearPlan plan = plan_linear(tokens, rows, cols, meta != nullptr);
     if (int st = validate_linear_i8(xq, xs, wq, meta, ws, bias, tokens, rows, cols, y, dtype,
-                                    workspace, workspace_bytes, need, &todo))
+                                    workspace, workspace_bytes, plan.few ? 0 : plan.cut.bytes, &todo))
         return st;
     if (!todo) return ok();
     const LinearArgs a{xq, xs, wq, meta, ws, bias, y, static_cast<int*>(workspace), (int)tokens,
                        (int)rows, (int)cols, {}};
-    return dtype == ROI_BF16 ? launch<uint16_t>(a, stream) : launch<float>(a, stream);
+    return dtype == ROI_BF16 ? launch<uint16_t>(a, plan, stream) : launch<float>(a, plan, stream);
 }

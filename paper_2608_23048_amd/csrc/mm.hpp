@@ -82,6 +82,13 @@ __device__ __forceinline__ void loads_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
 }
 
+// The wait alone, for what a wave has loaded to its own part of LDS.
+template <int kLater>
+__device__ __forceinline__ void loads_wait()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLater) : "memory");
+}
+
 template <typename V>
 __device__ __forceinline__ V lds_read(const ROI_LDS uint8_t* p)
 {

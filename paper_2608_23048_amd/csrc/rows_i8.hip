@@ -71,23 +71,30 @@ __device__ __forceinline__ uint32_t max_bits(const Eight<T>& e, uint32_t m)
     return m;
 }
 
+// rint(fl(x inv)) of four elements, a byte each.  Adding 1.5 2^23 rounds the
+// product to an integer, ties to even, and leaves it in the sum's low bits.
+template <typename T>
+__device__ __forceinline__ uint32_t quantize4(const Eight<T>& e, int first, float inv)
+{
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(e.get(first + i) * inv + 0x1.8p23f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0C0C0400),
+                                 __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400), 0x05040100);
+}
+
 template <typename T>
 __device__ __forceinline__ void store_quantized(const Eight<T>& e, float inv, bool finite,
                                                 int8_t* row, int64_t c, int64_t cols)
 {
-    uint32_t p[2] = {0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int v = finite ? (int)__builtin_rintf(e.get(i) * inv) : 0;
-        p[i / 4] |= (uint32_t)(v & 0xFF) << (8 * (i % 4));
-    }
+    Pair p{finite ? quantize4(e, 0, inv) : 0, finite ? quantize4(e, 4, inv) : 0};
     const int64_t k = 8 * c;
     if (k + 8 <= cols) {
-        store_any(row + k, Pair{p[0], p[1]});
+        store_any(row + k, p);
     } else if (k < cols) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (k + i < cols) row[k + i] = (int8_t)(p[i / 4] >> (8 * (i % 4)));
+            if (k + i < cols) row[k + i] = (int8_t)(p.w[i / 4] >> (8 * (i % 4)));
     }
 }
 
@@ -228,6 +235,8 @@ void quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols, h
         launch_quantize<T, 1, 4>(x, q, scale, rows, cols, stream);
     else if (cols <= 256 * 8 * 4)
         launch_quantize<T, 4, 4>(x, q, scale, rows, cols, stream);
+    else if (cols <= 512 * 8 * 3)
+        launch_quantize<T, 8, 3>(x, q, scale, rows, cols, stream);
     else if (cols <= 1024 * 8 * 4)
         launch_quantize<T, 16, 4>(x, q, scale, rows, cols, stream);
     else
