@@ -393,6 +393,27 @@ LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
     return p;
 }
 
+GradPlan plan_grad(int64_t m, int64_t n, int64_t k)
+{
+    constexpr int64_t kStep = 64;
+    GradPlan p{};
+    p.cut = cut_product(m, n, k, kStep, kGradCost);
+    p.bytes = p.cut.bytes;
+    // offsets within a tile of the transposed operand stay below 2^31
+    if (m == 0 || n == 0 || k == 0 || k > ((int64_t)1 << 21)) return p;
+    const int64_t ready_k = (k + kStep - 1) / kStep * kStep;
+    const Cut c = cut_tiles(m, n, k, kStep, 256, kReadyStep, kReadyRest);
+    const double us = c.us + 3 + 3 * (double)ready_k * (double)n / 4.0e6;
+    if (us < p.cut.us && c.fits) {
+        p.ready = true;
+        p.ready_k = ready_k;
+        p.ready_bytes = (2 * n * ready_k + 255) / 256 * 256;
+        p.cut = c;
+        p.bytes = p.ready_bytes + c.bytes;
+    }
+    return p;
+}
+
 int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uint32_t* meta,
                        const float* ws, const uint16_t* bias, int64_t tokens, int64_t rows,
                        int64_t cols, const void* y, int dtype, const void* workspace,

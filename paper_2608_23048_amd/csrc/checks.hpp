@@ -125,6 +125,7 @@ struct TileCost {
 constexpr TileCost kLinearCost = {1.36, 12, 0.80, 6};
 constexpr TileCost kPackedCost = {0.80, 12, 0.60, 5};
 constexpr TileCost kGradCost = {1.70, 14, 1.60, 10};
+constexpr double kReadyStep = 1.40, kReadyRest = 12; // of a 256-tile with both operands in bf16
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost);
 
 // The int8 product's way: with few tokens the kernel that streams the weight
@@ -134,6 +135,17 @@ struct LinearPlan {
     Cut cut;
 };
 LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed);
+
+// A gradient's way (out [m, n], summed over k): with `ready` the int8 operand is
+// first written to the workspace in bf16, transposed, [n, ready_k]; the parts of
+// cut tiles follow it.
+struct GradPlan {
+    bool ready;
+    int64_t ready_k, ready_bytes;
+    int64_t bytes; // of workspace
+    Cut cut;
+};
+GradPlan plan_grad(int64_t m, int64_t n, int64_t k);
 
 // Sizes of a linear call: ROI_OK, or why the call is refused.
 int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols);

@@ -40,6 +40,8 @@ struct GradArgs {
     const float* scale;
     uint16_t* out;
     float* partial; // fp32 parts of tiles (part_at)
+    uint16_t* ready; // s q, transposed: bf16 [cols, ready_k], or NULL
+    int ready_k;     // K rounded up to whole steps
     int K, D, cols;
     Grid grid; // tiles along d and c
 };
@@ -48,7 +50,7 @@ struct GradArgs {
 // row k at place j ^ 2 (k & 3) ^ (k & 8), so that the rows that 32 lanes read
 // together (four of each of two groups of 16) lie in different banks.  Otherwise [kTile d] k-rows (mm.hpp).
 // What lies past K is zero; past D, zero or the last row again.
-template <int kTile, bool kSumRows, bool kWhole>
+template <int kTile, bool kSumRows, bool kWhole, bool kUnseen = kSumRows>
 struct DyTile {
     static constexpr int kThreads = Tile<kTile>::kThreads;
     static constexpr int kLoads = kTile * kRowBytes / (16 * kThreads);
@@ -59,9 +61,9 @@ struct DyTile {
     int from[kSumRows ? 4 : 1]; // where read() starts, by block of 16 columns
 
     // block: the wave's first of 16 columns
-    __device__ __forceinline__ DyTile(const GradArgs& a, int d0_, int block)
-        : base(reinterpret_cast<const uint8_t*>(a.dy) + 2 * (kSumRows ? d0_ : (int64_t)d0_ * a.K)),
-          K(a.K), D(a.D), d0(d0_)
+    __device__ __forceinline__ DyTile(const uint16_t* p, int K_, int D_, int d0_, int block)
+        : base(reinterpret_cast<const uint8_t*>(p) + 2 * (kSumRows ? d0_ : (int64_t)d0_ * K_)),
+          K(K_), D(D_), d0(d0_)
     {
         at = 2 * ((uint32_t)row(0) * width() + 8 * chunk());
         if (kSumRows && 8 * chunk() >= D - d0) at = kNowhere;
@@ -100,7 +102,7 @@ struct DyTile {
         const bool live = row(i) < (kSumRows ? K - k0 : D - d0) &&
                           (kSumRows || 8 * chunk() < K - k0);
         if constexpr (kWhole) {
-            load_to_lds<kSumRows>(buffer_at(p), live ? at : kNowhere,
+            load_to_lds<kUnseen>(buffer_at(p), live ? at : kNowhere,
                                   2 * (i * kThreads / kAcrossRow) * width(),
                                   dst + (i * kThreads + wave * 64) * 16);
         } else {
@@ -212,6 +214,44 @@ struct QTile {
     }
 };
 
+// A tile's results from a wave's sums: a part of a cut tile as it is, else in
+// bf16 and through LDS (all of which is free) to out.
+template <int kTile>
+__device__ __forceinline__ void write_tile(const GradArgs& a, const Piece& piece,
+                                           const f32x4 (&acc)[Tile<kTile>::kI][Tile<kTile>::kJ],
+                                           ROI_LDS uint8_t* base)
+{
+    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int wave = scalar(threadIdx.x >> 6);
+    const int bc = wave / Tile<kTile>::kAcross * kI, bd = wave % Tile<kTile>::kAcross * kJ;
+    const int d0 = piece.m * kTile, c0 = piece.n * kTile;
+    if (piece.part >= 0) {
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+            for (int j = 0; j < kJ; ++j)
+                *reinterpret_cast<f32x4*>(a.partial + part_at<kTile>(piece.part, wave, i, j, lane)) =
+                    acc[i][j];
+        return;
+    }
+    using Out = RowsOut<kI, 8>;
+    ROI_LDS uint8_t* mine = base + wave * (16 * kJ * Out::kRow);
+#pragma unroll
+    for (int j = 0; j < kJ; ++j)
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+            *reinterpret_cast<ROI_LDS u32x2*>(Out::at(mine, 16 * j + (lane & 15), i, g)) =
+                u32x2{bf16x2_rne(acc[i][j][0], acc[i][j][1]), bf16x2_rne(acc[i][j][2], acc[i][j][3])};
+#pragma unroll 2 // code that runs once is fetched once: it is kept short
+    for (int n = 0; n < 16 * kJ / Out::kAtOnce; ++n) {
+        int row, chunk;
+        const Quad v = Out::get(mine, n, row, chunk);
+        const int d = d0 + 16 * bd + row, c = c0 + 16 * bc + 8 * chunk;
+        if (d < a.D) store_chunk(a.out + (int64_t)d * a.cols, c, a.cols, v);
+    }
+}
+
 // As in linear_i8.hip, a half step's products stand beside the reads of the
 // next, with one barrier a step.  LDS holds the int8 operand's bf16 tiles of two
 // steps and dy's of three: what is loaded to LDS in one step is awaited two
@@ -227,11 +267,8 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradAr
     using Dy = DyTile<kTile, kSumRows, kWhole>;
     using Q = QTile<kTile, kWhole>;
     static_assert(Dy::kLoads <= kI && kI >= 4, "a part a row");
-    using Out = RowsOut<kI, 8>;
-    static_assert(Tile<kTile>::kWaves * 16 * kJ * Out::kRow <= 5 * kTileBytes, "results pass LDS");
     __shared__ __attribute__((aligned(16))) uint8_t lds[5][kTileBytes];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0];
-    const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // first block of 16 of this wave along c and d
     const int bc = wave / Tile<kTile>::kAcross * kI, bd = wave % Tile<kTile>::kAcross * kJ;
@@ -240,7 +277,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradAr
     const int k0 = piece.first * kSum;
 
     f32x4 acc[kI][kJ] = {};
-    const Dy dy(a, d0, bd);
+    const Dy dy(a.dy, a.K, a.D, d0, bd);
     Q q(a, c0);
     struct Half {
         bf16x8 q[kI], y[kJ];
@@ -309,28 +346,99 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradAr
         }
         loads_barrier();
     }
-    if (piece.part >= 0) {
+    write_tile<kTile>(a, piece, acc, base);
+}
+
+// The same for both operands in bf16 (a.ready): nothing passes registers on its
+// way to LDS, which holds both tiles of two steps.  A step takes NN us where the
+// conversion beside it takes 1.7; the conversion by itself is one pass over q.
+template <bool kSumRows, bool kWhole>
+__global__ __launch_bounds__(Tile<256>::kThreads) void grad_ready_kernel(GradArgs a)
+{
+    constexpr int kTile = 256, kTileBytes = kTile * kRowBytes;
+    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    using Dy = DyTile<kTile, kSumRows, kWhole>;
+    using Q = DyTile<kTile, false, true, kSumRows>;
+    constexpr int kLoads = Dy::kLoads + Q::kLoads;
+    static_assert(kLoads == kI, "a load a row");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];
+    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0][0];
+    const int wave = scalar(threadIdx.x >> 6);
+    const int bc = wave / Tile<kTile>::kAcross * kI, bd = wave % Tile<kTile>::kAcross * kJ;
+    const Piece piece = piece_of(a.grid, blockIdx.x);
+    const int d0 = piece.m * kTile, c0 = piece.n * kTile;
+    const int k0 = piece.first * kSum;
+
+    f32x4 acc[kI][kJ] = {};
+    const Dy dy(a.dy, a.K, a.D, d0, bd);
+    const Q q(a.ready, a.ready_k, a.cols, c0, bc);
+    auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
+    auto stage = [&](int s, int i) {
+        if (i < Q::kLoads)
+            q.stage(i, k0 + s * kSum, buffer(s));
+        else
+            dy.stage(i - Q::kLoads, k0 + s * kSum, buffer(s) + kTileBytes);
+    };
+    struct Half {
+        bf16x8 q[kI], y[kJ];
+    };
+    // the products of a half, beside the reads of half h of step s and (load) the
+    // loads of step s + 1: past the end in bounds or zeros, and unused
+    auto half = [&](const Half& f, int s, int h, Half& next, auto load) {
+        ROI_LDS uint8_t* src = buffer(s);
 #pragma unroll
-        for (int i = 0; i < kI; ++i)
+        for (int i = 0; i < kI; ++i) {
+            if (i < kJ) next.y[i] = dy.read(src + kTileBytes, i, h);
+            next.q[i] = q.read(src, i, h);
+            if constexpr (decltype(load)::value) stage(s + 1, i);
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
-                *reinterpret_cast<f32x4*>(a.partial + part_at<kTile>(piece.part, wave, i, j, lane)) =
-                    acc[i][j];
-        return;
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.q[i], f.y[j], acc[i][j], 0, 0, 0);
+            keep_order();
+        }
+    };
+    if (piece.count > 0) {
+        Half lo, hi;
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) stage(s, i);
+        loads_barrier();
+#pragma unroll
+        for (int i = 0; i < kI; ++i) lo.q[i] = q.read(buffer(0), i, 0);
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) lo.y[j] = dy.read(buffer(0) + kTileBytes, j, 0);
+        for (int s = 0; s < piece.count; ++s) {
+            half(lo, s, 1, hi, std::false_type{});
+            loads_barrier();
+            half(hi, s + 1, 0, lo, std::true_type{});
+        }
+        loads_barrier();
     }
-    ROI_LDS uint8_t* mine = base + wave * (16 * kJ * Out::kRow);
+    write_tile<kTile>(a, piece, acc, base);
+}
+
+// s q in bf16, transposed to k-rows of 64 (zeros past K), for grad_ready_kernel:
+// 64 rows of 128 columns a block, by way of LDS, so that both the reads and the
+// writes are whole rows of at least 128 bytes.  Bound by 3 bytes an element.
+template <bool kWhole>
+__global__ __launch_bounds__(256) void ready_kernel(GradArgs a)
+{
+    using Q = QTile<128, kWhole>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[128 * kRowBytes];
+    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0];
+    const uint32_t across = (a.cols + 127) / 128;
+    const int c0 = scalar(blockIdx.x % across) * 128, k0 = scalar(blockIdx.x / across) * kSum;
+    Q q(a, c0);
+    q.load(k0);
 #pragma unroll
-    for (int j = 0; j < kJ; ++j)
+    for (int b = 0; b < 4; ++b) q.write(b, base);
+    __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kI; ++i)
-            *reinterpret_cast<ROI_LDS u32x2*>(Out::at(mine, 16 * j + (lane & 15), i, g)) =
-                u32x2{bf16x2_rne(acc[i][j][0], acc[i][j][1]), bf16x2_rne(acc[i][j][2], acc[i][j][3])};
-#pragma unroll
-    for (int n = 0; n < 16 * kJ / Out::kAtOnce; ++n) {
-        int row, chunk;
-        const Quad v = Out::get(mine, n, row, chunk);
-        const int d = d0 + 16 * bd + row, c = c0 + 16 * bc + 8 * chunk;
-        if (d < a.D) store_chunk(a.out + (int64_t)d * a.cols, c, a.cols, v);
+    for (int n = 0; n < 4; ++n) {
+        const int row = n * 32 + (int)threadIdx.x / 8, chunk = threadIdx.x % 8;
+        const u32x4 v = lds_read<u32x4>(base + Q::place(row, chunk));
+        if (c0 + row < a.cols)
+            *reinterpret_cast<u32x4*>(a.ready + (int64_t)(c0 + row) * a.ready_k + k0 + 8 * chunk) = v;
     }
 }
 
@@ -384,24 +492,41 @@ void launch_tiles(const GradArgs& a, hipStream_t stream)
 }
 
 template <bool kSumRows>
-int launch(GradArgs a, const Cut& c, const char* what, hipStream_t stream)
+void launch_ready(const GradArgs& a, hipStream_t stream)
 {
-    if (!c.fits) return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
-    a.grid = Grid{(uint32_t)c.tm, (uint32_t)c.tn, (uint32_t)c.full, (uint32_t)c.splits, (int)c.steps};
-    if (c.tile == 256)
-        launch_tiles<256, kSumRows>(a, stream);
+    const dim3 blocks((unsigned)((a.ready_k / kSum) * ((a.cols + 127) / 128)));
+    if (a.cols % 4 == 0)
+        hipLaunchKernelGGL((ready_kernel<true>), blocks, dim3(256), 0, stream, a);
     else
-        launch_tiles<128, kSumRows>(a, stream);
-    return launch_status(what);
+        hipLaunchKernelGGL((ready_kernel<false>), blocks, dim3(256), 0, stream, a);
+    const dim3 grid(a.grid.blocks()), block(Tile<256>::kThreads);
+    if ((kSumRows ? a.D : a.K) % 8 == 0)
+        hipLaunchKernelGGL((grad_ready_kernel<kSumRows, true>), grid, block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((grad_ready_kernel<kSumRows, false>), grid, block, 0, stream, a);
 }
 
-Cut cut_weight(int64_t tokens, int64_t rows, int64_t cols)
+template <bool kSumRows>
+int launch(GradArgs a, const GradPlan& plan, void* workspace, const char* what, hipStream_t stream)
 {
-    return cut_product(rows, cols, tokens, kSum, kGradCost);
-}
-Cut cut_input(int64_t tokens, int64_t rows, int64_t cols)
-{
-    return cut_product(tokens, cols, rows, kSum, kGradCost);
+    if (!plan.cut.fits)
+        return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
+    using T = Tile<256>;
+    a.grid = grid_of(plan.cut);
+    a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.ready_bytes);
+    if (plan.ready) {
+        a.ready = static_cast<uint16_t*>(workspace);
+        a.ready_k = (int)plan.ready_k;
+        launch_ready<kSumRows>(a, stream);
+        if (a.grid.rest() > 0)
+            hipLaunchKernelGGL((grad_sum_kernel<256>), dim3(a.grid.rest() * T::kI * T::kWaves),
+                               dim3(64), 0, stream, a);
+    } else if (plan.cut.tile == 256) {
+        launch_tiles<256, kSumRows>(a, stream);
+    } else {
+        launch_tiles<128, kSumRows>(a, stream);
+    }
+    return launch_status(what);
 }
 
 } // namespace
@@ -413,14 +538,14 @@ extern "C" int64_t roi_linear_i8_grad_weight_workspace(int64_t tokens, int64_t r
 {
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
-    return cut_weight(tokens, rows, cols).bytes;
+    return plan_grad(rows, cols, tokens).bytes;
 }
 
 extern "C" int64_t roi_linear_i8_grad_input_workspace(int64_t tokens, int64_t rows, int64_t cols)
 {
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
-    return cut_input(tokens, rows, cols).bytes;
+    return plan_grad(tokens, cols, rows).bytes;
 }
 
 extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* xq, const float* xs,
@@ -430,14 +555,13 @@ extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* x
 {
     bool todo;
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
-    const Cut c = cut_weight(tokens, rows, cols);
+    const GradPlan plan = plan_grad(rows, cols, tokens);
     if (int st = validate_grad_i8(grad_y, xq, xs, tokens, tokens, rows, cols, grad_w, rows,
-                                  workspace, workspace_bytes, c.bytes, &todo))
+                                  workspace, workspace_bytes, plan.bytes, &todo))
         return st;
     if (!todo) return ok();
-    const GradArgs a{grad_y, xq, xs, grad_w, static_cast<float*>(workspace), (int)tokens, (int)rows,
-                     (int)cols, {}};
-    return launch<true>(a, c, "roi_linear_i8_grad_weight", stream);
+    const GradArgs a{grad_y, xq, xs, grad_w, nullptr, nullptr, 0, (int)tokens, (int)rows, (int)cols, {}};
+    return launch<true>(a, plan, workspace, "roi_linear_i8_grad_weight", stream);
 }
 
 extern "C" int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq, const float* ws,
@@ -447,12 +571,11 @@ extern "C" int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq
 {
     bool todo;
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
-    const Cut c = cut_input(tokens, rows, cols);
+    const GradPlan plan = plan_grad(tokens, cols, rows);
     if (int st = validate_grad_i8(grad_y, wq, ws, rows, tokens, rows, cols, grad_x, tokens,
-                                  workspace, workspace_bytes, c.bytes, &todo))
+                                  workspace, workspace_bytes, plan.bytes, &todo))
         return st;
     if (!todo) return ok();
-    const GradArgs a{grad_y, wq, ws, grad_x, static_cast<float*>(workspace), (int)rows, (int)tokens,
-                     (int)cols, {}};
-    return launch<false>(a, c, "roi_linear_i8_grad_input", stream);
+    const GradArgs a{grad_y, wq, ws, grad_x, nullptr, nullptr, 0, (int)rows, (int)tokens, (int)cols, {}};
+    return launch<false>(a, plan, workspace, "roi_linear_i8_grad_input", stream);
 }

@@ -332,7 +332,7 @@ __device__ __forceinline__ void write_tile(const LinearArgs& a, const Piece& pie
                 else
                     *reinterpret_cast<ROI_LDS f32x4*>(at) = v;
             }
-#pragma unroll
+#pragma unroll 2 // code that runs once is fetched once: it is kept short
         for (int n = 0; n < 16 * kAtATime / Lines::kAtOnce; ++n) {
             int row, chunk;
             const Quad v = Lines::get(mine, n, row, chunk);
@@ -615,7 +615,7 @@ int launch(LinearArgs a, const LinearPlan& plan, hipStream_t stream)
         return a.meta ? launch_few<true, Out>(a, stream) : launch_few<false, Out>(a, stream);
     const Cut& c = plan.cut;
     if (!c.fits) return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
-    a.grid = Grid{(uint32_t)c.tm, (uint32_t)c.tn, (uint32_t)c.full, (uint32_t)c.splits, (int)c.steps};
+    a.grid = grid_of(c);
     if (c.tile == 256)
         launch_tiles<256, Out>(a, stream);
     else

@@ -115,10 +115,17 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t b, uint32_t n)
 // together.
 struct Grid {
     uint32_t tm, tn, full, splits;
-    int steps;
+    int steps;        // of the sum
+    int part, longer; // steps of a part; the first `longer` parts have one more
     __host__ __device__ uint32_t rest() const { return tm * tn - full; }
     __host__ __device__ uint32_t blocks() const { return full + rest() * splits; }
 };
+inline Grid grid_of(const Cut& c)
+{
+    return Grid{(uint32_t)c.tm,  (uint32_t)c.tn,           (uint32_t)c.full,
+                (uint32_t)c.splits, (int)c.steps, (int)(c.steps / c.splits),
+                (int)(c.steps % c.splits)};
+}
 struct Piece {
     int m, n, first, count, part;
 };
@@ -140,8 +147,8 @@ __device__ __forceinline__ Piece piece_of(const Grid& g, uint32_t block)
     const uint32_t b = xcd_order(block - g.full, g.rest() * g.splits);
     const uint32_t i = b % g.rest(), j = b / g.rest();
     Piece p = tile_piece(g, g.full + i);
-    p.first = scalar((int)((int64_t)g.steps * j / g.splits));
-    p.count = scalar((int)((int64_t)g.steps * (j + 1) / g.splits)) - p.first;
+    p.first = scalar((int)j * g.part + least((int)j, g.longer));
+    p.count = g.part + ((int)j < g.longer ? 1 : 0);
     p.part = scalar((int)(i * g.splits + j));
     return p;
 }
@@ -192,10 +199,12 @@ __device__ __forceinline__ void store_chunk(T* row, int first, int end, const Qu
     if (first + kN <= end) {
         store_any(row + first, v);
     } else {
-#pragma unroll
-        for (int e = 0; e < kN; ++e)
-            if (first + e < end)
-                row[first + e] = sizeof(T) == 2 ? (T)(v.w[e / 2] >> (16 * (e % 2))) : (T)v.w[e];
+        uint64_t lo = v.w[0] | ((uint64_t)v.w[1] << 32), hi = v.w[2] | ((uint64_t)v.w[3] << 32);
+        for (int e = first; e < end; ++e) {
+            row[e] = (T)lo;
+            lo = lo >> (8 * sizeof(T)) | hi << (64 - 8 * sizeof(T));
+            hi >>= 8 * sizeof(T);
+        }
     }
 }
 

@@ -428,6 +428,44 @@ def test_grads(tokens, rows, cols, by_tokens):
 
 
 @gpu
+@pytest.mark.parametrize("by_tokens", [True, False], ids=["weight", "input"])
+@pytest.mark.parametrize("k,d,c", [(1032, 4104, 4092), (1030, 4100, 4093), (2100, 520, 4096)])
+def test_grads_of_many_tiles(k, d, c, by_tokens):
+    """More tiles than compute units: the operand converted beforehand, whole
+    tiles and cut ones in one call, with and without whole chunks a row."""
+    dy, q, s = grad_inputs(*((k, d) if by_tokens else (d, k)), c, k + d, by_tokens)
+    fn = roi.linear_i8_grad_weight if by_tokens else roi.linear_i8_grad_input
+    got = f32(fn(dy.cuda(), dev(q), dev(s)).float())
+    dy = dy.float().numpy()
+    assert_grad(got, dy if by_tokens else np.ascontiguousarray(dy.T), q, s, f"{k}x{d}x{c}")
+
+
+@gpu
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("tokens,rows,cols", [(2200, 4112, 288), (500, 4100, 1312),
+                                              (4096, 4400, 160), (530, 700, 4000)])
+def test_linear_of_many_tiles(tokens, rows, cols, packed):
+    import torch
+    rng = np.random.default_rng(tokens)
+    xq = rng.integers(-128, 128, (tokens, cols)).astype(np.int8)
+    xs = rng.uniform(1e-3, 1, tokens).astype(np.float32)
+    ws = rng.uniform(1e-4, 1e-2, rows).astype(np.float32)
+    meta = None
+    if packed:
+        wq, idx = random_2of4(rng, rows, cols)
+        dense, meta = expand(wq, idx, cols), dev(meta_of(idx).view(np.int32))
+    else:
+        dense = wq = rng.integers(-128, 128, (rows, cols)).astype(np.int8)
+    # products and sums of integers below 2^53 are exact in fp64
+    total = xq.astype(np.float64) @ dense.astype(np.float64).T
+    want = total.astype(np.float32) * ws[None, :] * xs[:, None]
+    args = [dev(a) for a in (xq, xs, wq, ws)]
+    y = roi.linear_i8(*args, meta=meta, dtype=torch.float32)
+    assert np.array_equal(f32(y).view(np.uint32), want.view(np.uint32))
+    assert np.array_equal(bf16_bits(roi.linear_i8(*args, meta=meta)), bf16_rne_bits(want))
+
+
+@gpu
 def test_grads_against_differences():
     """Both gradients are the slopes of L = sum(grad_y y) along one weight or
     one activation: y is linear in each, so a difference quotient in 64 bits is
