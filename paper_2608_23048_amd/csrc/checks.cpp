@@ -328,14 +328,13 @@ namespace {
 
 constexpr int64_t kUnits = 256;           // compute units of an MI355X
 constexpr int64_t kMostSplits = 64;
-constexpr double kPartBytesPerUs = 2.5e6; // a part is written and read again
-constexpr double kSumLaunchUs = 4;
+constexpr double kPartBytesPerUs = 6.0e6; // of parts, written and read again
+constexpr double kSumLaunchUs = 5;
 
 // One tile size: the tiles of whole rounds over the units are whole.  The last
-// round's are cut if they fill half of it or less, so that all units have a
-// part.
-Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double step_us,
-              double rest_us)
+// round's are cut where that is expected to take less time, into as many parts
+// as do: more parts have fewer steps each, fewer have fewer bytes to pass on.
+Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, const TileCost& cost)
 {
     Cut c{};
     c.tile = tile;
@@ -343,24 +342,28 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double st
     c.tn = (n + tile - 1) / tile;
     c.steps = (k + step - 1) / step;
     const int64_t tiles = c.tm * c.tn, slots = kUnits * (tile == 256 ? 1 : 2);
-    const double whole = (double)c.steps * step_us + rest_us;
+    const double rest_us = tile == 256 ? cost.rest256 : cost.rest128;
+    // of a round of so many blocks, each of so many steps
+    auto round = [&](int64_t blocks, int64_t steps) {
+        const double one = tile == 256 ? cost.step256 : blocks > kUnits ? cost.two128 : cost.step128;
+        return (double)steps * one + rest_us;
+    };
     const int64_t rest = tiles % slots;
+    const double rounds = (double)(tiles / slots) * round(slots, c.steps);
     c.full = tiles;
     c.splits = 1;
-    c.us = (double)((tiles + slots - 1) / slots) * whole;
+    c.us = rounds + (rest ? round(rest, c.steps) : 0);
     // a part of a sum has four steps at least
-    const int64_t splits =
-        rest ? std::min(std::min(slots / rest, c.steps / 4), kMostSplits) : 1;
-    if (splits > 1) {
-        const double part_bytes = (double)(rest * splits) * tile * tile * 4;
-        const double cut = (double)(tiles / slots) * whole +
-                           (double)((c.steps + splits - 1) / splits) * step_us + rest_us +
-                           part_bytes / kPartBytesPerUs + kSumLaunchUs;
-        if (cut < c.us) {
-            c.us = cut;
+    const int64_t most = rest ? std::min(std::min(slots / rest, c.steps / 4), kMostSplits) : 0;
+    for (int64_t splits = 2; splits <= most; ++splits) {
+        const int64_t bytes = rest * splits * tile * tile * 4;
+        const double us = rounds + round(rest * splits, (c.steps + splits - 1) / splits) +
+                          (double)bytes / kPartBytesPerUs + kSumLaunchUs;
+        if (us < c.us) {
+            c.us = us;
             c.full = tiles - rest;
             c.splits = splits;
-            c.bytes = rest * splits * tile * tile * 4;
+            c.bytes = bytes;
         }
     }
     // a launch has fewer than 2^32 threads
@@ -372,8 +375,8 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, double st
 
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost)
 {
-    const Cut big = cut_tiles(m, n, k, step, 256, cost.step256, cost.rest256);
-    const Cut small = cut_tiles(m, n, k, step, 128, cost.step128, cost.rest128);
+    const Cut big = cut_tiles(m, n, k, step, 256, cost);
+    const Cut small = cut_tiles(m, n, k, step, 128, cost);
     return small.us < big.us && small.fits ? small : big;
 }
 
@@ -402,7 +405,7 @@ GradPlan plan_grad(int64_t m, int64_t n, int64_t k)
     // offsets within a tile of the transposed operand stay below 2^31
     if (m == 0 || n == 0 || k == 0 || k > ((int64_t)1 << 21)) return p;
     const int64_t ready_k = (k + kStep - 1) / kStep * kStep;
-    const Cut c = cut_tiles(m, n, k, kStep, 256, kReadyStep, kReadyRest);
+    const Cut c = cut_tiles(m, n, k, kStep, 256, kReadyCost);
     const double us = c.us + 3 + 3 * (double)ready_k * (double)n / 4.0e6;
     if (us < p.cut.us && c.fits) {
         p.ready = true;

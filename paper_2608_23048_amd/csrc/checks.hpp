@@ -116,16 +116,17 @@ struct Cut {
     double us;     // what the call is expected to take
     bool fits;     // fewer blocks than a launch takes
 };
-// Times of the tiled kernels in microseconds: a step of a 256-tile on every
-// compute unit, of two 128-tiles on every unit, and what a tile costs beside
-// its steps.
+// Times of the tiled kernels in microseconds, as measured: a step of a 256-tile
+// on every compute unit, of one 128-tile on every unit and of two, and what a
+// tile takes beside its steps (the launch, its first loads, its results).
 struct TileCost {
-    double step256, rest256, step128, rest128;
+    double step256, rest256, step128, two128, rest128;
 };
-constexpr TileCost kLinearCost = {1.36, 12, 0.80, 6};
-constexpr TileCost kPackedCost = {0.80, 12, 0.60, 5};
-constexpr TileCost kGradCost = {1.70, 14, 1.60, 10};
-constexpr double kReadyStep = 1.40, kReadyRest = 12; // of a 256-tile with both operands in bf16
+constexpr TileCost kLinearCost = {1.36, 12, 0.55, 0.80, 6};
+constexpr TileCost kPackedCost = {0.80, 12, 0.45, 0.60, 5};
+constexpr TileCost kGradCost = {1.70, 14, 0.95, 1.50, 9};
+// Of a 256-tile with both operands in bf16 (there is no 128-tile).
+constexpr TileCost kReadyCost = {1.40, 12, 0, 0, 0};
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost);
 
 // The int8 product's way: with few tokens the kernel that streams the weight

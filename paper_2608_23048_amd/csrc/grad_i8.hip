@@ -258,7 +258,7 @@ __device__ __forceinline__ void write_tile(const GradArgs& a, const Piece& piece
 // steps later.  The int8 tile of step s + 3 goes to registers in step s and to
 // LDS, scaled, in step s + 1.
 template <int kTile, bool kSumRows, bool kWhole>
-__global__ __launch_bounds__(Tile<kTile>::kThreads) void grad_tile_kernel(GradArgs a)
+__global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void grad_tile_kernel(GradArgs a)
 {
     constexpr int kTileBytes = kTile * kRowBytes;
     static_assert(kTileBytes == kSum * kTile * 2, "both layouts of dy take the same LDS");
@@ -442,36 +442,33 @@ __global__ __launch_bounds__(256) void ready_kernel(GradArgs a)
     }
 }
 
-// The sums of the tiles that were cut: one wave for the 16 x 64 results that a
-// wave of the tile's kernel held at one i, the parts in their order.
+// The sums of the tiles that were cut: one wave for 16 x 16 results, the parts
+// in their order, eight of them on their way at a time.
 template <int kTile>
 __global__ __launch_bounds__(64) void grad_sum_kernel(GradArgs a)
 {
     using T = Tile<kTile>;
-    const int lane = threadIdx.x, g = lane >> 4;
-    const int i = blockIdx.x % T::kI, wave = blockIdx.x / T::kI % T::kWaves;
-    const uint32_t tile = blockIdx.x / (T::kI * T::kWaves);
+    const int lane = threadIdx.x;
+    const int j = blockIdx.x % T::kJ, i = blockIdx.x / T::kJ % T::kI;
+    const int wave = blockIdx.x / (T::kJ * T::kI) % T::kWaves;
+    const uint32_t tile = blockIdx.x / (T::kJ * T::kI * T::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
-    f32x4 sum[T::kJ] = {};
+    const float* from = a.partial + part_at<kTile>((int64_t)tile * a.grid.splits, wave, i, j, lane);
+    f32x4 sum = {};
+#pragma unroll 8
     for (uint32_t p = 0; p < a.grid.splits; ++p)
+        sum += *reinterpret_cast<const f32x4*>(from + (int64_t)p * (kTile * kTile));
+    const int c = piece.n * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * (lane >> 4);
+    const int d = piece.m * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
+    if (d >= a.D) return;
+    uint16_t* p = a.out + (int64_t)d * a.cols + c;
+    const Pair v{bf16x2_rne(sum[0], sum[1]), bf16x2_rne(sum[2], sum[3])};
+    if (c + 4 <= a.cols) {
+        store_any(p, v);
+    } else {
 #pragma unroll
-        for (int j = 0; j < T::kJ; ++j)
-            sum[j] += *reinterpret_cast<const f32x4*>(
-                a.partial + part_at<kTile>((int64_t)tile * a.grid.splits + p, wave, i, j, lane));
-    const int c = piece.n * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * g;
-#pragma unroll
-    for (int j = 0; j < T::kJ; ++j) {
-        const int d = piece.m * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
-        if (d >= a.D) continue;
-        uint16_t* p = a.out + (int64_t)d * a.cols + c;
-        const Pair v{bf16x2_rne(sum[j][0], sum[j][1]), bf16x2_rne(sum[j][2], sum[j][3])};
-        if (c + 4 <= a.cols) {
-            store_any(p, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c + e < a.cols) p[e] = (uint16_t)(v.w[e / 2] >> (16 * (e % 2)));
-        }
+        for (int e = 0; e < 4; ++e)
+            if (c + e < a.cols) p[e] = (uint16_t)(v.w[e / 2] >> (16 * (e % 2)));
     }
 }
 
@@ -487,7 +484,7 @@ void launch_tiles(const GradArgs& a, hipStream_t stream)
     else
         hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows, false>), grid, block, 0, stream, a);
     if (a.grid.rest() > 0)
-        hipLaunchKernelGGL((grad_sum_kernel<kTile>), dim3(a.grid.rest() * T::kI * T::kWaves), dim3(64),
+        hipLaunchKernelGGL((grad_sum_kernel<kTile>), dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves), dim3(64),
                            0, stream, a);
 }
 
@@ -519,7 +516,7 @@ int launch(GradArgs a, const GradPlan& plan, void* workspace, const char* what, 
         a.ready_k = (int)plan.ready_k;
         launch_ready<kSumRows>(a, stream);
         if (a.grid.rest() > 0)
-            hipLaunchKernelGGL((grad_sum_kernel<256>), dim3(a.grid.rest() * T::kI * T::kWaves),
+            hipLaunchKernelGGL((grad_sum_kernel<256>), dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves),
                                dim3(64), 0, stream, a);
     } else if (plan.cut.tile == 256) {
         launch_tiles<256, kSumRows>(a, stream);

@@ -346,7 +346,7 @@ __device__ __forceinline__ void write_tile(const LinearArgs& a, const Piece& pie
 }
 
 template <int kTile, bool kWhole, typename Out>
-__global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(LinearArgs a)
+__global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(LinearArgs a)
 {
     constexpr int kTileBytes = kTile * kRowBytes;
     constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
@@ -423,7 +423,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_tile_kernel(Line
 // step's tiles (64 bytes a weight row, its four metadata words, 128 bytes a
 // token) have two steps to arrive, in three LDS buffers.
 template <int kTile, typename Out>
-__global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_packed_kernel(LinearArgs a)
+__global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel(LinearArgs a)
 {
     constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
     constexpr int kThreads = Tile<kTile>::kThreads;
@@ -534,31 +534,28 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads) void linear_packed_kernel(Li
     write_tile<kTile, Out>(a, piece, acc, base);
 }
 
-// The sums of the tiles that were cut: one wave for the 16 x 64 results that a
-// wave of the tile's kernel held at one i.
+// The sums of the tiles that were cut: one wave for 16 x 16 results, eight parts
+// on their way at a time.
 template <int kTile, typename Out>
 __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
 {
     using T = Tile<kTile>;
-    const int lane = threadIdx.x, g = lane >> 4;
-    const int i = blockIdx.x % T::kI, wave = blockIdx.x / T::kI % T::kWaves;
-    const uint32_t tile = blockIdx.x / (T::kI * T::kWaves);
+    const int lane = threadIdx.x;
+    const int j = blockIdx.x % T::kJ, i = blockIdx.x / T::kJ % T::kI;
+    const int wave = blockIdx.x / (T::kJ * T::kI) % T::kWaves;
+    const uint32_t tile = blockIdx.x / (T::kJ * T::kI * T::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
-    i32x4 sum[T::kJ] = {};
+    const int* from = a.partial + part_at<kTile>((int64_t)tile * a.grid.splits, wave, i, j, lane);
+    i32x4 sum = {};
+#pragma unroll 8
     for (uint32_t p = 0; p < a.grid.splits; ++p)
-#pragma unroll
-        for (int j = 0; j < T::kJ; ++j)
-            sum[j] += *reinterpret_cast<const i32x4*>(
-                a.partial + part_at<kTile>((int64_t)tile * a.grid.splits + p, wave, i, j, lane));
-    const int r = piece.m * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * g;
-    if (r >= a.rows) return;
+        sum += *reinterpret_cast<const i32x4*>(from + (int64_t)p * (kTile * kTile));
+    const int r = piece.m * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * (lane >> 4);
+    const int t = piece.n * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
+    if (r >= a.rows || t >= a.tokens) return;
     float ws[4], add[4];
     row_scales(a, r, ws, add);
-#pragma unroll
-    for (int j = 0; j < T::kJ; ++j) {
-        const int t = piece.n * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
-        if (t < a.tokens) store4<Out>(a, t, r, finish4(sum[j], ws, add, a.xs[t]));
-    }
+    store4<Out>(a, t, r, finish4(sum, ws, add, a.xs[t]));
 }
 
 template <int kTile, typename Out>
@@ -573,7 +570,7 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
     else
         hipLaunchKernelGGL((linear_tile_kernel<kTile, false, Out>), grid, block, 0, stream, a);
     if (a.grid.rest() > 0)
-        hipLaunchKernelGGL((linear_sum_kernel<kTile, Out>), dim3(a.grid.rest() * T::kI * T::kWaves),
+        hipLaunchKernelGGL((linear_sum_kernel<kTile, Out>), dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves),
                            dim3(64), 0, stream, a);
 }
 

@@ -26,7 +26,10 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 constexpr int kRowBytes = 128; // of a k-row in LDS
 
 // Blocks of a product: a square tile over kWaves waves, two by kAcross, each
-// with kI x kJ results of 16 x 16.
+// with kI x kJ results of 16 x 16.  Their kernels are bound to two waves a SIMD,
+// which they run at (a 256-tile, or two 128-tiles, on a compute unit): with more
+// registers than that the compiler keeps the sums in accumulation registers and
+// moves them about, 100 moves a step.
 template <int kTile>
 struct Tile {
     static constexpr int kWaves = kTile == 256 ? 8 : 4;
