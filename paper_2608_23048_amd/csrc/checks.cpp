@@ -329,7 +329,7 @@ namespace {
 constexpr int64_t kUnits = 256;           // compute units of an MI355X
 constexpr int64_t kMostSplits = 64;
 constexpr double kPartBytesPerUs = 6.0e6; // of parts, written and read again
-constexpr double kSumLaunchUs = 5;
+constexpr double kSumLaunchUs = 6.5;
 
 // One tile size: the tiles of whole rounds over the units are whole.  The last
 // round's are cut where that is expected to take less time, into as many parts
@@ -380,7 +380,7 @@ Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& c
     return small.us < big.us && small.fits ? small : big;
 }
 
-// The streaming kernel takes 32 tokens at a time, each time at 7.5e6 bytes of a
+// The streaming kernel takes 32 tokens at a time, each time at 7e6 bytes of a
 // dense weight a microsecond from the caches (6e6 at 2:4, of the dense weight it
 // stands for).  64 tokens through 3584 x 3584 take 5.6 us so and 17.5 in tiles,
 // through 18944 x 3584 25 and 29; 128 tokens 8.3 and 17.4, 44 and 30.
@@ -391,7 +391,7 @@ LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
     if (p.few) return p;
     p.cut = cut_product(rows, tokens, cols, 128, packed ? kPackedCost : kLinearCost);
     const double few_us = 3 + (double)((tokens + 31) / 32) * (double)rows * (double)cols /
-                                  (packed ? 6.0e6 : 7.5e6);
+                                  (packed ? 6.0e6 : 7.0e6);
     p.few = tokens <= 1024 && few_us < p.cut.us;
     return p;
 }

@@ -122,7 +122,7 @@ struct Cut {
 struct TileCost {
     double step256, rest256, step128, two128, rest128;
 };
-constexpr TileCost kLinearCost = {1.36, 12, 0.55, 0.80, 6};
+constexpr TileCost kLinearCost = {1.36, 12, 0.55, 0.80, 5.5};
 constexpr TileCost kPackedCost = {0.80, 12, 0.45, 0.60, 5};
 constexpr TileCost kGradCost = {1.70, 14, 0.95, 1.50, 9};
 // Of a 256-tile with both operands in bf16 (there is no 128-tile).
