@@ -34,6 +34,29 @@ __device__ __forceinline__ void store_any(void* p, const V& v)
     static_cast<AnyAddress<V>*>(p)->v = v;
 }
 
+// The same past the caches' usual order, for what is touched once.
+template <typename V>
+__device__ __forceinline__ V stream_load_any(const void* p)
+{
+    constexpr int kWords = sizeof(V) / 4;
+    typedef uint32_t Vec __attribute__((ext_vector_type(kWords < 4 ? kWords : 4), aligned(1)));
+    V v;
+#pragma unroll
+    for (int i = 0; i < kWords / (kWords < 4 ? kWords : 4); ++i) {
+        const Vec x = __builtin_nontemporal_load(static_cast<const Vec*>(p) + i);
+        __builtin_memcpy(reinterpret_cast<char*>(&v) + sizeof(Vec) * i, &x, sizeof(Vec));
+    }
+    return v;
+}
+template <typename V>
+__device__ __forceinline__ void stream_store_any(void* p, const V& v)
+{
+    typedef uint32_t Vec __attribute__((ext_vector_type(sizeof(V) / 4), aligned(1)));
+    Vec x;
+    __builtin_memcpy(&x, &v, sizeof(V));
+    __builtin_nontemporal_store(x, static_cast<Vec*>(p));
+}
+
 // Bytes k .. k + N - 1 of a row of `len` bytes, zeros past its end (nothing
 // past it is read).
 template <typename V>
