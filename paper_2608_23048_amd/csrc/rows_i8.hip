@@ -236,7 +236,9 @@ void launch_quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t 
 template <typename T>
 void quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols, hipStream_t stream)
 {
-    if (cols <= 64 * 8 * 4)
+    if (cols <= 64 * 8 * 2)
+        launch_quantize<T, 1, 2>(x, q, scale, rows, cols, stream);
+    else if (cols <= 64 * 8 * 4)
         launch_quantize<T, 1, 4>(x, q, scale, rows, cols, stream);
     else if (cols <= 256 * 8 * 4)
         launch_quantize<T, 4, 4>(x, q, scale, rows, cols, stream);
