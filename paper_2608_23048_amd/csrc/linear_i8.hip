@@ -12,6 +12,9 @@
 //     of the dense columns 32 g .. 32 g + 31 and its index operand their eight
 //     4-bit fields, which is one metadata word; the second's lane holds dense
 //     columns 16 g .. 16 g + 15 and 64 + 16 g .. 64 + 16 g + 15; result as above.
+//   v_smfmac_i32_32x32x64_i8: the same with 32 rows, g = l / 32 and 64 columns
+//     (the second operand's at 16 g and 32 + 16 g); result rows 8 (i / 4) + 4 g +
+//     i % 4 of column l % 32 in element i of 16.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -31,7 +34,7 @@ struct LinearArgs {
     const float* ws;
     const uint16_t* bias;
     void* y;
-    int* partial; // int32 parts of tiles (part_at)
+    int* partial; // int32 parts of tiles (Held::part_at)
     int tokens, rows, cols;
     Grid grid; // tiles along the rows and the tokens (few tokens: grid.tm alone)
 };
@@ -90,8 +93,8 @@ __device__ __forceinline__ void store4(const LinearArgs& a, int64_t t, int r, f3
 // to a ring of kDepth slots in LDS of its own and needs no barrier.  Through LDS,
 // because eight lanes then read 128 consecutive bytes of a row; operands loaded
 // straight to registers are 64 separate pieces of 16 bytes a load, and the
-// vector cache takes one a cycle: 14 us against NN for a token through the 2:4
-// 18944 x 3584 layer.
+// vector cache takes one a cycle: 14 us against 11 for a token through the 2:4
+// 18944 x 3584 layer, 21.5 against 16 for 16 tokens through the dense 3584 x 18944.
 template <int kWaves, int kRow, int kTokens, int kDepth, bool kPacked, bool kWhole, typename Out>
 __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
 {
@@ -239,15 +242,17 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
 // buffer, loading for a whole step, is complete.
 
 // Rows row0 .. of an operand of `n` rows of `len` bytes, kBytes of each, that
-// this thread brings to LDS.  Rows of 128 bytes lie as k-rows (mm.hpp); in rows
-// of 64, place j ^ spread(row) holds chunk j, so that 16 lanes reading the same
-// chunk of 16 rows cover all the LDS banks, and so do any aligned eight.
-// kWhole: rows are whole 16-byte chunks.
-template <int kTile, int kBytes, bool kWhole>
+// this thread brings to LDS, where place j ^ spread(row) of a row holds its chunk
+// j.  A 16-byte LDS read goes by 16 lanes at a time, which are, of the wave's
+// first half, 0-3, 12-15, 20-23 and 24-27, then the others; the spreads give any
+// such 16 lanes all the banks when 16 consecutive lanes (kBlock 16) or 32 read
+// the same chunk of as many rows.  kWhole: rows are whole 16-byte chunks.
+template <int kTile, int kBytes, int kBlock, bool kWhole>
 struct Rows {
     static constexpr int kThreads = Tile<kTile>::kThreads;
     static constexpr int kLoads = kTile * kBytes / (16 * kThreads);
     static constexpr int kChunks = kBytes / 16;
+    static_assert(kBlock == 32 || kChunks == 8, "the spreads below");
     const uint8_t* base;
     int left, len; // rows from row0 on, and their bytes
     uint32_t at;   // byte offset of load 0 from base
@@ -259,7 +264,7 @@ struct Rows {
     }
     __device__ __forceinline__ static int spread(int row)
     {
-        return kChunks == 8 ? row & 7 : ((row >> 1) & 3) ^ ((row >> 3) & 1);
+        return kBlock == 16 ? row & 7 : kChunks == 8 ? (row >> 1) & 7 : (row >> 2) & 3;
     }
     // Row and chunk of this thread's load i (the chunk is the same for all: the
     // rows differ by a multiple of sixteen).
@@ -283,60 +288,73 @@ struct Rows {
     }
 };
 
+// Quad q of a block's sums.
+__device__ __forceinline__ i32x4 quad_of(const i32x4& v, int) { return v; }
+__device__ __forceinline__ i32x4 quad_of(const i32x16& v, int q)
+{
+    return i32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+}
+
 // A tile's results from a wave's sums: a part of a cut tile as it is, else scaled
 // and through LDS (all of which is free) to y.
-template <int kTile, typename Out>
-__device__ __forceinline__ void write_tile(const LinearArgs& a, const Piece& piece,
-                                           const i32x4 (&acc)[Tile<kTile>::kI][Tile<kTile>::kJ],
-                                           ROI_LDS uint8_t* base)
+template <int kTile, int kBlock, typename Out, typename Sum>
+__device__ __forceinline__ void write_tile(
+    const LinearArgs& a, const Piece& piece,
+    const Sum (&acc)[Held<kTile, kBlock>::kI][Held<kTile, kBlock>::kJ], ROI_LDS uint8_t* base)
 {
-    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
-    const int lane = threadIdx.x & 63, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r0 = piece.m * kTile + wave / Tile<kTile>::kAcross * 16 * kI;
-    const int t0 = piece.n * kTile + wave % Tile<kTile>::kAcross * 16 * kJ;
+    using H = Held<kTile, kBlock>;
+    const int wave = scalar(threadIdx.x >> 6);
+    const int r0 = piece.m * kTile + wave / Tile<kTile>::kAcross * 16 * Tile<kTile>::kI;
+    const int t0 = piece.n * kTile + wave % Tile<kTile>::kAcross * 16 * Tile<kTile>::kJ;
     if (piece.part >= 0) {
 #pragma unroll
-        for (int i = 0; i < kI; ++i)
+        for (int i = 0; i < H::kI; ++i)
 #pragma unroll
-            for (int j = 0; j < kJ; ++j)
-                *reinterpret_cast<i32x4*>(a.partial + part_at<kTile>(piece.part, wave, i, j, lane)) =
-                    acc[i][j];
+            for (int j = 0; j < H::kJ; ++j)
+#pragma unroll
+                for (int q = 0; q < H::kQuads; ++q)
+                    *reinterpret_cast<i32x4*>(a.partial + H::part_at(piece.part, wave, i, j, q)) =
+                        quad_of(acc[i][j], q);
         return;
     }
     // every scale before the first store, which might overwrite one for all the
     // compiler knows
-    float ws[kI][4], add[kI][4], xs[kJ];
+    float ws[H::kI][H::kQuads][4], add[H::kI][H::kQuads][4], xs[H::kJ];
 #pragma unroll
-    for (int i = 0; i < kI; ++i) row_scales(a, r0 + 16 * i + 4 * g, ws[i], add[i]);
+    for (int i = 0; i < H::kI; ++i)
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) xs[j] = a.xs[least(t0 + 16 * j + (lane & 15), a.tokens - 1)];
-    // as many blocks of 16 tokens at a time as fit this wave's LDS
-    using Lines = RowsOut<kI, 4 * sizeof(Out)>;
-    constexpr int kAtATime = kTile * kRowBytes * 4 / Tile<kTile>::kWaves / (16 * Lines::kRow) < kJ
-                                 ? kTile * kRowBytes * 4 / Tile<kTile>::kWaves / (16 * Lines::kRow)
-                                 : kJ;
-    static_assert(kAtATime >= 1 && kJ % kAtATime == 0, "results pass LDS");
-    ROI_LDS uint8_t* mine = base + wave * (kAtATime * 16 * Lines::kRow);
+        for (int q = 0; q < H::kQuads; ++q)
+            row_scales(a, r0 + 4 * H::quad(i, q), ws[i][q], add[i][q]);
 #pragma unroll
-    for (int first = 0; first < kJ; first += kAtATime) {
+    for (int j = 0; j < H::kJ; ++j) xs[j] = a.xs[least(t0 + H::column(j), a.tokens - 1)];
+    // as many blocks of tokens at a time as fit this wave's LDS
+    using Lines = RowsOut<Tile<kTile>::kI, 4 * sizeof(Out)>;
+    constexpr int kFit = kTile * kRowBytes * 4 / Tile<kTile>::kWaves / (kBlock * Lines::kRow);
+    constexpr int kAtATime = kFit < H::kJ ? kFit : H::kJ;
+    static_assert(kAtATime >= 1 && H::kJ % kAtATime == 0, "results pass LDS");
+    ROI_LDS uint8_t* mine = base + wave * (kAtATime * kBlock * Lines::kRow);
+#pragma unroll
+    for (int first = 0; first < H::kJ; first += kAtATime) {
 #pragma unroll
         for (int j = 0; j < kAtATime; ++j)
 #pragma unroll
-            for (int i = 0; i < kI; ++i) {
-                const f32x4 v = finish4(acc[i][first + j], ws[i], add[i], xs[first + j]);
-                ROI_LDS uint8_t* at = Lines::at(mine, 16 * j + (lane & 15), i, g);
-                if constexpr (sizeof(Out) == 2)
-                    *reinterpret_cast<ROI_LDS u32x2*>(at) =
-                        u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
-                else
-                    *reinterpret_cast<ROI_LDS f32x4*>(at) = v;
-            }
+            for (int i = 0; i < H::kI; ++i)
+#pragma unroll
+                for (int q = 0; q < H::kQuads; ++q) {
+                    const f32x4 v = finish4(quad_of(acc[i][first + j], q), ws[i][q], add[i][q],
+                                            xs[first + j]);
+                    ROI_LDS uint8_t* at = Lines::at(mine, H::column(j), H::quad(i, q));
+                    if constexpr (sizeof(Out) == 2)
+                        *reinterpret_cast<ROI_LDS u32x2*>(at) =
+                            u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
+                    else
+                        *reinterpret_cast<ROI_LDS f32x4*>(at) = v;
+                }
 #pragma unroll 2 // code that runs once is fetched once: it is kept short
-        for (int n = 0; n < 16 * kAtATime / Lines::kAtOnce; ++n) {
+        for (int n = 0; n < kBlock * kAtATime / Lines::kAtOnce; ++n) {
             int row, chunk;
             const Quad v = Lines::get(mine, n, row, chunk);
-            const int t = t0 + 16 * first + row;
+            const int t = t0 + kBlock * first + row;
             const int r = r0 + chunk * (int)(16 / sizeof(Out));
             using Bits = std::conditional_t<sizeof(Out) == 2, uint16_t, uint32_t>;
             if (t < a.tokens)
@@ -359,7 +377,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x4 acc[kI][kJ] = {};
-    using R = Rows<kTile, kRowBytes, kWhole>;
+    using R = Rows<kTile, kRowBytes, 16, kWhole>;
     const R wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
     constexpr int kLoads = R::kLoads;
     auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
@@ -415,35 +433,44 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
         }
         loads_barrier();
     }
-    write_tile<kTile, Out>(a, piece, acc, base);
+    write_tile<kTile, 16, Out>(a, piece, acc, base);
 }
 
-// The same with 2:4 weights: a step of 128 columns is one instruction's sum, so
-// that a step's operands are read while the step before is multiplied, and a
-// step's tiles (64 bytes a weight row, its four metadata words, 128 bytes a
-// token) have two steps to arrive, in three LDS buffers.
+// The same with 2:4 weights, on the 32 x 32 sparse instructions: a half step is
+// 64 columns, whose second operand is 8 registers a block of 32 tokens (the 16 x
+// 16 form takes 128 columns at once and twice the registers, too many to read
+// ahead).  A step's tiles (64 bytes a weight row, its four metadata words, 128
+// bytes a token) have two steps to arrive, in three LDS buffers.  4096 tokens
+// through 3584 x 18944 take 169 us.  Bound by requests to the L2: a step makes 256
+// each for the tokens, the half lines of weights and the metadata's 16 bytes a
+// row (26 million in all, one every 6.4 ps), where the matrix cores are busy for
+// 48 % of the time.
 template <int kTile, typename Out>
 __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel(LinearArgs a)
 {
-    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    using H = Held<kTile, 32>;
+    constexpr int kI = H::kI, kJ = H::kJ;
     constexpr int kThreads = Tile<kTile>::kThreads;
     constexpr int kW = kTile * 64, kX = kTile * 128, kM = kTile * 16, kStage = kW + kX + kM;
+    static_assert(3 * kStage >= 4 * kTile * kRowBytes, "results pass LDS");
     __shared__ __attribute__((aligned(16))) uint8_t lds[3][kStage];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0];
-    const int lane = threadIdx.x & 63, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / Tile<kTile>::kAcross * 16 * kI, wn = wave % Tile<kTile>::kAcross * 16 * kJ;
+    const int lane = threadIdx.x & 63, half_of = lane >> 5, in = lane & 31;
+    const int wave = scalar(threadIdx.x >> 6);
+    const int wm = wave / Tile<kTile>::kAcross * 32 * kI, wn = wave % Tile<kTile>::kAcross * 32 * kJ;
     const Piece piece = piece_of(a.grid, blockIdx.x);
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
-    i32x4 acc[kI][kJ] = {};
-    using W = Rows<kTile, 64, true>;
-    using X = Rows<kTile, 128, true>;
+    i32x16 acc[kI][kJ] = {};
+    using W = Rows<kTile, 64, 32, true>;
+    using X = Rows<kTile, 128, 32, true>;
     const W wrows(a.w, r0, a.rows, a.cols / 2);
     const X xrows(a.x, t0, a.tokens, a.cols);
-    // metadata: a word a lane, four words a row
+    // metadata: a word a lane, four words a row, word j at place j ^ (2 in the
+    // second 16 of 32 rows), so that 32 rows' words lie in different banks
     constexpr int kMetaLoads = kTile * 4 / kThreads;
-    const int words = a.cols / 32, word = threadIdx.x % 4;
+    const int words = a.cols / 32, word = (threadIdx.x % 4) ^ (threadIdx.x / 4 >> 3 & 2);
+    static_assert(kThreads / 4 % 32 == 0, "the same word for all of a thread's loads");
     const uint32_t* meta = a.meta + (int64_t)r0 * words;
     constexpr int kLoads = W::kLoads + X::kLoads + kMetaLoads;
     static_assert(kLoads % kI == 0, "loads are spread over the rows");
@@ -465,93 +492,88 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
             }
         }
     };
-    struct Step {
+    struct Half {
         i32x4 w[kI];
         int m[kI];
         i32x8 x[kJ];
     };
-    const int from_w = (wm + (lane & 15)) * 64 + (g ^ W::spread(lane & 15)) * 16;
-    const int from_m = kW + kX + (wm + (lane & 15)) * 16 + g * 4;
-    const int from_x = kW + (wn + (lane & 15)) * 128 + (g ^ X::spread(lane & 15)) * 16;
-    auto read_w = [&](ROI_LDS uint8_t* src, Step& f, int i) {
-        f.w[i] = lds_read<i32x4>(src + from_w + i * 16 * 64);
-        f.m[i] = lds_read<int>(src + from_m + i * 16 * 16);
+    // Half h: the weight's chunk and word 2 h + half_of, the tokens' chunks 4 h +
+    // half_of and 4 h + 2 + half_of; the places' bits flip with the chunks'.
+    const int from_w = (wm + in) * 64 + (half_of ^ W::spread(in)) * 16;
+    const int from_m = kW + kX + (wm + in) * 16 + (half_of ^ (in >> 3 & 2)) * 4;
+    const int from_x = kW + (wn + in) * 128 + (half_of ^ X::spread(in)) * 16;
+    auto read_w = [&](ROI_LDS uint8_t* src, int h, Half& f, int i) {
+        f.w[i] = lds_read<i32x4>(src + i * 32 * 64 + (from_w ^ (32 * h)));
+        f.m[i] = lds_read<int>(src + i * 32 * 16 + (from_m ^ (8 * h)));
     };
-    auto read_x = [&](ROI_LDS uint8_t* src, Step& f, int j) {
-        const i32x4 lo = lds_read<i32x4>(src + from_x + j * 16 * 128);
-        const i32x4 hi = lds_read<i32x4>(src + (from_x ^ 64) + j * 16 * 128);
+    auto read_x = [&](ROI_LDS uint8_t* src, int h, Half& f, int j) {
+        const i32x4 lo = lds_read<i32x4>(src + j * 32 * 128 + (from_x ^ (64 * h)));
+        const i32x4 hi = lds_read<i32x4>(src + j * 32 * 128 + (from_x ^ (64 * h) ^ 32));
         f.x[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // the products of a step, beside the reads of the next (at src) and the loads
-    // of step s, to dst; a block of tokens is read past the last product of the
-    // one before it (there are no registers for both)
-    auto step = [&](const Step& f, Step& next, ROI_LDS uint8_t* src, int s, ROI_LDS uint8_t* dst) {
+    // the products of a half, beside the reads of half h at src and (load) the
+    // loads of step s, to dst
+    auto half = [&](const Half& f, ROI_LDS uint8_t* src, int h, Half& next, auto load, int s,
+                    ROI_LDS uint8_t* dst) {
         constexpr int kPart = kLoads / kI;
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
-            read_w(src, next, i);
-            stage(s, i * kPart, kPart, dst);
+            if (i < kJ) read_x(src, h, next, i);
+            read_w(src, h, next, i);
+            if constexpr (decltype(load)::value) stage(s, i * kPart, kPart, dst);
 #pragma unroll
-            for (int j = 0; j < kJ; ++j) {
-                acc[i][j] = __builtin_amdgcn_smfmac_i32_16x16x128_i8(f.w[i], f.x[j], acc[i][j],
-                                                                     f.m[i], 0, 0);
-                if (i == kI - 1) read_x(src, next, j);
-            }
+            for (int j = 0; j < kJ; ++j)
+                acc[i][j] = __builtin_amdgcn_smfmac_i32_32x32x64_i8(f.w[i], f.x[j], acc[i][j],
+                                                                    f.m[i], 0, 0);
             keep_order();
         }
     };
     if (piece.count > 0) {
         ROI_LDS uint8_t *b0 = base, *b1 = base + kStage, *b2 = base + 2 * kStage;
-        Step even, odd;
+        Half lo, hi;
         stage(0, 0, kLoads, b0);
         stage(1, 0, kLoads, b1);
         stage(2, 0, kLoads, b2);
         loads_barrier<2 * kLoads>();
 #pragma unroll
-        for (int i = 0; i < kI; ++i) read_w(b0, even, i);
+        for (int i = 0; i < kI; ++i) read_w(b0, 0, lo, i);
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) read_x(b0, even, j);
+        for (int j = 0; j < kJ; ++j) read_x(b0, 0, lo, j);
         // past the end of the sum or of this part, loads are in bounds or zeros,
         // and unused
-        int s = 0;
-        for (; s + 2 <= piece.count; s += 2) {
+        for (int s = 0; s < piece.count; ++s) {
+            half(lo, b0, 1, hi, std::false_type{}, 0, b0);
             loads_barrier<kLoads>();
-            step(even, odd, b1, s + 3, b0);
-            loads_barrier<kLoads>();
-            step(odd, even, b2, s + 4, b1);
+            half(hi, b1, 0, lo, std::true_type{}, s + 3, b0);
             ROI_LDS uint8_t* const t = b0;
-            b0 = b2;
-            b2 = b1;
-            b1 = t;
-        }
-        if (s < piece.count) {
-            loads_barrier<kLoads>();
-            step(even, odd, b1, s + 3, b0);
+            b0 = b1;
+            b1 = b2;
+            b2 = t;
         }
         loads_barrier();
     }
-    static_assert(3 * kStage >= 4 * kTile * kRowBytes, "results pass LDS");
-    write_tile<kTile, Out>(a, piece, acc, base);
+    write_tile<kTile, 32, Out>(a, piece, acc, base);
 }
 
-// The sums of the tiles that were cut: one wave for 16 x 16 results, eight parts
-// on their way at a time.
-template <int kTile, typename Out>
+// The sums of the tiles that were cut: one wave for a quad of results a lane,
+// eight parts on their way at a time.
+template <int kTile, int kBlock, typename Out>
 __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
 {
-    using T = Tile<kTile>;
-    const int lane = threadIdx.x;
-    const int j = blockIdx.x % T::kJ, i = blockIdx.x / T::kJ % T::kI;
-    const int wave = blockIdx.x / (T::kJ * T::kI) % T::kWaves;
-    const uint32_t tile = blockIdx.x / (T::kJ * T::kI * T::kWaves);
+    using H = Held<kTile, kBlock>;
+    constexpr int kAll = H::kI * H::kJ * H::kQuads;
+    const int q = blockIdx.x % H::kQuads, j = blockIdx.x / H::kQuads % H::kJ;
+    const int i = blockIdx.x / (H::kQuads * H::kJ) % H::kI;
+    const int wave = blockIdx.x / kAll % Tile<kTile>::kWaves;
+    const uint32_t tile = blockIdx.x / (kAll * Tile<kTile>::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
-    const int* from = a.partial + part_at<kTile>((int64_t)tile * a.grid.splits, wave, i, j, lane);
+    const int* from = a.partial + H::part_at((int64_t)tile * a.grid.splits, wave, i, j, q);
     i32x4 sum = {};
 #pragma unroll 8
     for (uint32_t p = 0; p < a.grid.splits; ++p)
         sum += *reinterpret_cast<const i32x4*>(from + (int64_t)p * (kTile * kTile));
-    const int r = piece.m * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * (lane >> 4);
-    const int t = piece.n * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
+    const int r = piece.m * kTile + wave / Tile<kTile>::kAcross * 16 * Tile<kTile>::kI + 4 * H::quad(i, q);
+    const int t = piece.n * kTile + wave % Tile<kTile>::kAcross * 16 * Tile<kTile>::kJ + H::column(j);
     if (r >= a.rows || t >= a.tokens) return;
     float ws[4], add[4];
     row_scales(a, r, ws, add);
@@ -569,9 +591,13 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
         hipLaunchKernelGGL((linear_tile_kernel<kTile, true, Out>), grid, block, 0, stream, a);
     else
         hipLaunchKernelGGL((linear_tile_kernel<kTile, false, Out>), grid, block, 0, stream, a);
-    if (a.grid.rest() > 0)
-        hipLaunchKernelGGL((linear_sum_kernel<kTile, Out>), dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves),
-                           dim3(64), 0, stream, a);
+    if (a.grid.rest() > 0) {
+        const dim3 sums(a.grid.rest() * T::kI * T::kJ * T::kWaves);
+        if (a.meta)
+            hipLaunchKernelGGL((linear_sum_kernel<kTile, 32, Out>), sums, dim3(64), 0, stream, a);
+        else
+            hipLaunchKernelGGL((linear_sum_kernel<kTile, 16, Out>), sums, dim3(64), 0, stream, a);
+    }
 }
 
 template <int kWaves, int kRow, int kTokens, int kDepth, bool kPacked, typename Out>

@@ -20,6 +20,7 @@ namespace roi {
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 #define ROI_LDS __attribute__((address_space(3)))
 
@@ -156,13 +157,31 @@ __device__ __forceinline__ Piece piece_of(const Grid& g, uint32_t block)
     return p;
 }
 
-// Where a wave's 16 x 16 results (i, j) of a part lie in the workspace: four
-// values a lane, in the order of the tile's threads.
-template <int kTile>
-__device__ __forceinline__ int64_t part_at(int64_t part, int wave, int i, int j, int lane)
-{
-    return part * (kTile * kTile) + (((wave * Tile<kTile>::kI + i) * Tile<kTile>::kJ + j) * 64 + lane) * 4;
-}
+// Which results a lane holds of a wave's, by the matrix instructions' blocks of
+// 16 x 16 (v_mfma 16x16: a quad of four consecutive rows of one column) or
+// 32 x 32 (four such quads).  Quads are counted along the rows, four each.
+template <int kTile, int kBlock>
+struct Held {
+    static constexpr int kI = Tile<kTile>::kI * 16 / kBlock, kJ = Tile<kTile>::kJ * 16 / kBlock;
+    static constexpr int kQuads = kBlock == 16 ? 1 : 4; // of a block
+    __device__ __forceinline__ static int quad(int i, int q)
+    {
+        const int lane = threadIdx.x & 63;
+        return kBlock == 16 ? 4 * i + lane / 16 : 8 * i + 2 * q + lane / 32;
+    }
+    __device__ __forceinline__ static int column(int j)
+    {
+        return kBlock * j + (int)(threadIdx.x & 63) % kBlock;
+    }
+    // Where quad q of block (i, j) of a part of a tile lies in the workspace: four
+    // values a lane, in the order of the tile's threads.
+    __device__ __forceinline__ static int64_t part_at(int64_t part, int wave, int i, int j, int q)
+    {
+        constexpr int kAll = kI * kJ * kQuads;
+        return part * (kTile * kTile) +
+               ((wave * kAll + (i * kJ + j) * kQuads + q) * 64 + (int)(threadIdx.x & 63)) * 4;
+    }
+};
 
 // Results of a wave to memory, by way of its own part of LDS: a lane holds four
 // consecutive columns, and 16 lanes 16 different rows, so stored as they are
@@ -176,10 +195,10 @@ struct RowsOut {
     static constexpr int kAtOnce = 64 / kChunks;         // rows a wave stores at once
     static_assert(kChunks >= 8 && kChunks <= 64, "rows of 128 to 1024 bytes");
 
-    // The results of block i for row `row` (of 16 lanes' rows), lane group g.
-    __device__ __forceinline__ static ROI_LDS uint8_t* at(ROI_LDS uint8_t* lds, int row, int i, int g)
+    // The four results of a quad in row `row`.
+    __device__ __forceinline__ static ROI_LDS uint8_t* at(ROI_LDS uint8_t* lds, int row, int quad)
     {
-        const int byte = (4 * i + g) * kBytes;
+        const int byte = quad * kBytes;
         return lds + row * kRow + ((byte / 16) ^ (row % kChunks)) * 16 + byte % 16;
     }
     // Store number n: this lane's row, its chunk, and the chunk's bytes.
