@@ -497,6 +497,17 @@ def _workspace(given, need, like):
     return given, given.numel()
 
 
+def _rows_cols(t, name):
+    """Rows and columns of a tensor whose rows have scales: 2-D, or 1-D as one row."""
+    shape = t.shape
+    if len(shape) == 2:
+        return shape
+    if len(shape) == 1:
+        return 1, shape[0]
+    raise ValueError(f"{name} must be 1-D or 2-D, got {len(shape)}-D (flatten the leading "
+                     f"dimensions first: every row has its scale)")
+
+
 def quantize_rows(x, out=None):
     """int8 rows with one fp32 scale each: x bf16 or fp32 [rows, cols] (1-D: one
     row) -> (q int8 like x, scale fp32 [rows]), x ~ q scale[:, None], |q| <= 127.
@@ -510,7 +521,7 @@ def quantize_rows(x, out=None):
     code = _dtype_code(x.dtype, "x")
     if not (x.is_cuda and x.is_contiguous()):
         _check_tensor(x, x.dtype, "x")
-    rows, cols = _shape2d(x)
+    rows, cols = _rows_cols(x, "x")
     device = x.get_device()
     if out is None:
         q = torch.empty_like(x, dtype=torch.int8)
@@ -529,7 +540,7 @@ def dequantize_rows(q, scale, dtype=None, out=None):
     quantize_rows' rows where the backward of another operation needs them."""
     torch = _torch or _load_torch()
     _check_tensor(q, torch.int8, "q")
-    rows, cols = _shape2d(q)
+    rows, cols = _rows_cols(q, "q")
     device = q.get_device()
     _check_sized(scale, torch.float32, "scale", (rows,), device)
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype

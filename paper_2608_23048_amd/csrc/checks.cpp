@@ -402,9 +402,11 @@ GradPlan plan_grad(int64_t m, int64_t n, int64_t k)
     GradPlan p{};
     p.cut = cut_product(m, n, k, kStep, kGradCost);
     p.bytes = p.cut.bytes;
-    // offsets within a tile of the transposed operand stay below 2^31
+    // offsets within a tile of the transposed operand stay below 2^31, and the
+    // pass that writes it has fewer than 2^32 threads (256 for 64 x 128 elements)
     if (m == 0 || n == 0 || k == 0 || k > ((int64_t)1 << 21)) return p;
     const int64_t ready_k = (k + kStep - 1) / kStep * kStep;
+    if (ready_k / 64 * ((n + 127) / 128) >= (int64_t)1 << 24) return p;
     const Cut c = cut_tiles(m, n, k, kStep, 256, kReadyCost);
     const double us = c.us + 3 + 3 * (double)ready_k * (double)n / 4.0e6;
     if (us < p.cut.us && c.fits) {

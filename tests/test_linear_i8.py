@@ -143,6 +143,24 @@ def test_host_tensors_are_refused():
         roi.quantize_rows([1.0])
 
 
+def test_checks_and_plans_under_sanitizers(tmp_path):
+    import os
+    import shutil
+    pytest.importorskip("tests.test_sanitizers")
+    from tests.test_sanitizers import CSRC, HERE, ROOT, SAN, build_and_run
+    gxx = shutil.which("g++")
+    if not gxx or not os.path.exists("/opt/rocm/include/hip/hip_runtime_api.h"):
+        pytest.skip("g++ or the HIP headers not available")
+    exe = tmp_path / "linear_checks_driver"
+    out = build_and_run([gxx, "-std=c++17", *SAN, "-Wall", "-Wextra", "-Werror",
+                         "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                         f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}",
+                         os.path.join(CSRC, "checks.cpp"),
+                         os.path.join(HERE, "linear_checks_driver.cpp"), "-o", str(exe)], exe,
+                        tmp_path)
+    assert "linear checks ok" in out
+
+
 # ------------------------------------------------------------------ references
 FLOOR = np.float32(2.0 ** -126)
 
@@ -280,6 +298,10 @@ def test_rows_given_outputs_and_empty():
         assert roi.dequantize_rows(e, se).shape == shape
     with pytest.raises(ValueError, match="contiguous"):
         roi.quantize_rows(x.t())
+    with pytest.raises(ValueError, match="2-D"):
+        roi.quantize_rows(x.view(5, 11, 3))
+    with pytest.raises(ValueError, match="2-D"):
+        roi.dequantize_rows(q.view(5, 11, 3), s)
     with pytest.raises(ValueError, match="shape"):
         roi.quantize_rows(x, out=(q2[:4], s2))
     with pytest.raises(ValueError, match="shape"):
@@ -336,11 +358,13 @@ def test_linear_2of4_bit_exact(tokens, rows, cols):
 
 
 @gpu
-@pytest.mark.parametrize("tokens", [1, 70, 300])
-def test_linear_extremes(tokens):
+@pytest.mark.filterwarnings("ignore:overflow:RuntimeWarning")
+@pytest.mark.parametrize("cols", [131071, 131056])
+@pytest.mark.parametrize("tokens", [1, 12, 30, 70, 300, 1100])
+def test_linear_extremes(tokens, cols):
     """The largest sums, rows of zeros with the smallest scale, a NaN row."""
     import torch
-    cols, rows = 131071, 5
+    rows = 5
     xq = np.full((tokens, cols), -128, np.int8)
     wq = np.full((rows, cols), -128, np.int8)
     wq[1] = 127
@@ -353,6 +377,25 @@ def test_linear_extremes(tokens):
     row = (want.astype(np.float32) * ws) * np.float32(2.0 ** -126)
     assert np.array_equal(y[:-1], np.broadcast_to(row, (tokens - 1, rows)))
     assert np.isnan(y[-1]).all()
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [1, 12, 30, 70, 1100])
+def test_linear_2of4_longest_sum(tokens):
+    """131040 columns, half of them kept, and fields of every value."""
+    import torch
+    cols, rows = 131040, 6
+    rng = np.random.default_rng(tokens)
+    xq = np.full((tokens, cols), -128, np.int8)
+    xq[-1] = rng.integers(-128, 128, cols)
+    values, idx = random_2of4(rng, rows, cols)
+    values[:3] = np.array([-128, 127, 1], np.int8)[:, None]
+    y = roi.linear_i8(dev(xq), torch.ones(tokens, device="cuda"), dev(values),
+                      torch.ones(rows, device="cuda"), meta=dev(meta_of(idx).view(np.int32)),
+                      dtype=torch.float32)
+    dense = expand(values, idx, cols).astype(np.float64)
+    want = xq.astype(np.float64) @ dense.T
+    assert np.array_equal(f32(y), want.astype(np.float32))
 
 
 @gpu
@@ -515,11 +558,11 @@ def test_grads_empty_sums_and_nan(by_tokens):
 
 
 @gpu
-def test_padding_and_neighbours_are_left_alone():
+@pytest.mark.parametrize("tokens,rows,cols", [(70, 45, 77), (300, 257, 144), (1030, 1100, 390)])
+def test_padding_and_neighbours_are_left_alone(tokens, rows, cols):
     """Outputs are written exactly; what lies behind them in memory stays, and
     padded (zero) rows give zeros."""
     import torch
-    tokens, rows, cols = 70, 45, 77
     guard = 64
 
     def framed(n, dtype):
@@ -543,7 +586,9 @@ def test_padding_and_neighbours_are_left_alone():
     roi.linear_i8_grad_input(gy, wq, ws, out=gx.view(tokens, cols))
     bd, xd = framed(tokens * cols, torch.float32)
     roi.dequantize_rows(q, s, out=xd.view(tokens, cols))
-    for b in (bq, bs, by, bw, bx, bd):
+    bz, z = framed(tokens * rows, torch.float32)
+    roi.linear_i8(q, s, wq, ws, out=z.view(tokens, rows))
+    for b in (bq, bs, by, bw, bx, bd, bz):
         assert (b[-guard:] == 77).all()
     assert (y[50:] == 0).all() and (xd.view(tokens, cols)[50:] == 0).all()
 
@@ -608,12 +653,14 @@ def test_masked_layer_step(n, m):
 
 
 @gpu
-def test_step_in_a_graph_and_on_a_stream():
+@pytest.mark.parametrize("tokens,rows,cols", [(200, 136, 272), (2000, 256, 1024)])
+def test_step_in_a_graph_and_on_a_stream(tokens, rows, cols):
     """The step captured once and replayed on new inputs, with eager work
-    between the replays, and on a stream of its own: the eager bits each time."""
+    between the replays, and on a stream of its own: the eager bits each time.
+    The second size cuts its sums (a workspace in every gradient)."""
     import torch
     from paper_2608_23048_amd import workloads as wl
-    tokens, rows, cols = 200, 136, 272
+    assert tokens == 200 or roi.linear_i8_grad_weight_workspace(tokens, rows, cols) > 0
     W, logits, _ = wl.small_case(rows, cols, 1, device="cuda")
     x = torch.randn(tokens, cols, device="cuda").bfloat16()
     gy = torch.randn(tokens, rows, device="cuda").bfloat16()
@@ -637,3 +684,86 @@ def test_step_in_a_graph_and_on_a_stream():
     side.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@gpu
+def test_two_graphs_of_cut_sums_in_turn():
+    """Two captured calls with workspaces of their own, replayed one after the
+    other and on two streams at once."""
+    import torch
+    tokens, rows, cols = 3000, 300, 520
+    data = [(torch.randn(tokens, rows, device="cuda").bfloat16(),
+             *roi.quantize_rows(torch.randn(tokens, cols, device="cuda"))) for _ in range(2)]
+    want = [roi.linear_i8_grad_weight(*d) for d in data]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for d in data:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(roi.linear_i8_grad_weight(*d))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for turn in range(3):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            if turn == 2:
+                with torch.cuda.stream(s):
+                    g.replay()
+            else:
+                g.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+
+
+@gpu
+def test_given_workspace():
+    import torch
+    tokens, rows, cols = 3000, 300, 520
+    gy = torch.randn(tokens, rows, device="cuda").bfloat16()
+    x = roi.quantize_rows(torch.randn(tokens, cols, device="cuda"))
+    w = roi.quantize_rows(torch.randn(rows, cols, device="cuda"))
+    for fn, need, args in (
+            (roi.linear_i8_grad_weight, roi.linear_i8_grad_weight_workspace, (gy, *x)),
+            (roi.linear_i8_grad_input, roi.linear_i8_grad_input_workspace, (gy, *w)),
+            (roi.linear_i8, roi.linear_i8_workspace, (*x, *w))):
+        n = need(tokens, rows, cols)
+        work = torch.full((n + 64,), 255, dtype=torch.uint8, device="cuda")  # NaN as fp32
+        assert torch.equal(fn(*args, workspace=work[:n] if n else None), fn(*args))
+        assert (work[n:] == 255).all()
+        if n:
+            with pytest.raises(roi.RoiError, match="workspace"):
+                fn(*args, workspace=work[:n - 16])
+    assert roi.linear_i8_grad_weight_workspace(tokens, rows, cols) > 0
+    with pytest.raises(roi.RoiError):
+        roi.linear_i8_workspace(-1, 4, 4)
+
+
+@gpu
+def test_past_32_bits():
+    """Rows whose elements lie past 2^32, through every operator: checked on the
+    last rows."""
+    import torch
+    tokens, cols, rows = 67000, 65536, 24     # 4.4e9 elements
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(tokens, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    xq, xs = roi.quantize_rows(x)
+    tail = x[-3:].clone()
+    tq, ts = roi.quantize_rows(tail)
+    assert torch.equal(xq[-3:], tq) and torch.equal(xs[-3:], ts)
+    roi.dequantize_rows(xq, xs, out=x)
+    assert torch.equal(x[-3:], roi.dequantize_rows(tq, ts))
+    del x
+    wq, ws = roi.quantize_rows(torch.empty(rows, cols, device="cuda").normal_(generator=g))
+    y = roi.linear_i8(xq, xs, wq, ws)
+    assert torch.equal(y[-3:], roi.linear_i8(tq, ts, wq, ws))
+    gy = torch.zeros(tokens, rows, dtype=torch.bfloat16, device="cuda")
+    gy[-3:].normal_(generator=g)
+    gw = roi.linear_i8_grad_weight(gy, xq, xs)
+    h = lambda t: t.cpu().numpy()  # noqa: E731
+    assert_grad(f32(gw.float()), f32(gy[-3:].float()), h(tq), h(ts), "grad_w")
+    gx = roi.linear_i8_grad_input(gy, wq, ws)
+    assert torch.equal(gx[-3:], roi.linear_i8_grad_input(gy[-3:].clone(), wq, ws))
+    assert (gx[:-3] == 0).all()
