@@ -478,6 +478,9 @@ def test_grads_of_many_tiles(k, d, c, by_tokens):
     tiles and cut ones in one call, with and without whole chunks a row."""
     dy, q, s = grad_inputs(*((k, d) if by_tokens else (d, k)), c, k + d, by_tokens)
     fn = roi.linear_i8_grad_weight if by_tokens else roi.linear_i8_grad_input
+    need = (roi.linear_i8_grad_weight_workspace(k, d, c) if by_tokens
+            else roi.linear_i8_grad_input_workspace(d, k, c))
+    assert need >= 2 * k * c
     got = f32(fn(dy.cuda(), dev(q), dev(s)).float())
     dy = dy.float().numpy()
     assert_grad(got, dy if by_tokens else np.ascontiguousarray(dy.T), q, s, f"{k}x{d}x{c}")
@@ -506,6 +509,31 @@ def test_linear_of_many_tiles(tokens, rows, cols, packed):
     y = roi.linear_i8(*args, meta=meta, dtype=torch.float32)
     assert np.array_equal(f32(y).view(np.uint32), want.view(np.uint32))
     assert np.array_equal(bf16_bits(roi.linear_i8(*args, meta=meta)), bf16_rne_bits(want))
+
+
+@gpu
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("tokens,rows,cols", [(1100, 130, 8192), (4096, 4352, 4096)])
+def test_linear_of_cut_sums(tokens, rows, cols, packed):
+    """Long sums of few tiles, and a last round of few tiles: cut and added up."""
+    import torch
+    assert roi.linear_i8_workspace(tokens, rows, cols, packed) > 0
+    rng = np.random.default_rng(tokens)
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    draw = lambda *n: torch.randint(-128, 128, n, device="cuda", generator=g,  # noqa: E731
+                                    dtype=torch.int8)
+    xq, xs = draw(tokens, cols), torch.rand(tokens, device="cuda", generator=g)
+    ws, meta = torch.rand(rows, device="cuda", generator=g), None
+    if packed:
+        values, idx = random_2of4(rng, rows, cols)
+        wq, dense = dev(values), dev(expand(values, idx, cols))
+        meta = dev(meta_of(idx).view(np.int32))
+    else:
+        dense = wq = draw(rows, cols)
+    # products and sums of integers below 2^53 are exact in fp64
+    want = torch.mm(xq.double(), dense.double().t().contiguous()).float() * ws * xs[:, None]
+    assert torch.equal(roi.linear_i8(xq, xs, wq, ws, meta=meta, dtype=torch.float32), want)
+    assert torch.equal(roi.linear_i8(xq, xs, wq, ws, meta=meta), want.bfloat16())
 
 
 @gpu
