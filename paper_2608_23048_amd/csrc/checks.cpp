@@ -380,42 +380,68 @@ Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& c
     return small.us < big.us && small.fits ? small : big;
 }
 
+namespace {
+
+// Of a copy of rows into the workspace: bytes read and written.
+double copy_us(double bytes) { return 2 + bytes / 4.0e6; }
+
+} // namespace
+
 // The streaming kernel takes 32 tokens at a time, each time at 7e6 bytes of a
 // dense weight a microsecond from the caches (6e6 at 2:4, of the dense weight it
-// stands for).  64 tokens through 3584 x 3584 take 5.6 us so and 17.5 in tiles,
-// through 18944 x 3584 25 and 29; 128 tokens 8.3 and 17.4, 44 and 30.
+// stands for; 2.5e6 where rows end within 16 bytes).  64 tokens through 3584 x
+// 3584 take 5.6 us so and 17.5 in tiles, through 18944 x 3584 25 and 29; 128
+// tokens 8.3 and 17.4, 44 and 30.
 LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
 {
     LinearPlan p{};
     p.few = tokens <= 32;
     if (p.few) return p;
     p.cut = cut_product(rows, tokens, cols, 128, packed ? kPackedCost : kLinearCost);
-    const double few_us = 3 + (double)((tokens + 31) / 32) * (double)rows * (double)cols /
-                                  (packed ? 6.0e6 : 7.0e6);
-    p.few = tokens <= 1024 && few_us < p.cut.us;
+    p.row = (cols + 15) / 16 * 16;
+    double tiles_us = p.cut.us;
+    if (p.row != cols) {
+        p.x_bytes = padded256(tokens * p.row);
+        p.w_bytes = padded256(rows * p.row);
+        tiles_us += 2 + copy_us(2.0 * (double)(tokens + rows) * (double)cols);
+    }
+    p.bytes = p.x_bytes + p.w_bytes + p.cut.bytes;
+    const double rate = packed ? 6.0e6 : p.row == cols ? 7.0e6 : 2.5e6;
+    const double few_us =
+        3 + (double)((tokens + 31) / 32) * (double)rows * (double)cols / rate;
+    p.few = tokens <= 1024 && few_us < tiles_us;
     return p;
 }
 
-GradPlan plan_grad(int64_t m, int64_t n, int64_t k)
+GradPlan plan_grad(int64_t m, int64_t n, int64_t k, bool sum_rows)
 {
     constexpr int64_t kStep = 64;
     GradPlan p{};
     p.cut = cut_product(m, n, k, kStep, kGradCost);
-    p.bytes = p.cut.bytes;
+    const int64_t dy_len = sum_rows ? m : k, dy_rows = sum_rows ? k : m;
+    p.dy_row = (dy_len + 7) / 8 * 8;
+    if (p.dy_row != dy_len) p.dy_bytes = padded256(2 * dy_rows * p.dy_row);
+    const int64_t ready_k = (k + kStep - 1) / kStep * kStep;
     // offsets within a tile of the transposed operand stay below 2^31, and the
     // pass that writes it has fewer than 2^32 threads (256 for 64 x 128 elements)
-    if (m == 0 || n == 0 || k == 0 || k > ((int64_t)1 << 21)) return p;
-    const int64_t ready_k = (k + kStep - 1) / kStep * kStep;
-    if (ready_k / 64 * ((n + 127) / 128) >= (int64_t)1 << 24) return p;
-    const Cut c = cut_tiles(m, n, k, kStep, 256, kReadyCost);
-    const double us = c.us + 3 + 3 * (double)ready_k * (double)n / 4.0e6;
-    if (us < p.cut.us && c.fits) {
-        p.ready = true;
-        p.ready_k = ready_k;
-        p.ready_bytes = (2 * n * ready_k + 255) / 256 * 256;
-        p.cut = c;
-        p.bytes = p.ready_bytes + c.bytes;
+    if (m > 0 && n > 0 && k > 0 && k <= ((int64_t)1 << 21) &&
+        ready_k / 64 * ((n + 127) / 128) < (int64_t)1 << 24) {
+        const Cut c = cut_tiles(m, n, k, kStep, 256, kReadyCost);
+        const double us = c.us + 3 + 3 * (double)ready_k * (double)n / 4.0e6;
+        const double fused_us = p.cut.us + (n % 4 ? copy_us(2.0 * (double)k * (double)n) : 0);
+        if (us < fused_us && c.fits) {
+            p.ready = true;
+            p.ready_k = ready_k;
+            p.ready_bytes = padded256(2 * n * ready_k);
+            p.cut = c;
+        }
     }
+    p.q_row = n;
+    if (!p.ready && n % 4) {
+        p.q_row = (n + 15) / 16 * 16;
+        p.q_bytes = padded256(k * p.q_row);
+    }
+    p.bytes = p.dy_bytes + p.q_bytes + p.ready_bytes + p.cut.bytes;
     return p;
 }
 

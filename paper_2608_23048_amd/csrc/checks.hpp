@@ -97,8 +97,8 @@ int validate_rows_i8(const void* x, int dtype, const int8_t* q, const float* sca
                      int64_t cols, bool x_out, bool* todo);
 
 // The longest int8 row and the most of them; the largest product and gradient
-// sizes (kernels count tokens, rows and columns in 32 bits); and the longest exact int32 sum of
-// products of two int8 values (131071 * 2^14 < 2^31).
+// sizes (kernels count tokens, rows and columns in 32 bits); and the longest
+// exact int32 sum of products of two int8 values (131071 * 2^14 < 2^31).
 constexpr int64_t kMaxRowsI8 = (int64_t)1 << 31;
 constexpr int64_t kMaxLinearDim = (int64_t)1 << 22;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
@@ -130,23 +130,34 @@ constexpr TileCost kReadyCost = {1.40, 12, 0, 0, 0};
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost);
 
 // The int8 product's way: with few tokens the kernel that streams the weight
-// past them (no workspace), else the tiles of `cut`.
+// past them (no workspace), else the tiles of `cut`, before which rows of a
+// length that is no multiple of 16 are copied to the workspace (x_bytes, w_bytes),
+// to rows of `row` bytes; the parts of cut tiles follow.
 struct LinearPlan {
     bool few;
+    int64_t row, x_bytes, w_bytes;
+    int64_t bytes; // of workspace
     Cut cut;
 };
 LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed);
 
-// A gradient's way (out [m, n], summed over k): with `ready` the int8 operand is
-// first written to the workspace in bf16, transposed, [n, ready_k]; the parts of
-// cut tiles follow it.
+// Bytes of workspace arrays, each from a multiple of 256 bytes on.
+constexpr int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// A gradient's way (out [m, n], summed over k).  The tiles' loads take whole
+// 16-byte pieces of grad_y's rows (k values with `sum_rows` false, else m) and
+// words of q's: rows that end within one are first copied to the workspace, to
+// rows of dy_row and q_row elements.  With `ready` q is first written there in
+// bf16, transposed, [n, ready_k].  The workspace holds these arrays in this order
+// (dy_bytes, q_bytes, ready_bytes; 0: not there), then the parts of cut tiles.
 struct GradPlan {
     bool ready;
-    int64_t ready_k, ready_bytes;
+    int64_t dy_row, q_row, ready_k;
+    int64_t dy_bytes, q_bytes, ready_bytes;
     int64_t bytes; // of workspace
     Cut cut;
 };
-GradPlan plan_grad(int64_t m, int64_t n, int64_t k);
+GradPlan plan_grad(int64_t m, int64_t n, int64_t k, bool sum_rows);
 
 // Sizes of a linear call: ROI_OK, or why the call is refused.
 int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols);

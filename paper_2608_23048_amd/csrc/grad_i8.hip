@@ -43,6 +43,7 @@ struct GradArgs {
     uint16_t* ready; // s q, transposed: bf16 [cols, ready_k], or NULL
     int ready_k;     // K rounded up to whole steps
     int K, D, cols;
+    int dy_row, q_row; // elements of a row of dy and of q
     Grid grid; // tiles along d and c
 };
 
@@ -50,7 +51,7 @@ struct GradArgs {
 // row k at place j ^ 2 (k & 3) ^ (k & 8), so that the rows that 32 lanes read
 // together (four of each of two groups of 16) lie in different banks.  Otherwise [kTile d] k-rows (mm.hpp).
 // What lies past K is zero; past D, zero or the last row again.
-template <int kTile, bool kSumRows, bool kWhole, bool kUnseen = kSumRows>
+template <int kTile, bool kSumRows, bool kUnseen = kSumRows>
 struct DyTile {
     static constexpr int kThreads = Tile<kTile>::kThreads;
     static constexpr int kLoads = kTile * kRowBytes / (16 * kThreads);
@@ -101,19 +102,9 @@ struct DyTile {
         const uint8_t* p = base + 2 * (kSumRows ? (int64_t)k0 * D : k0);
         const bool live = row(i) < (kSumRows ? K - k0 : D - d0) &&
                           (kSumRows || 8 * chunk() < K - k0);
-        if constexpr (kWhole) {
-            load_to_lds<kUnseen>(buffer_at(p), live ? at : kNowhere,
-                                  2 * (i * kThreads / kAcrossRow) * width(),
-                                  dst + (i * kThreads + wave * 64) * 16);
-        } else {
-            Quad v{};
-            if (live && at != kNowhere) {
-                const int64_t k = (kSumRows ? d0 : k0) + 8 * chunk(); // within dy's row
-                v = load_row<Quad>(p + 2 * ((int64_t)row(i) * width() - (kSumRows ? d0 : k0)), 2 * k,
-                                   2 * (int64_t)width());
-            }
-            lds_write(dst + (i * kThreads + threadIdx.x) * 16, v);
-        }
+        load_to_lds<kUnseen>(buffer_at(p), live ? at : kNowhere,
+                             2 * (i * kThreads / kAcrossRow) * width(),
+                             dst + (i * kThreads + wave * 64) * 16);
     }
     // The 16 columns d of the wave's block j, sum indices 32 h + 8 g .. + 7.
     __device__ __forceinline__ bf16x8 read(const ROI_LDS uint8_t* src, int j, int h) const
@@ -151,7 +142,7 @@ struct QTile {
 
     __device__ __forceinline__ QTile(const GradArgs& a, int c0)
         : base(reinterpret_cast<const uint8_t*>(a.q) + c0), scale(a.scale), K(a.K),
-          left(a.cols - c0 - 4 * group()), cols(a.cols)
+          left(a.cols - c0 - 4 * group()), cols(a.q_row)
     {
         const int lane = threadIdx.x & 63;
         to = place(4 * group(), oct());
@@ -257,15 +248,15 @@ __device__ __forceinline__ void write_tile(const GradArgs& a, const Piece& piece
 // steps and dy's of three: what is loaded to LDS in one step is awaited two
 // steps later.  The int8 tile of step s + 3 goes to registers in step s and to
 // LDS, scaled, in step s + 1.
-template <int kTile, bool kSumRows, bool kWhole>
+template <int kTile, bool kSumRows>
 __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void grad_tile_kernel(GradArgs a)
 {
     constexpr int kTileBytes = kTile * kRowBytes;
     static_assert(kTileBytes == kSum * kTile * 2, "both layouts of dy take the same LDS");
     constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
     static_assert(kJ == 4 && kI % 2 == 0, "DyTile::read and QTile::read");
-    using Dy = DyTile<kTile, kSumRows, kWhole>;
-    using Q = QTile<kTile, kWhole>;
+    using Dy = DyTile<kTile, kSumRows>;
+    using Q = QTile<kTile, true>;
     static_assert(Dy::kLoads <= kI && kI >= 4, "a part a row");
     __shared__ __attribute__((aligned(16))) uint8_t lds[5][kTileBytes];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0];
@@ -277,7 +268,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void grad_tile_kernel(Gra
     const int k0 = piece.first * kSum;
 
     f32x4 acc[kI][kJ] = {};
-    const Dy dy(a.dy, a.K, a.D, d0, bd);
+    const Dy dy(a.dy, kSumRows ? a.K : a.dy_row, kSumRows ? a.dy_row : a.D, d0, bd);
     Q q(a, c0);
     struct Half {
         bf16x8 q[kI], y[kJ];
@@ -354,13 +345,13 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void grad_tile_kernel(Gra
 // conversion beside it takes 1.7; the conversion by itself is one pass over q.
 // The matrix cores are busy for 75 % of the time (8192 x 3584 x 18944), and the
 // clock goes down to 1.8 GHz under that load.
-template <bool kSumRows, bool kWhole>
+template <bool kSumRows>
 __global__ __launch_bounds__(Tile<256>::kThreads) void grad_ready_kernel(GradArgs a)
 {
     constexpr int kTile = 256, kTileBytes = kTile * kRowBytes;
     constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
-    using Dy = DyTile<kTile, kSumRows, kWhole>;
-    using Q = DyTile<kTile, false, true, kSumRows>;
+    using Dy = DyTile<kTile, kSumRows>;
+    using Q = DyTile<kTile, false, kSumRows>;
     constexpr int kLoads = Dy::kLoads + Q::kLoads;
     static_assert(kLoads == kI, "a load a row");
     __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];
@@ -372,7 +363,7 @@ __global__ __launch_bounds__(Tile<256>::kThreads) void grad_ready_kernel(GradArg
     const int k0 = piece.first * kSum;
 
     f32x4 acc[kI][kJ] = {};
-    const Dy dy(a.dy, a.K, a.D, d0, bd);
+    const Dy dy(a.dy, kSumRows ? a.K : a.dy_row, kSumRows ? a.dy_row : a.D, d0, bd);
     const Q q(a.ready, a.ready_k, a.cols, c0, bc);
     auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
     auto stage = [&](int s, int i) {
@@ -474,20 +465,21 @@ __global__ __launch_bounds__(64) void grad_sum_kernel(GradArgs a)
     }
 }
 
+template <int kTile>
+void launch_sums(const GradArgs& a, hipStream_t stream)
+{
+    using T = Tile<kTile>;
+    if (a.grid.rest() > 0)
+        hipLaunchKernelGGL((grad_sum_kernel<kTile>),
+                           dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves), dim3(64), 0, stream, a);
+}
+
 template <int kTile, bool kSumRows>
 void launch_tiles(const GradArgs& a, hipStream_t stream)
 {
-    using T = Tile<kTile>;
-    const dim3 grid(a.grid.blocks()), block(T::kThreads);
-    // 16-byte chunks of dy's rows and 4-byte words of q's that end with the row
-    const bool whole = (kSumRows ? a.D : a.K) % 8 == 0 && a.cols % 4 == 0;
-    if (whole)
-        hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows, true>), grid, block, 0, stream, a);
-    else
-        hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows, false>), grid, block, 0, stream, a);
-    if (a.grid.rest() > 0)
-        hipLaunchKernelGGL((grad_sum_kernel<kTile>), dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves), dim3(64),
-                           0, stream, a);
+    hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows>), dim3(a.grid.blocks()),
+                       dim3(Tile<kTile>::kThreads), 0, stream, a);
+    launch_sums<kTile>(a, stream);
 }
 
 template <bool kSumRows>
@@ -498,11 +490,9 @@ void launch_ready(const GradArgs& a, hipStream_t stream)
         hipLaunchKernelGGL((ready_kernel<true>), blocks, dim3(256), 0, stream, a);
     else
         hipLaunchKernelGGL((ready_kernel<false>), blocks, dim3(256), 0, stream, a);
-    const dim3 grid(a.grid.blocks()), block(Tile<256>::kThreads);
-    if ((kSumRows ? a.D : a.K) % 8 == 0)
-        hipLaunchKernelGGL((grad_ready_kernel<kSumRows, true>), grid, block, 0, stream, a);
-    else
-        hipLaunchKernelGGL((grad_ready_kernel<kSumRows, false>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((grad_ready_kernel<kSumRows>), dim3(a.grid.blocks()),
+                       dim3(Tile<256>::kThreads), 0, stream, a);
+    launch_sums<256>(a, stream);
 }
 
 template <bool kSumRows>
@@ -510,21 +500,30 @@ int launch(GradArgs a, const GradPlan& plan, void* workspace, const char* what, 
 {
     if (!plan.cut.fits)
         return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
-    using T = Tile<256>;
-    a.grid = grid_of(plan.cut);
-    a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.ready_bytes);
-    if (plan.ready) {
-        a.ready = static_cast<uint16_t*>(workspace);
-        a.ready_k = (int)plan.ready_k;
-        launch_ready<kSumRows>(a, stream);
-        if (a.grid.rest() > 0)
-            hipLaunchKernelGGL((grad_sum_kernel<256>), dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves),
-                               dim3(64), 0, stream, a);
-    } else if (plan.cut.tile == 256) {
-        launch_tiles<256, kSumRows>(a, stream);
-    } else {
-        launch_tiles<128, kSumRows>(a, stream);
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    if (plan.dy_bytes) {
+        launch_copy_rows(a.dy, at, kSumRows ? a.K : a.D, 2 * (int64_t)(kSumRows ? a.D : a.K),
+                         2 * plan.dy_row, stream);
+        a.dy = reinterpret_cast<uint16_t*>(at);
+        at += plan.dy_bytes;
     }
+    if (plan.q_bytes) {
+        launch_copy_rows(a.q, at, a.K, a.cols, plan.q_row, stream);
+        a.q = reinterpret_cast<int8_t*>(at);
+        at += plan.q_bytes;
+    }
+    a.dy_row = (int)plan.dy_row;
+    a.q_row = (int)plan.q_row;
+    a.ready = reinterpret_cast<uint16_t*>(at);
+    a.ready_k = (int)plan.ready_k;
+    a.partial = reinterpret_cast<float*>(at + plan.ready_bytes);
+    a.grid = grid_of(plan.cut);
+    if (plan.ready)
+        launch_ready<kSumRows>(a, stream);
+    else if (plan.cut.tile == 256)
+        launch_tiles<256, kSumRows>(a, stream);
+    else
+        launch_tiles<128, kSumRows>(a, stream);
     return launch_status(what);
 }
 
@@ -537,14 +536,14 @@ extern "C" int64_t roi_linear_i8_grad_weight_workspace(int64_t tokens, int64_t r
 {
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
-    return plan_grad(rows, cols, tokens).bytes;
+    return plan_grad(rows, cols, tokens, true).bytes;
 }
 
 extern "C" int64_t roi_linear_i8_grad_input_workspace(int64_t tokens, int64_t rows, int64_t cols)
 {
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
-    return plan_grad(tokens, cols, rows).bytes;
+    return plan_grad(tokens, cols, rows, false).bytes;
 }
 
 extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* xq, const float* xs,
@@ -554,12 +553,12 @@ extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* x
 {
     bool todo;
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
-    const GradPlan plan = plan_grad(rows, cols, tokens);
+    const GradPlan plan = plan_grad(rows, cols, tokens, true);
     if (int st = validate_grad_i8(grad_y, xq, xs, tokens, tokens, rows, cols, grad_w, rows,
                                   workspace, workspace_bytes, plan.bytes, &todo))
         return st;
     if (!todo) return ok();
-    const GradArgs a{grad_y, xq, xs, grad_w, nullptr, nullptr, 0, (int)tokens, (int)rows, (int)cols, {}};
+    const GradArgs a{grad_y, xq, xs, grad_w, nullptr, nullptr, 0, (int)tokens, (int)rows, (int)cols, 0, 0, {}};
     return launch<true>(a, plan, workspace, "roi_linear_i8_grad_weight", stream);
 }
 
@@ -570,11 +569,11 @@ extern "C" int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq
 {
     bool todo;
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
-    const GradPlan plan = plan_grad(tokens, cols, rows);
+    const GradPlan plan = plan_grad(tokens, cols, rows, false);
     if (int st = validate_grad_i8(grad_y, wq, ws, rows, tokens, rows, cols, grad_x, tokens,
                                   workspace, workspace_bytes, plan.bytes, &todo))
         return st;
     if (!todo) return ok();
-    const GradArgs a{grad_y, wq, ws, grad_x, nullptr, nullptr, 0, (int)rows, (int)tokens, (int)cols, {}};
+    const GradArgs a{grad_y, wq, ws, grad_x, nullptr, nullptr, 0, (int)rows, (int)tokens, (int)cols, 0, 0, {}};
     return launch<false>(a, plan, workspace, "roi_linear_i8_grad_input", stream);
 }

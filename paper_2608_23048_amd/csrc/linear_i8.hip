@@ -120,19 +120,15 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
     const uint8_t* wbase = reinterpret_cast<const uint8_t*>(a.w) + (int64_t)r0 * wlen;
     const uint8_t* xbase = reinterpret_cast<const uint8_t*>(a.x) + (int64_t)t0 * a.cols;
     const uint32_t* mbase = kPacked ? a.meta + (int64_t)r0 * words : nullptr;
-    auto bring = [&](const uint8_t* base, int first, int rows, int k, int len, ROI_LDS uint8_t* dst) {
-        const bool live = first + row < rows && k + 16 * chunk < len;
-        if constexpr (kWhole)
-            load_to_lds<false>(buffer_at(base + k),
-                               live ? (uint32_t)row * len + 16 * chunk : kNowhere, first * len, dst);
-        else
-            lds_write(dst + lane * 16, live ? load_row<Quad>(base + (int64_t)(first + row) * len,
-                                                             k + 16 * chunk, len)
-                                            : Quad{});
-    };
     // step s of the sum (past its end: zeros) into a slot
     auto stage = [&](int s, ROI_LDS uint8_t* slot) {
         const int k = s * kColumns;
+        auto bring = [&](const uint8_t* base, int first, int rows, int from, int len,
+                         ROI_LDS uint8_t* dst) {
+            const bool live = first + row < rows && from + 16 * chunk < len;
+            load_to_lds<false>(buffer_at(base + from),
+                               live ? (uint32_t)row * len + 16 * chunk : kNowhere, first * len, dst);
+        };
 #pragma unroll
         for (int i = 0; i < 2 * kRow; ++i)
             bring(wbase, 8 * i, a.rows - r0, k / kHalves, wlen, slot + i * 1024);
@@ -149,6 +145,29 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
                     live ? 4 * (row * words + word) : (int)kNowhere, 4 * 8 * i * words, 0, 0);
             }
         }
+    };
+    // Rows that end within 16 bytes (dense weights) go by registers: fetched a step
+    // ahead, at any address, rows past the end the last again.
+    Quad held[kWhole ? 1 : 2 * kRow + kTokens / 8];
+    auto fetch = [&](int s) {
+        const int k = s * 128;
+#pragma unroll
+        for (int i = 0; i < 2 * kRow + kTokens / 8; ++i) {
+            const bool w = i < 2 * kRow;
+            const int rows = w ? a.rows - r0 : a.tokens - t0;
+            const uint8_t* p = (w ? wbase : xbase) +
+                               (int64_t)least(8 * (w ? i : i - 2 * kRow) + row, rows - 1) * a.cols;
+            if (k + 128 <= a.cols) // the same for the wave
+                held[kWhole ? 0 : i] = load_any<Quad>(p + k + 16 * chunk);
+            else
+                held[kWhole ? 0 : i] = load_row<Quad>(p, k + 16 * chunk, a.cols);
+        }
+    };
+    auto put = [&](ROI_LDS uint8_t* slot) {
+#pragma unroll
+        for (int i = 0; i < 2 * kRow + kTokens / 8; ++i)
+            lds_write(slot + (i < 2 * kRow ? i * 1024 : kW + (i - 2 * kRow) * 1024) + lane * 16,
+                      held[kWhole ? 0 : i]);
     };
     i32x4 acc[kRow][kTok] = {};
     const int from = (lane & 15) * 128 + (g ^ (lane & 7)) * 16;
@@ -197,19 +216,30 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
     const int steps = (a.cols + kColumns - 1) / kColumns;
     const int mine = steps > wave ? (steps - wave + kWaves - 1) / kWaves : 0;
     if (mine > 0) {
-#pragma unroll
-        for (int n = 0; n < kDepth; ++n) stage(wave + n * kWaves, ring + n * kSlot);
         int slot = 0;
-        for (int n = 0; n < mine; ++n) {
-            loads_wait<(kDepth - 1) * kLoads>();
-            multiply(ring + slot);
-            // the slot is read: its values are in registers before its next loads
-            keep_order();
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            stage(wave + (n + kDepth) * kWaves, ring + slot);
-            slot = slot + kSlot < kDepth * kSlot ? slot + kSlot : 0;
+        auto next_slot = [&] { slot = slot + kSlot < kDepth * kSlot ? slot + kSlot : 0; };
+        if constexpr (kWhole) {
+#pragma unroll
+            for (int n = 0; n < kDepth; ++n) stage(wave + n * kWaves, ring + n * kSlot);
+            for (int n = 0; n < mine; ++n) {
+                loads_wait<(kDepth - 1) * kLoads>();
+                multiply(ring + slot);
+                // the slot is read: its values are in registers before its next loads
+                keep_order();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                stage(wave + (n + kDepth) * kWaves, ring + slot);
+                next_slot();
+            }
+            loads_wait<0>();
+        } else {
+            fetch(wave);
+            for (int n = 0; n < mine; ++n) {
+                put(ring + slot); // a wave's LDS operations are done in their order
+                fetch(wave + (n + 1) * kWaves);
+                multiply(ring + slot);
+                next_slot();
+            }
         }
-        loads_wait<0>();
     }
 #pragma unroll
     for (int i = 0; i < kRow; ++i)
@@ -246,8 +276,8 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
 // j.  A 16-byte LDS read goes by 16 lanes at a time, which are, of the wave's
 // first half, 0-3, 12-15, 20-23 and 24-27, then the others; the spreads give any
 // such 16 lanes all the banks when 16 consecutive lanes (kBlock 16) or 32 read
-// the same chunk of as many rows.  kWhole: rows are whole 16-byte chunks.
-template <int kTile, int kBytes, int kBlock, bool kWhole>
+// the same chunk of as many rows.  Their lengths are multiples of 16 bytes.
+template <int kTile, int kBytes, int kBlock>
 struct Rows {
     static constexpr int kThreads = Tile<kTile>::kThreads;
     static constexpr int kLoads = kTile * kBytes / (16 * kThreads);
@@ -278,13 +308,8 @@ struct Rows {
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const bool live = row(i) < left && k + 16 * chunk() < len;
-        if constexpr (kWhole)
-            load_to_lds<false>(buffer_at(base + k), live ? at : kNowhere,
-                               i * (kThreads / kChunks) * len, dst + (i * kThreads + wave * 64) * 16);
-        else
-            lds_write(dst + (i * kThreads + threadIdx.x) * 16,
-                      live ? load_row<Quad>(base + (int64_t)row(i) * len, k + 16 * chunk(), len)
-                           : Quad{});
+        load_to_lds<false>(buffer_at(base + k), live ? at : kNowhere, i * (kThreads / kChunks) * len,
+                           dst + (i * kThreads + wave * 64) * 16);
     }
 };
 
@@ -363,7 +388,7 @@ __device__ __forceinline__ void write_tile(
     }
 }
 
-template <int kTile, bool kWhole, typename Out>
+template <int kTile, typename Out>
 __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(LinearArgs a)
 {
     constexpr int kTileBytes = kTile * kRowBytes;
@@ -377,7 +402,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x4 acc[kI][kJ] = {};
-    using R = Rows<kTile, kRowBytes, 16, kWhole>;
+    using R = Rows<kTile, kRowBytes, 16>;
     const R wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
     constexpr int kLoads = R::kLoads;
     auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
@@ -462,8 +487,8 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x16 acc[kI][kJ] = {};
-    using W = Rows<kTile, 64, 32, true>;
-    using X = Rows<kTile, 128, 32, true>;
+    using W = Rows<kTile, 64, 32>;
+    using X = Rows<kTile, 128, 32>;
     const W wrows(a.w, r0, a.rows, a.cols / 2);
     const X xrows(a.x, t0, a.tokens, a.cols);
     // metadata: a word a lane, four words a row, word j at place j ^ (2 in the
@@ -587,10 +612,8 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
     const dim3 grid(a.grid.blocks()), block(T::kThreads);
     if (a.meta)
         hipLaunchKernelGGL((linear_packed_kernel<kTile, Out>), grid, block, 0, stream, a);
-    else if (a.cols % 16 == 0)
-        hipLaunchKernelGGL((linear_tile_kernel<kTile, true, Out>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((linear_tile_kernel<kTile, false, Out>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((linear_tile_kernel<kTile, Out>), grid, block, 0, stream, a);
     if (a.grid.rest() > 0) {
         const dim3 sums(a.grid.rest() * T::kI * T::kJ * T::kWaves);
         if (a.meta)
@@ -632,12 +655,23 @@ int launch_few(const LinearArgs& a, hipStream_t stream)
 }
 
 template <typename Out>
-int launch(LinearArgs a, const LinearPlan& plan, hipStream_t stream)
+int launch(LinearArgs a, const LinearPlan& plan, void* workspace, hipStream_t stream)
 {
     if (plan.few)
         return a.meta ? launch_few<true, Out>(a, stream) : launch_few<false, Out>(a, stream);
     const Cut& c = plan.cut;
     if (!c.fits) return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    if (plan.x_bytes) {
+        launch_copy_rows(a.x, at, a.tokens, a.cols, plan.row, stream);
+        a.x = reinterpret_cast<int8_t*>(at);
+        at += plan.x_bytes;
+        launch_copy_rows(a.w, at, a.rows, a.cols, plan.row, stream);
+        a.w = reinterpret_cast<int8_t*>(at);
+        at += plan.w_bytes;
+        a.cols = (int)plan.row;
+    }
+    a.partial = reinterpret_cast<int*>(at);
     a.grid = grid_of(c);
     if (c.tile == 256)
         launch_tiles<256, Out>(a, stream);
@@ -656,7 +690,7 @@ extern "C" int64_t roi_linear_i8_workspace(int64_t tokens, int64_t rows, int64_t
     if (check_linear_sizes(tokens, rows, cols)) return -1;
     ok();
     const LinearPlan plan = plan_linear(tokens, rows, cols, packed != 0);
-    return plan.few ? 0 : plan.cut.bytes;
+    return plan.few ? 0 : plan.bytes;
 }
 
 extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq,
@@ -668,10 +702,11 @@ extern "C" int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
     const LinearPlan plan = plan_linear(tokens, rows, cols, meta != nullptr);
     if (int st = validate_linear_i8(xq, xs, wq, meta, ws, bias, tokens, rows, cols, y, dtype,
-                                    workspace, workspace_bytes, plan.few ? 0 : plan.cut.bytes, &todo))
+                                    workspace, workspace_bytes, plan.few ? 0 : plan.bytes, &todo))
         return st;
     if (!todo) return ok();
-    const LinearArgs a{xq, xs, wq, meta, ws, bias, y, static_cast<int*>(workspace), (int)tokens,
+    const LinearArgs a{xq, xs, wq, meta, ws, bias, y, nullptr, (int)tokens,
                        (int)rows, (int)cols, {}};
-    return dtype == ROI_BF16 ? launch<uint16_t>(a, plan, stream) : launch<float>(a, plan, stream);
+    return dtype == ROI_BF16 ? launch<uint16_t>(a, plan, workspace, stream)
+                             : launch<float>(a, plan, workspace, stream);
 }

@@ -216,6 +216,23 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(const int8_t* q, c
     }
 }
 
+// Rows to rows of whole 16-byte pieces, one piece a lane.
+__global__ __launch_bounds__(256) void copy_rows_kernel(const uint8_t* from, uint8_t* to,
+                                                        int64_t rows, int64_t len, int64_t pieces)
+{
+    const int64_t per_row = (pieces + 63) / 64, waves = rows * per_row;
+    const int lane = threadIdx.x & 63;
+    for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < waves;
+         w += (int64_t)gridDim.x * 4) {
+        const int64_t r = w / per_row, piece = (w % per_row) * 64 + lane;
+        if (piece < pieces) {
+            const Quad v = load_row<Quad>(from + r * len, 16 * piece, len);
+            *reinterpret_cast<u32x4*>(to + (r * pieces + piece) * 16) =
+                u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+        }
+    }
+}
+
 template <typename T, int kWaves, int kChunks>
 void launch_quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols,
                      hipStream_t stream)
@@ -251,6 +268,17 @@ void quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols, h
 }
 
 } // namespace
+
+void launch_copy_rows(const void* from, void* to, int64_t rows, int64_t len, int64_t row,
+                      hipStream_t stream)
+{
+    const int64_t blocks = (rows * ((row / 16 + 63) / 64) + 3) / 4;
+    if (blocks == 0) return;
+    hipLaunchKernelGGL(copy_rows_kernel, dim3((unsigned)(blocks < 0xFFFFFF ? blocks : 0xFFFFFF)),
+                       dim3(256), 0, stream, static_cast<const uint8_t*>(from),
+                       static_cast<uint8_t*>(to), rows, len, row / 16);
+}
+
 } // namespace roi
 
 using namespace roi;

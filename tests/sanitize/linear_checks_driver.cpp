@@ -80,25 +80,41 @@ int main()
     for (int64_t m : sizes)
         for (int64_t n : sizes)
             for (int64_t k : sizes) {
-                const GradPlan p = plan_grad(m, n, k);
-                check_cut(p.cut, m, n, k, 64);
-                expect("grad bytes", p.bytes, p.ready_bytes + p.cut.bytes);
-                if (p.ready) {
-                    expect("ready tile", p.cut.tile, 256);
-                    expect("ready k", p.ready_k >= k && p.ready_k % 64 == 0, 1);
-                    expect("ready bytes", p.ready_bytes >= 2 * n * p.ready_k &&
-                                              p.ready_bytes % 256 == 0, 1);
-                    expect("ready launch", p.ready_k / 64 * ((n + 127) / 128) < (1 << 24), 1);
+                for (int sum_rows = 0; sum_rows < 2; ++sum_rows) {
+                    const GradPlan p = plan_grad(m, n, k, sum_rows != 0);
+                    const int64_t len = sum_rows ? m : k, dy_rows = sum_rows ? k : m;
+                    check_cut(p.cut, m, n, k, 64);
+                    expect("grad bytes", p.bytes,
+                           p.dy_bytes + p.q_bytes + p.ready_bytes + p.cut.bytes);
+                    expect("dy rows", p.dy_row >= len && p.dy_row < len + 8 && p.dy_row % 8 == 0, 1);
+                    expect("dy copied", p.dy_bytes,
+                           p.dy_row == len ? 0 : (2 * dy_rows * p.dy_row + 255) / 256 * 256);
+                    expect("q rows", p.q_row >= n && (p.ready || p.q_row % 4 == 0), 1);
+                    expect("q copied", p.q_bytes,
+                           p.q_row == n ? 0 : (k * p.q_row + 255) / 256 * 256);
+                    expect("ready bytes", p.ready_bytes,
+                           p.ready ? (2 * n * p.ready_k + 255) / 256 * 256 : 0);
+                    if (p.ready) {
+                        expect("ready tile", p.cut.tile, 256);
+                        expect("ready k", p.ready_k >= k && p.ready_k % 64 == 0, 1);
+                        expect("ready launch", p.ready_k / 64 * ((n + 127) / 128) < (1 << 24), 1);
+                    }
                 }
                 for (int packed = 0; packed < 2; ++packed) {
                     const LinearPlan l = plan_linear(n, m, k, packed != 0);
                     if (n <= 32) expect("few", l.few, 1);
                     if (n > 1024) expect("many", l.few, 0);
-                    if (!l.few) check_cut(l.cut, m, n, k, 128);
+                    if (l.few) continue;
+                    check_cut(l.cut, m, n, k, 128);
+                    expect("row", l.row >= k && l.row < k + 16 && l.row % 16 == 0, 1);
+                    expect("copied", (l.x_bytes > 0) == (l.row != k), 1);
+                    expect("linear bytes", l.bytes, l.x_bytes + l.w_bytes + l.cut.bytes);
+                    if (l.x_bytes)
+                        expect("room", l.x_bytes >= n * l.row && l.w_bytes >= m * l.row, 1);
                 }
             }
     // the longest sums and the most tokens
-    check_cut(plan_grad(64, 64, ((int64_t)1 << 30) - 1).cut, 64, 64, ((int64_t)1 << 30) - 1, 64);
+    check_cut(plan_grad(64, 64, ((int64_t)1 << 30) - 1, true).cut, 64, 64, ((int64_t)1 << 30) - 1, 64);
     check_cut(plan_linear(((int64_t)1 << 30) - 1, 16, 64, false).cut, 16, ((int64_t)1 << 30) - 1, 64,
               128);
     const Cut huge = plan_linear(((int64_t)1 << 30) - 1, ((int64_t)1 << 22) - 1, 64, false).cut;
