@@ -287,8 +287,8 @@ int roi_cat_mask_bwd(const uint16_t* grad_W_masked, const uint16_t* W, const flo
  *
  * Conventions beside the shared ones above:
  *  - x [tokens, cols], weight [rows, cols], y [tokens, rows]; any sizes >= 0
- *    with rows and cols below 2^22 and tokens below 2^30.  Rows of a length
- *    that is no multiple of 16 bytes are read by slower loads.
+ *    with rows and cols below 2^22 and tokens below 2^30.  Operands whose rows
+ *    are no multiple of 16 bytes cost a copy to the workspace, or slower loads.
  *  - An empty tensor's pointer may be NULL.  A sum over nothing is 0.
  *  - workspace: device memory of at least the bytes that the matching
  *    *_workspace call returns (it may be NULL where that is 0), 16-byte

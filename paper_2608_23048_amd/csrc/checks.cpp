@@ -428,7 +428,7 @@ GradPlan plan_grad(int64_t m, int64_t n, int64_t k, bool sum_rows)
         ready_k / 64 * ((n + 127) / 128) < (int64_t)1 << 24) {
         const Cut c = cut_tiles(m, n, k, kStep, 256, kReadyCost);
         const double us = c.us + 3 + 3 * (double)ready_k * (double)n / 4.0e6;
-        const double fused_us = p.cut.us + (n % 4 ? copy_us(2.0 * (double)k * (double)n) : 0);
+        const double fused_us = p.cut.us + (n % 16 ? copy_us(2.0 * (double)k * (double)n) : 0);
         if (us < fused_us && c.fits) {
             p.ready = true;
             p.ready_k = ready_k;
@@ -436,8 +436,10 @@ GradPlan plan_grad(int64_t m, int64_t n, int64_t k, bool sum_rows)
             p.cut = c;
         }
     }
+    const Cut& c = p.cut;
+    p.deep = !p.ready && c.tile == 128 && c.full + (c.tm * c.tn - c.full) * c.splits <= kUnits;
     p.q_row = n;
-    if (!p.ready && n % 4) {
+    if (!p.ready && n % (p.deep ? 16 : 4)) {
         p.q_row = (n + 15) / 16 * 16;
         p.q_bytes = padded256(k * p.q_row);
     }

@@ -124,7 +124,7 @@ struct TileCost {
 };
 constexpr TileCost kLinearCost = {1.36, 12, 0.55, 0.80, 5.5};
 constexpr TileCost kPackedCost = {0.80, 12, 0.45, 0.60, 5};
-constexpr TileCost kGradCost = {1.70, 14, 0.95, 1.50, 9};
+constexpr TileCost kGradCost = {1.70, 14, 0.62, 1.50, 8};
 // Of a 256-tile with both operands in bf16 (there is no 128-tile).
 constexpr TileCost kReadyCost = {1.40, 12, 0, 0, 0};
 Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& cost);
@@ -150,8 +150,10 @@ constexpr int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // rows of dy_row and q_row elements.  With `ready` q is first written there in
 // bf16, transposed, [n, ready_k].  The workspace holds these arrays in this order
 // (dy_bytes, q_bytes, ready_bytes; 0: not there), then the parts of cut tiles.
+// With `deep` the 128-tiles are no more than the compute units, and q's rows are
+// in whole 16-byte pieces.
 struct GradPlan {
-    bool ready;
+    bool ready, deep;
     int64_t dy_row, q_row, ready_k;
     int64_t dy_bytes, q_bytes, ready_bytes;
     int64_t bytes; // of workspace

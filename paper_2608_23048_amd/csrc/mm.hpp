@@ -58,8 +58,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p)
 // waits for it.  kUnseen: in assembly, because the compiler has every transposing
 // LDS read wait for all loads to LDS that it knows of.  (It has no result
 // register.  The s_nop covers the wait states between a write of m0 or of a
-// scalar operand and this read.)  The compiler's own form is faster where it
-// serves: 8192^3 int8 402 us against 427.
+// scalar operand and this read.)
 template <bool kUnseen>
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t offset,
                                             uint32_t more, ROI_LDS uint8_t* dst)
@@ -72,6 +71,20 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t
     else
         __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (ROI_LDS void*)dst, 16, (int)offset, (int)more,
                                                  0, 0);
+}
+
+// The same with 4 bytes a lane, lane l's at dst + 4 l.
+template <bool kUnseen>
+__device__ __forceinline__ void load_words_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t offset,
+                                                  ROI_LDS uint8_t* dst)
+{
+    if constexpr (kUnseen)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                     :
+                     : "s"((uint32_t)(uintptr_t)dst), "v"(offset), "s"(src)
+                     : "memory");
+    else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (ROI_LDS void*)dst, 4, (int)offset, 0, 0, 0);
 }
 
 __device__ __forceinline__ int least(int a, int b) { return a < b ? a : b; }

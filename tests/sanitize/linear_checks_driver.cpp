@@ -89,7 +89,10 @@ int main()
                     expect("dy rows", p.dy_row >= len && p.dy_row < len + 8 && p.dy_row % 8 == 0, 1);
                     expect("dy copied", p.dy_bytes,
                            p.dy_row == len ? 0 : (2 * dy_rows * p.dy_row + 255) / 256 * 256);
-                    expect("q rows", p.q_row >= n && (p.ready || p.q_row % 4 == 0), 1);
+                    expect("q rows", p.q_row >= n && (p.ready || p.q_row % (p.deep ? 16 : 4) == 0), 1);
+                    if (p.deep)
+                        expect("deep blocks", p.cut.tile == 128 && p.cut.full + (p.cut.tm * p.cut.tn - p.cut.full) *
+                                                  p.cut.splits <= 256, 1);
                     expect("q copied", p.q_bytes,
                            p.q_row == n ? 0 : (k * p.q_row + 255) / 256 * 256);
                     expect("ready bytes", p.ready_bytes,

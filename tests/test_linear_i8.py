@@ -445,7 +445,9 @@ def test_linear_binding_refusals():
 
 
 GRAD = [(1, 1, 1), (3, 17, 5), (64, 128, 128), (65, 136, 132), (63, 120, 124), (130, 129, 131),
-        (200, 300, 77), (333, 96, 256), (1000, 257, 260), (128, 8, 520), (70, 520, 4)]
+        (200, 300, 77), (333, 96, 256), (1000, 257, 260), (128, 8, 520), (70, 520, 4),
+        # more 128-tiles than compute units and few sums: two tiles a unit
+        (130, 2100, 2500), (2500, 130, 2100)]
 
 
 def grad_inputs(tokens, rows, cols, seed, by_tokens):
@@ -472,7 +474,7 @@ def test_grads(tokens, rows, cols, by_tokens):
 
 @gpu
 @pytest.mark.parametrize("by_tokens", [True, False], ids=["weight", "input"])
-@pytest.mark.parametrize("k,d,c", [(1032, 4104, 4092), (1030, 4100, 4093), (2100, 520, 4096)])
+@pytest.mark.parametrize("k,d,c", [(1032, 4104, 4092), (1030, 4100, 4093), (2100, 1032, 4096)])
 def test_grads_of_many_tiles(k, d, c, by_tokens):
     """More tiles than compute units: the operand converted beforehand, whole
     tiles and cut ones in one call, with and without whole chunks a row."""
