@@ -476,10 +476,11 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
     using H = Held<kTile, 32>;
     constexpr int kI = H::kI, kJ = H::kJ;
     constexpr int kThreads = Tile<kTile>::kThreads;
-    constexpr int kW = kTile * 64, kX = kTile * 128, kM = kTile * 16, kStage = kW + kX + kM;
+    constexpr int kW = kTile * 64, kX = kTile * 128, kStage = kW + kX;
+    constexpr int kM = kTile * 32; // of two steps
     static_assert(3 * kStage >= 4 * kTile * kRowBytes, "results pass LDS");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[3][kStage];
-    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[3 * kStage + 2 * kM];
+    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0];
     const int lane = threadIdx.x & 63, half_of = lane >> 5, in = lane & 31;
     const int wave = scalar(threadIdx.x >> 6);
     const int wm = wave / Tile<kTile>::kAcross * 32 * kI, wn = wave % Tile<kTile>::kAcross * 32 * kJ;
@@ -491,29 +492,28 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
     using X = Rows<kTile, 128, 32>;
     const W wrows(a.w, r0, a.rows, a.cols / 2);
     const X xrows(a.x, t0, a.tokens, a.cols);
-    // metadata: a word a lane, four words a row, word j at place j ^ (2 in the
-    // second 16 of 32 rows), so that 32 rows' words lie in different banks
-    constexpr int kMetaLoads = kTile * 4 / kThreads;
-    const int words = a.cols / 32, word = (threadIdx.x % 4) ^ (threadIdx.x / 4 >> 3 & 2);
-    static_assert(kThreads / 4 % 32 == 0, "the same word for all of a thread's loads");
+    // metadata: a word a lane, eight words a row, word j at place j ^ 2 (row / 8 &
+    // 3), so that the words that a wave reads lie in different banks
+    constexpr int kMetaLoads = kTile * 8 / kThreads;
+    const int words = a.cols / 32, word = (threadIdx.x % 8) ^ (threadIdx.x / 8 >> 2 & 6);
+    static_assert(kThreads / 8 % 32 == 0, "the same word for all of a thread's loads");
     const uint32_t* meta = a.meta + (int64_t)r0 * words;
-    constexpr int kLoads = W::kLoads + X::kLoads + kMetaLoads;
-    static_assert(kLoads % kI == 0, "loads are spread over the rows");
-    auto stage = [&](int s, int first, int count, ROI_LDS uint8_t* dst) {
+    // loads of an odd step and of an even one, which brings the metadata of two
+    constexpr int kOdd = W::kLoads + X::kLoads, kEven = kOdd + kMetaLoads;
+    auto stage = [&](int s, int first, int count, ROI_LDS uint8_t* dst, ROI_LDS uint8_t* mdst) {
         const int k = (piece.first + s) * 128;
         for (int i = first; i < first + count; ++i) {
             if (i < W::kLoads) {
                 wrows.stage(i, k / 2, dst);
-            } else if (i < W::kLoads + X::kLoads) {
+            } else if (i < kOdd) {
                 xrows.stage(i - W::kLoads, k, dst + kW);
             } else {
-                const int l = i - W::kLoads - X::kLoads;
-                const int row = (l * kThreads + (int)threadIdx.x) / 4;
+                const int l = i - kOdd;
+                const int row = (l * kThreads + (int)threadIdx.x) / 8;
                 const bool live = row < a.rows - r0 && k + 32 * word < a.cols;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    buffer_at(meta + k / 32),
-                    (ROI_LDS void*)(dst + kW + kX + (l * kThreads + wave * 64) * 4), 4,
-                    live ? 4 * (row * words + word) : (int)kNowhere, 0, 0, 0);
+                    buffer_at(meta + k / 32), (ROI_LDS void*)(mdst + (l * kThreads + wave * 64) * 4),
+                    4, live ? 4 * (row * words + word) : (int)kNowhere, 0, 0, 0);
             }
         }
     };
@@ -522,30 +522,33 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
         int m[kI];
         i32x8 x[kJ];
     };
-    // Half h: the weight's chunk and word 2 h + half_of, the tokens' chunks 4 h +
-    // half_of and 4 h + 2 + half_of; the places' bits flip with the chunks'.
+    // Half h: the weight's chunk 2 h + half_of, the tokens' chunks 4 h + half_of and
+    // 4 h + 2 + half_of, the word 2 h + half_of, in an odd step 4 more; the places'
+    // bits flip with theirs.
     const int from_w = (wm + in) * 64 + (half_of ^ W::spread(in)) * 16;
-    const int from_m = kW + kX + (wm + in) * 16 + (half_of ^ (in >> 3 & 2)) * 4;
+    const int from_m = (wm + in) * 32 + (half_of ^ (in >> 2 & 6)) * 4;
     const int from_x = kW + (wn + in) * 128 + (half_of ^ X::spread(in)) * 16;
-    auto read_w = [&](ROI_LDS uint8_t* src, int h, Half& f, int i) {
+    // first: 4 in an odd step
+    auto read_w = [&](ROI_LDS uint8_t* src, ROI_LDS uint8_t* msrc, int h, int first, Half& f,
+                      int i) {
         f.w[i] = lds_read<i32x4>(src + i * 32 * 64 + (from_w ^ (32 * h)));
-        f.m[i] = lds_read<int>(src + i * 32 * 16 + (from_m ^ (8 * h)));
+        f.m[i] = lds_read<int>(msrc + i * 32 * 32 + (from_m ^ (8 * h + 4 * first)));
     };
     auto read_x = [&](ROI_LDS uint8_t* src, int h, Half& f, int j) {
         const i32x4 lo = lds_read<i32x4>(src + j * 32 * 128 + (from_x ^ (64 * h)));
         const i32x4 hi = lds_read<i32x4>(src + j * 32 * 128 + (from_x ^ (64 * h) ^ 32));
         f.x[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // the products of a half, beside the reads of half h at src and (load) the
-    // loads of step s, to dst
-    auto half = [&](const Half& f, ROI_LDS uint8_t* src, int h, Half& next, auto load, int s,
-                    ROI_LDS uint8_t* dst) {
-        constexpr int kPart = kLoads / kI;
+    // the products of a half, beside the reads of half h at src and (kLoads > 0)
+    // the loads of step s, to dst
+    auto half = [&](const Half& f, ROI_LDS uint8_t* src, ROI_LDS uint8_t* msrc, int h, int first,
+                    Half& next, auto loads, int s, ROI_LDS uint8_t* dst, ROI_LDS uint8_t* mdst) {
+        constexpr int kLoads = decltype(loads)::value;
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
             if (i < kJ) read_x(src, h, next, i);
-            read_w(src, h, next, i);
-            if constexpr (decltype(load)::value) stage(s, i * kPart, kPart, dst);
+            read_w(src, msrc, h, first, next, i);
+            stage(s, kLoads * i / kI, kLoads * (i + 1) / kI - kLoads * i / kI, dst, mdst);
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
                 acc[i][j] = __builtin_amdgcn_smfmac_i32_32x32x64_i8(f.w[i], f.x[j], acc[i][j],
@@ -555,25 +558,35 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
     };
     if (piece.count > 0) {
         ROI_LDS uint8_t *b0 = base, *b1 = base + kStage, *b2 = base + 2 * kStage;
+        ROI_LDS uint8_t *m0 = base + 3 * kStage, *m1 = m0 + kM; // of this pair of steps and the next
+        using None = std::integral_constant<int, 0>;
         Half lo, hi;
-        stage(0, 0, kLoads, b0);
-        stage(1, 0, kLoads, b1);
-        stage(2, 0, kLoads, b2);
-        loads_barrier<2 * kLoads>();
+        stage(0, 0, kEven, b0, m0);
+        stage(1, 0, kOdd, b1, m0);
+        stage(2, 0, kEven, b2, m1);
+        loads_barrier<kOdd + kEven>();
 #pragma unroll
-        for (int i = 0; i < kI; ++i) read_w(b0, 0, lo, i);
+        for (int i = 0; i < kI; ++i) read_w(b0, m0, 0, 0, lo, i);
 #pragma unroll
         for (int j = 0; j < kJ; ++j) read_x(b0, 0, lo, j);
         // past the end of the sum or of this part, loads are in bounds or zeros,
         // and unused
-        for (int s = 0; s < piece.count; ++s) {
-            half(lo, b0, 1, hi, std::false_type{}, 0, b0);
-            loads_barrier<kLoads>();
-            half(hi, b1, 0, lo, std::true_type{}, s + 3, b0);
+        for (int s = 0; s < piece.count; s += 2) {
+            half(lo, b0, m0, 1, 0, hi, None{}, 0, b0, m0);
+            loads_barrier<kEven>();
+            half(hi, b1, m0, 0, 4, lo, std::integral_constant<int, kOdd>{}, s + 3, b0, m0);
+            if (s + 1 == piece.count) break;
+            half(lo, b1, m0, 1, 4, hi, None{}, 0, b0, m0);
+            loads_barrier<kOdd>();
+            // this pair's metadata is read: the pair's after the next takes its place
+            half(hi, b2, m1, 0, 0, lo, std::integral_constant<int, kEven>{}, s + 4, b1, m0);
             ROI_LDS uint8_t* const t = b0;
-            b0 = b1;
-            b1 = b2;
-            b2 = t;
+            b0 = b2;
+            b2 = b1;
+            b1 = t;
+            ROI_LDS uint8_t* const u = m0;
+            m0 = m1;
+            m1 = u;
         }
         loads_barrier();
     }
