@@ -326,7 +326,6 @@ int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols)
 
 namespace {
 
-constexpr int64_t kUnits = 256;           // compute units of an MI355X
 constexpr int64_t kMostSplits = 64;
 constexpr double kPartBytesPerUs = 6.0e6; // of parts, written and read again
 constexpr double kSumLaunchUs = 6.5;

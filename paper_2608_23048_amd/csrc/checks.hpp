@@ -104,6 +104,8 @@ constexpr int64_t kMaxLinearDim = (int64_t)1 << 22;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 constexpr int64_t kMaxI8Sum = 131071;
 
+constexpr int64_t kUnits = 256; // compute units of an MI355X
+
 // How a product of m x n results over a sum of k is cut: square tiles, of which
 // the first `full` are whole and the sums of the others are cut into `splits`
 // parts, which pass through the workspace as 32-bit values.

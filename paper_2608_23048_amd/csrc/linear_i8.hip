@@ -470,16 +470,19 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
 // each for the tokens, the half lines of weights and the metadata's 16 bytes a
 // row (26 million in all, one every 6.4 ps), where the matrix cores are busy for
 // 48 % of the time.
-template <int kTile, typename Out>
+template <int kTile, int kRing>
+constexpr int packed_lds() { return kRing * kTile * 128 + 2 * kTile * (128 + 32); }
+template <int kTile, int kRing, typename Out>
 __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel(LinearArgs a)
 {
     using H = Held<kTile, 32>;
     constexpr int kI = H::kI, kJ = H::kJ;
     constexpr int kThreads = Tile<kTile>::kThreads;
-    constexpr int kW = kTile * 64, kX = kTile * 128, kStage = kW + kX;
-    constexpr int kM = kTile * 32; // of two steps
-    static_assert(3 * kStage >= 4 * kTile * kRowBytes, "results pass LDS");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[3 * kStage + 2 * kM];
+    constexpr int kX = kTile * 128;                                    // of a step
+    constexpr int kW = kTile * 128, kM = kTile * 32, kPair = kW + kM; // of two
+    static_assert(kRing == 2 || kRing == 3, "the waits below");
+    static_assert(packed_lds<kTile, kRing>() == kRing * kX + 2 * kPair, "the launch's");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0];
     const int lane = threadIdx.x & 63, half_of = lane >> 5, in = lane & 31;
     const int wave = scalar(threadIdx.x >> 6);
@@ -488,32 +491,34 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x16 acc[kI][kJ] = {};
-    using W = Rows<kTile, 64, 32>;
-    using X = Rows<kTile, 128, 32>;
-    const W wrows(a.w, r0, a.rows, a.cols / 2);
-    const X xrows(a.x, t0, a.tokens, a.cols);
+    using R = Rows<kTile, 128, 32>;
+    const R wrows(a.w, r0, a.rows, a.cols / 2), xrows(a.x, t0, a.tokens, a.cols);
     // metadata: a word a lane, eight words a row, word j at place j ^ 2 (row / 8 &
     // 3), so that the words that a wave reads lie in different banks
     constexpr int kMetaLoads = kTile * 8 / kThreads;
     const int words = a.cols / 32, word = (threadIdx.x % 8) ^ (threadIdx.x / 8 >> 2 & 6);
     static_assert(kThreads / 8 % 32 == 0, "the same word for all of a thread's loads");
     const uint32_t* meta = a.meta + (int64_t)r0 * words;
-    // loads of an odd step and of an even one, which brings the metadata of two
-    constexpr int kOdd = W::kLoads + X::kLoads, kEven = kOdd + kMetaLoads;
-    auto stage = [&](int s, int first, int count, ROI_LDS uint8_t* dst, ROI_LDS uint8_t* mdst) {
+    constexpr int kPairLoads = R::kLoads + kMetaLoads;
+    // loads first .. of the tokens of step s
+    auto stage_x = [&](int s, int first, int count, ROI_LDS uint8_t* dst) {
+        for (int i = first; i < first + count; ++i)
+            xrows.stage(i, (piece.first + s) * 128, dst);
+    };
+    // and of the weights and metadata of steps s and s + 1
+    auto stage_w = [&](int s, int first, int count, ROI_LDS uint8_t* dst) {
         const int k = (piece.first + s) * 128;
         for (int i = first; i < first + count; ++i) {
-            if (i < W::kLoads) {
+            if (i < R::kLoads) {
                 wrows.stage(i, k / 2, dst);
-            } else if (i < kOdd) {
-                xrows.stage(i - W::kLoads, k, dst + kW);
             } else {
-                const int l = i - kOdd;
+                const int l = i - R::kLoads;
                 const int row = (l * kThreads + (int)threadIdx.x) / 8;
                 const bool live = row < a.rows - r0 && k + 32 * word < a.cols;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                    buffer_at(meta + k / 32), (ROI_LDS void*)(mdst + (l * kThreads + wave * 64) * 4),
-                    4, live ? 4 * (row * words + word) : (int)kNowhere, 0, 0, 0);
+                    buffer_at(meta + k / 32),
+                    (ROI_LDS void*)(dst + kW + (l * kThreads + wave * 64) * 4), 4,
+                    live ? 4 * (row * words + word) : (int)kNowhere, 0, 0, 0);
             }
         }
     };
@@ -522,33 +527,30 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
         int m[kI];
         i32x8 x[kJ];
     };
-    // Half h: the weight's chunk 2 h + half_of, the tokens' chunks 4 h + half_of and
-    // 4 h + 2 + half_of, the word 2 h + half_of, in an odd step 4 more; the places'
-    // bits flip with theirs.
-    const int from_w = (wm + in) * 64 + (half_of ^ W::spread(in)) * 16;
-    const int from_m = (wm + in) * 32 + (half_of ^ (in >> 2 & 6)) * 4;
-    const int from_x = kW + (wn + in) * 128 + (half_of ^ X::spread(in)) * 16;
-    // first: 4 in an odd step
-    auto read_w = [&](ROI_LDS uint8_t* src, ROI_LDS uint8_t* msrc, int h, int first, Half& f,
-                      int i) {
-        f.w[i] = lds_read<i32x4>(src + i * 32 * 64 + (from_w ^ (32 * h)));
-        f.m[i] = lds_read<int>(msrc + i * 32 * 32 + (from_m ^ (8 * h + 4 * first)));
+    // Half h of a step: the weight's chunk and the word 2 h + half_of, in the
+    // second of two steps 4 more, the tokens' chunks 4 h + half_of and 4 h + 2 +
+    // half_of; the places' bits flip with these.
+    const int from_w = (wm + in) * 128 + (half_of ^ R::spread(in)) * 16;
+    const int from_m = kW + (wm + in) * 32 + (half_of ^ (in >> 2 & 6)) * 4;
+    const int from_x = (wn + in) * 128 + (half_of ^ R::spread(in)) * 16;
+    auto read_w = [&](ROI_LDS uint8_t* src, int quarter, Half& f, int i) {
+        f.w[i] = lds_read<i32x4>(src + i * 32 * 128 + (from_w ^ (32 * quarter)));
+        f.m[i] = lds_read<int>(src + i * 32 * 32 + (from_m ^ (8 * quarter)));
     };
     auto read_x = [&](ROI_LDS uint8_t* src, int h, Half& f, int j) {
         const i32x4 lo = lds_read<i32x4>(src + j * 32 * 128 + (from_x ^ (64 * h)));
         const i32x4 hi = lds_read<i32x4>(src + j * 32 * 128 + (from_x ^ (64 * h) ^ 32));
         f.x[j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    // the products of a half, beside the reads of half h at src and (kLoads > 0)
-    // the loads of step s, to dst
-    auto half = [&](const Half& f, ROI_LDS uint8_t* src, ROI_LDS uint8_t* msrc, int h, int first,
-                    Half& next, auto loads, int s, ROI_LDS uint8_t* dst, ROI_LDS uint8_t* mdst) {
-        constexpr int kLoads = decltype(loads)::value;
+    // the products of a half, beside the reads of quarter q of the two steps whose
+    // weights are at ws, tokens at xs, and `load(i)`
+    auto half = [&](const Half& f, ROI_LDS uint8_t* ws, ROI_LDS uint8_t* xs, int q, Half& next,
+                    auto load) {
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
-            if (i < kJ) read_x(src, h, next, i);
-            read_w(src, msrc, h, first, next, i);
-            stage(s, kLoads * i / kI, kLoads * (i + 1) / kI - kLoads * i / kI, dst, mdst);
+            if (i < kJ) read_x(xs, q & 1, next, i);
+            read_w(ws, q, next, i);
+            load(i);
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
                 acc[i][j] = __builtin_amdgcn_smfmac_i32_32x32x64_i8(f.w[i], f.x[j], acc[i][j],
@@ -557,36 +559,47 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
         }
     };
     if (piece.count > 0) {
-        ROI_LDS uint8_t *b0 = base, *b1 = base + kStage, *b2 = base + 2 * kStage;
-        ROI_LDS uint8_t *m0 = base + 3 * kStage, *m1 = m0 + kM; // of this pair of steps and the next
-        using None = std::integral_constant<int, 0>;
+        ROI_LDS uint8_t *x0 = base, *x1 = base + kX, *x2 = base + (kRing - 1) * kX;
+        ROI_LDS uint8_t *w0 = base + kRing * kX, *w1 = w0 + kPair; // of this pair of steps and the next
+        constexpr int kXPart = R::kLoads / kI, kWPart = kPairLoads / kI;
+        static_assert(R::kLoads % kI == 0 && kPairLoads % kI == 0, "loads are spread over the rows");
+        auto none = [](int) {};
         Half lo, hi;
-        stage(0, 0, kEven, b0, m0);
-        stage(1, 0, kOdd, b1, m0);
-        stage(2, 0, kEven, b2, m1);
-        loads_barrier<kOdd + kEven>();
+        stage_x(0, 0, R::kLoads, x0);
+        stage_w(0, 0, kPairLoads, w0);
+        stage_x(1, 0, R::kLoads, x1);
+        if (kRing > 2) stage_x(2, 0, R::kLoads, x2);
+        stage_w(2, 0, kPairLoads, w1);
+        loads_barrier<(kRing - 1) * R::kLoads + kPairLoads>();
 #pragma unroll
-        for (int i = 0; i < kI; ++i) read_w(b0, m0, 0, 0, lo, i);
+        for (int i = 0; i < kI; ++i) read_w(w0, 0, lo, i);
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) read_x(b0, 0, lo, j);
+        for (int j = 0; j < kJ; ++j) read_x(x0, 0, lo, j);
         // past the end of the sum or of this part, loads are in bounds or zeros,
         // and unused
         for (int s = 0; s < piece.count; s += 2) {
-            half(lo, b0, m0, 1, 0, hi, None{}, 0, b0, m0);
-            loads_barrier<kEven>();
-            half(hi, b1, m0, 0, 4, lo, std::integral_constant<int, kOdd>{}, s + 3, b0, m0);
+            half(lo, w0, x0, 1, hi, none);
+            // the next pair's weights are the last loads
+            loads_barrier<(kRing - 2) * R::kLoads + kPairLoads>();
+            half(hi, w0, x1, 2, lo, [&](int i) { stage_x(s + kRing, i * kXPart, kXPart, x0); });
             if (s + 1 == piece.count) break;
-            half(lo, b1, m0, 1, 4, hi, None{}, 0, b0, m0);
-            loads_barrier<kOdd>();
-            // this pair's metadata is read: the pair's after the next takes its place
-            half(hi, b2, m1, 0, 0, lo, std::integral_constant<int, kEven>{}, s + 4, b1, m0);
-            ROI_LDS uint8_t* const t = b0;
-            b0 = b2;
-            b2 = b1;
-            b1 = t;
-            ROI_LDS uint8_t* const u = m0;
-            m0 = m1;
-            m1 = u;
+            half(lo, w0, x1, 3, hi, none);
+            loads_barrier<(kRing - 2) * R::kLoads>();
+            half(hi, w1, kRing == 2 ? x0 : x2, 0, lo, [&](int i) {
+                if (i < kI / 2)
+                    stage_x(s + 1 + kRing, i * 2 * kXPart, 2 * kXPart, x1);
+                else
+                    stage_w(s + 4, (i - kI / 2) * 2 * kWPart, 2 * kWPart, w0);
+            });
+            ROI_LDS uint8_t* const t = w0;
+            w0 = w1;
+            w1 = t;
+            if (kRing > 2) {
+                ROI_LDS uint8_t* const x = x2;
+                x2 = x1;
+                x1 = x0;
+                x0 = x;
+            }
         }
         loads_barrier();
     }
@@ -618,13 +631,23 @@ __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
     store4<Out>(a, t, r, finish4(sum, ws, add, a.xs[t]));
 }
 
+template <int kTile, int kRing, typename Out>
+void launch_packed(const LinearArgs& a, hipStream_t stream)
+{
+    constexpr int kLds = packed_lds<kTile, kRing>();
+    hipLaunchKernelGGL((linear_packed_kernel<kTile, kRing, Out>), dim3(a.grid.blocks()),
+                       dim3(Tile<kTile>::kThreads), kLds, stream, a);
+}
+
 template <int kTile, typename Out>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
     using T = Tile<kTile>;
     const dim3 grid(a.grid.blocks()), block(T::kThreads);
-    if (a.meta)
-        hipLaunchKernelGGL((linear_packed_kernel<kTile, Out>), grid, block, 0, stream, a);
+    if (a.meta && kTile == 128 && a.grid.blocks() <= kUnits)
+        launch_packed<128, 3, Out>(a, stream);
+    else if (a.meta)
+        launch_packed<kTile, 2, Out>(a, stream);
     else
         hipLaunchKernelGGL((linear_tile_kernel<kTile, Out>), grid, block, 0, stream, a);
     if (a.grid.rest() > 0) {
