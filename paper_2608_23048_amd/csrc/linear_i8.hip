@@ -87,9 +87,10 @@ __device__ __forceinline__ void store4(const LinearArgs& a, int64_t t, int r, f3
 }
 
 // ---------------------------------------------------------------- few tokens
-// A block owns 16 kRow weight rows and up to kTokens (8, or a multiple of 16); its waves share out
-// the sum and add up their parts in LDS.  The weight is read once: bound by its
-// bytes.  A wave brings its steps of the sum (128 columns, 256 of a 2:4 weight)
+// A block owns 16 kRow weight rows and up to kTokens tokens (8, or a multiple of
+// 16); its waves share out the sum and add up their parts in LDS.  The weight is
+// read once: bound by its bytes (68 MB in 12 us by itself: 16 tokens through 3584 x
+// 18944).  A wave brings its steps of the sum (128 columns, 256 of a 2:4 weight)
 // to a ring of kDepth slots in LDS of its own and needs no barrier.  Through LDS,
 // because eight lanes then read 128 consecutive bytes of a row; operands loaded
 // straight to registers are 64 separate pieces of 16 bytes a load, and the
@@ -464,12 +465,15 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
 // The same with 2:4 weights, on the 32 x 32 sparse instructions: a half step is
 // 64 columns, whose second operand is 8 registers a block of 32 tokens (the 16 x
 // 16 form takes 128 columns at once and twice the registers, too many to read
-// ahead).  A step's tiles (64 bytes a weight row, its four metadata words, 128
-// bytes a token) have two steps to arrive, in three LDS buffers.  4096 tokens
-// through 3584 x 18944 take 169 us.  Bound by requests to the L2: a step makes 256
-// each for the tokens, the half lines of weights and the metadata's 16 bytes a
-// row (26 million in all, one every 6.4 ps), where the matrix cores are busy for
-// 48 % of the time.
+// ahead).  Weights and metadata come for two steps at a time, 128 and 32 bytes a
+// row: requests to the L2 were what bound the step (a step at a time 26 million in
+// 175 us for 4096 tokens through 3584 x 18944; so, 18 million in 163).  The
+// tokens' tiles have kRing - 1 steps to arrive: two where a tile has a compute unit
+// to itself (512 tokens through 3584 x 3584: 15.7 us, 17.6 with one), else one, for
+// which there is LDS.  The matrix cores are busy for 53 % of the time on the units
+// that have a tile; of a 256-tile's step of 1940 cycles they take 1024, the LDS
+// reads 790 and the loads to LDS about 420.  LDS is given at the launch, as in
+// grad_i8.hip's deep kernel.
 template <int kTile, int kRing>
 constexpr int packed_lds() { return kRing * kTile * 128 + 2 * kTile * (128 + 32); }
 template <int kTile, int kRing, typename Out>
