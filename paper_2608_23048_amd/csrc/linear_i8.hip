@@ -470,10 +470,10 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
 // 175 us for 4096 tokens through 3584 x 18944; so, 18 million in 163).  The
 // tokens' tiles have kRing - 1 steps to arrive: two where a tile has a compute unit
 // to itself (512 tokens through 3584 x 3584: 15.7 us, 17.6 with one), else one, for
-// which there is LDS.  The matrix cores are busy for 53 % of the time on the units
-// that have a tile; of a 256-tile's step of 1940 cycles they take 1024, the LDS
-// reads 790 and the loads to LDS about 420.  LDS is given at the launch, as in
-// grad_i8.hip's deep kernel.
+// which there is LDS.  Of a 256-tile's step of 1940 cycles (at 1.8 GHz, which is
+// what this load leaves) the matrix cores take 1024, the LDS reads 660 and the loads
+// to LDS about 420; waves wait for a third of it, at the barrier and for the
+// tokens.  LDS is given at the launch, as in grad_i8.hip's deep kernel.
 template <int kTile, int kRing>
 constexpr int packed_lds() { return kRing * kTile * 128 + 2 * kTile * (128 + 32); }
 template <int kTile, int kRing, typename Out>
@@ -497,10 +497,10 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
     i32x16 acc[kI][kJ] = {};
     using R = Rows<kTile, 128, 32>;
     const R wrows(a.w, r0, a.rows, a.cols / 2), xrows(a.x, t0, a.tokens, a.cols);
-    // metadata: a word a lane, eight words a row, word j at place j ^ 2 (row / 8 &
-    // 3), so that the words that a wave reads lie in different banks
+    // metadata: a word a lane, eight words a row, word j at place j ^ (row / 4 & 7),
+    // so that the words that 32 lanes read lie in the 32 banks of a 4-byte read
     constexpr int kMetaLoads = kTile * 8 / kThreads;
-    const int words = a.cols / 32, word = (threadIdx.x % 8) ^ (threadIdx.x / 8 >> 2 & 6);
+    const int words = a.cols / 32, word = (threadIdx.x % 8) ^ (threadIdx.x / 32 & 7);
     static_assert(kThreads / 8 % 32 == 0, "the same word for all of a thread's loads");
     const uint32_t* meta = a.meta + (int64_t)r0 * words;
     constexpr int kPairLoads = R::kLoads + kMetaLoads;
@@ -535,7 +535,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
     // second of two steps 4 more, the tokens' chunks 4 h + half_of and 4 h + 2 +
     // half_of; the places' bits flip with these.
     const int from_w = (wm + in) * 128 + (half_of ^ R::spread(in)) * 16;
-    const int from_m = kW + (wm + in) * 32 + (half_of ^ (in >> 2 & 6)) * 4;
+    const int from_m = kW + (wm + in) * 32 + (half_of ^ (in >> 2 & 7)) * 4;
     const int from_x = (wn + in) * 128 + (half_of ^ R::spread(in)) * 16;
     auto read_w = [&](ROI_LDS uint8_t* src, int quarter, Half& f, int i) {
         f.w[i] = lds_read<i32x4>(src + i * 32 * 128 + (from_w ^ (32 * quarter)));
