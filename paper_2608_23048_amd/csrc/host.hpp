@@ -21,10 +21,6 @@ int grid_for(int64_t items, int block = kBlock);
 float quotient_reciprocal(float lambda);
 // Philox key and step words of a call.
 NoiseKey make_key(uint64_t seed, uint64_t step, uint64_t block);
-// Copies `rows` rows of `len` bytes to rows of `row` bytes (a multiple of 16, at
-// least len), zeros behind each (rows_i8.hip).
-void launch_copy_rows(const void* from, void* to, int64_t rows, int64_t len, int64_t row,
-                      hipStream_t stream);
 // ROI_OK, or ROI_E_HIP with the runtime's error after a launch.
 int launch_status(const char* what);
 

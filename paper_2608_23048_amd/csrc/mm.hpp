@@ -58,7 +58,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p)
 // waits for it.  kUnseen: in assembly, because the compiler has every transposing
 // LDS read wait for all loads to LDS that it knows of.  (It has no result
 // register.  The s_nop covers the wait states between a write of m0 or of a
-// scalar operand and this read.)
+// scalar operand and this read.  The compiler, which reserves m0, may take its value
+// from before: a kernel uses one form or the other for all of its loads to LDS.)
 template <bool kUnseen>
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t offset,
                                             uint32_t more, ROI_LDS uint8_t* dst)
