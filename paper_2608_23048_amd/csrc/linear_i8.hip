@@ -389,13 +389,14 @@ __device__ __forceinline__ void write_tile(
     }
 }
 
-template <int kTile, typename Out>
+template <int kTile, int kRing, typename Out>
 __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(LinearArgs a)
 {
     constexpr int kTileBytes = kTile * kRowBytes;
     constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][kTileBytes];
-    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0][0][0];
+    static_assert(kRing == 2 || kRing == 4, "slots are counted in bits");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[]; // kRing steps of two tiles
+    ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0];
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / Tile<kTile>::kAcross * 16 * kI, wn = wave % Tile<kTile>::kAcross * 16 * kJ;
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
     using R = Rows<kTile, kRowBytes, 16>;
     const R wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
     constexpr int kLoads = R::kLoads;
-    auto buffer = [&](int s) { return base + (s & 1) * 2 * kTileBytes; };
+    auto buffer = [&](int s) { return base + (s & (kRing - 1)) * 2 * kTileBytes; };
     // loads `first` .. of step s, of the 2 kLoads that bring both tiles
     auto stage = [&](int s, int first, int count) {
         for (int i = first; i < first + count; ++i)
@@ -426,8 +427,8 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
         f.x[j] = lds_read<i32x4>(buffer(s) + kTileBytes + (wn + 16 * j + (lane & 15)) * kRowBytes +
                                  ((4 * h + g) ^ (lane & 7)) * 16);
     };
-    // the products of a half, beside the reads of half h of step s and (kLoad)
-    // the loads of step s + 1: past the sum's end these bring zeros and those
+    // the products of a half, beside the reads of half h of step s and (kLoad) the
+    // loads of step s + kRing - 1: past the sum's end these bring zeros and those
     // read them, and neither is used
     auto half = [&](const Half& f, int s, int h, Half& next, auto load) {
         constexpr int kPart = 2 * kLoads / kI;
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
         for (int i = 0; i < kI; ++i) {
             if (i < kJ) read_x(s, h, next, i);
             read_w(s, h, next, i);
-            if (decltype(load)::value) stage(s + 1, i * kPart, kPart);
+            if (decltype(load)::value) stage(s + kRing - 1, i * kPart, kPart);
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.w[i], f.x[j], acc[i][j], 0, 0, 0);
@@ -445,16 +446,15 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
     static_assert(2 * kLoads % kI == 0, "loads are spread over the rows");
     if (piece.count > 0) {
         Half lo, hi;
-        stage(0, 0, 2 * kLoads);
-        stage(1, 0, 2 * kLoads);
-        loads_barrier();
+        for (int s = 0; s < kRing; ++s) stage(s, 0, 2 * kLoads);
+        loads_barrier<(kRing - 1) * 2 * kLoads>();
 #pragma unroll
         for (int i = 0; i < kI; ++i) read_w(0, 0, lo, i);
 #pragma unroll
         for (int j = 0; j < kJ; ++j) read_x(0, 0, lo, j);
         for (int s = 0; s < piece.count; ++s) {
             half(lo, s, 1, hi, std::false_type{});
-            loads_barrier();
+            loads_barrier<(kRing - 2) * 2 * kLoads>();
             half(hi, s + 1, 0, lo, std::true_type{});
         }
         loads_barrier();
@@ -636,24 +636,26 @@ __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
 }
 
 template <int kTile, int kRing, typename Out>
-void launch_packed(const LinearArgs& a, hipStream_t stream)
+void launch_tiles_as(const LinearArgs& a, hipStream_t stream)
 {
-    constexpr int kLds = packed_lds<kTile, kRing>();
-    hipLaunchKernelGGL((linear_packed_kernel<kTile, kRing, Out>), dim3(a.grid.blocks()),
-                       dim3(Tile<kTile>::kThreads), kLds, stream, a);
+    const dim3 grid(a.grid.blocks()), block(Tile<kTile>::kThreads);
+    constexpr int kPackedLds = packed_lds<kTile, kRing == 2 ? 2 : 3>();
+    if (a.meta)
+        hipLaunchKernelGGL((linear_packed_kernel<kTile, kRing == 2 ? 2 : 3, Out>), grid, block,
+                           kPackedLds, stream, a);
+    else
+        hipLaunchKernelGGL((linear_tile_kernel<kTile, kRing, Out>), grid, block,
+                           kRing * 2 * kTile * kRowBytes, stream, a);
 }
 
 template <int kTile, typename Out>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
     using T = Tile<kTile>;
-    const dim3 grid(a.grid.blocks()), block(T::kThreads);
-    if (a.meta && kTile == 128 && a.grid.blocks() <= kUnits)
-        launch_packed<128, 3, Out>(a, stream);
-    else if (a.meta)
-        launch_packed<kTile, 2, Out>(a, stream);
+    if (kTile == 128 && a.grid.blocks() <= kUnits)
+        launch_tiles_as<128, 4, Out>(a, stream);
     else
-        hipLaunchKernelGGL((linear_tile_kernel<kTile, Out>), grid, block, 0, stream, a);
+        launch_tiles_as<kTile, 2, Out>(a, stream);
     if (a.grid.rest() > 0) {
         const dim3 sums(a.grid.rest() * T::kI * T::kJ * T::kWaves);
         if (a.meta)
