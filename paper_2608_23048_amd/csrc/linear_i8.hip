@@ -684,7 +684,14 @@ int launch_few_as(LinearArgs a, hipStream_t stream)
 template <bool kPacked, typename Out>
 int launch_few(const LinearArgs& a, hipStream_t stream)
 {
-    if (a.tokens > 16) return launch_few_as<4, 2, 32, 2, kPacked, Out>(a, stream);
+    // Blocks of 32 rows read the tokens half as often, those of 16 are twice as many:
+    // 32 tokens through 3584 x 18944 take 20.5 us in blocks of 16 rows and 26.3 of
+    // 32, through 4864 x 4864 (more than a block a compute unit) 9.9 and 8.6.
+    if (a.tokens > 16) {
+        const int64_t blocks = (int64_t)((a.rows + 15) / 16) * ((a.tokens + 31) / 32);
+        return blocks <= kUnits ? launch_few_as<4, 1, 32, 2, kPacked, Out>(a, stream)
+                                : launch_few_as<4, 2, 32, 2, kPacked, Out>(a, stream);
+    }
     // With at least two blocks a compute unit a shallow ring lets more of them
     // run at once: one token through 18944 x 3584 at 2:4 takes 11.2 us with two
     // slots and 13.8 with three, through 3584 x 18944 13.2 and 10.5.
