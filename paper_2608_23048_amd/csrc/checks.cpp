@@ -384,6 +384,9 @@ namespace {
 // Of a copy of rows into the workspace: bytes read and written.
 double copy_us(double bytes) { return 2 + bytes / 4.0e6; }
 
+// The length of copied rows: what a tile loads of a row is then one cache line.
+int64_t whole_lines(int64_t bytes) { return (bytes + 127) / 128 * 128; }
+
 } // namespace
 
 // The streaming kernel takes 32 tokens at a time, each time at 7e6 bytes of a
@@ -397,7 +400,7 @@ LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
     p.few = tokens <= 32;
     if (p.few) return p;
     p.cut = cut_product(rows, tokens, cols, 128, packed ? kPackedCost : kLinearCost);
-    p.row = (cols + 15) / 16 * 16;
+    p.row = cols % 16 == 0 ? cols : whole_lines(cols);
     double tiles_us = p.cut.us;
     if (p.row != cols) {
         p.x_bytes = padded256(tokens * p.row);
@@ -418,7 +421,7 @@ GradPlan plan_grad(int64_t m, int64_t n, int64_t k, bool sum_rows)
     GradPlan p{};
     p.cut = cut_product(m, n, k, kStep, kGradCost);
     const int64_t dy_len = sum_rows ? m : k, dy_rows = sum_rows ? k : m;
-    p.dy_row = (dy_len + 7) / 8 * 8;
+    p.dy_row = dy_len % 8 == 0 ? dy_len : whole_lines(2 * dy_len) / 2;
     if (p.dy_row != dy_len) p.dy_bytes = padded256(2 * dy_rows * p.dy_row);
     const int64_t ready_k = (k + kStep - 1) / kStep * kStep;
     // offsets within a tile of the transposed operand stay below 2^31, and the
@@ -439,7 +442,7 @@ GradPlan plan_grad(int64_t m, int64_t n, int64_t k, bool sum_rows)
     p.deep = !p.ready && c.tile == 128 && c.full + (c.tm * c.tn - c.full) * c.splits <= kUnits;
     p.q_row = n;
     if (!p.ready && n % (p.deep ? 16 : 4)) {
-        p.q_row = (n + 15) / 16 * 16;
+        p.q_row = whole_lines(n);
         p.q_bytes = padded256(k * p.q_row);
     }
     p.bytes = p.dy_bytes + p.q_bytes + p.ready_bytes + p.cut.bytes;

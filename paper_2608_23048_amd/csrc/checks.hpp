@@ -134,7 +134,7 @@ Cut cut_product(int64_t m, int64_t n, int64_t k, int64_t step, const TileCost& c
 // The int8 product's way: with few tokens the kernel that streams the weight
 // past them (no workspace), else the tiles of `cut`, before which rows of a
 // length that is no multiple of 16 are copied to the workspace (x_bytes, w_bytes),
-// to rows of `row` bytes; the parts of cut tiles follow.
+// to rows of `row` bytes (whole cache lines); the parts of cut tiles follow.
 struct LinearPlan {
     bool few;
     int64_t row, x_bytes, w_bytes;
@@ -149,7 +149,7 @@ constexpr int64_t padded256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 // A gradient's way (out [m, n], summed over k).  The tiles' loads take whole
 // 16-byte pieces of grad_y's rows (k values with `sum_rows` false, else m) and
 // words of q's: rows that end within one are first copied to the workspace, to
-// rows of dy_row and q_row elements.  With `ready` q is first written there in
+// rows of dy_row and q_row elements (whole cache lines).  With `ready` q is first written there in
 // bf16, transposed, [n, ready_k].  The workspace holds these arrays in this order
 // (dy_bytes, q_bytes, ready_bytes; 0: not there), then the parts of cut tiles.
 // With `deep` the 128-tiles are no more than the compute units, and q's rows are

@@ -86,10 +86,10 @@ int main()
                     check_cut(p.cut, m, n, k, 64);
                     expect("grad bytes", p.bytes,
                            p.dy_bytes + p.q_bytes + p.ready_bytes + p.cut.bytes);
-                    expect("dy rows", p.dy_row >= len && p.dy_row < len + 8 && p.dy_row % 8 == 0, 1);
+                    expect("dy rows", p.dy_row >= len && p.dy_row < len + 64 && p.dy_row % 8 == 0, 1);
                     expect("dy copied", p.dy_bytes,
                            p.dy_row == len ? 0 : (2 * dy_rows * p.dy_row + 255) / 256 * 256);
-                    expect("q rows", p.q_row >= n && (p.ready || p.q_row % (p.deep ? 16 : 4) == 0), 1);
+                    expect("q rows", p.q_row >= n && p.q_row < n + 128 && (p.ready || p.q_row % (p.deep ? 16 : 4) == 0), 1);
                     if (p.deep)
                         expect("deep blocks", p.cut.tile == 128 && p.cut.full + (p.cut.tm * p.cut.tn - p.cut.full) *
                                                   p.cut.splits <= 256, 1);
@@ -109,7 +109,7 @@ int main()
                     if (n > 1024) expect("many", l.few, 0);
                     if (l.few) continue;
                     check_cut(l.cut, m, n, k, 128);
-                    expect("row", l.row >= k && l.row < k + 16 && l.row % 16 == 0, 1);
+                    expect("row", l.row >= k && l.row < k + 128 && l.row % 16 == 0, 1);
                     expect("copied", (l.x_bytes > 0) == (l.row != k), 1);
                     expect("linear bytes", l.bytes, l.x_bytes + l.w_bytes + l.cut.bytes);
                     if (l.x_bytes)
