@@ -405,7 +405,7 @@ LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
     if (p.row != cols) {
         p.x_bytes = padded256(tokens * p.row);
         p.w_bytes = padded256(rows * p.row);
-        tiles_us += 2 + copy_us(2.0 * (double)(tokens + rows) * (double)cols);
+        tiles_us += copy_us(2.0 * (double)(tokens + rows) * (double)cols);
     }
     p.bytes = p.x_bytes + p.w_bytes + p.cut.bytes;
     const double rate = packed ? 6.0e6 : p.row == cols ? 7.0e6 : 2.5e6;

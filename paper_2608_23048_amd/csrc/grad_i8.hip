@@ -653,17 +653,14 @@ int launch(GradArgs a, const GradPlan& plan, void* workspace, const char* what, 
     if (!plan.cut.fits)
         return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
     uint8_t* at = static_cast<uint8_t*>(workspace);
-    if (plan.dy_bytes) {
-        launch_copy_rows(a.dy, at, kSumRows ? a.K : a.D, 2 * (int64_t)(kSumRows ? a.D : a.K),
-                         2 * plan.dy_row, stream);
-        a.dy = reinterpret_cast<uint16_t*>(at);
-        at += plan.dy_bytes;
-    }
-    if (plan.q_bytes) {
-        launch_copy_rows(a.q, at, a.K, a.cols, plan.q_row, stream);
-        a.q = reinterpret_cast<int8_t*>(at);
-        at += plan.q_bytes;
-    }
+    uint8_t* const dy = at;
+    uint8_t* const q = dy + plan.dy_bytes;
+    launch_copy_rows(RowsCopy{a.dy, dy, plan.dy_bytes ? (kSumRows ? a.K : a.D) : 0,
+                              2 * (int64_t)(kSumRows ? a.D : a.K), 2 * plan.dy_row},
+                     RowsCopy{a.q, q, plan.q_bytes ? a.K : 0, a.cols, plan.q_row}, stream);
+    if (plan.dy_bytes) a.dy = reinterpret_cast<uint16_t*>(dy);
+    if (plan.q_bytes) a.q = reinterpret_cast<int8_t*>(q);
+    at = q + plan.q_bytes;
     a.dy_row = (int)plan.dy_row;
     a.q_row = (int)plan.q_row;
     a.ready = reinterpret_cast<uint16_t*>(at);

@@ -712,12 +712,13 @@ int launch(LinearArgs a, const LinearPlan& plan, void* workspace, hipStream_t st
     if (!c.fits) return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
     uint8_t* at = static_cast<uint8_t*>(workspace);
     if (plan.x_bytes) {
-        launch_copy_rows(a.x, at, a.tokens, a.cols, plan.row, stream);
-        a.x = reinterpret_cast<int8_t*>(at);
-        at += plan.x_bytes;
-        launch_copy_rows(a.w, at, a.rows, a.cols, plan.row, stream);
-        a.w = reinterpret_cast<int8_t*>(at);
-        at += plan.w_bytes;
+        uint8_t* const x = at;
+        uint8_t* const w = x + plan.x_bytes;
+        launch_copy_rows(RowsCopy{a.x, x, a.tokens, a.cols, plan.row},
+                         RowsCopy{a.w, w, a.rows, a.cols, plan.row}, stream);
+        a.x = reinterpret_cast<int8_t*>(x);
+        a.w = reinterpret_cast<int8_t*>(w);
+        at = w + plan.w_bytes;
         a.cols = (int)plan.row;
     }
     a.partial = reinterpret_cast<int*>(at);

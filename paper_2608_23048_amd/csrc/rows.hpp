@@ -70,9 +70,14 @@ __device__ __forceinline__ V load_row(const uint8_t* row, int64_t k, int64_t len
     return v;
 }
 
-// Copies `rows` rows of `len` bytes to rows of `row` bytes (a multiple of 16, at
-// least len; `to` is aligned to 16), zeros behind each (rows_i8.hip).
-void launch_copy_rows(const void* from, void* to, int64_t rows, int64_t len, int64_t row,
-                      hipStream_t stream);
+// Rows of `len` bytes to rows of `row` bytes (a multiple of 16, at least len; `to`
+// is aligned to 16), zeros behind each; with `rows` 0 nothing.
+struct RowsCopy {
+    const void* from;
+    void* to;
+    int64_t rows, len, row;
+};
+// Both copies in one launch (rows_i8.hip).
+void launch_copy_rows(const RowsCopy& a, const RowsCopy& b, hipStream_t stream);
 
 } // namespace roi

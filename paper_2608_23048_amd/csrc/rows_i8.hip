@@ -216,18 +216,20 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(const int8_t* q, c
     }
 }
 
-// Rows to rows of whole 16-byte pieces, one piece a lane.
-__global__ __launch_bounds__(256) void copy_rows_kernel(const uint8_t* from, uint8_t* to,
-                                                        int64_t rows, int64_t len, int64_t pieces)
+// Rows to rows of whole 16-byte pieces, one piece a lane, a wave within a row.
+__host__ __device__ int64_t copy_waves(const RowsCopy& c) { return c.rows * ((c.row + 1023) / 1024); }
+__global__ __launch_bounds__(256) void copy_rows_kernel(RowsCopy a, RowsCopy b)
 {
-    const int64_t per_row = (pieces + 63) / 64, waves = rows * per_row;
+    const int64_t first = copy_waves(a), waves = first + copy_waves(b);
     const int lane = threadIdx.x & 63;
     for (int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); w < waves;
          w += (int64_t)gridDim.x * 4) {
-        const int64_t r = w / per_row, piece = (w % per_row) * 64 + lane;
-        if (piece < pieces) {
-            const Quad v = load_row<Quad>(from + r * len, 16 * piece, len);
-            *reinterpret_cast<u32x4*>(to + (r * pieces + piece) * 16) =
+        const RowsCopy& c = w < first ? a : b;
+        const int64_t in = w < first ? w : w - first, per_row = (c.row + 1023) / 1024;
+        const int64_t r = in / per_row, k = (in % per_row) * 1024 + 16 * lane;
+        if (k < c.row) {
+            const Quad v = load_row<Quad>(static_cast<const uint8_t*>(c.from) + r * c.len, k, c.len);
+            *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(c.to) + r * c.row + k) =
                 u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
         }
     }
@@ -269,14 +271,12 @@ void quantize(const T* x, int8_t* q, float* scale, int64_t rows, int64_t cols, h
 
 } // namespace
 
-void launch_copy_rows(const void* from, void* to, int64_t rows, int64_t len, int64_t row,
-                      hipStream_t stream)
+void launch_copy_rows(const RowsCopy& a, const RowsCopy& b, hipStream_t stream)
 {
-    const int64_t blocks = (rows * ((row / 16 + 63) / 64) + 3) / 4;
+    const int64_t blocks = (copy_waves(a) + copy_waves(b) + 3) / 4;
     if (blocks == 0) return;
     hipLaunchKernelGGL(copy_rows_kernel, dim3((unsigned)(blocks < 0xFFFFFF ? blocks : 0xFFFFFF)),
-                       dim3(256), 0, stream, static_cast<const uint8_t*>(from),
-                       static_cast<uint8_t*>(to), rows, len, row / 16);
+                       dim3(256), 0, stream, a, b);
 }
 
 } // namespace roi
