@@ -51,9 +51,9 @@ struct GradArgs {
 // row k at place j ^ 2 (k & 3) ^ (k & 8), so that the rows that 32 lanes read
 // together (four of each of two groups of 16) lie in different banks.  Otherwise
 // [kTile d] k-rows (mm.hpp).  What lies past K is zero; past D, zero or the last row again.
-template <int kTile, bool kSumRows, bool kUnseen = kSumRows>
+template <int kTile, bool kSumRows, bool kUnseen = kSumRows, int kWaves = waves_of(kTile)>
 struct DyTile {
-    static constexpr int kThreads = Tile<kTile>::kThreads;
+    static constexpr int kThreads = 64 * kWaves;
     static constexpr int kLoads = kTile * kRowBytes / (16 * kThreads);
     static constexpr int kAcrossRow = kSumRows ? kTile / 8 : 8; // chunks of a row
     const uint8_t* base; // of row 0, column d0 (kSumRows), or of row d0
@@ -207,23 +207,22 @@ struct QTile {
 
 // A tile's results from a wave's sums: a part of a cut tile as it is, else in
 // bf16 and through LDS (all of which is free) to out.
-template <int kTile>
+template <typename T>
 __device__ __forceinline__ void write_tile(const GradArgs& a, const Piece& piece,
-                                           const f32x4 (&acc)[Tile<kTile>::kI][Tile<kTile>::kJ],
-                                           ROI_LDS uint8_t* base)
+                                           const f32x4 (&acc)[T::kI][T::kJ], ROI_LDS uint8_t* base)
 {
-    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    constexpr int kTile = T::kTile, kI = T::kI, kJ = T::kJ;
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = scalar(threadIdx.x >> 6);
-    const int bc = wave / Tile<kTile>::kAcross * kI, bd = wave % Tile<kTile>::kAcross * kJ;
+    const int bc = wave / T::kAcross * kI, bd = wave % T::kAcross * kJ;
     const int d0 = piece.m * kTile, c0 = piece.n * kTile;
     if (piece.part >= 0) {
 #pragma unroll
         for (int i = 0; i < kI; ++i)
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
-                *reinterpret_cast<f32x4*>(a.partial + Held<kTile, 16>::part_at(piece.part, wave, i, j, 0)) =
-                    acc[i][j];
+                *reinterpret_cast<f32x4*>(
+                    a.partial + Held<kTile, 16, T::kWaves>::part_at(piece.part, wave, i, j, 0)) = acc[i][j];
         return;
     }
     using Out = RowsOut<kI, 8>;
@@ -337,7 +336,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void grad_tile_kernel(Gra
         }
         loads_barrier();
     }
-    write_tile<kTile>(a, piece, acc, base);
+    write_tile<Tile<kTile>>(a, piece, acc, base);
 }
 
 // The same for both operands in bf16 (a.ready): nothing passes registers on its
@@ -408,46 +407,43 @@ __global__ __launch_bounds__(Tile<256>::kThreads) void grad_ready_kernel(GradArg
         }
         loads_barrier();
     }
-    write_tile<kTile>(a, piece, acc, base);
+    write_tile<Tile<kTile>>(a, piece, acc, base);
 }
 
 // For up to one 128-tile a compute unit: nothing else runs there while a block
-// waits, so it keeps more on its way.  Everything is loaded to LDS, q as it is; a
-// step's tiles have between two and three steps to arrive (of kDeepRing slots),
-// and q's go from there through registers, scaled and rounded, to k-rows.  A step
-// takes 0.62 us where the kernel above takes 0.80 (4096 x 896 x 896: the weight
-// gradient 25.4 us against 28.3, the input's 16.3 against 18.2).  LDS is given at
-// the launch: the compiler, which knows that one block fits, would otherwise take
-// accumulation registers as with one wave a SIMD (Tile).
-constexpr int kDeepRing = 5;
-constexpr int kDeepRaw = kSum * 128, kDeepSlot = 128 * kRowBytes + kDeepRaw + 4 * kSum;
-constexpr int kDeepLds = 2 * 128 * kRowBytes + kDeepRing * kDeepSlot;
+// waits, so it has eight waves, which convert and multiply beside each other, and
+// keeps more on its way.  Everything is loaded to LDS, q as it is; a step's tiles
+// have between two and three steps to arrive (of kRing slots), and q's go from
+// there through registers, scaled and rounded, to k-rows.  A step takes 0.57 us
+// where the kernel above takes 0.80 (4096 x 896 x 896: the weight gradient 24.2 us
+// against 28.3, the input's 16.1 against 18.2).  Short sums are bound by what comes
+// before and after their steps, half of the time of 13 steps: the first loads, and
+// the parts of cut tiles.
+using DeepTile = Tile<128, 8>;
 template <bool kSumRows>
-__global__ __launch_bounds__(Tile<128>::kThreads, 2) void grad_deep_kernel(GradArgs a)
+__global__ __launch_bounds__(DeepTile::kThreads) void grad_deep_kernel(GradArgs a)
 {
-    constexpr int kTile = 128, kTileBytes = kTile * kRowBytes, kRing = kDeepRing;
-    constexpr int kThreads = Tile<kTile>::kThreads;
-    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
-    static_assert(kI == 4 && kJ == 4, "laid out for four rows");
-    using Dy = DyTile<kTile, kSumRows>;
+    using T = DeepTile;
+    constexpr int kTile = 128, kTileBytes = kTile * kRowBytes, kRing = 5;
+    constexpr int kThreads = T::kThreads, kI = T::kI, kJ = T::kJ;
+    static_assert(kI == 4 && kJ == 2 && kThreads == 512, "laid out for these");
+    using Dy = DyTile<kTile, kSumRows, kSumRows, T::kWaves>;
     using Q = QTile<kTile, true>;
-    constexpr int kRaw = kDeepRaw, kSlot = kDeepSlot;
+    constexpr int kRaw = kSum * kTile, kSlot = kTileBytes + kRaw + 4 * kSum;
     constexpr int kRawLoads = kRaw / (16 * kThreads), kLoads = Dy::kLoads + kRawLoads + 1;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kTileBytes + kRing * kSlot];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0];
     const int lane = threadIdx.x & 63;
     const int wave = scalar(threadIdx.x >> 6);
-    const int bc = wave / Tile<kTile>::kAcross * kI, bd = wave % Tile<kTile>::kAcross * kJ;
+    const int bc = wave / T::kAcross * kI, bd = wave % T::kAcross * kJ;
     const Piece piece = piece_of(a.grid, blockIdx.x);
     const int d0 = piece.m * kTile, c0 = piece.n * kTile;
     const int k0 = piece.first * kSum;
 
     f32x4 acc[kI][kJ] = {};
     const Dy dy(a.dy, kSumRows ? a.K : a.dy_row, kSumRows ? a.dy_row : a.D, d0, bd);
-    Q q(a, c0);
+    const Q q(a, c0);
     ROI_LDS uint8_t* ring = base + 2 * kTileBytes;
-    // q's rows of 128 bytes; row r lies at place r ^ (bit 3 of r), so that the two
-    // rows eight apart that a wave reads at a time lie in different banks
     const uint8_t* raw = reinterpret_cast<const uint8_t*>(a.q) + c0;
     // step s of this part (past its end or the sum's: in bounds or zeros) to a slot
     auto stage = [&](int s, ROI_LDS uint8_t* slot) {
@@ -456,8 +452,7 @@ __global__ __launch_bounds__(Tile<128>::kThreads, 2) void grad_deep_kernel(GradA
         for (int i = 0; i < Dy::kLoads; ++i) dy.stage(i, k, slot);
 #pragma unroll
         for (int i = 0; i < kRawLoads; ++i) {
-            const int place = (i * kThreads + (int)threadIdx.x) / 8, chunk = threadIdx.x % 8;
-            const int row = place ^ (place >> 3 & 1);
+            const int row = (i * kThreads + (int)threadIdx.x) / 8, chunk = threadIdx.x % 8;
             const bool live = row < a.K - k && 16 * chunk < a.q_row - c0;
             load_to_lds<kSumRows>(buffer_at(raw + (int64_t)k * a.q_row),
                                   live ? (uint32_t)row * a.q_row + 16 * chunk : kNowhere, 0,
@@ -470,26 +465,27 @@ __global__ __launch_bounds__(Tile<128>::kThreads, 2) void grad_deep_kernel(GradA
     struct Half {
         bf16x8 q[kI], y[kJ];
     };
-    const int oct = Q::oct(), group = Q::group();
+    // a thread takes four sum indices of four columns: half a chunk of each
+    const int four = threadIdx.x / 32, group = threadIdx.x % 32;
+    const int to = Q::place(4 * group, four / 2) + 8 * (four % 2);
     struct Raw {
-        uint32_t v[8];
-        f32x4 s[2];
+        uint32_t v[4];
+        f32x4 s;
     };
     auto read_raw = [&](ROI_LDS uint8_t* slot, Raw& r) {
         ROI_LDS uint8_t* p = slot + kTileBytes;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            r.v[j] = lds_read<uint32_t>(p + 8 * oct * kTile + (j ^ (oct & 1)) * kTile + 4 * group);
-        r.s[0] = lds_read<f32x4>(p + kRaw + 32 * oct);
-        r.s[1] = lds_read<f32x4>(p + kRaw + 32 * oct + 16);
+        for (int j = 0; j < 4; ++j)
+            r.v[j] = lds_read<uint32_t>(p + (4 * four + j) * kTile + 4 * group);
+        r.s = lds_read<f32x4>(p + kRaw + 16 * four);
     };
+    // column b: its place is that of column 0 with its low bits flipped by b
     auto write_column = [&](const Raw& r, int b, ROI_LDS uint8_t* dst) {
-        float f[8];
+        float f[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = (float)(int8_t)(r.v[j] >> (8 * b)) * r.s[j / 4][j % 4];
-        lds_write(dst + (q.to ^ (16 * b)) + b * kRowBytes,
-                  Quad{bf16x2_rne(f[0], f[1]), bf16x2_rne(f[2], f[3]), bf16x2_rne(f[4], f[5]),
-                       bf16x2_rne(f[6], f[7])});
+        for (int j = 0; j < 4; ++j) f[j] = (float)(int8_t)(r.v[j] >> (8 * b)) * r.s[j];
+        *reinterpret_cast<ROI_LDS u32x2*>(dst + (to ^ (16 * b)) + b * kRowBytes) =
+            u32x2{bf16x2_rne(f[0], f[1]), bf16x2_rne(f[2], f[3])};
     };
     // the products of a half, beside the reads of half h of the step whose tiles
     // are at qs and ys; kLoad: also q's tile at `from` to qd and step s to `slot`
@@ -500,7 +496,7 @@ __global__ __launch_bounds__(Tile<128>::kThreads, 2) void grad_deep_kernel(GradA
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
             if (decltype(load)::value && i == 0) read_raw(from, r);
-            next.y[i] = dy.read(ys, i, h);
+            if (i < kJ) next.y[i] = dy.read(ys, i, h);
             next.q[i] = q.read(qs, bc + i, i, h);
             if constexpr (decltype(load)::value) {
                 if (i == 1) write_column(r, 0, qd);
@@ -551,7 +547,7 @@ __global__ __launch_bounds__(Tile<128>::kThreads, 2) void grad_deep_kernel(GradA
         }
         loads_barrier();
     }
-    write_tile<kTile>(a, piece, acc, base);
+    write_tile<T>(a, piece, acc, base);
 }
 
 // s q in bf16, transposed to k-rows of 64 (zeros past K), for grad_ready_kernel:
@@ -581,16 +577,16 @@ __global__ __launch_bounds__(256) void ready_kernel(GradArgs a)
 
 // The sums of the tiles that were cut: one wave for 16 x 16 results, the parts
 // in their order, eight of them on their way at a time.
-template <int kTile>
+template <typename T>
 __global__ __launch_bounds__(64) void grad_sum_kernel(GradArgs a)
 {
-    using T = Tile<kTile>;
+    constexpr int kTile = T::kTile;
     const int lane = threadIdx.x;
     const int j = blockIdx.x % T::kJ, i = blockIdx.x / T::kJ % T::kI;
     const int wave = blockIdx.x / (T::kJ * T::kI) % T::kWaves;
     const uint32_t tile = blockIdx.x / (T::kJ * T::kI * T::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
-    const float* from = a.partial + Held<kTile, 16>::part_at((int64_t)tile * a.grid.splits, wave, i, j, 0);
+    const float* from = a.partial + Held<kTile, 16, T::kWaves>::part_at((int64_t)tile * a.grid.splits, wave, i, j, 0);
     f32x4 sum = {};
 #pragma unroll 8
     for (uint32_t p = 0; p < a.grid.splits; ++p)
@@ -609,12 +605,11 @@ __global__ __launch_bounds__(64) void grad_sum_kernel(GradArgs a)
     }
 }
 
-template <int kTile>
+template <typename T>
 void launch_sums(const GradArgs& a, hipStream_t stream)
 {
-    using T = Tile<kTile>;
     if (a.grid.rest() > 0)
-        hipLaunchKernelGGL((grad_sum_kernel<kTile>),
+        hipLaunchKernelGGL((grad_sum_kernel<T>),
                            dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves), dim3(64), 0, stream, a);
 }
 
@@ -623,15 +618,15 @@ void launch_tiles(const GradArgs& a, hipStream_t stream)
 {
     hipLaunchKernelGGL((grad_tile_kernel<kTile, kSumRows>), dim3(a.grid.blocks()),
                        dim3(Tile<kTile>::kThreads), 0, stream, a);
-    launch_sums<kTile>(a, stream);
+    launch_sums<Tile<kTile>>(a, stream);
 }
 
 template <bool kSumRows>
 void launch_deep(const GradArgs& a, hipStream_t stream)
 {
     hipLaunchKernelGGL((grad_deep_kernel<kSumRows>), dim3(a.grid.blocks()),
-                       dim3(Tile<128>::kThreads), kDeepLds, stream, a);
-    launch_sums<128>(a, stream);
+                       dim3(DeepTile::kThreads), 0, stream, a);
+    launch_sums<DeepTile>(a, stream);
 }
 
 template <bool kSumRows>
@@ -644,7 +639,7 @@ void launch_ready(const GradArgs& a, hipStream_t stream)
         hipLaunchKernelGGL((ready_kernel<false>), blocks, dim3(256), 0, stream, a);
     hipLaunchKernelGGL((grad_ready_kernel<kSumRows>), dim3(a.grid.blocks()),
                        dim3(Tile<256>::kThreads), 0, stream, a);
-    launch_sums<256>(a, stream);
+    launch_sums<Tile<256>>(a, stream);
 }
 
 template <bool kSumRows>

@@ -473,7 +473,8 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
 // which there is LDS.  Of a 256-tile's step of 1940 cycles (at 1.8 GHz, which is
 // what this load leaves) the matrix cores take 1024, the LDS reads 660 and the loads
 // to LDS about 420; waves wait for a third of it, at the barrier and for the
-// tokens.  LDS is given at the launch, as in grad_i8.hip's deep kernel.
+// tokens.  LDS is given at the launch: where one block of four waves fits, the
+// compiler would otherwise take accumulation registers (Tile).
 template <int kTile, int kRing>
 constexpr int packed_lds() { return kRing * kTile * 128 + 2 * kTile * (128 + 32); }
 template <int kTile, int kRing, typename Out>

@@ -28,12 +28,13 @@ constexpr int kRowBytes = 128; // of a k-row in LDS
 
 // Blocks of a product: a square tile over kWaves waves, two by kAcross, each
 // with kI x kJ results of 16 x 16.  Their kernels are bound to two waves a SIMD,
-// which they run at (a 256-tile, or two 128-tiles, on a compute unit): with more
-// registers than that the compiler keeps the sums in accumulation registers and
-// moves them about, 100 moves a step.
-template <int kTile>
+// which they run at (a 256-tile, two 128-tiles, or one over eight waves, on a
+// compute unit): with more registers than that the compiler keeps the sums in
+// accumulation registers and moves them about, 100 moves a step.
+constexpr int waves_of(int tile) { return tile == 256 ? 8 : 4; }
+template <int kTile_, int kWaves_ = waves_of(kTile_)>
 struct Tile {
-    static constexpr int kWaves = kTile == 256 ? 8 : 4;
+    static constexpr int kTile = kTile_, kWaves = kWaves_;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kAcross = kWaves / 2;
     static constexpr int kI = kTile / 32, kJ = kTile / (16 * kAcross);
@@ -174,9 +175,10 @@ __device__ __forceinline__ Piece piece_of(const Grid& g, uint32_t block)
 // Which results a lane holds of a wave's, by the matrix instructions' blocks of
 // 16 x 16 (v_mfma 16x16: a quad of four consecutive rows of one column) or
 // 32 x 32 (four such quads).  Quads are counted along the rows, four each.
-template <int kTile, int kBlock>
+template <int kTile, int kBlock, int kWaves = waves_of(kTile)>
 struct Held {
-    static constexpr int kI = Tile<kTile>::kI * 16 / kBlock, kJ = Tile<kTile>::kJ * 16 / kBlock;
+    using T = Tile<kTile, kWaves>;
+    static constexpr int kI = T::kI * 16 / kBlock, kJ = T::kJ * 16 / kBlock;
     static constexpr int kQuads = kBlock == 16 ? 1 : 4; // of a block
     __device__ __forceinline__ static int quad(int i, int q)
     {
