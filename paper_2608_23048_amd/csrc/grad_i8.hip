@@ -222,7 +222,7 @@ __device__ __forceinline__ void write_tile(const GradArgs& a, const Piece& piece
 #pragma unroll
             for (int j = 0; j < kJ; ++j)
                 *reinterpret_cast<f32x4*>(
-                    a.partial + Held<kTile, 16, T::kWaves>::part_at(piece.part, wave, i, j, 0)) = acc[i][j];
+                    a.partial + Held<T, 16>::part_at(piece.part, wave, i, j, 0)) = acc[i][j];
         return;
     }
     using Out = RowsOut<kI, 8>;
@@ -586,7 +586,7 @@ __global__ __launch_bounds__(64) void grad_sum_kernel(GradArgs a)
     const int wave = blockIdx.x / (T::kJ * T::kI) % T::kWaves;
     const uint32_t tile = blockIdx.x / (T::kJ * T::kI * T::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
-    const float* from = a.partial + Held<kTile, 16, T::kWaves>::part_at((int64_t)tile * a.grid.splits, wave, i, j, 0);
+    const float* from = a.partial + Held<T, 16>::part_at((int64_t)tile * a.grid.splits, wave, i, j, 0);
     f32x4 sum = {};
 #pragma unroll 8
     for (uint32_t p = 0; p < a.grid.splits; ++p)

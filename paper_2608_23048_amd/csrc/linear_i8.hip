@@ -278,10 +278,10 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
 // first half, 0-3, 12-15, 20-23 and 24-27, then the others; the spreads give any
 // such 16 lanes all the banks when 16 consecutive lanes (kBlock 16) or 32 read
 // the same chunk of as many rows.  Their lengths are multiples of 16 bytes.
-template <int kTile, int kBytes, int kBlock>
+template <typename T, int kBytes, int kBlock>
 struct Rows {
-    static constexpr int kThreads = Tile<kTile>::kThreads;
-    static constexpr int kLoads = kTile * kBytes / (16 * kThreads);
+    static constexpr int kThreads = T::kThreads;
+    static constexpr int kLoads = T::kTile * kBytes / (16 * kThreads);
     static constexpr int kChunks = kBytes / 16;
     static_assert(kBlock == 32 || kChunks == 8, "the spreads below");
     const uint8_t* base;
@@ -323,15 +323,15 @@ __device__ __forceinline__ i32x4 quad_of(const i32x16& v, int q)
 
 // A tile's results from a wave's sums: a part of a cut tile as it is, else scaled
 // and through LDS (all of which is free) to y.
-template <int kTile, int kBlock, typename Out, typename Sum>
+template <typename T, int kBlock, typename Out, typename Sum>
 __device__ __forceinline__ void write_tile(
     const LinearArgs& a, const Piece& piece,
-    const Sum (&acc)[Held<kTile, kBlock>::kI][Held<kTile, kBlock>::kJ], ROI_LDS uint8_t* base)
+    const Sum (&acc)[Held<T, kBlock>::kI][Held<T, kBlock>::kJ], ROI_LDS uint8_t* base)
 {
-    using H = Held<kTile, kBlock>;
+    using H = Held<T, kBlock>;
     const int wave = scalar(threadIdx.x >> 6);
-    const int r0 = piece.m * kTile + wave / Tile<kTile>::kAcross * 16 * Tile<kTile>::kI;
-    const int t0 = piece.n * kTile + wave % Tile<kTile>::kAcross * 16 * Tile<kTile>::kJ;
+    const int r0 = piece.m * T::kTile + wave / T::kAcross * 16 * T::kI;
+    const int t0 = piece.n * T::kTile + wave % T::kAcross * 16 * T::kJ;
     if (piece.part >= 0) {
 #pragma unroll
         for (int i = 0; i < H::kI; ++i)
@@ -354,8 +354,8 @@ __device__ __forceinline__ void write_tile(
 #pragma unroll
     for (int j = 0; j < H::kJ; ++j) xs[j] = a.xs[least(t0 + H::column(j), a.tokens - 1)];
     // as many blocks of tokens at a time as fit this wave's LDS
-    using Lines = RowsOut<Tile<kTile>::kI, 4 * sizeof(Out)>;
-    constexpr int kFit = kTile * kRowBytes * 4 / Tile<kTile>::kWaves / (kBlock * Lines::kRow);
+    using Lines = RowsOut<T::kI, 4 * sizeof(Out)>;
+    constexpr int kFit = T::kTile * kRowBytes * 4 / T::kWaves / (kBlock * Lines::kRow);
     constexpr int kAtATime = kFit < H::kJ ? kFit : H::kJ;
     static_assert(kAtATime >= 1 && H::kJ % kAtATime == 0, "results pass LDS");
     ROI_LDS uint8_t* mine = base + wave * (kAtATime * kBlock * Lines::kRow);
@@ -389,22 +389,22 @@ __device__ __forceinline__ void write_tile(
     }
 }
 
-template <int kTile, int kRing, typename Out>
-__global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(LinearArgs a)
+template <typename T, int kRing, typename Out>
+__global__ __launch_bounds__(T::kThreads, 2) void linear_tile_kernel(LinearArgs a)
 {
-    constexpr int kTileBytes = kTile * kRowBytes;
-    constexpr int kI = Tile<kTile>::kI, kJ = Tile<kTile>::kJ;
+    constexpr int kTile = T::kTile, kTileBytes = kTile * kRowBytes;
+    constexpr int kI = T::kI, kJ = T::kJ;
     static_assert(kRing == 2 || kRing == 4, "slots are counted in bits");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[]; // kRing steps of two tiles
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0];
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / Tile<kTile>::kAcross * 16 * kI, wn = wave % Tile<kTile>::kAcross * 16 * kJ;
+    const int wm = wave / T::kAcross * 16 * kI, wn = wave % T::kAcross * 16 * kJ;
     const Piece piece = piece_of(a.grid, blockIdx.x);
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x4 acc[kI][kJ] = {};
-    using R = Rows<kTile, kRowBytes, 16>;
+    using R = Rows<T, kRowBytes, 16>;
     const R wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
     constexpr int kLoads = R::kLoads;
     auto buffer = [&](int s) { return base + (s & (kRing - 1)) * 2 * kTileBytes; };
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
         }
         loads_barrier();
     }
-    write_tile<kTile, 16, Out>(a, piece, acc, base);
+    write_tile<T, 16, Out>(a, piece, acc, base);
 }
 
 // The same with 2:4 weights, on the 32 x 32 sparse instructions: a half step is
@@ -477,26 +477,27 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_tile_kernel(L
 // compiler would otherwise take accumulation registers (Tile).
 template <int kTile, int kRing>
 constexpr int packed_lds() { return kRing * kTile * 128 + 2 * kTile * (128 + 32); }
-template <int kTile, int kRing, typename Out>
-__global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel(LinearArgs a)
+template <typename T, int kRing, typename Out>
+__global__ __launch_bounds__(T::kThreads, 2) void linear_packed_kernel(LinearArgs a)
 {
-    using H = Held<kTile, 32>;
+    using H = Held<T, 32>;
+    constexpr int kTile = T::kTile;
     constexpr int kI = H::kI, kJ = H::kJ;
-    constexpr int kThreads = Tile<kTile>::kThreads;
+    constexpr int kThreads = T::kThreads;
     constexpr int kX = kTile * 128;                                    // of a step
     constexpr int kW = kTile * 128, kM = kTile * 32, kPair = kW + kM; // of two
     static_assert(kRing == 2 || kRing == 3, "the waits below");
-    static_assert(packed_lds<kTile, kRing>() == kRing * kX + 2 * kPair, "the launch's");
+    static_assert(packed_lds<T::kTile, kRing>() == kRing * kX + 2 * kPair, "the launch's");
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     ROI_LDS uint8_t* base = (ROI_LDS uint8_t*)&lds[0];
     const int lane = threadIdx.x & 63, half_of = lane >> 5, in = lane & 31;
     const int wave = scalar(threadIdx.x >> 6);
-    const int wm = wave / Tile<kTile>::kAcross * 32 * kI, wn = wave % Tile<kTile>::kAcross * 32 * kJ;
+    const int wm = wave / T::kAcross * 32 * kI, wn = wave % T::kAcross * 32 * kJ;
     const Piece piece = piece_of(a.grid, blockIdx.x);
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x16 acc[kI][kJ] = {};
-    using R = Rows<kTile, 128, 32>;
+    using R = Rows<T, 128, 32>;
     const R wrows(a.w, r0, a.rows, a.cols / 2), xrows(a.x, t0, a.tokens, a.cols);
     // metadata: a word a lane, eight words a row, word j at place j ^ (row / 4 & 7),
     // so that the words that 32 lanes read lie in the 32 banks of a 4-byte read
@@ -608,61 +609,50 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void linear_packed_kernel
         }
         loads_barrier();
     }
-    write_tile<kTile, 32, Out>(a, piece, acc, base);
+    write_tile<T, 32, Out>(a, piece, acc, base);
 }
 
 // The sums of the tiles that were cut: one wave for a quad of results a lane,
 // eight parts on their way at a time.
-template <int kTile, int kBlock, typename Out>
+template <typename T, int kBlock, typename Out>
 __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
 {
-    using H = Held<kTile, kBlock>;
+    using H = Held<T, kBlock>;
+    constexpr int kTile = T::kTile;
     constexpr int kAll = H::kI * H::kJ * H::kQuads;
     const int q = blockIdx.x % H::kQuads, j = blockIdx.x / H::kQuads % H::kJ;
     const int i = blockIdx.x / (H::kQuads * H::kJ) % H::kI;
-    const int wave = blockIdx.x / kAll % Tile<kTile>::kWaves;
-    const uint32_t tile = blockIdx.x / (kAll * Tile<kTile>::kWaves);
+    const int wave = blockIdx.x / kAll % T::kWaves;
+    const uint32_t tile = blockIdx.x / (kAll * T::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
     const int* from = a.partial + H::part_at((int64_t)tile * a.grid.splits, wave, i, j, q);
     i32x4 sum = {};
 #pragma unroll 8
     for (uint32_t p = 0; p < a.grid.splits; ++p)
         sum += *reinterpret_cast<const i32x4*>(from + (int64_t)p * (kTile * kTile));
-    const int r = piece.m * kTile + wave / Tile<kTile>::kAcross * 16 * Tile<kTile>::kI + 4 * H::quad(i, q);
-    const int t = piece.n * kTile + wave % Tile<kTile>::kAcross * 16 * Tile<kTile>::kJ + H::column(j);
+    const int r = piece.m * kTile + wave / T::kAcross * 16 * T::kI + 4 * H::quad(i, q);
+    const int t = piece.n * kTile + wave % T::kAcross * 16 * T::kJ + H::column(j);
     if (r >= a.rows || t >= a.tokens) return;
     float ws[4], add[4];
     row_scales(a, r, ws, add);
     store4<Out>(a, t, r, finish4(sum, ws, add, a.xs[t]));
 }
 
-template <int kTile, int kRing, typename Out>
-void launch_tiles_as(const LinearArgs& a, hipStream_t stream)
-{
-    const dim3 grid(a.grid.blocks()), block(Tile<kTile>::kThreads);
-    constexpr int kPackedLds = packed_lds<kTile, kRing == 2 ? 2 : 3>();
-    if (a.meta)
-        hipLaunchKernelGGL((linear_packed_kernel<kTile, kRing == 2 ? 2 : 3, Out>), grid, block,
-                           kPackedLds, stream, a);
-    else
-        hipLaunchKernelGGL((linear_tile_kernel<kTile, kRing, Out>), grid, block,
-                           kRing * 2 * kTile * kRowBytes, stream, a);
-}
-
-template <int kTile, typename Out>
+template <typename T, int kRing, int kPackedRing, typename Out>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
-    using T = Tile<kTile>;
-    if (kTile == 128 && a.grid.blocks() <= kUnits)
-        launch_tiles_as<128, 4, Out>(a, stream);
-    else
-        launch_tiles_as<kTile, 2, Out>(a, stream);
-    if (a.grid.rest() > 0) {
-        const dim3 sums(a.grid.rest() * T::kI * T::kJ * T::kWaves);
-        if (a.meta)
-            hipLaunchKernelGGL((linear_sum_kernel<kTile, 32, Out>), sums, dim3(64), 0, stream, a);
-        else
-            hipLaunchKernelGGL((linear_sum_kernel<kTile, 16, Out>), sums, dim3(64), 0, stream, a);
+    const dim3 grid(a.grid.blocks()), block(T::kThreads), sums(a.grid.rest() * T::kI * T::kJ * T::kWaves);
+    constexpr int kPackedLds = packed_lds<T::kTile, kPackedRing>();
+    if (a.meta) {
+        hipLaunchKernelGGL((linear_packed_kernel<T, kPackedRing, Out>), grid, block, kPackedLds,
+                           stream, a);
+        if (sums.x > 0)
+            hipLaunchKernelGGL((linear_sum_kernel<T, 32, Out>), sums, dim3(64), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL((linear_tile_kernel<T, kRing, Out>), grid, block,
+                           kRing * 2 * T::kTile * kRowBytes, stream, a);
+        if (sums.x > 0)
+            hipLaunchKernelGGL((linear_sum_kernel<T, 16, Out>), sums, dim3(64), 0, stream, a);
     }
 }
 
@@ -725,9 +715,11 @@ int launch(LinearArgs a, const LinearPlan& plan, void* workspace, hipStream_t st
     a.partial = reinterpret_cast<int*>(at);
     a.grid = grid_of(c);
     if (c.tile == 256)
-        launch_tiles<256, Out>(a, stream);
+        launch_tiles<Tile<256>, 2, 2, Out>(a, stream);
+    else if (a.grid.blocks() <= kUnits)
+        launch_tiles<Tile<128, 8>, 4, 3, Out>(a, stream);
     else
-        launch_tiles<128, Out>(a, stream);
+        launch_tiles<Tile<128>, 2, 2, Out>(a, stream);
     return launch_status("roi_linear_i8");
 }
 

@@ -175,9 +175,8 @@ __device__ __forceinline__ Piece piece_of(const Grid& g, uint32_t block)
 // Which results a lane holds of a wave's, by the matrix instructions' blocks of
 // 16 x 16 (v_mfma 16x16: a quad of four consecutive rows of one column) or
 // 32 x 32 (four such quads).  Quads are counted along the rows, four each.
-template <int kTile, int kBlock, int kWaves = waves_of(kTile)>
+template <typename T, int kBlock>
 struct Held {
-    using T = Tile<kTile, kWaves>;
     static constexpr int kI = T::kI * 16 / kBlock, kJ = T::kJ * 16 / kBlock;
     static constexpr int kQuads = kBlock == 16 ? 1 : 4; // of a block
     __device__ __forceinline__ static int quad(int i, int q)
@@ -194,7 +193,7 @@ struct Held {
     __device__ __forceinline__ static int64_t part_at(int64_t part, int wave, int i, int j, int q)
     {
         constexpr int kAll = kI * kJ * kQuads;
-        return part * (kTile * kTile) +
+        return part * (T::kTile * T::kTile) +
                ((wave * kAll + (i * kJ + j) * kQuads + q) * 64 + (int)(threadIdx.x & 63)) * 4;
     }
 };
