@@ -387,31 +387,44 @@ double copy_us(double bytes) { return 2 + bytes / 4.0e6; }
 // The length of copied rows: what a tile loads of a row is then one cache line.
 int64_t whole_lines(int64_t bytes) { return (bytes + 127) / 128 * 128; }
 
+// The streaming kernel's expected time: it takes 32 tokens at a time, the first
+// with the weight from memory, the others from the caches, in blocks of 32 or 16
+// rows of which 512 (256 at 2:4) run at once.  Fitted to 40 to 512 tokens through
+// ten weights: 64 tokens through 3584 x 3584 take 5.6 us so and 14.7 in tiles,
+// through 18944 x 3584 26 and 20; 128 tokens 8.3 and 14.8, 44 and 23.
+double few_us(int64_t tokens, int64_t rows, int64_t cols, bool packed)
+{
+    const int64_t groups = (tokens + 31) / 32;
+    const double blocks = (double)((rows + 31) / 32) * (double)groups;
+    const double weight = (double)rows * (double)cols;
+    const double first = packed ? 8.0e6 : 5.0e6, again = packed ? 10.0e6 : 8.0e6;
+    if (cols % 16) return 2.2 + (double)groups * weight / 1.5e6;
+    return 2.2 + blocks * (packed ? 1.77 / 256 : 1.5 / 512) + weight / first +
+           (double)(groups - 1) * weight / again;
+}
+
 } // namespace
 
-// The streaming kernel takes 32 tokens at a time, each time at 7e6 bytes of a
-// dense weight a microsecond from the caches (6e6 at 2:4, of the dense weight it
-// stands for; 2.5e6 where rows end within 16 bytes).  64 tokens through 3584 x
-// 3584 take 5.6 us so and 17.5 in tiles, through 18944 x 3584 25 and 29; 128
-// tokens 8.3 and 17.4, 44 and 30.
 LinearPlan plan_linear(int64_t tokens, int64_t rows, int64_t cols, bool packed)
 {
     LinearPlan p{};
     p.few = tokens <= 32;
     if (p.few) return p;
-    p.cut = cut_product(rows, tokens, cols, 128, packed ? kPackedCost : kLinearCost);
+    const TileCost& cost = packed ? kPackedCost : kLinearCost;
+    p.cut = cut_product(rows, tokens, cols, 128, cost);
     p.row = cols % 16 == 0 ? cols : whole_lines(cols);
     double tiles_us = p.cut.us;
+    // few tiles: their steps may be less work than reading the weight
+    if (tokens <= 128)
+        tiles_us += std::max(0.0, (double)rows * (double)cols * (packed ? 0.625 : 1) / 5.0e6 -
+                                      (double)(p.cut.steps / p.cut.splits) * cost.step128);
     if (p.row != cols) {
         p.x_bytes = padded256(tokens * p.row);
         p.w_bytes = padded256(rows * p.row);
         tiles_us += copy_us(2.0 * (double)(tokens + rows) * (double)cols);
     }
     p.bytes = p.x_bytes + p.w_bytes + p.cut.bytes;
-    const double rate = packed ? 6.0e6 : p.row == cols ? 7.0e6 : 2.5e6;
-    const double few_us =
-        3 + (double)((tokens + 31) / 32) * (double)rows * (double)cols / rate;
-    p.few = tokens <= 1024 && few_us < tiles_us;
+    p.few = tokens <= 1024 && few_us(tokens, rows, cols, packed) < tiles_us;
     return p;
 }
 

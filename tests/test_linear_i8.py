@@ -334,6 +334,14 @@ def test_linear_dense_bit_exact(tokens, rows, cols):
         assert np.array_equal(bf16_bits(y), bf16_rne_bits(want))
 
 
+@gpu
+@pytest.mark.parametrize("tokens,rows,cols", [(1030, 40, 257), (1100, 300, 1001), (1025, 5, 3)])
+def test_linear_of_copied_rows(tokens, rows, cols):
+    """Rows that end within 16 bytes, through the tiles."""
+    assert roi.linear_i8_workspace(tokens, rows, cols) >= (tokens + rows) * cols
+    test_linear_dense_bit_exact(tokens, rows, cols)
+
+
 PACKED = [(1, 1, 32), (1, 16, 256), (3, 17, 96), (16, 40, 896), (17, 33, 288), (40, 64, 128),
           (64, 130, 512), (65, 128, 160), (130, 129, 1024), (200, 260, 352), (300, 48, 32)]
 
