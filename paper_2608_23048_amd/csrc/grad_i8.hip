@@ -452,7 +452,8 @@ __global__ __launch_bounds__(DeepTile::kThreads) void grad_deep_kernel(GradArgs 
         for (int i = 0; i < Dy::kLoads; ++i) dy.stage(i, k, slot);
 #pragma unroll
         for (int i = 0; i < kRawLoads; ++i) {
-            const int row = (i * kThreads + (int)threadIdx.x) / 8, chunk = threadIdx.x % 8;
+            const int row = (i * kThreads + (int)threadIdx.x) / 8;
+            const int chunk = (threadIdx.x % 8) ^ (row & 4);
             const bool live = row < a.K - k && 16 * chunk < a.q_row - c0;
             load_to_lds<kSumRows>(buffer_at(raw + (int64_t)k * a.q_row),
                                   live ? (uint32_t)row * a.q_row + 16 * chunk : kNowhere, 0,
@@ -465,8 +466,10 @@ __global__ __launch_bounds__(DeepTile::kThreads) void grad_deep_kernel(GradArgs 
     struct Half {
         bf16x8 q[kI], y[kJ];
     };
-    // a thread takes four sum indices of four columns: half a chunk of each
-    const int four = threadIdx.x / 32, group = threadIdx.x % 32;
+    // a thread takes four sum indices of four columns: half a chunk of each, its
+    // neighbour the other half, so that 16 lanes write 128 bytes of all banks; the
+    // two read rows four apart, whose halves lie in LDS the other way round
+    const int four = threadIdx.x / 64 * 2 + threadIdx.x % 2, group = threadIdx.x % 64 / 2;
     const int to = Q::place(4 * group, four / 2) + 8 * (four % 2);
     struct Raw {
         uint32_t v[4];
@@ -476,7 +479,7 @@ __global__ __launch_bounds__(DeepTile::kThreads) void grad_deep_kernel(GradArgs 
         ROI_LDS uint8_t* p = slot + kTileBytes;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            r.v[j] = lds_read<uint32_t>(p + (4 * four + j) * kTile + 4 * group);
+            r.v[j] = lds_read<uint32_t>(p + (4 * four + j) * kTile + ((4 * group) ^ (64 * (four % 2))));
         r.s = lds_read<f32x4>(p + kRaw + 16 * four);
     };
     // column b: its place is that of column 0 with its low bits flipped by b
