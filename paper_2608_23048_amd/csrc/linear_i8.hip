@@ -41,8 +41,7 @@ struct LinearArgs {
 
 // The scales of rows r .. r + 3, and what is added to their results: without a
 // bias -0, which changes nothing.
-__device__ __forceinline__ void row_scales(const LinearArgs& a, int r, float (&ws)[4],
-                                           float (&add)[4])
+__device__ __forceinline__ void row_scales(const LinearArgs& a, int r, f32x4& ws, f32x4& add)
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -54,8 +53,7 @@ __device__ __forceinline__ void row_scales(const LinearArgs& a, int r, float (&w
 
 // Four results from their exact sums.  The scale of the weight comes first: sum
 // ws stays far from overflow for any weight.
-__device__ __forceinline__ f32x4 finish4(i32x4 sum, const float (&ws)[4], const float (&add)[4],
-                                         float xs)
+__device__ __forceinline__ f32x4 finish4(i32x4 sum, f32x4 ws, f32x4 add, float xs)
 {
     f32x4 v;
 #pragma unroll
@@ -252,7 +250,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
         const int in = 16 * (b % kTok) + (lane & 15);
         const int t = t0 + in, r = r0 + 16 * (b / kTok) + 4 * g;
         if (in >= kTokens || t >= a.tokens || r >= a.rows) continue;
-        float ws[4], add[4];
+        f32x4 ws, add;
         row_scales(a, r, ws, add);
         const float xs = a.xs[t];
         i32x4 sum = {};
@@ -326,12 +324,40 @@ __device__ __forceinline__ i32x4 quad_of(const i32x16& v, int q)
     return i32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
 }
 
+// The scales of a whole tile's rows and tokens, and what is added to the rows'
+// results: loaded ahead of the tile's first steps and kept in LDS to its end, where
+// a wave would otherwise wait for them.
+template <typename T>
+struct Scales {
+    static constexpr int kBytes = 3 * 4 * T::kTile;
+    static_assert(T::kTile <= T::kThreads, "one of each a thread");
+    float ws, add, xs;
+
+    __device__ __forceinline__ Scales(const LinearArgs& a, const Piece& piece)
+    {
+        if (piece.part >= 0 || threadIdx.x >= T::kTile) return;
+        const int r = least(piece.m * T::kTile + (int)threadIdx.x, a.rows - 1);
+        ws = a.ws[r];
+        xs = a.xs[least(piece.n * T::kTile + (int)threadIdx.x, a.tokens - 1)];
+        add = a.bias ? bf16_bits_to_float(a.bias[r]) : -0.0f;
+    }
+    __device__ __forceinline__ void keep(const Piece& piece, ROI_LDS uint8_t* lds) const
+    {
+        if (piece.part >= 0 || threadIdx.x >= T::kTile) return;
+        ROI_LDS float* p = reinterpret_cast<ROI_LDS float*>(lds) + threadIdx.x;
+        p[0] = ws;
+        p[T::kTile] = add;
+        p[2 * T::kTile] = xs;
+    }
+};
+
 // A tile's results from a wave's sums: a part of a cut tile as it is, else scaled
 // and through LDS (all of which is free) to y.
 template <typename T, int kBlock, typename Out, typename Sum>
 __device__ __forceinline__ void write_tile(
     const LinearArgs& a, const Piece& piece,
-    const Sum (&acc)[Held<T, kBlock>::kI][Held<T, kBlock>::kJ], ROI_LDS uint8_t* base)
+    const Sum (&acc)[Held<T, kBlock>::kI][Held<T, kBlock>::kJ], ROI_LDS uint8_t* base,
+    const ROI_LDS uint8_t* scales)
 {
     using H = Held<T, kBlock>;
     const int wave = scalar(threadIdx.x >> 6);
@@ -348,16 +374,12 @@ __device__ __forceinline__ void write_tile(
                         quad_of(acc[i][j], q);
         return;
     }
-    // every scale before the first store, which might overwrite one for all the
-    // compiler knows
-    float ws[H::kI][H::kQuads][4], add[H::kI][H::kQuads][4], xs[H::kJ];
+    const ROI_LDS uint8_t* row_scale = scales + 4 * (wave / T::kAcross * 16 * T::kI);
+    const ROI_LDS uint8_t* token_scale =
+        scales + 4 * (2 * T::kTile + wave % T::kAcross * 16 * T::kJ);
+    float xs[H::kJ];
 #pragma unroll
-    for (int i = 0; i < H::kI; ++i)
-#pragma unroll
-        for (int q = 0; q < H::kQuads; ++q)
-            row_scales(a, r0 + 4 * H::quad(i, q), ws[i][q], add[i][q]);
-#pragma unroll
-    for (int j = 0; j < H::kJ; ++j) xs[j] = a.xs[least(t0 + H::column(j), a.tokens - 1)];
+    for (int j = 0; j < H::kJ; ++j) xs[j] = lds_read<float>(token_scale + 4 * H::column(j));
     // as many blocks of tokens at a time as fit this wave's LDS
     using Lines = RowsOut<T::kI, 4 * sizeof(Out)>;
     constexpr int kFit = T::kTile * kRowBytes * 4 / T::kWaves / (kBlock * Lines::kRow);
@@ -366,14 +388,26 @@ __device__ __forceinline__ void write_tile(
     ROI_LDS uint8_t* mine = base + wave * (kAtATime * kBlock * Lines::kRow);
 #pragma unroll
     for (int first = 0; first < H::kJ; first += kAtATime) {
+        // a row of blocks' scales are read ahead of the results before it: the
+        // compiler keeps reads of LDS behind writes
+        f32x4 ws[2][H::kQuads], add[2][H::kQuads];
+        auto read = [&](int i) {
 #pragma unroll
-        for (int j = 0; j < kAtATime; ++j)
+            for (int q = 0; q < H::kQuads; ++q) {
+                ws[i & 1][q] = lds_read<f32x4>(row_scale + 16 * H::quad(i, q));
+                add[i & 1][q] = lds_read<f32x4>(row_scale + 16 * H::quad(i, q) + 4 * T::kTile);
+            }
+        };
+        read(0);
 #pragma unroll
-            for (int i = 0; i < H::kI; ++i)
+        for (int i = 0; i < H::kI; ++i) {
+            if (i + 1 < H::kI) read(i + 1);
+#pragma unroll
+            for (int j = 0; j < kAtATime; ++j)
 #pragma unroll
                 for (int q = 0; q < H::kQuads; ++q) {
-                    const f32x4 v = finish4(quad_of(acc[i][first + j], q), ws[i][q], add[i][q],
-                                            xs[first + j]);
+                    const f32x4 v = finish4(quad_of(acc[i][first + j], q), ws[i & 1][q],
+                                            add[i & 1][q], xs[first + j]);
                     ROI_LDS uint8_t* at = Lines::at(mine, H::column(j), H::quad(i, q));
                     if constexpr (sizeof(Out) == 2)
                         *reinterpret_cast<ROI_LDS u32x2*>(at) =
@@ -381,6 +415,7 @@ __device__ __forceinline__ void write_tile(
                     else
                         *reinterpret_cast<ROI_LDS f32x4*>(at) = v;
                 }
+        }
 #pragma unroll 2 // code that runs once is fetched once: it is kept short
         for (int n = 0; n < kBlock * kAtATime / Lines::kAtOnce; ++n) {
             int row, chunk;
@@ -449,9 +484,11 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_tile_kernel(LinearArgs 
         }
     };
     static_assert(2 * kLoads % kI == 0, "loads are spread over the rows");
+    const Scales<T> scales(a, piece);
     if (piece.count > 0) {
         Half lo, hi;
         for (int s = 0; s < kRing; ++s) stage(s, 0, 2 * kLoads);
+        scales.keep(piece, base + kRing * 2 * kTileBytes);
         loads_barrier<(kRing - 1) * 2 * kLoads>();
 #pragma unroll
         for (int i = 0; i < kI; ++i) read_w(0, 0, lo, i);
@@ -463,8 +500,11 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_tile_kernel(LinearArgs 
             half(hi, s + 1, 0, lo, std::true_type{});
         }
         loads_barrier();
+    } else { // a sum over nothing
+        scales.keep(piece, base + kRing * 2 * kTileBytes);
+        __syncthreads();
     }
-    write_tile<T, 16, Out>(a, piece, acc, base);
+    write_tile<T, 16, Out>(a, piece, acc, base, base + kRing * 2 * kTileBytes);
 }
 
 // The same with 2:4 weights, on the 32 x 32 sparse instructions: a half step is
@@ -569,6 +609,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_packed_kernel(LinearArg
             keep_order();
         }
     };
+    const Scales<T> scales(a, piece);
     if (piece.count > 0) {
         ROI_LDS uint8_t *x0 = base, *x1 = base + kX, *x2 = base + (kRing - 1) * kX;
         ROI_LDS uint8_t *w0 = base + kRing * kX, *w1 = w0 + kPair; // of this pair of steps and the next
@@ -581,6 +622,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_packed_kernel(LinearArg
         stage_x(1, 0, R::kLoads, x1);
         if (kRing > 2) stage_x(2, 0, R::kLoads, x2);
         stage_w(2, 0, kPairLoads, w1);
+        scales.keep(piece, base + packed_lds<T::kTile, kRing>());
         loads_barrier<(kRing - 1) * R::kLoads + kPairLoads>();
 #pragma unroll
         for (int i = 0; i < kI; ++i) read_w(w0, 0, lo, i);
@@ -613,8 +655,11 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_packed_kernel(LinearArg
             }
         }
         loads_barrier();
+    } else { // a sum over nothing
+        scales.keep(piece, base + packed_lds<T::kTile, kRing>());
+        __syncthreads();
     }
-    write_tile<T, 32, Out>(a, piece, acc, base);
+    write_tile<T, 32, Out>(a, piece, acc, base, base + packed_lds<T::kTile, kRing>());
 }
 
 // The sums of the tiles that were cut: one wave for a quad of results a lane,
@@ -638,7 +683,7 @@ __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
     const int r = piece.m * kTile + wave / T::kAcross * 16 * T::kI + 4 * H::quad(i, q);
     const int t = piece.n * kTile + wave % T::kAcross * 16 * T::kJ + H::column(j);
     if (r >= a.rows || t >= a.tokens) return;
-    float ws[4], add[4];
+    f32x4 ws, add;
     row_scales(a, r, ws, add);
     store4<Out>(a, t, r, finish4(sum, ws, add, a.xs[t]));
 }
@@ -647,7 +692,7 @@ template <typename T, int kRing, int kPackedRing, typename Out>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
     const dim3 grid(a.grid.blocks()), block(T::kThreads), sums(a.grid.rest() * T::kI * T::kJ * T::kWaves);
-    constexpr int kPackedLds = packed_lds<T::kTile, kPackedRing>();
+    constexpr int kPackedLds = packed_lds<T::kTile, kPackedRing>() + Scales<T>::kBytes;
     if (a.meta) {
         hipLaunchKernelGGL((linear_packed_kernel<T, kPackedRing, Out>), grid, block, kPackedLds,
                            stream, a);
@@ -655,7 +700,7 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
             hipLaunchKernelGGL((linear_sum_kernel<T, 32, Out>), sums, dim3(64), 0, stream, a);
     } else {
         hipLaunchKernelGGL((linear_tile_kernel<T, kRing, Out>), grid, block,
-                           kRing * 2 * T::kTile * kRowBytes, stream, a);
+                           kRing * 2 * T::kTile * kRowBytes + Scales<T>::kBytes, stream, a);
         if (sums.x > 0)
             hipLaunchKernelGGL((linear_sum_kernel<T, 16, Out>), sums, dim3(64), 0, stream, a);
     }

@@ -418,7 +418,7 @@ def test_linear_empty(packed):
     assert roi.linear_i8(z(0, 32), o(0), z(4, 32 // k), o(4), meta=meta(4, 32)).shape == (0, 4)
     assert roi.linear_i8(z(3, 32), o(3), z(0, 32 // k), o(0), meta=meta(0, 32)).shape == (3, 0)
     b = torch.randn(4, device="cuda").bfloat16()
-    for tokens in (3, 100):  # a sum over nothing is 0: the bias remains
+    for tokens in (3, 100, 1100):  # a sum over nothing is 0: the bias remains
         y = roi.linear_i8(z(tokens, 0), o(tokens), z(4, 0), o(4), meta=meta(4, 0), bias=b)
         assert torch.equal(y, b.expand(tokens, 4))
 
