@@ -125,7 +125,7 @@ struct TileCost {
     double step256, rest256, step128, two128, rest128;
 };
 constexpr TileCost kLinearCost = {1.36, 9, 0.39, 0.80, 5.5};
-constexpr TileCost kPackedCost = {0.84, 12, 0.38, 0.72, 5};
+constexpr TileCost kPackedCost = {0.80, 8, 0.38, 0.72, 5};
 constexpr TileCost kGradCost = {1.70, 14, 0.57, 1.50, 8};
 // Of a 256-tile with both operands in bf16 (there is no 128-tile).
 constexpr TileCost kReadyCost = {1.40, 12, 0, 0, 0};
