@@ -512,13 +512,13 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_tile_kernel(LinearArgs 
 // 16 form takes 128 columns at once and twice the registers, too many to read
 // ahead).  Weights and metadata come for two steps at a time, 128 and 32 bytes a
 // row: requests to the L2 were what bound the step (a step at a time 26 million in
-// 175 us for 4096 tokens through 3584 x 18944; so, 18 million in 163).  The
+// 175 us for 4096 tokens through 3584 x 18944; so, 18 million in 163, and with no
+// registers in scratch 156).  The
 // tokens' tiles have kRing - 1 steps to arrive: two where a tile has a compute unit
 // to itself (512 tokens through 3584 x 3584: 15.7 us, 17.6 with one), else one, for
-// which there is LDS.  Of a 256-tile's step of 1940 cycles (at 1.8 GHz, which is
+// which there is LDS.  Of a 256-tile's step of 1870 cycles (at 1.8 GHz, which is
 // what this load leaves) the matrix cores take 1024, the LDS reads 660 and the loads
-// to LDS about 420; waves wait for a third of it, at the barrier and for the
-// tokens.  LDS is given at the launch: where one block of four waves fits, the
+// to LDS about 420; waves wait for 29 % of it, at the barrier and for the tokens.  LDS is given at the launch: where one block of four waves fits, the
 // compiler would otherwise take accumulation registers (Tile).
 template <int kTile, int kRing>
 constexpr int packed_lds() { return kRing * kTile * 128 + 2 * kTile * (128 + 32); }
