@@ -145,28 +145,30 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
             }
         }
     };
-    // Rows that end within 16 bytes (dense weights) go by registers: fetched a step
-    // ahead, at any address, rows past the end the last again.
-    Quad held[kWhole ? 1 : 2 * kRow + kTokens / 8];
-    auto fetch = [&](int s) {
+    // Rows that end within 16 bytes (dense weights) go by registers: fetched kAhead
+    // steps ahead, at any address, rows past the end the last again.
+    constexpr int kAhead = kWhole ? 1 : 4, kPieces = kWhole ? 1 : 2 * kRow + kTokens / 8;
+    Quad held[kAhead][kPieces];
+    auto fetch = [&](int s, Quad (&to)[kPieces]) {
         const int k = s * 128;
+        if (k >= a.cols) return;
 #pragma unroll
-        for (int i = 0; i < 2 * kRow + kTokens / 8; ++i) {
+        for (int i = 0; i < kPieces; ++i) {
             const bool w = i < 2 * kRow;
             const int rows = w ? a.rows - r0 : a.tokens - t0;
             const uint8_t* p = (w ? wbase : xbase) +
                                (int64_t)least(8 * (w ? i : i - 2 * kRow) + row, rows - 1) * a.cols;
             if (k + 128 <= a.cols) // the same for the wave
-                held[kWhole ? 0 : i] = load_any<Quad>(p + k + 16 * chunk);
+                to[i] = load_any<Quad>(p + k + 16 * chunk);
             else
-                held[kWhole ? 0 : i] = load_row<Quad>(p, k + 16 * chunk, a.cols);
+                to[i] = load_row<Quad>(p, k + 16 * chunk, a.cols);
         }
     };
-    auto put = [&](ROI_LDS uint8_t* slot) {
+    auto put = [&](ROI_LDS uint8_t* slot, const Quad (&from)[kPieces]) {
 #pragma unroll
-        for (int i = 0; i < 2 * kRow + kTokens / 8; ++i)
+        for (int i = 0; i < kPieces; ++i)
             lds_write(slot + (i < 2 * kRow ? i * 1024 : kW + (i - 2 * kRow) * 1024) + lane * 16,
-                      held[kWhole ? 0 : i]);
+                      from[i]);
     };
     i32x4 acc[kRow][kTok] = {};
     const int from = (lane & 15) * 128 + (g ^ (lane & 7)) * 16;
@@ -231,12 +233,17 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
             }
             loads_wait<0>();
         } else {
-            fetch(wave);
-            for (int n = 0; n < mine; ++n) {
-                put(ring + slot); // a wave's LDS operations are done in their order
-                fetch(wave + (n + 1) * kWaves);
-                multiply(ring + slot);
-                next_slot();
+#pragma unroll
+            for (int n = 0; n < kAhead; ++n) fetch(wave + n * kWaves, held[n]);
+            for (int n = 0; n < mine; n += kAhead) {
+#pragma unroll
+                for (int h = 0; h < kAhead; ++h) {
+                    if (n + h >= mine) break;
+                    put(ring + slot, held[h]); // a wave's LDS operations are done in order
+                    fetch(wave + (n + h + kAhead) * kWaves, held[h]);
+                    multiply(ring + slot);
+                    next_slot();
+                }
             }
         }
     }
@@ -518,8 +525,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_tile_kernel(LinearArgs 
 // to itself (512 tokens through 3584 x 3584: 15.7 us, 17.6 with one), else one, for
 // which there is LDS.  Of a 256-tile's step of 1870 cycles (at 1.8 GHz, which is
 // what this load leaves) the matrix cores take 1024, the LDS reads 660 and the loads
-// to LDS about 420; waves wait for 29 % of it, at the barrier and for the tokens.  LDS is given at the launch: where one block of four waves fits, the
-// compiler would otherwise take accumulation registers (Tile).
+// to LDS about 420; waves wait for 29 % of it, at the barrier and for the tokens.
 template <int kTile, int kRing>
 constexpr int packed_lds() { return kRing * kTile * 128 + 2 * kTile * (128 + 32); }
 template <typename T, int kRing, typename Out>
