@@ -398,7 +398,7 @@ double few_us(int64_t tokens, int64_t rows, int64_t cols, bool packed)
     const double blocks = (double)((rows + 31) / 32) * (double)groups;
     const double weight = (double)rows * (double)cols;
     const double first = packed ? 8.0e6 : 5.0e6, again = packed ? 10.0e6 : 8.0e6;
-    if (cols % 16) return 2.2 + (double)groups * weight / 1.5e6;
+    if (cols % 16) return 3.5 + (double)groups * weight / 2.5e6;
     return 2.2 + blocks * (packed ? 1.77 / 256 : 1.5 / 512) + weight / first +
            (double)(groups - 1) * weight / again;
 }

@@ -151,17 +151,19 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
     Quad held[kAhead][kPieces];
     auto fetch = [&](int s, Quad (&to)[kPieces]) {
         const int k = s * 128;
-        if (k >= a.cols) return;
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
+        auto start = [&](int i) {
             const bool w = i < 2 * kRow;
             const int rows = w ? a.rows - r0 : a.tokens - t0;
-            const uint8_t* p = (w ? wbase : xbase) +
-                               (int64_t)least(8 * (w ? i : i - 2 * kRow) + row, rows - 1) * a.cols;
-            if (k + 128 <= a.cols) // the same for the wave
-                to[i] = load_any<Quad>(p + k + 16 * chunk);
-            else
-                to[i] = load_row<Quad>(p, k + 16 * chunk, a.cols);
+            return (w ? wbase : xbase) +
+                   (int64_t)least(8 * (w ? i : i - 2 * kRow) + row, rows - 1) * a.cols;
+        };
+        if (k + 128 <= a.cols) { // the same for the wave
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) to[i] = load_any<Quad>(start(i) + k + 16 * chunk);
+        } else if (k < a.cols) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                to[i] = load_row<Quad>(start(i), k + 16 * chunk, a.cols);
         }
     };
     auto put = [&](ROI_LDS uint8_t* slot, const Quad (&from)[kPieces]) {

@@ -58,13 +58,35 @@ __device__ __forceinline__ void stream_store_any(void* p, const V& v)
 }
 
 // Bytes k .. k + N - 1 of a row of `len` bytes, zeros past its end (nothing
-// past it is read).
+// past it is read): the row's last N bytes, moved down, where it ends within them.
 template <typename V>
 __device__ __forceinline__ V load_row(const uint8_t* row, int64_t k, int64_t len)
 {
     constexpr int N = sizeof(V);
     if (k + N <= len) return load_any<V>(row + k);
     V v{};
+    if (k >= len) return v;
+    if (len >= N) {
+        v = load_any<V>(row + len - N);
+        const int bits = 8 * (int)(k + N - len); // 8 .. 8 N - 8
+        if constexpr (N == 4) {
+            v.w[0] >>= bits;
+        } else if constexpr (N == 8) {
+            const uint64_t x = (v.w[0] | (uint64_t)v.w[1] << 32) >> bits;
+            v = V{(uint32_t)x, (uint32_t)(x >> 32)};
+        } else {
+            uint64_t lo = v.w[0] | (uint64_t)v.w[1] << 32, hi = v.w[2] | (uint64_t)v.w[3] << 32;
+            if (bits >= 64) {
+                lo = hi >> (bits - 64);
+                hi = 0;
+            } else {
+                lo = lo >> bits | hi << (64 - bits);
+                hi >>= bits;
+            }
+            v = V{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+        }
+        return v;
+    }
     for (int i = 0; i < N; ++i)
         if (k + i < len) v.w[i / 4] |= (uint32_t)row[k + i] << (8 * (i % 4));
     return v;
