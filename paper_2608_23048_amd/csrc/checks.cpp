@@ -329,6 +329,7 @@ namespace {
 constexpr int64_t kMostSplits = 64;
 constexpr double kPartBytesPerUs = 6.0e6; // of parts, written and read again
 constexpr double kSumLaunchUs = 6.5;
+constexpr double kSumPartUs = 0.06;       // of a sum, for each of its parts: eight are read at a time
 
 // One tile size: the tiles of whole rounds over the units are whole.  The last
 // round's are cut where that is expected to take less time, into as many parts
@@ -352,12 +353,12 @@ Cut cut_tiles(int64_t m, int64_t n, int64_t k, int64_t step, int tile, const Til
     c.full = tiles;
     c.splits = 1;
     c.us = rounds + (rest ? round(rest, c.steps) : 0);
-    // a part of a sum has four steps at least
-    const int64_t most = rest ? std::min(std::min(slots / rest, c.steps / 4), kMostSplits) : 0;
+    // a part of a sum has two steps at least
+    const int64_t most = rest ? std::min(std::min(slots / rest, c.steps / 2), kMostSplits) : 0;
     for (int64_t splits = 2; splits <= most; ++splits) {
         const int64_t bytes = rest * splits * tile * tile * 4;
         const double us = rounds + round(rest * splits, (c.steps + splits - 1) / splits) +
-                          (double)bytes / kPartBytesPerUs + kSumLaunchUs;
+                          (double)bytes / kPartBytesPerUs + kSumLaunchUs + kSumPartUs * (double)splits;
         if (us < c.us) {
             c.us = us;
             c.full = tiles - rest;

@@ -32,7 +32,7 @@ static void check_cut(const Cut& c, int64_t m, int64_t n, int64_t k, int64_t ste
     expect("steps", c.steps, (k + step - 1) / step);
     const int64_t rest = c.tm * c.tn - c.full;
     expect("full", c.full >= 0 && rest >= 0, 1);
-    expect("splits", c.splits >= 1 && (c.splits == 1 || c.splits * 4 <= c.steps), 1);
+    expect("splits", c.splits >= 1 && (c.splits == 1 || c.splits * 2 <= c.steps), 1);
     expect("cut only with parts", (rest > 0) == (c.splits > 1), 1);
     expect("bytes", c.bytes, rest > 0 ? rest * c.splits * c.tile * c.tile * 4 : 0);
     if (rest > 0) expect("parts within a round", rest * c.splits <= 512, 1);
