@@ -329,7 +329,7 @@ namespace {
 constexpr int64_t kMostSplits = 64;
 constexpr double kPartBytesPerUs = 6.0e6; // of parts, written and read again
 constexpr double kSumLaunchUs = 6.5;
-constexpr double kSumPartUs = 0.06;       // of a sum, for each of its parts: eight are read at a time
+constexpr double kSumPartUs = 0.06;       // of a sum, for each of its parts
 
 // One tile size: the tiles of whole rounds over the units are whole.  The last
 // round's are cut where that is expected to take less time, into as many parts

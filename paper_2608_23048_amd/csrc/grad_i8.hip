@@ -578,22 +578,19 @@ __global__ __launch_bounds__(256) void ready_kernel(GradArgs a)
     }
 }
 
-// The sums of the tiles that were cut: one wave for 16 x 16 results, the parts
-// in their order, eight of them on their way at a time.
+// The sums of the tiles that were cut: one wave for 16 x 16 results.
 template <typename T>
-__global__ __launch_bounds__(64) void grad_sum_kernel(GradArgs a)
+__global__ __launch_bounds__(256) void grad_sum_kernel(GradArgs a)
 {
     constexpr int kTile = T::kTile;
-    const int lane = threadIdx.x;
-    const int j = blockIdx.x % T::kJ, i = blockIdx.x / T::kJ % T::kI;
-    const int wave = blockIdx.x / (T::kJ * T::kI) % T::kWaves;
-    const uint32_t tile = blockIdx.x / (T::kJ * T::kI * T::kWaves);
+    const int lane = threadIdx.x & 63;
+    const uint32_t id = scalar(blockIdx.x * 4 + threadIdx.x / 64);
+    const int i = id % T::kI, j = id / T::kI % T::kJ;
+    const int wave = id / (T::kJ * T::kI) % T::kWaves;
+    const uint32_t tile = id / (T::kJ * T::kI * T::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
     const float* from = a.partial + Held<T, 16>::part_at((int64_t)tile * a.grid.splits, wave, i, j, 0);
-    f32x4 sum = {};
-#pragma unroll 8
-    for (uint32_t p = 0; p < a.grid.splits; ++p)
-        sum += *reinterpret_cast<const f32x4*>(from + (int64_t)p * (kTile * kTile));
+    const f32x4 sum = sum_of_parts<T, f32x4>(from, (int)a.grid.splits);
     const int c = piece.n * kTile + 16 * (wave / T::kAcross * T::kI + i) + 4 * (lane >> 4);
     const int d = piece.m * kTile + 16 * (wave % T::kAcross * T::kJ + j) + (lane & 15);
     if (d >= a.D) return;
@@ -613,7 +610,7 @@ void launch_sums(const GradArgs& a, hipStream_t stream)
 {
     if (a.grid.rest() > 0)
         hipLaunchKernelGGL((grad_sum_kernel<T>),
-                           dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves), dim3(64), 0, stream, a);
+                           dim3(a.grid.rest() * T::kI * T::kJ * T::kWaves / 4), dim3(256), 0, stream, a);
 }
 
 template <int kTile, bool kSumRows>

@@ -670,24 +670,21 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_packed_kernel(LinearArg
     write_tile<T, 32, Out>(a, piece, acc, base, base + packed_lds<T::kTile, kRing>());
 }
 
-// The sums of the tiles that were cut: one wave for a quad of results a lane,
-// eight parts on their way at a time.
+// The sums of the tiles that were cut: one wave for a quad of results a lane.
 template <typename T, int kBlock, typename Out>
-__global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
+__global__ __launch_bounds__(256) void linear_sum_kernel(LinearArgs a)
 {
     using H = Held<T, kBlock>;
     constexpr int kTile = T::kTile;
     constexpr int kAll = H::kI * H::kJ * H::kQuads;
-    const int q = blockIdx.x % H::kQuads, j = blockIdx.x / H::kQuads % H::kJ;
-    const int i = blockIdx.x / (H::kQuads * H::kJ) % H::kI;
-    const int wave = blockIdx.x / kAll % T::kWaves;
-    const uint32_t tile = blockIdx.x / (kAll * T::kWaves);
+    const uint32_t id = scalar(blockIdx.x * 4 + threadIdx.x / 64);
+    const int q = id % H::kQuads, i = id / H::kQuads % H::kI;
+    const int j = id / (H::kQuads * H::kI) % H::kJ;
+    const int wave = id / kAll % T::kWaves;
+    const uint32_t tile = id / (kAll * T::kWaves);
     const Piece piece = tile_piece(a.grid, a.grid.full + tile);
     const int* from = a.partial + H::part_at((int64_t)tile * a.grid.splits, wave, i, j, q);
-    i32x4 sum = {};
-#pragma unroll 8
-    for (uint32_t p = 0; p < a.grid.splits; ++p)
-        sum += *reinterpret_cast<const i32x4*>(from + (int64_t)p * (kTile * kTile));
+    const i32x4 sum = sum_of_parts<T, i32x4>(from, (int)a.grid.splits);
     const int r = piece.m * kTile + wave / T::kAcross * 16 * T::kI + 4 * H::quad(i, q);
     const int t = piece.n * kTile + wave % T::kAcross * 16 * T::kJ + H::column(j);
     if (r >= a.rows || t >= a.tokens) return;
@@ -699,18 +696,18 @@ __global__ __launch_bounds__(64) void linear_sum_kernel(LinearArgs a)
 template <typename T, int kRing, int kPackedRing, typename Out>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
-    const dim3 grid(a.grid.blocks()), block(T::kThreads), sums(a.grid.rest() * T::kI * T::kJ * T::kWaves);
+    const dim3 grid(a.grid.blocks()), block(T::kThreads), sums(a.grid.rest() * T::kI * T::kJ * T::kWaves / 4);
     constexpr int kPackedLds = packed_lds<T::kTile, kPackedRing>() + Scales<T>::kBytes;
     if (a.meta) {
         hipLaunchKernelGGL((linear_packed_kernel<T, kPackedRing, Out>), grid, block, kPackedLds,
                            stream, a);
         if (sums.x > 0)
-            hipLaunchKernelGGL((linear_sum_kernel<T, 32, Out>), sums, dim3(64), 0, stream, a);
+            hipLaunchKernelGGL((linear_sum_kernel<T, 32, Out>), sums, dim3(256), 0, stream, a);
     } else {
         hipLaunchKernelGGL((linear_tile_kernel<T, kRing, Out>), grid, block,
                            kRing * 2 * T::kTile * kRowBytes + Scales<T>::kBytes, stream, a);
         if (sums.x > 0)
-            hipLaunchKernelGGL((linear_sum_kernel<T, 16, Out>), sums, dim3(64), 0, stream, a);
+            hipLaunchKernelGGL((linear_sum_kernel<T, 16, Out>), sums, dim3(256), 0, stream, a);
     }
 }
 

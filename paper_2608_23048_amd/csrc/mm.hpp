@@ -198,6 +198,32 @@ struct Held {
     }
 };
 
+// The sum of a lane's quad over the parts of a tile, in their order; `from` is its
+// place in the first.  Four (eight where there are more) are on their way at a
+// time, past the last that one again.
+template <typename T, int kAtATime, typename Quad4, typename Value>
+__device__ __forceinline__ Quad4 sum_batches(const Value* from, int splits)
+{
+    Quad4 sum = {};
+    for (int p = 0; p < splits; p += kAtATime) {
+        Quad4 v[kAtATime];
+#pragma unroll
+        for (int e = 0; e < kAtATime; ++e)
+            v[e] = *reinterpret_cast<const Quad4*>(
+                from + (int64_t)least(p + e, splits - 1) * (T::kTile * T::kTile));
+#pragma unroll
+        for (int e = 0; e < kAtATime; ++e)
+            if (p + e < splits) sum += v[e];
+    }
+    return sum;
+}
+template <typename T, typename Quad4, typename Value>
+__device__ __forceinline__ Quad4 sum_of_parts(const Value* from, int splits)
+{
+    return splits <= 4 ? sum_batches<T, 4, Quad4>(from, splits)
+                       : sum_batches<T, 8, Quad4>(from, splits);
+}
+
 // Results of a wave to memory, by way of its own part of LDS: a lane holds four
 // consecutive columns, and 16 lanes 16 different rows, so stored as they are
 // they would be 32-byte pieces; past LDS a wave stores whole rows.  kBytes: of
