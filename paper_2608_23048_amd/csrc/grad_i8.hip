@@ -167,12 +167,13 @@ struct QTile {
         const uint8_t* p = base + (int64_t)k0 * cols;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            // a row past the end is the last again, times a scale of zero
+            // a row past the sum's last is the last again, times a scale of zero; from
+            // a step past the sum's end nothing is read (row below 0)
             const int row = least(8 * oct() + j, K - k0 - 1);
-            if constexpr (kWhole && kOneOct)
-                v[j] = __builtin_amdgcn_raw_buffer_load_b32(
-                    buffer_at(p), left > 0 ? 4 * group() : kNowhere, row * (int)cols, 0);
-            else if constexpr (kWhole)
+            if constexpr (kWhole && kOneOct) {
+                const LoadAt at = row_load(8 * oct() + j, K - k0, 4 * group(), left > 0, cols);
+                v[j] = __builtin_amdgcn_raw_buffer_load_b32(buffer_at(p), at.lane, at.wave, 0);
+            } else if constexpr (kWhole)
                 v[j] = __builtin_amdgcn_raw_buffer_load_b32(
                     buffer_at(p), left > 0 && row >= 0 ? row * cols + 4 * group() : kNowhere, 0, 0);
             else

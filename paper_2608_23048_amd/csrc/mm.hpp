@@ -13,6 +13,7 @@
 #include <stdint.h>
 
 #include "common.hpp"
+#include "reach.hpp"
 #include "rows.hpp"
 
 namespace roi {
@@ -43,9 +44,6 @@ struct Tile {
 // Keeps the compiler from moving instructions across: the loops below are laid
 // out by hand.
 __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
-
-// A byte offset that no buffer below reaches: a load from there gives zeros.
-constexpr uint32_t kNowhere = 0x80000000u;
 
 // The buffer that starts at p.  Its size is the largest that offsets below
 // kNowhere use; every other offset is checked by the kernels themselves.
