@@ -294,6 +294,10 @@ int roi_cat_mask_bwd(const uint16_t* grad_W_masked, const uint16_t* W, const flo
  *    *_workspace call returns (it may be NULL where that is 0), 16-byte
  *    aligned, overlapping nothing; its contents need no preparation and are
  *    undefined afterwards.  Calls that may run at the same time need one each.
+ *    For sizes that the call refuses the *_workspace call returns the same
+ *    negative roi_status.
+ *  - A product or gradient of more than about 2^39 results in tiles of 256 x 256
+ *    (more blocks than a launch takes) is refused with ROI_E_UNSUPPORTED.
  *  - Results do not depend on the order in which blocks run: the same inputs
  *    give the same bits.
  */

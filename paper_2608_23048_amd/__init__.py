@@ -488,8 +488,8 @@ def _workspace(given, need, like):
     if given is None:
         if need > 0:
             return like.new_empty(need, dtype=_torch.uint8), need
-        if need < 0:
-            _raise_on(ROI_E_UNSUPPORTED)
+        if need < 0:  # a status: why the call is refused
+            _raise_on(need)
         return None, 0
     _check_tensor(given, _torch.uint8, "workspace")
     if given.get_device() != like.get_device():
@@ -601,8 +601,8 @@ def linear_i8_workspace(tokens: int, rows: int, cols: int, packed: bool = False)
 
 
 def _workspace_bytes(n):
-    if n < 0:
-        _raise_on(ROI_E_INVAL)
+    if n < 0:  # a status
+        _raise_on(n)
     return int(n)
 
 

@@ -324,6 +324,16 @@ int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols)
     return ROI_OK;
 }
 
+int check_linear_sum(int64_t cols, bool packed)
+{
+    if (cols > kMaxI8Sum)
+        return fail(ROI_E_UNSUPPORTED, "cols (%lld) must be at most %lld for an exact int32 sum",
+                    (long long)cols, (long long)kMaxI8Sum);
+    if (packed && cols % 32 != 0)
+        return fail(ROI_E_INVAL, "2:4 weights need cols %% 32 == 0 (got %lld)", (long long)cols);
+    return ROI_OK;
+}
+
 namespace {
 
 constexpr int64_t kMostSplits = 64;
@@ -471,11 +481,7 @@ int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, cons
     *todo = false;
     if (int st = check_dtype(dtype)) return st;
     if (int st = check_linear_sizes(tokens, rows, cols)) return st;
-    if (cols > kMaxI8Sum)
-        return fail(ROI_E_UNSUPPORTED, "cols (%lld) must be at most %lld for an exact int32 sum",
-                    (long long)cols, (long long)kMaxI8Sum);
-    if (meta && cols % 32 != 0)
-        return fail(ROI_E_INVAL, "2:4 weights need cols %% 32 == 0 (got %lld)", (long long)cols);
+    if (int st = check_linear_sum(cols, meta != nullptr)) return st;
     if (int st = check_workspace(workspace, workspace_bytes, need)) return st;
     const size_t t = (size_t)tokens, r = (size_t)rows, c = (size_t)cols;
     const Buffer b[] = {{xq, t * c, false},

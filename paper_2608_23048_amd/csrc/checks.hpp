@@ -165,6 +165,8 @@ GradPlan plan_grad(int64_t m, int64_t n, int64_t k, bool sum_rows);
 
 // Sizes of a linear call: ROI_OK, or why the call is refused.
 int check_linear_sizes(int64_t tokens, int64_t rows, int64_t cols);
+// What a product asks of its sum beside (packed: 2:4 weights).
+int check_linear_sum(int64_t cols, bool packed);
 int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uint32_t* meta,
                        const float* ws, const uint16_t* bias, int64_t tokens, int64_t rows,
                        int64_t cols, const void* y, int dtype, const void* workspace,

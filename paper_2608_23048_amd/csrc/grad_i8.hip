@@ -643,11 +643,27 @@ void launch_ready(const GradArgs& a, hipStream_t stream)
     launch_sums<Tile<256>>(a, stream);
 }
 
+int check_fits(const GradPlan& plan)
+{
+    return plan.cut.fits ? ROI_OK
+                         : fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
+}
+
+// Bytes of a gradient's workspace, or why it is refused.
+int64_t workspace_of(int64_t tokens, int64_t rows, int64_t cols, bool by_tokens)
+{
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    const GradPlan plan = by_tokens ? plan_grad(rows, cols, tokens, true)
+                                    : plan_grad(tokens, cols, rows, false);
+    if (int st = check_fits(plan)) return st;
+    ok();
+    return plan.bytes;
+}
+
 template <bool kSumRows>
 int launch(GradArgs a, const GradPlan& plan, void* workspace, const char* what, hipStream_t stream)
 {
-    if (!plan.cut.fits)
-        return fail(ROI_E_UNSUPPORTED, "the gradient has too many elements for one call");
+    if (int st = check_fits(plan)) return st;
     uint8_t* at = static_cast<uint8_t*>(workspace);
     uint8_t* const dy = at;
     uint8_t* const q = dy + plan.dy_bytes;
@@ -681,16 +697,12 @@ using namespace roi;
 
 extern "C" int64_t roi_linear_i8_grad_weight_workspace(int64_t tokens, int64_t rows, int64_t cols)
 {
-    if (check_linear_sizes(tokens, rows, cols)) return -1;
-    ok();
-    return plan_grad(rows, cols, tokens, true).bytes;
+    return workspace_of(tokens, rows, cols, true);
 }
 
 extern "C" int64_t roi_linear_i8_grad_input_workspace(int64_t tokens, int64_t rows, int64_t cols)
 {
-    if (check_linear_sizes(tokens, rows, cols)) return -1;
-    ok();
-    return plan_grad(tokens, cols, rows, false).bytes;
+    return workspace_of(tokens, rows, cols, false);
 }
 
 extern "C" int roi_linear_i8_grad_weight(const uint16_t* grad_y, const int8_t* xq, const float* xs,

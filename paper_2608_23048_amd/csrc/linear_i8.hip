@@ -749,13 +749,19 @@ int launch_few(const LinearArgs& a, hipStream_t stream)
                 : launch_few_as<4, 1, 8, 3, kPacked, Out>(a, stream);
 }
 
+int check_fits(const LinearPlan& plan)
+{
+    return plan.few || plan.cut.fits ? ROI_OK
+                                     : fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
+}
+
 template <typename Out>
 int launch(LinearArgs a, const LinearPlan& plan, void* workspace, hipStream_t stream)
 {
     if (plan.few)
         return a.meta ? launch_few<true, Out>(a, stream) : launch_few<false, Out>(a, stream);
+    if (int st = check_fits(plan)) return st;
     const Cut& c = plan.cut;
-    if (!c.fits) return fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
     uint8_t* at = static_cast<uint8_t*>(workspace);
     if (plan.x_bytes) {
         uint8_t* const x = at;
@@ -785,9 +791,11 @@ using namespace roi;
 
 extern "C" int64_t roi_linear_i8_workspace(int64_t tokens, int64_t rows, int64_t cols, int packed)
 {
-    if (check_linear_sizes(tokens, rows, cols)) return -1;
-    ok();
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    if (int st = check_linear_sum(cols, packed != 0)) return st;
     const LinearPlan plan = plan_linear(tokens, rows, cols, packed != 0);
+    if (int st = check_fits(plan)) return st;
+    ok();
     return plan.few ? 0 : plan.bytes;
 }
 

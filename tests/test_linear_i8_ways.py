@@ -175,3 +175,51 @@ def test_exported_layer_at_many_tokens(tokens):
     b = torch.randn(rows, device="cuda").bfloat16()
     assert torch.equal(roi.linear_i8(xq, xs, dq, ds, bias=b),
                        roi.linear_i8(xq, xs, pq, ps, meta=meta, bias=b))
+
+
+# ------------------------------------------------------------------ workspaces
+MOST_TOKENS, MOST = (1 << 30) - 1, (1 << 22) - 1
+
+
+@pytest.mark.parametrize("tokens,rows,cols,packed,status", [
+    (40, 8, 131072, 0, roi.ROI_E_UNSUPPORTED),   # a sum that may pass 32 bits
+    (1100, 8, 131104, 1, roi.ROI_E_UNSUPPORTED),
+    (0, 0, 131072, 0, roi.ROI_E_UNSUPPORTED),
+    (40, 8, 48, 1, roi.ROI_E_INVAL),             # 2:4 rows end within a metadata word
+    (MOST_TOKENS, MOST, 64, 0, roi.ROI_E_UNSUPPORTED),  # more blocks than a launch
+    (-1, 8, 64, 0, roi.ROI_E_INVAL), (1 << 30, 8, 64, 0, roi.ROI_E_UNSUPPORTED),
+])
+def test_workspace_refuses_what_the_product_refuses(tokens, rows, cols, packed, status):
+    L = roi.lib()
+    assert L.roi_linear_i8_workspace(tokens, rows, cols, packed) == status
+    assert L.roi_last_error()
+    with pytest.raises(roi.RoiError) as e:
+        roi.linear_i8_workspace(tokens, rows, cols, bool(packed))
+    assert e.value.status == status
+
+
+@pytest.mark.parametrize("name", ["linear_i8_grad_weight", "linear_i8_grad_input"])
+def test_workspace_refuses_what_the_gradients_refuse(name):
+    L = roi.lib()
+    fn = getattr(L, f"roi_{name}_workspace")
+    sizes = (64, MOST, MOST) if name.endswith("weight") else (MOST_TOKENS, 64, MOST)
+    assert fn(*sizes) == roi.ROI_E_UNSUPPORTED and L.roi_last_error()
+    assert fn(64, 1 << 22, 64) == roi.ROI_E_UNSUPPORTED
+    assert fn(64, -1, 64) == roi.ROI_E_INVAL
+    with pytest.raises(roi.RoiError, match="too many elements"):
+        getattr(roi, name + "_workspace")(*sizes)
+    assert fn(64, 64, 64) >= 0 and not L.roi_last_error()
+
+
+@gpu
+def test_refused_product_allocates_nothing():
+    import torch
+    q = torch.zeros(3000, 131073, dtype=torch.int8, device="cuda")
+    s = torch.ones(3000, device="cuda")
+    out = torch.empty(3000, 3000, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.reset_peak_memory_stats()
+    held = torch.cuda.memory_allocated()
+    with pytest.raises(roi.RoiError, match="exact int32 sum") as e:
+        roi.linear_i8(q, s, q, s, out=out)
+    assert e.value.status == roi.ROI_E_UNSUPPORTED
+    assert torch.cuda.max_memory_allocated() == held
