@@ -290,6 +290,9 @@ int roi_cat_mask_bwd(const uint16_t* grad_W_masked, const uint16_t* W, const flo
  *    with rows and cols below 2^22 and tokens below 2^30.  Operands whose rows
  *    are no multiple of 16 bytes cost a copy to the workspace, or slower loads.
  *  - An empty tensor's pointer may be NULL.  A sum over nothing is 0.
+ *  - The scales that the product and the gradients read (xs, ws) need only the
+ *    4-byte alignment of a float, so that a batch may be cut at any token whose
+ *    int8 row is 16-byte aligned.
  *  - workspace: device memory of at least the bytes that the matching
  *    *_workspace call returns (it may be NULL where that is 0), 16-byte
  *    aligned, overlapping nothing; its contents need no preparation and are

@@ -258,7 +258,12 @@ struct Buffer {
     const void* p;
     size_t n;
     bool out;
+    unsigned align = 16;
 };
+
+// The products and gradients read scales one by one: those of a batch cut at any
+// token serve.
+constexpr unsigned kScaleAlign = 4;
 
 // Present, aligned, and no output over anything else (an empty buffer's
 // pointer is not looked at).
@@ -267,7 +272,9 @@ int check_buffers(const Buffer* b, int count)
     for (int i = 0; i < count; ++i) {
         if (b[i].n == 0) continue;
         if (!b[i].p) return fail(ROI_E_INVAL, "a required pointer is NULL");
-        if (!aligned16(b[i].p)) return fail(ROI_E_INVAL, "device pointers must be 16-byte aligned");
+        if ((uintptr_t)b[i].p % b[i].align)
+            return fail(ROI_E_INVAL, "device pointers must be 16-byte aligned%s",
+                        b[i].align < 16 ? " (scales: to their 4 bytes)" : "");
     }
     for (int i = 0; i < count; ++i)
         for (int j = i + 1; j < count; ++j)
@@ -485,10 +492,10 @@ int validate_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, cons
     if (int st = check_workspace(workspace, workspace_bytes, need)) return st;
     const size_t t = (size_t)tokens, r = (size_t)rows, c = (size_t)cols;
     const Buffer b[] = {{xq, t * c, false},
-                        {xs, t * 4, false},
+                        {xs, t * 4, false, kScaleAlign},
                         {wq, meta ? r * (c / 2) : r * c, false},
                         {meta, meta ? r * (c / 32) * 4 : 0, false},
-                        {ws, r * 4, false},
+                        {ws, r * 4, false, kScaleAlign},
                         {bias, bias ? r * 2 : 0, false},
                         {y, t * r * (dtype == ROI_FP32 ? 4 : 2), true},
                         {workspace, (size_t)need, true}};
@@ -508,7 +515,7 @@ int validate_grad_i8(const uint16_t* grad_y, const int8_t* q, const float* scale
     const size_t c = (size_t)cols;
     const Buffer b[] = {{grad_y, (size_t)tokens * (size_t)rows * 2, false},
                         {q, (size_t)krows * c, false},
-                        {scale, (size_t)krows * 4, false},
+                        {scale, (size_t)krows * 4, false, kScaleAlign},
                         {out, (size_t)out_rows * c * 2, true},
                         {workspace, (size_t)need, true}};
     if (int st = check_buffers(b, 5)) return st;

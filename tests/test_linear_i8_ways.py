@@ -223,3 +223,43 @@ def test_refused_product_allocates_nothing():
         roi.linear_i8(q, s, q, s, out=out)
     assert e.value.status == roi.ROI_E_UNSUPPORTED
     assert torch.cuda.max_memory_allocated() == held
+
+
+# ------------------------------------------------------------------ alignments
+def test_alignments_that_calls_take(tmp_path):
+    pytest.importorskip("tests.test_sanitizers")
+    from tests.test_sanitizers import HERE, SAN, build_and_run
+    gxx = shutil.which("g++")
+    if not gxx or not os.path.exists("/opt/rocm/include/hip/hip_runtime_api.h"):
+        pytest.skip("g++ or the HIP headers not available")
+    exe = tmp_path / "linear_align_driver"
+    out = build_and_run([gxx, "-std=c++17", *SAN, "-Wall", "-Wextra", "-Werror",
+                         "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                         f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}",
+                         os.path.join(CSRC, "checks.cpp"),
+                         os.path.join(HERE, "linear_align_driver.cpp"), "-o", str(exe)], exe,
+                        tmp_path)
+    assert "linear alignments ok" in out
+
+
+@gpu
+@pytest.mark.parametrize("cut", [333, 1102, 5])
+def test_batch_cut_at_any_token(cut):
+    """Rows from any token on, through the product at few and many tokens, and both
+    gradients: as of copies of them, whose scales start at 16 bytes."""
+    import torch
+    tokens, rows, cols = 2300, 264, 144
+    xq, xs = roi.quantize_rows(torch.randn(tokens, cols, device="cuda"))
+    wq, ws = roi.quantize_rows(torch.randn(rows + cut, cols, device="cuda"))
+    gy = torch.randn(tokens, rows, device="cuda").bfloat16()
+    assert xs[cut:].data_ptr() % 16 and ws[cut:].data_ptr() % 16
+    parts = (xq[cut:], xs[cut:], wq[cut:], ws[cut:])
+    whole = [p.clone() for p in parts]
+    for count in (tokens - cut, 70, 9):
+        few = [parts[0][:count], parts[1][:count], *parts[2:]]
+        assert torch.equal(roi.linear_i8(*few),
+                           roi.linear_i8(whole[0][:count], whole[1][:count], *whole[2:]))
+    assert torch.equal(roi.linear_i8_grad_weight(gy[cut:], *parts[:2]),
+                       roi.linear_i8_grad_weight(gy[cut:], *whole[:2]))
+    assert torch.equal(roi.linear_i8_grad_input(gy, *parts[2:]),
+                       roi.linear_i8_grad_input(gy, *whole[2:]))
