@@ -284,18 +284,18 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
 // POP/s, with the matrix cores busy for 66 % of the time at 1.8 GHz; a tile's first
 // loads and its results are a quarter of its 28 steps' time.
 
-// Rows row0 .. of an operand of `n` rows of `len` bytes, kBytes of each, that
+// Rows row0 .. of an operand of `n` rows of `len` bytes, kRowBytes of each, that
 // this thread brings to LDS, where place j ^ spread(row) of a row holds its chunk
 // j.  A 16-byte LDS read goes by 16 lanes at a time, which are, of the wave's
 // first half, 0-3, 12-15, 20-23 and 24-27, then the others; the spreads give any
 // such 16 lanes all the banks when 16 consecutive lanes (kBlock 16) or 32 read
 // the same chunk of as many rows.  Their lengths are multiples of 16 bytes.
-template <typename T, int kBytes, int kBlock>
+template <typename T, int kBlock>
 struct Rows {
     static constexpr int kThreads = T::kThreads;
-    static constexpr int kLoads = T::kTile * kBytes / (16 * kThreads);
-    static constexpr int kChunks = kBytes / 16;
-    static_assert(kBlock == 32 || kChunks == 8, "the spreads below");
+    static constexpr int kLoads = T::kTile * kRowBytes / (16 * kThreads);
+    static constexpr int kChunks = kRowBytes / 16;
+    static_assert(kChunks == 8, "the spreads below");
     const uint8_t* base;
     int left, len; // rows from row0 on, and their bytes
     uint32_t at;   // byte offset of load 0 from base
@@ -307,7 +307,7 @@ struct Rows {
     }
     __device__ __forceinline__ static int spread(int row)
     {
-        return kBlock == 16 ? row & 7 : kChunks == 8 ? (row >> 1) & 7 : (row >> 2) & 3;
+        return kBlock == 16 ? row & 7 : (row >> 1) & 7;
     }
     // Row and chunk of this thread's load i (the chunk is the same for all: the
     // rows differ by a multiple of sixteen).
@@ -316,7 +316,7 @@ struct Rows {
         return (i * kThreads + (int)threadIdx.x) / kChunks;
     }
     __device__ __forceinline__ static int chunk() { return (threadIdx.x % kChunks) ^ spread(row(0)); }
-    // Load i of bytes k .. k + kBytes - 1 of the rows; zeros past the end.
+    // Load i of bytes k .. k + kRowBytes - 1 of the rows; zeros past the end.
     __device__ __forceinline__ void stage(int i, int k, ROI_LDS uint8_t* dst) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_tile_kernel(LinearArgs 
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x4 acc[kI][kJ] = {};
-    using R = Rows<T, kRowBytes, 16>;
+    using R = Rows<T, 16>;
     const R wrows(a.w, r0, a.rows, a.cols), xrows(a.x, t0, a.tokens, a.cols);
     constexpr int kLoads = R::kLoads;
     auto buffer = [&](int s) { return base + (s & (kRing - 1)) * 2 * kTileBytes; };
@@ -550,7 +550,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_packed_kernel(LinearArg
     const int r0 = piece.m * kTile, t0 = piece.n * kTile;
 
     i32x16 acc[kI][kJ] = {};
-    using R = Rows<T, 128, 32>;
+    using R = Rows<T, 32>;
     const R wrows(a.w, r0, a.rows, a.cols / 2), xrows(a.x, t0, a.tokens, a.cols);
     // metadata: a word a lane, eight words a row, word j at place j ^ (row / 4 & 7),
     // so that the words that 32 lanes read lie in the 32 banks of a 4-byte read
