@@ -312,6 +312,8 @@ typedef enum { ROI_BF16 = 0, ROI_FP32 = 1 } roi_dtype;
  *   amax = max_c |x[c]|, scale = max(fl(amax / 127), 2^-126),
  *   inv  = fl(127 fl(1 / amax)), or 2^126 where scale is 2^-126,
  *   q[c] = rint(fl(x[c] inv))            (ties to even; -127 .. 127).
+ * inv is 127 / amax to within 2^-23 of it (2^-21 for amax above 2^126, whose
+ * reciprocal is subnormal), so x inv is within 2^-14 of a step of x / scale.
  * A row of zeros gets q = 0.  A row that holds a NaN or an infinity gets
  * q = 0 and scale = NaN, so that everything computed from that row is NaN.
  *  x     bf16 or fp32 [rows, cols] (read; dtype says which)
@@ -331,8 +333,10 @@ int roi_dequantize_rows(const int8_t* q, const float* scale, int64_t rows, int64
 /*
  * roi_linear_i8 -- y[t, r] = xs[t] ws[r] sum_c xq[t, c] wq[r, c] (+ bias[r]).
  * The sum is exact in int32 (cols <= 131071, so that no int8 values can
- * overflow it); then fl(fl(sum ws) xs), the bias added, in fp32, and one
- * rounding to y's type.
+ * overflow it); then fl(fl(fl(sum) ws) xs), the bias added, in fp32, and one
+ * rounding to y's type.  fl(sum) is exact up to 2^24.  Where |sum| ws passes the
+ * largest fp32 value, y is infinite, also if xs would bring it back; with ws
+ * below 2^97 (weights below 2e31) no sum does that.
  *  xq    int8 [tokens, cols], xs fp32 [tokens]  (roi_quantize_rows)
  *  wq    int8 [rows, cols], or with meta int8 [rows, cols / 2]: the two kept
  *        values of every group of four in increasing index order (the rows of
@@ -354,8 +358,8 @@ int roi_linear_i8(const int8_t* xq, const float* xs, const int8_t* wq, const uin
  * roi_linear_i8_grad_weight: grad_w[r, c] = sum_t grad_y[t, r] xs[t] xq[t, c],
  * the dL/dW_masked that roi_mask_bwd takes, from the checkpoint (xq, xs).
  * roi_linear_i8_grad_input:  grad_x[t, c] = sum_r grad_y[t, r] ws[r] wq[r, c]
- * (wq dense).  The scaled int8 operand is rounded once to bf16 (the type of
- * the other operand and of the result, and what the bf16 matrix cores take);
+ * (wq dense).  The scaled int8 operand is rounded once to bf16 (the value that
+ * roi_dequantize_rows gives in bf16, and what the bf16 matrix cores take);
  * products and sums are fp32, and the result is rounded to bf16.
  *  grad_y bf16 [tokens, rows] (read)
  *  grad_w bf16 [rows, cols], grad_x bf16 [tokens, cols] (overwritten)

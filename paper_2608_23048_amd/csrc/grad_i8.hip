@@ -5,9 +5,13 @@
 // scale a row, and dy bf16 with its sum index k in rows (the weight gradient:
 // dy is [K, D]) or contiguous (the input gradient: dy is [D, K]).
 //
-// s q is formed in fp32 and rounded once to bf16 on its way to LDS (the other
-// operand and the result are bf16, and so are the matrix instructions); the
-// products and sums are fp32.  The int8 operand is the matrix instruction's
+// s q is formed in fp32 and rounded once to bf16 on its way to LDS (the value that
+// dequantize_rows gives in bf16; the other operand and the result are bf16, and so
+// are the matrix instructions); the products and sums are fp32.  With that rounding
+// the gradients are off from 64 bits by 0.0023 in norm, without it, by the result's
+// own, 0.0017.  q by itself is exact in bf16, but s goes with the summed index and
+// stays in the sum; s q in two bf16 terms would be twice the matrix instructions,
+// which bound the large gradients.  The int8 operand is the matrix instruction's
 // first, so that a lane of the result holds four consecutive c of one d: a
 // vector store.  Layouts, as measured on gfx950 (lane l, g = l / 16):
 //   v_mfma_f32_16x16x32_bf16: operand row l % 16, sum indices 8 g .. 8 g + 7;
@@ -245,9 +249,13 @@ __device__ __forceinline__ void write_tile(const GradArgs& a, const Piece& piece
 
 // As in linear_i8.hip, a half step's products stand beside the reads of the
 // next, with one barrier a step.  LDS holds the int8 operand's bf16 tiles of two
-// steps and dy's of three: what is loaded to LDS in one step is awaited two
-// steps later.  The int8 tile of step s + 3 goes to registers in step s and to
-// LDS, scaled, in step s + 1.
+// steps and dy's of three.  The int8 tile of step s + 3 goes to registers in step s
+// and to LDS, scaled, in step s + 1.  dy's tile of step s + 3 is loaded to LDS in step
+// s behind it.  In the input gradient it is awaited two steps later.  In the weight
+// gradient it has until step s + 1 writes the int8 tile: its loads are in assembly,
+// where the compiler does not count them, so that the waits it puts ahead of the int8
+// registers' use are for dy's later loads too.  (2048 x 3584 x 3584 input gradient 56
+// us without the sums of its parts, 2100 x 1032 x 4096 weight gradient 32.)
 template <int kTile, bool kSumRows>
 __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void grad_tile_kernel(GradArgs a)
 {
@@ -343,9 +351,10 @@ __global__ __launch_bounds__(Tile<kTile>::kThreads, 2) void grad_tile_kernel(Gra
 // The same for both operands in bf16 (a.ready): nothing passes registers on its
 // way to LDS, which holds both tiles of two steps.  A step takes 1.4 us where the
 // conversion beside it takes 1.7; the conversion by itself is one pass over q (17
-// to 35 us of the 880 that either gradient takes at 8192 x 3584 x 18944).  Bound by
+// to 35 us of the 870 that either gradient takes at 8192 x 3584 x 18944).  Bound by
 // the matrix cores and their clock: busy for 73 % of the time, at 1.8 GHz under
-// that load, 1.33 PFLOP/s where the library's 8192^3 product reaches 1.30.
+// that load, 1.33 PFLOP/s where the library's 8192^3 product reaches 1.30 (1.28 to
+// 1.32 in the median of passes back to back, as the clock falls).
 template <bool kSumRows>
 __global__ __launch_bounds__(Tile<256>::kThreads) void grad_ready_kernel(GradArgs a)
 {

@@ -51,8 +51,10 @@ __device__ __forceinline__ void row_scales(const LinearArgs& a, int r, f32x4& ws
     }
 }
 
-// Four results from their exact sums.  The scale of the weight comes first: sum
-// ws stays far from overflow for any weight.
+// Four results from their exact sums, which are rounded to fp32 first (exact there
+// up to 2^24).  The scale of the weight comes first: sums are below 2^31, so with ws
+// below 2^97 (weights below 2e31) sum ws is finite; past that it can be an infinity,
+// and so can the result, also where xs would bring it back.
 __device__ __forceinline__ f32x4 finish4(i32x4 sum, f32x4 ws, f32x4 add, float xs)
 {
     f32x4 v;
@@ -280,8 +282,9 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(LinearArgs a)
 // buffer, loading for kRing - 1 steps, is complete.  256-tiles, and two 128-tiles
 // on a compute unit, have LDS for two; a 128-tile that has a compute unit to
 // itself takes four, and eight waves: 512 tokens through 3584 x 3584 take 16.1 us
-// so and 21.3 with two and four.  8192 tokens through 18944 x 3584: 442 us, 2.5
-// POP/s, with the matrix cores busy for 66 % of the time at 1.8 GHz; a tile's first
+// so and 21.3 with two and four.  8192 tokens through 18944 x 3584: 440 us in
+// single passes, 2.5 POP/s, with the matrix cores busy for 66 % of the time at 1.8
+// GHz (476 in the median of passes back to back, as the clock falls); a tile's first
 // loads and its results are a quarter of its 28 steps' time.
 
 // Rows row0 .. of an operand of `n` rows of `len` bytes, kRowBytes of each, that
