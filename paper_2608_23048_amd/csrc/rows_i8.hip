@@ -1,8 +1,8 @@
 // rows_i8.hip -- gfx950 kernels of the int8 rows: quantize_rows and
 // dequantize_rows.
 //
-// scale = max(fl(amax / 127), 2^-126), inv = fl(127 fl(1 / amax)) (2^126 at that
-// floor), q = rint(fl(x inv)): the two divisions are one per row and IEEE, the
+// scale = fl(amax / 127), at least 2^-126 and at most the largest whose 127-fold is
+// finite, inv = fl(127 fl(1 / amax)) (2^126 at that floor), q = rint(fl(x inv)): the two divisions are one per row and IEEE, the
 // per-element work is a product, a rounding and a pack.  Both kernels are bound
 // by HBM: 3 bytes an element from bf16 (5 from fp32), once each.  The row is
 // read once: it stays in the registers of the waves that own it between the
@@ -17,6 +17,9 @@ namespace roi {
 namespace {
 
 constexpr float kScaleFloor = 0x1p-126f;
+// The largest fp32 value whose 127-fold rounds to a finite one: fl(amax / 127) of
+// amax = FLT_MAX, the one row it is for, lies one step above.
+constexpr float kScaleTop = 0x1.020406p+121f;
 constexpr uint32_t kInfBits = 0x7F800000u;
 
 // Eight consecutive elements of a row, as loaded.
@@ -152,7 +155,9 @@ __global__ __launch_bounds__(kWaves > 4 ? 64 * kWaves : 256) void quantize_rows_
     const float s = amax / 127.0f;
     const bool low = !(s > kScaleFloor);
     const float inv = low ? 0x1p126f : 127.0f * (1.0f / amax);
-    if (lane == 0) scale[r] = finite ? (low ? kScaleFloor : s) : __uint_as_float(0x7FC00000u);
+    if (lane == 0)
+        scale[r] = finite ? (low ? kScaleFloor : s < kScaleTop ? s : kScaleTop)
+                          : __uint_as_float(0x7FC00000u);
     if constexpr (kChunks > 0) {
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {

@@ -263,3 +263,28 @@ def test_batch_cut_at_any_token(cut):
                        roi.linear_i8_grad_weight(gy[cut:], *whole[:2]))
     assert torch.equal(roi.linear_i8_grad_input(gy, *parts[2:]),
                        roi.linear_i8_grad_input(gy, *whole[2:]))
+
+
+# ------------------------------------------------------- the type's largest rows
+@gpu
+@pytest.mark.parametrize("cols", [1, 9, 1025, 8193, 20000, 40000])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_at_the_largest_values(cols, dtype):
+    """Rows that hold the type's lowest or largest value (a mask's, say) and their
+    neighbours come back finite, half a step off at most (q is within 2^-14 of a
+    step of x / scale, and the restored value is rounded once more)."""
+    import torch
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    top = torch.finfo(t).max
+    x = torch.randn(6, cols).to(t)
+    x[0, -1], x[1, 0], x[2, cols // 2] = torch.finfo(t).min, top, 2.0 ** 127
+    x[3] = top
+    x[4, 0] = top * (1 - torch.finfo(t).eps)
+    x[5] = torch.finfo(t).min
+    q, s = roi.quantize_rows(x.cuda())
+    back = roi.dequantize_rows(q, s, dtype=t)
+    assert torch.isfinite(s).all() and torch.isfinite(back).all()
+    want, got, step = x.double(), back.cpu().double(), s.cpu().double()[:, None]
+    off = (got - want).abs()
+    assert (off <= step * (0.5 + 2.0 ** -14) + got.abs() * torch.finfo(t).eps / 2).all()
+    assert (q[3] == 127).all() and (q[5] == -127).all()
