@@ -311,7 +311,7 @@ typedef enum { ROI_BF16 = 0, ROI_FP32 = 1 } roi_dtype;
  * sequence of IEEE fp32 operations, so that the integers are reproducible:
  *   amax = max_c |x[c]|,
  *   scale = min(max(fl(amax / 127), 2^-126), 0x1.020406p+121)  (the largest fp32
- *          value whose 127-fold is finite: amax = FLT_MAX alone reaches it),
+ *          value whose 127-fold is finite: only amax = FLT_MAX is cut to it),
  *   inv  = fl(127 fl(1 / amax)), or 2^126 where scale is 2^-126,
  *   q[c] = rint(fl(x[c] inv))            (ties to even; -127 .. 127).
  * inv is 127 / amax to within 2^-23 of it (2^-21 for amax above 2^126, whose

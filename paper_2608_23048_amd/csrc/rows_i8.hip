@@ -2,8 +2,9 @@
 // dequantize_rows.
 //
 // scale = fl(amax / 127), at least 2^-126 and at most the largest whose 127-fold is
-// finite, inv = fl(127 fl(1 / amax)) (2^126 at that floor), q = rint(fl(x inv)): the two divisions are one per row and IEEE, the
-// per-element work is a product, a rounding and a pack.  Both kernels are bound
+// finite, inv = fl(127 fl(1 / amax)) (2^126 at that floor), q = rint(fl(x inv)): the
+// two divisions are one per row and IEEE, the per-element work is a product, a
+// rounding and a pack.  Both kernels are bound
 // by HBM: 3 bytes an element from bf16 (5 from fp32), once each.  The row is
 // read once: it stays in the registers of the waves that own it between the
 // maximum and the rounding.
