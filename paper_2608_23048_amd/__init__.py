@@ -124,6 +124,20 @@ def lib() -> ctypes.CDLL:
             getattr(L, name + "_workspace").restype = _i64
             getattr(L, name).argtypes = [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp]
             getattr(L, name).restype = _int
+        L.roi_block_scales.argtypes = [_i64]
+        L.roi_block_scales.restype = _i64
+        L.roi_quantize_blocks.argtypes = [_vp, _int, _i64, _i64, _int, _int, _vp, _i64, _vp, _vp,
+                                          _i64, _vp, _vp]
+        L.roi_quantize_blocks.restype = _int
+        L.roi_dequantize_blocks.argtypes = [_vp, _i64, _vp, _i64, _i64, _int, _int, _vp, _int, _vp]
+        L.roi_dequantize_blocks.restype = _int
+        L.roi_linear_f8_workspace.argtypes = [_i64, _i64, _i64]
+        L.roi_linear_f8_workspace.restype = _i64
+        L.roi_linear_f8.argtypes = [_vp, _i64, _vp, _int, _vp, _i64, _vp, _int, _vp, _i64, _i64,
+                                    _i64, _vp, _vp, _i64, _vp]
+        L.roi_linear_f8.restype = _int
+        L.roi_adamw_grouped.argtypes = [_vp, _int, _int, _int, _u64, _u64, _vp, _vp]
+        L.roi_adamw_grouped.restype = _int
         L.roi_anneal.argtypes = [_f32, _f32, _i64, _i64]
         L.roi_anneal.restype = _f32
         L.roi_status_string.argtypes = [_int]
@@ -650,6 +664,305 @@ def linear_i8_grad_weight_workspace(tokens: int, rows: int, cols: int) -> int:
 def linear_i8_grad_input_workspace(tokens: int, rows: int, cols: int) -> int:
     """Bytes of linear_i8_grad_input's workspace."""
     return _workspace_bytes(lib().roi_linear_i8_grad_input_workspace(tokens, rows, cols))
+
+
+# ------------------------------------------- the training step in 8-bit floats
+ROI_E4M3, ROI_E5M2 = 0, 1
+
+
+def _format_code(dtype, name):
+    if dtype is _torch.float8_e4m3fn:
+        return ROI_E4M3
+    if dtype is _torch.float8_e5m2:
+        return ROI_E5M2
+    raise TypeError(f"{name} must be torch.float8_e4m3fn or torch.float8_e5m2, got {dtype}")
+
+
+def block_scales(cols: int) -> int:
+    """Scales kept for a row of ``cols`` values: one byte a block of 128, in whole words."""
+    return (cols + 511) // 512 * 4
+
+
+def _f8_new(like, rows, cols, dtype):
+    """[rows, cols] of 8-bit values whose rows start at multiples of 16 bytes."""
+    room = (cols + 15) // 16 * 16
+    t = like.new_empty(rows, room, dtype=dtype)
+    return t if room == cols else t[:, :cols]
+
+
+def _f8_stride(t, name):
+    """Bytes between the rows of a 2-D tensor of 8-bit values."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D, got {t.dim()}-D")
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if rows <= 1 or cols == 0:  # any stride says the same
+        stride = (cols + 15) // 16 * 16
+    if (step != 1 and cols > 1) or stride % 16 or stride < cols:
+        raise ValueError(f"{name} must have consecutive columns and rows that start at multiples "
+                         f"of 16 bytes (quantize_blocks lays them out so), got strides "
+                         f"{tuple(t.stride())}")
+    return stride
+
+
+def _check_scales(t, name, rows, cols, device):
+    """The scales of `rows` rows (of blocks) of `cols` values."""
+    _check_sized(t, _torch.float8_e8m0fnu, name, (rows, block_scales(cols)), device)
+
+
+def quantize_blocks(x, square: bool = False, transposed: bool = False, dtype=None, out=None):
+    """8-bit floats with one power-of-two scale for each block of 128 values.
+
+    x bf16 or fp32 [rows, cols] -> (q, scale): q in ``dtype`` (float8_e4m3fn, the
+    default, or float8_e5m2) [rows, cols], its rows at multiples of 16 bytes;
+    scale float8_e8m0fnu [rows, block_scales(cols)], scale[r, b] that of q[r, 128 b
+    : 128 b + 128].  square: blocks are 128 x 128 (a weight's), scale
+    [ceil(rows / 128), block_scales(cols)].  transposed: also (qt, scale_t) of the
+    transposed x, [cols, rows], with blocks along the rows of x; with square the
+    transposed q.  Tokens' rows are linear_f8's left operand, their transposed
+    copies (the checkpoint, and dL/dy's) its weight gradient's; a weight's square
+    blocks its right operand, and their transposed copy that of the input's
+    gradient.  A 1-D x is one row: q and scale are 1-D.  ``out``: what is returned,
+    preallocated."""
+    torch = _torch or _load_torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a torch.Tensor")
+    code = _dtype_code(x.dtype, "x")
+    if not (x.is_cuda and x.is_contiguous()):
+        _check_tensor(x, x.dtype, "x")
+    rows, cols = _rows_cols(x, "x")
+    flat = x.dim() == 1
+    if flat and transposed:
+        raise ValueError("a transposed copy is made of a 2-D x")
+    device = x.get_device()
+    above, below = ((rows + 127) // 128, (cols + 127) // 128) if square else (rows, cols)
+    qt = scale_t = None
+    if out is None:
+        dtype = torch.float8_e4m3fn if dtype is None else dtype
+        fmt = _format_code(dtype, "dtype")
+        q = x.new_empty(cols, dtype=dtype) if flat else _f8_new(x, rows, cols, dtype)
+        shape = (block_scales(cols),) if flat else (above, block_scales(cols))
+        scale = x.new_empty(shape, dtype=torch.float8_e8m0fnu)
+        if transposed:
+            qt = _f8_new(x, cols, rows, dtype)
+            scale_t = x.new_empty(below, block_scales(rows), dtype=torch.float8_e8m0fnu)
+        out = (q, scale, qt, scale_t) if transposed else (q, scale)
+        stride = (cols + 15) // 16 * 16
+        stride_t = (rows + 15) // 16 * 16
+    else:
+        q, scale = out[:2]
+        if len(out) != (4 if transposed else 2):
+            raise ValueError(f"out must hold {4 if transposed else 2} tensors, got {len(out)}")
+        fmt = _format_code(q.dtype, "q")
+        if dtype is not None and q.dtype is not dtype:
+            raise TypeError(f"q must be {dtype}, got {q.dtype}")
+
+        def check(q, scale, name, rows, cols, blocks):
+            if q.dtype is not out[0].dtype:
+                raise TypeError(f"{name} must be {out[0].dtype}, got {q.dtype}")
+            if q.shape != (rows, cols) or q.get_device() != device:
+                raise ValueError(f"{name} must have shape {(rows, cols)} on {x.device}, got "
+                                 f"{tuple(q.shape)} on {q.device}")
+            _check_scales(scale, "scale" + name[1:].replace("t", "_t"), blocks, cols, device)
+            return _f8_stride(q, name)
+
+        if flat:
+            _check_sized(q, q.dtype, "q", x.shape, device)
+            _check_sized(scale, torch.float8_e8m0fnu, "scale", (block_scales(cols),), device)
+            stride = (cols + 15) // 16 * 16
+        else:
+            stride = check(q, scale, "q", rows, cols, above)
+        stride_t = 0
+        if transposed:
+            qt, scale_t = out[2:]
+            stride_t = check(qt, scale_t, "qt", cols, rows, below)
+    _call(device, lib().roi_quantize_blocks, x.data_ptr(), code, rows, cols, square, fmt,
+          q.data_ptr(), stride, scale.data_ptr(), _ptr(qt), stride_t, _ptr(scale_t))
+    return out
+
+
+def dequantize_blocks(q, scale, dtype=None, out=None):
+    """x = q times its blocks' scales in ``dtype`` (bf16, the default, or fp32).
+    ``scale`` as quantize_blocks gives it: with a row for each row of q, or for each
+    128 (square blocks)."""
+    torch = _torch or _load_torch()
+    if not isinstance(q, torch.Tensor):
+        raise TypeError("q must be a torch.Tensor")
+    fmt = _format_code(q.dtype, "q")
+    flat = q.dim() == 1
+    square = False
+    device = q.get_device()
+    if flat:
+        _check_tensor(q, q.dtype, "q")
+        rows, cols = 1, q.shape[0]
+        stride = (cols + 15) // 16 * 16
+        _check_sized(scale, torch.float8_e8m0fnu, "scale", (block_scales(cols),), device)
+    else:
+        stride = _f8_stride(q, "q")
+        rows, cols = q.shape
+        square = _square_scales(scale, rows)
+        _check_scales(scale, "scale", (rows + 127) // 128 if square else rows, cols, device)
+    dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
+    code = _dtype_code(dtype)
+    if out is None:
+        out = q.new_empty(q.shape, dtype=dtype)
+    else:
+        _check_sized(out, dtype, "out", q.shape, device)
+    _call(device, lib().roi_dequantize_blocks, q.data_ptr(), stride, scale.data_ptr(), rows, cols,
+          square, fmt, out.data_ptr(), code)
+    return out
+
+
+def _square_scales(scale, rows):
+    """Whether scales are those of square blocks (with one row both are the same)."""
+    return (rows > 1 and isinstance(scale, _torch.Tensor) and scale.dim() == 2
+            and scale.shape[0] == (rows + 127) // 128)
+
+
+def linear_f8(xq, xs, wq, ws, bias=None, out=None, workspace=None):
+    """y[t, r] = sum_c x[t, c] w[r, c] (+ bias[r]) of operands in blocks, bf16.
+
+    xq [tokens, cols] (e4m3 or e5m2) with xs, quantize_blocks of the tokens' rows;
+    wq e4m3 [rows, cols] with ws, the scales of square blocks or of rows.  bias bf16
+    [rows].  ``workspace``: a uint8 tensor of linear_f8_workspace bytes."""
+    torch = _torch or _load_torch()
+    if not (isinstance(xq, torch.Tensor) and isinstance(wq, torch.Tensor)):
+        raise TypeError("xq and wq must be torch.Tensors")
+    fmt = _format_code(xq.dtype, "xq")
+    if wq.dtype is not torch.float8_e4m3fn:
+        raise TypeError(f"wq must be torch.float8_e4m3fn, got {wq.dtype}")
+    x_stride, w_stride = _f8_stride(xq, "xq"), _f8_stride(wq, "wq")
+    (tokens, cols), (rows, held), device = xq.shape, wq.shape, xq.get_device()
+    if held != cols:
+        raise ValueError(f"wq has {held} columns, expected {cols}")
+    if wq.get_device() != device:
+        raise ValueError(f"wq is on {wq.device}, expected device {device}")
+    square = _square_scales(ws, rows)
+    _check_scales(xs, "xs", tokens, cols, device)
+    _check_scales(ws, "ws", (rows + 127) // 128 if square else rows, cols, device)
+    if bias is not None:
+        _check_sized(bias, torch.bfloat16, "bias", (rows,), device)
+    if out is None:
+        out = xq.new_empty(tokens, rows, dtype=torch.bfloat16)
+    else:
+        _check_sized(out, torch.bfloat16, "out", (tokens, rows), device)
+    L = lib()
+    work, nbytes = _workspace(workspace, L.roi_linear_f8_workspace(tokens, rows, cols), xq)
+    _call(device, L.roi_linear_f8, xq.data_ptr(), x_stride, xs.data_ptr(), fmt, wq.data_ptr(),
+          w_stride, ws.data_ptr(), square, _ptr(bias), tokens, rows, cols, out.data_ptr(),
+          _ptr(work), nbytes)
+    return out
+
+
+def linear_f8_grad_input(gq, gs, wqt, wst, out=None, workspace=None):
+    """dL/dx (bf16 [tokens, cols]): sum_r dy[t, r] w[r, c], from quantize_blocks of
+    dL/dy (gq [tokens, rows], gs) and the weight's transposed copy (wqt [cols, rows],
+    wst)."""
+    return linear_f8(gq, gs, wqt, wst, None, out, workspace)
+
+
+def linear_f8_grad_weight(gqt, gst, xqt, xst, out=None, workspace=None):
+    """dL/dW (bf16 [rows, cols], mask_bwd's grad_W_masked): sum_t dy[t, r] x[t, c],
+    from the transposed copies of dL/dy (gqt [rows, tokens], gst) and of the forward's
+    x (xqt e4m3 [cols, tokens], xst)."""
+    return linear_f8(gqt, gst, xqt, xst, None, out, workspace)
+
+
+def linear_f8_workspace(tokens: int, rows: int, cols: int) -> int:
+    """Bytes of the workspace of linear_f8 with xq [tokens, cols] and wq [rows, cols]
+    (of the gradients: with the shapes of their operands)."""
+    return _workspace_bytes(lib().roi_linear_f8_workspace(tokens, rows, cols))
+
+
+def adamw_moments(param, bits: int = 8):
+    """The moments of a tensor before the first step: (exp_avg, exp_avg_sq) for
+    adamw_grouped, fp32 zeros like param (bits 32), or each (q float8_e4m3fn like
+    param, scale float8_e8m0fnu [block_scales(param.numel())]) (bits 8; exp_avg_sq
+    holds the root of the second moment)."""
+    torch = _torch or _load_torch()
+    if bits == 32:
+        return torch.zeros_like(param), torch.zeros_like(param)
+    if bits != 8:
+        raise ValueError(f"bits must be 8 or 32, got {bits}")
+
+    def zeros():
+        scale = torch.zeros(block_scales(param.numel()), dtype=torch.uint8, device=param.device)
+        q = torch.zeros(param.shape, dtype=torch.uint8, device=param.device)
+        return q.view(torch.float8_e4m3fn), scale.view(torch.float8_e8m0fnu)
+
+    return zeros(), zeros()
+
+
+class AdamWPlan:
+    """The checked tensors of adamw_grouped, kept for many steps (adamw_plan)."""
+
+    def __init__(self, tensors, offsets=None):
+        torch = _torch or _load_torch()
+        self.tensors = [tuple(t) for t in tensors]
+        self.count = len(self.tensors)
+        sizes = [p.numel() for p, *_ in self.tensors]
+        self.offsets = _offsets([(n + 3) // 4 * 4 for n in sizes], offsets)
+        self.bits, self.grad_code, self.device = 32, ROI_FP32, -1
+        fields = []
+        for i, ((param, grad, avg, sq), n, off) in enumerate(zip(self.tensors, sizes,
+                                                                 self.offsets)):
+            eight = isinstance(avg, (tuple, list))
+            if eight != isinstance(sq, (tuple, list)):
+                raise TypeError(f"tensor {i}: both moments are tensors, or both (q, scale)")
+            _check_tensor(param, torch.float32, "param")
+            if i == 0:
+                self.bits, self.device = 8 if eight else 32, param.get_device()
+                self.grad_code = _dtype_code(grad.dtype, "grad")
+            if (8 if eight else 32) != self.bits or _dtype_code(grad.dtype, "grad") != self.grad_code:
+                raise TypeError(f"tensor {i}: its moments or its gradient are of another type than "
+                                f"tensor 0's")
+            if param.get_device() != self.device:
+                raise ValueError(f"tensor {i} is on {param.device}, expected device {self.device}")
+            shape = param.shape
+            _check_sized(grad, grad.dtype, "grad", shape, self.device)
+            if eight:
+                for (q, s), name in ((avg, "exp_avg"), (sq, "exp_avg_sq")):
+                    _check_sized(q, torch.float8_e4m3fn, name, shape, self.device)
+                    _check_sized(s, torch.float8_e8m0fnu, name + "'s scale", (block_scales(n),),
+                                 self.device)
+                fields += (param.data_ptr(), grad.data_ptr(), avg[0].data_ptr(), sq[0].data_ptr(),
+                           avg[1].data_ptr(), sq[1].data_ptr(), n, off)
+            else:
+                _check_sized(avg, torch.float32, "exp_avg", shape, self.device)
+                _check_sized(sq, torch.float32, "exp_avg_sq", shape, self.device)
+                fields += (param.data_ptr(), grad.data_ptr(), avg.data_ptr(), sq.data_ptr(), 0, 0, n,
+                           off)
+        self.descriptors = _descriptors(fields)  # roi_step_tensor
+        self.address = ctypes.addressof(self.descriptors)
+
+
+def adamw_plan(tensors, offsets=None) -> AdamWPlan:
+    """Checks adamw_grouped's list of tensors once and keeps it: what a training loop
+    whose gradients stay in place passes to each step instead of the list."""
+    return AdamWPlan(tensors, offsets)
+
+
+def adamw_grouped(tensors, opt: AdamWParams, seed: int = 0, step: int = 0, offsets=None):
+    """One AdamW step over a list of (param, grad, exp_avg, exp_avg_sq), in place, in
+    one call; or over an adamw_plan of it.
+
+    param fp32; grad fp32 or bf16; the moments fp32, or each (q, scale) in 8 bits
+    (adamw_moments; about half the memory traffic and a quarter of the memory).  The
+    8-bit moments are rounded by the noise of (seed, step, offsets[i] + element):
+    use a seed of its own and the step's number; offsets are multiples of 4 and
+    default to the running sum of the sizes, each rounded up to one."""
+    if opt is None:
+        raise ValueError("opt (AdamWParams) is required")
+    plan = tensors
+    if type(plan) is not AdamWPlan:
+        plan = AdamWPlan(tensors, offsets)
+    elif offsets is not None:
+        raise ValueError("the plan has its offsets")
+    if plan.count:
+        _call(plan.device, lib().roi_adamw_grouped, plan.address, plan.count, plan.grad_code,
+              plan.bits, seed, step, ctypes.addressof(opt))
 
 
 def gumbel_noise(count: int, seed: int = 0, step: int = 0, elem_offset: int = 0, device="cuda",

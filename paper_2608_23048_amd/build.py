@@ -23,7 +23,8 @@ SOURCES = [os.path.join(CSRC, "roi.hip"), os.path.join(CSRC, "wide_fwd.hip"),
            os.path.join(CSRC, "wide_bwd.hip"),
            os.path.join(CSRC, "export.hip"), os.path.join(CSRC, "cat.hip"),
            os.path.join(CSRC, "rows_i8.hip"), os.path.join(CSRC, "linear_i8.hip"),
-           os.path.join(CSRC, "grad_i8.hip"),
+           os.path.join(CSRC, "grad_i8.hip"), os.path.join(CSRC, "blocks_f8.hip"),
+           os.path.join(CSRC, "linear_f8.hip"), os.path.join(CSRC, "adamw.hip"),
            os.path.join(CSRC, "stream_copy.hip"), os.path.join(CSRC, "checks.cpp")]
 ARCH = "gfx950"
 

@@ -523,4 +523,161 @@ int validate_grad_i8(const uint16_t* grad_y, const int8_t* q, const float* scale
     return ok();
 }
 
+namespace {
+
+constexpr int64_t scale_bytes(int64_t cols) { return (cols + 511) / 512 * 4; }
+
+// Rows of 8-bit values, `stride` bytes apart: the bytes from the first to the last.
+size_t f8_bytes(int64_t rows, int64_t cols, int64_t stride)
+{
+    return rows > 0 && cols > 0 ? (size_t)(rows - 1) * (size_t)stride + (size_t)cols : 0;
+}
+size_t f8_scales(int64_t rows, int64_t cols, bool square)
+{
+    return (size_t)(square ? (rows + 127) / 128 : rows) * (size_t)scale_bytes(cols);
+}
+
+int check_stride(const char* what, int64_t stride, int64_t cols, int64_t most)
+{
+    if (stride % 16 != 0 || stride < cols)
+        return fail(ROI_E_INVAL, "%s (%lld) must be a multiple of 16 and at least %lld", what,
+                    (long long)stride, (long long)cols);
+    if (stride > most)
+        return fail(ROI_E_UNSUPPORTED, "%s (%lld) must be at most %lld", what, (long long)stride,
+                    (long long)most);
+    return ROI_OK;
+}
+
+int check_format(int format)
+{
+    if (format != ROI_E4M3 && format != ROI_E5M2)
+        return fail(ROI_E_INVAL, "the format must be ROI_E4M3 or ROI_E5M2 (got %d)", format);
+    return ROI_OK;
+}
+
+int check_f8_sizes(int64_t rows, int64_t cols)
+{
+    if (rows < 0 || cols < 0)
+        return fail(ROI_E_INVAL, "rows (%lld) and cols (%lld) must be >= 0", (long long)rows,
+                    (long long)cols);
+    if (rows >= kMaxRowsI8 || cols >= kMaxRowsI8)
+        return fail(ROI_E_UNSUPPORTED, "rows and cols must be below 2^31");
+    return ROI_OK;
+}
+
+} // namespace
+
+int validate_quantize_f8(const void* x, int dtype, int64_t rows, int64_t cols, bool square, int format,
+                         const uint8_t* q, int64_t q_stride, const uint8_t* scale, const uint8_t* qt,
+                         int64_t qt_stride, const uint8_t* scale_t, bool* todo)
+{
+    *todo = false;
+    if (int st = check_dtype(dtype)) return st;
+    if (int st = check_format(format)) return st;
+    if (int st = check_f8_sizes(rows, cols)) return st;
+    if (int st = check_stride("q_stride", q_stride, cols, kMaxRowsI8)) return st;
+    if (!qt != !scale_t && rows > 0 && cols > 0)
+        return fail(ROI_E_INVAL, "qt and scale_t are given together or not at all");
+    if (qt)
+        if (int st = check_stride("qt_stride", qt_stride, rows, kMaxRowsI8)) return st;
+    const Buffer b[] = {{x, (size_t)rows * (size_t)cols * (dtype == ROI_FP32 ? 4 : 2), false},
+                        {q, f8_bytes(rows, cols, q_stride), true},
+                        {scale, f8_scales(rows, cols, square), true, kScaleAlign},
+                        {qt, qt ? f8_bytes(cols, rows, qt_stride) : 0, true},
+                        {scale_t, qt ? f8_scales(cols, rows, square) : 0, true, kScaleAlign}};
+    if (int st = check_buffers(b, 5)) return st;
+    *todo = rows > 0 && cols > 0;
+    return ok();
+}
+
+int validate_dequantize_f8(const uint8_t* q, int64_t q_stride, const uint8_t* scale, int64_t rows,
+                           int64_t cols, bool square, int format, const void* x, int dtype,
+                           bool* todo)
+{
+    *todo = false;
+    if (int st = check_dtype(dtype)) return st;
+    if (int st = check_format(format)) return st;
+    if (int st = check_f8_sizes(rows, cols)) return st;
+    if (int st = check_stride("q_stride", q_stride, cols, kMaxRowsI8)) return st;
+    const Buffer b[] = {{x, (size_t)rows * (size_t)cols * (dtype == ROI_FP32 ? 4 : 2), true},
+                        {q, f8_bytes(rows, cols, q_stride), false},
+                        {scale, f8_scales(rows, cols, square), false, kScaleAlign}};
+    if (int st = check_buffers(b, 3)) return st;
+    *todo = rows > 0 && cols > 0;
+    return ok();
+}
+
+int validate_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_format,
+                       const uint8_t* wq, int64_t w_stride, const uint8_t* ws, bool w_square,
+                       const uint16_t* bias, int64_t tokens, int64_t rows, int64_t cols,
+                       const uint16_t* y, const void* workspace, int64_t workspace_bytes,
+                       int64_t need, bool* todo)
+{
+    *todo = false;
+    if (int st = check_format(x_format)) return st;
+    if (int st = check_linear_sizes(tokens, rows, cols)) return st;
+    if (int st = check_stride("x_stride", x_stride, cols, kMaxStride)) return st;
+    if (int st = check_stride("w_stride", w_stride, cols, kMaxStride)) return st;
+    if (int st = check_workspace(workspace, workspace_bytes, need)) return st;
+    const size_t t = (size_t)tokens, r = (size_t)rows;
+    const Buffer b[] = {{xq, f8_bytes(tokens, cols, x_stride), false},
+                        {xs, f8_scales(tokens, cols, false), false, kScaleAlign},
+                        {wq, f8_bytes(rows, cols, w_stride), false},
+                        {ws, f8_scales(rows, cols, w_square), false, kScaleAlign},
+                        {bias, bias ? r * 2 : 0, false},
+                        {y, t * r * 2, true},
+                        {workspace, (size_t)need, true}};
+    if (int st = check_buffers(b, 7)) return st;
+    *todo = tokens > 0 && rows > 0;
+    return ok();
+}
+
+int validate_step(const roi_step_tensor* t, int count, int grad_dtype, int bits,
+                  const roi_adamw_params* opt, AdamStep* step, bool* todo)
+{
+    *todo = false;
+    if (int st = check_dtype(grad_dtype)) return st;
+    if (bits != 8 && bits != 32)
+        return fail(ROI_E_INVAL, "the moments' bits must be 8 or 32 (got %d)", bits);
+    if (int st = check_adamw(opt, step)) return st;
+    if (int st = check_count(t, count)) return st;
+    std::vector<Range> ranges;
+    ranges.reserve((size_t)count * 6);
+    for (int i = 0; i < count; ++i) {
+        const roi_step_tensor& s = t[i];
+        if (s.numel < 0)
+            return fail(ROI_E_INVAL, "tensor %d: numel (%lld) must be >= 0", i, (long long)s.numel);
+        if (s.numel >= kMaxStepValues)
+            return fail(ROI_E_UNSUPPORTED, "tensor %d: numel must be below 2^40", i);
+        if (s.elem_offset % 4 != 0)
+            return fail(ROI_E_INVAL, "tensor %d: elem_offset must be a multiple of 4", i);
+        if (s.elem_offset > UINT64_MAX - (uint64_t)s.numel)
+            return fail(ROI_E_INVAL, "tensor %d: elem_offset + numel overflows 64 bits", i);
+        if (s.numel == 0) continue;
+        if (!s.param || !s.grad || !s.exp_avg || !s.exp_avg_sq ||
+            (bits == 8 && (!s.avg_scale || !s.sq_scale)))
+            return fail(ROI_E_INVAL, "tensor %d: a required pointer is NULL", i);
+        if (!aligned16(s.param) || !aligned16(s.grad) || !aligned16(s.exp_avg) ||
+            !aligned16(s.exp_avg_sq) ||
+            (bits == 8 && ((uintptr_t)s.avg_scale % kScaleAlign || (uintptr_t)s.sq_scale % kScaleAlign)))
+            return fail(ROI_E_INVAL,
+                        "tensor %d: device pointers must be 16-byte aligned (scales: to 4 bytes)", i);
+        const size_t n = (size_t)s.numel, moment = bits == 8 ? n : 4 * n;
+        add_range(ranges, s.param, 4 * n, true);
+        add_range(ranges, s.grad, n * (grad_dtype == ROI_FP32 ? 4 : 2), false);
+        add_range(ranges, s.exp_avg, moment, true);
+        add_range(ranges, s.exp_avg_sq, moment, true);
+        if (bits == 8) {
+            add_range(ranges, s.avg_scale, (size_t)scale_bytes(s.numel), true);
+            add_range(ranges, s.sq_scale, (size_t)scale_bytes(s.numel), true);
+        }
+        *todo = true;
+    }
+    if (int st = check_overlaps(ranges)) {
+        *todo = false;
+        return st;
+    }
+    return ok();
+}
+
 } // namespace roi

@@ -178,6 +178,28 @@ int validate_grad_i8(const uint16_t* grad_y, const int8_t* q, const float* scale
                      int64_t out_rows, const void* workspace, int64_t workspace_bytes,
                      int64_t need, bool* todo);
 
+// Operands in 8-bit floats (roi_quantize_blocks, roi_dequantize_blocks, roi_linear_f8):
+// *todo is false when there is nothing to write.  The products count bytes within
+// 256 rows in 32 bits, so rows are at most kMaxStride bytes apart.
+constexpr int64_t kMaxStride = kMaxLinearDim;
+int validate_quantize_f8(const void* x, int dtype, int64_t rows, int64_t cols, bool square, int format,
+                         const uint8_t* q, int64_t q_stride, const uint8_t* scale, const uint8_t* qt,
+                         int64_t qt_stride, const uint8_t* scale_t, bool* todo);
+int validate_dequantize_f8(const uint8_t* q, int64_t q_stride, const uint8_t* scale, int64_t rows,
+                           int64_t cols, bool square, int format, const void* x, int dtype,
+                           bool* todo);
+int validate_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_format,
+                       const uint8_t* wq, int64_t w_stride, const uint8_t* ws, bool w_square,
+                       const uint16_t* bias, int64_t tokens, int64_t rows, int64_t cols,
+                       const uint16_t* y, const void* workspace, int64_t workspace_bytes,
+                       int64_t need, bool* todo);
+
+// roi_adamw_grouped's tensors; folds the step into *step.  *todo is false when all
+// are empty.
+constexpr int64_t kMaxStepValues = (int64_t)1 << 40;
+int validate_step(const roi_step_tensor* t, int count, int grad_dtype, int bits,
+                  const roi_adamw_params* opt, AdamStep* step, bool* todo);
+
 // Calls launch(first, count, elem0) for consecutive pieces of [0, items) --
 // items of `per_item` elements starting at global element elem_offset -- so
 // that within a piece every Philox block index (element / 4) has the same high
