@@ -567,6 +567,24 @@ int check_f8_sizes(int64_t rows, int64_t cols)
 
 } // namespace
 
+LinearPlan plan_linear_f8(int64_t tokens, int64_t rows, int64_t cols)
+{
+    LinearPlan p{};
+    p.few = tokens <= 32 || cols == 0;
+    if (p.few) return p;
+    p.row = cols;
+    p.cut = cut_product(rows, tokens, cols, 128, kF8Cost);
+    double tiles_us = p.cut.us;
+    // few tiles: their steps may be less work than reading the weight
+    if (tokens <= 128)
+        tiles_us += std::max(0.0, (double)rows * (double)cols / 5.0e6 -
+                                      (double)(p.cut.steps / p.cut.splits) * kF8Cost.step128);
+    p.bytes = p.cut.bytes;
+    p.few = tokens <= 1024 && few_us(tokens, rows, cols / 16 * 16, false) < tiles_us;
+    if (p.few) p.bytes = 0;
+    return p;
+}
+
 int validate_quantize_f8(const void* x, int dtype, int64_t rows, int64_t cols, bool square, int format,
                          const uint8_t* q, int64_t q_stride, const uint8_t* scale, const uint8_t* qt,
                          int64_t qt_stride, const uint8_t* scale_t, bool* todo)
