@@ -194,13 +194,14 @@ __global__ __launch_bounds__(256) void linear_f8_few_kernel(LinearF8Args a)
 }
 
 // --------------------------------------------------------------- many tokens
-// A block makes one tile (mm.hpp) over steps of 128 values, in kRing LDS buffers of
-// two operands.  A wave holds its tokens' operands of a step (kJ blocks of 16) and
-// passes the weight's rows (kI) by, two rows read ahead; in the last row it reads the
-// next step's tokens, block by block.  One barrier a step, ahead of the last two rows: past it every
-// wave holds all it needs of this step's buffer, which takes the step kRing later,
-// and the next step's buffer, loading for kRing - 1 steps, is complete.  The scales of
-// four steps are a word a row, which comes beside the operands four steps ahead.
+// A block makes one tile (mm.hpp) over steps of 128 values, with kRing LDS buffers of
+// each operand.  A wave holds its tokens' operands of a step (kJ blocks of 16) and
+// passes the weight's rows (kI) by, two rows read ahead; beside them it reads the
+// next step's tokens.  One barrier a step, ahead of the last two rows: past it every
+// wave holds all it needs of this step's weight and the next step's tokens, whose
+// buffers take the loads kRing steps on, and the next step's weight and the tokens
+// behind it, loading for kRing - 1 steps, are complete.  The scales of four steps
+// are a word a row, which comes beside the operands four steps ahead.
 
 // Rows row0 .. of an operand that this thread brings to LDS, where place j ^ (row & 7)
 // of a row holds its chunk j.
@@ -281,7 +282,7 @@ template <typename T, int kRing>
 constexpr int f8_lds() { return kRing * 2 * T::kTile * kRowBytes + 2 * 2 * T::kTile * 4; }
 
 template <typename T, int kRing, int kFormat>
-__global__ __launch_bounds__(T::kThreads, 2) void linear_f8_tile_kernel(LinearF8Args a)
+__global__ __launch_bounds__(T::kThreads, T::kTile == 256 && T::kWaves == 4 ? 1 : 2) void linear_f8_tile_kernel(LinearF8Args a)
 {
     constexpr int kTile = T::kTile, kTileBytes = kTile * kRowBytes;
     constexpr int kI = T::kI, kJ = T::kJ;
@@ -299,14 +300,21 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_f8_tile_kernel(LinearF8
     using R = F8Rows<T>;
     const R wrows(a.w, r0, a.rows, a.cols, a.w_stride), xrows(a.x, t0, a.tokens, a.cols, a.x_stride);
     constexpr int kLoads = R::kLoads;
-    auto buffer = [&](int s) { return base + (s & (kRing - 1)) * 2 * kTileBytes; };
-    // loads `first` .. of step s, of the 2 kLoads that bring both operands
-    auto stage = [&](int s, int first, int count) {
-        for (int i = first; i < first + count; ++i)
-            if (i < kLoads)
-                wrows.stage(i, (piece.first + s) * kRowBytes, buffer(s));
+    auto w_buffer = [&](int s) { return base + (s & (kRing - 1)) * kTileBytes; };
+    auto x_buffer = [&](int s) { return base + (kRing + (s & (kRing - 1))) * kTileBytes; };
+    auto stage_w = [&](int s, int i) { wrows.stage(i, (piece.first + s) * kRowBytes, w_buffer(s)); };
+    auto stage_x = [&](int s, int i) { xrows.stage(i, (piece.first + s) * kRowBytes, x_buffer(s)); };
+    // quarter n of the loads that step s frees its buffers for: the weight of step
+    // s + kRing and the tokens of the step behind that
+    constexpr int kQuarter = kLoads / 2;
+    auto stage = [&](int s, int n) {
+#pragma unroll
+        for (int i = 0; i < kQuarter; ++i) {
+            if (n < 2)
+                stage_w(s + kRing, n * kQuarter + i);
             else
-                xrows.stage(i - kLoads, (piece.first + s) * kRowBytes, buffer(s) + kTileBytes);
+                stage_x(s + 1 + kRing, (n - 2) * kQuarter + i);
+        }
     };
     // the words of scales of group q (steps 4 q .. 4 q + 3 of the sum): kTile of the
     // weight's rows, then kTile of the tokens'; past the last group that one again
@@ -326,13 +334,13 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_f8_tile_kernel(LinearF8
         }
     };
     const int from_w = (wm + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
-    const int from_x = kTileBytes + (wn + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
+    const int from_x = (wn + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
     auto read_w = [&](int s, int i) {
-        ROI_LDS uint8_t* p = buffer(s) + i * 16 * kRowBytes;
+        ROI_LDS uint8_t* p = w_buffer(s) + i * 16 * kRowBytes;
         return joined(lds_read<i32x4>(p + from_w), lds_read<i32x4>(p + (from_w ^ 64)));
     };
     auto read_x = [&](int s, int j) {
-        ROI_LDS uint8_t* p = buffer(s) + j * 16 * kRowBytes;
+        ROI_LDS uint8_t* p = x_buffer(s) + j * 16 * kRowBytes;
         return joined(lds_read<i32x4>(p + from_x), lds_read<i32x4>(p + (from_x ^ 64)));
     };
     int ws[kI], xs[kJ];
@@ -343,24 +351,19 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_f8_tile_kernel(LinearF8
 #pragma unroll
         for (int j = 0; j < kJ; ++j) xs[j] = lds_read<int>(p + (kTile + wn + 16 * j) * 4);
     };
-    // the rows' ends in the last step of the sum: what its last piece holds behind them
+    static_assert(kI % 4 == 0 && kLoads % 2 == 0, "registers and loads by quarters");
+    i32x8 w[4], now[kJ], next[kJ];
     const int tail = a.cols % 16;
-    auto cut = [&](int s) {
-        if (tail && piece.first + s == a.grid.steps - 1) {
-            const int last = a.cols % 128 / 16;
-            for (int at = threadIdx.x; at < 2 * kTile; at += T::kThreads)
-                cut_piece(buffer(s) + at * kRowBytes + (last ^ (at & 7)) * 16, tail);
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        }
-    };
-    static_assert(2 * kLoads % kI == 0 && kI % 4 == 0, "loads are spread over the rows");
-    constexpr int kPart = 2 * kLoads / kI;
-    i32x8 w[4], x[kJ];
+    // step s from the tokens in `now`, reading the next step's into `next`.  One step a
+    // turn of the loop, and the tokens moved at its end: with two the compiler holds the
+    // sums twice.
     auto step = [&](int s) {
+        // Branches stand here only: the compiler moves products past those further on.
         const int S = piece.first + s;
         if (s > 0) {
             if ((S & 3) == 0) {
                 read_scales(S >> 2);
+                stage_scales((S >> 2) + 1);
             } else {
 #pragma unroll
                 for (int i = 0; i < kI; ++i) ws[i] >>= 8;
@@ -368,37 +371,70 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_f8_tile_kernel(LinearF8
                 for (int j = 0; j < kJ; ++j) xs[j] >>= 8;
             }
         }
+        if (tail && S == a.grid.steps - 1) {
+            // zeros for what the last piece of the rows holds behind their ends: the
+            // tokens' in registers, the weight's in LDS, where its first rows are read
+            // again
+            const int last = a.cols % 128 / 16;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int have = tail - e % 4 * 4; // of this word's bytes
+                const uint32_t keep = g + e / 4 * 4 < last    ? 0xFFFFFFFFu
+                                      : g + e / 4 * 4 > last || have <= 0 ? 0u
+                                      : have >= 4             ? 0xFFFFFFFFu
+                                                              : 0xFFFFFFFFu >> (32 - 8 * have);
+#pragma unroll
+                for (int j = 0; j < kJ; ++j) now[j][e] &= (int)keep;
+            }
+            for (int at = threadIdx.x; at < kTile; at += T::kThreads)
+                cut_piece(w_buffer(s) + at * kRowBytes + (last ^ (at & 7)) * 16, tail);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            w[0] = read_w(s, 0);
+            w[1] = read_w(s, 1);
+        }
+        constexpr int kAhead = kI - 2; // rows ahead of the barrier
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
-            if (i + 2 < kI) {
-                w[(i + 2) % 4] = read_w(s, i + 2);
-            } else {
-                const int n = i + 2 - kI;
-                w[n] = read_w(s + 1, n);
-            }
-            if (i < kI - 2) stage(s + kRing - 1, (i + 2) * kPart, kPart);
-            else stage(s + kRing, (i - (kI - 2)) * kPart, kPart);
 #pragma unroll
             for (int j = 0; j < kJ; ++j) {
-                acc[i][j] = multiply_block<kFormat>(w[i % 4], x[j], acc[i][j], ws[i], xs[j]);
-                if (i == kI - 1) x[j] = read_x(s + 1, j);
+                acc[i][j] = multiply_block<kFormat>(w[i % 4], now[j], acc[i][j], ws[i], xs[j]);
+                if (j == 0) {
+                    keep_order();
+                    if (i < kAhead) {
+                        w[(i + 2) % 4] = read_w(s, i + 2);
+#pragma unroll
+                        for (int n = i * kJ / kAhead; n < (i + 1) * kJ / kAhead; ++n)
+                            next[n] = read_x(s + 1, n);
+                        if (i < 2) stage(s - 1, 2 + i);
+                    } else {
+                        w[i - kAhead] = read_w(s + 1, i - kAhead);
+                        stage(s, i - kAhead);
+                    }
+                }
             }
             keep_order();
-            if (i == kI - 3) {
-                if ((S & 3) == 0 && s > 0) stage_scales((S >> 2) + 1);
+            if (i == kAhead - 1) {
                 loads_barrier<(kRing - 2) * 2 * kLoads>();
-                cut(s + 1);
+                keep_order();
             }
         }
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) now[j] = next[j];
     };
     if (piece.count > 0) {
         stage_scales(piece.first >> 2);
         stage_scales((piece.first >> 2) + 1);
-        for (int s = 0; s < kRing - 1; ++s) stage(s, 0, 2 * kLoads);
-        // of the last of the ring's, what the first step's rows do not bring
-        stage(kRing - 1, 0, 2 * kPart);
-        loads_barrier<(kRing - 2) * 2 * kLoads + 2 * kPart>();
-        cut(0);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) stage_x(0, i);
+#pragma unroll
+        for (int s = 0; s < kRing; ++s) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) stage_w(s, i);
+            if (s + 1 == kRing) break;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) stage_x(s + 1, i);
+        }
+        loads_barrier<(kRing - 2) * 2 * kLoads + kLoads>();
         read_scales(piece.first >> 2);
 #pragma unroll
         for (int i = 0; i < kI; ++i) ws[i] >>= 8 * (piece.first & 3);
@@ -407,7 +443,9 @@ __global__ __launch_bounds__(T::kThreads, 2) void linear_f8_tile_kernel(LinearF8
         w[0] = read_w(0, 0);
         w[1] = read_w(0, 1);
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) x[j] = read_x(0, j);
+        for (int j = 0; j < kJ; ++j) now[j] = read_x(0, j);
+        // every wave has its tokens of step 0: their buffer takes those of step kRing
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         // past the end of the sum or of this part, loads are in bounds or zeros, and unused
         for (int s = 0; s < piece.count; ++s) step(s);
     }
@@ -475,7 +513,7 @@ void launch_f8(LinearF8Args a, const LinearPlan& plan, void* workspace, hipStrea
     a.partial = static_cast<float*>(workspace);
     a.grid = grid_of(plan.cut);
     if (plan.cut.tile == 256)
-        launch_f8_tiles<Tile<256>, 2, kFormat>(a, stream);
+        launch_f8_tiles<Tile<256, 4>, 2, kFormat>(a, stream);
     else if (a.grid.blocks() <= kUnits)
         launch_f8_tiles<Tile<128, 8>, 4, kFormat>(a, stream);
     else
