@@ -194,49 +194,62 @@ __global__ __launch_bounds__(256) void linear_f8_few_kernel(LinearF8Args a)
 }
 
 // --------------------------------------------------------------- many tokens
-// A block makes one tile (mm.hpp) over steps of 128 values, with kRing LDS buffers of
-// each operand.  A wave holds its tokens' operands of a step (kJ blocks of 16) and
-// passes the weight's rows (kI) by, two rows read ahead; beside them it reads the
-// next step's tokens.  One barrier a step, ahead of the last two rows: past it every
-// wave holds all it needs of this step's weight and the next step's tokens, whose
-// buffers take the loads kRing steps on, and the next step's weight and the tokens
-// behind it, loading for kRing - 1 steps, are complete.  The scales of four steps
-// are a word a row, which comes beside the operands four steps ahead.
+// A block makes one tile (mm.hpp) over steps of 128 values, in kRing LDS buffers of
+// both operands.  A wave holds its tokens' operands of a step (kJ blocks of 16) and
+// passes the weight's rows (kI) by in pairs, the next pair read ahead.  In the last
+// pair a block of tokens is read again, for the next step, as soon as both its
+// products are under way.  One barrier a step, ahead of that pair: past it every wave
+// holds all it needs of this step's buffer, which takes the step kRing later, and the
+// next step's, loading for kRing - 1 steps, is complete.  The scales of four steps
+// are a word a row, which comes beside the operands.
+//
+// A block goes through its tiles without a pause: the loads run kRing steps ahead
+// of the products, past a tile's end into the next one.
 
-// Rows row0 .. of an operand that this thread brings to LDS, where place j ^ (row & 7)
-// of a row holds its chunk j.
+// Rows of an operand that a thread brings to LDS, where place j ^ (row & 7) of a row
+// holds its chunk j.  What lies behind the last of the operand's bytes is left out
+// by the buffer's size (the offsets of the lane and of the wave count) and becomes
+// zeros; what lies behind a row's values, but before that, comes along.
 template <typename T>
 struct F8Rows {
     static constexpr int kThreads = T::kThreads;
     static constexpr int kLoads = T::kTile * kRowBytes / (16 * kThreads);
-    const uint8_t* base;
-    int left, len, stride; // rows from row0 on, their values and the bytes between them
-    uint32_t at;           // byte offset of load 0 from base
+    // a tile's rows: the first one and the bytes of all (0: none)
+    struct At {
+        const uint8_t* base;
+        int size;
+    };
+    int stride;
+    uint32_t at; // byte offset of load 0 from the first row; those of load i are i kThreads / 8 rows on
 
-    __device__ __forceinline__ F8Rows(const uint8_t* p, int row0, int n, int len_, int64_t stride_)
-        : base(p + (int64_t)row0 * stride_), left(n - row0), len(len_), stride((int)stride_),
-          at((uint32_t)row(0) * (uint32_t)stride_ + 16 * chunk())
+    __device__ __forceinline__ explicit F8Rows(int64_t stride_) : stride((int)stride_)
     {
+        const int row = threadIdx.x / 8;
+        at = (uint32_t)row * (uint32_t)stride_ + 16 * ((threadIdx.x % 8) ^ (row & 7));
     }
-    // Row and chunk of this thread's load i (the chunk is the same for all: the rows
-    // differ by a multiple of sixteen).
-    __device__ __forceinline__ static int row(int i) { return (i * kThreads + (int)threadIdx.x) / 8; }
-    __device__ __forceinline__ static int chunk() { return (threadIdx.x % 8) ^ (row(0) & 7); }
-    // Load i of values k .. k + 127 of the rows; zeros past the end.
-    __device__ __forceinline__ void stage(int i, int k, ROI_LDS uint8_t* dst) const
+    __device__ __forceinline__ At rows(const uint8_t* p, int row0, int n, int len) const
     {
-        const int wave = scalar(threadIdx.x >> 6);
-        const bool live = row(i) < left && k + 16 * chunk() < len;
-        load_to_lds<false>(buffer_at(base + k), live ? at : kNowhere, i * (kThreads / 8) * stride,
-                           dst + (i * kThreads + wave * 64) * 16);
+        return At{p + (int64_t)row0 * stride, (least(n - row0, T::kTile) - 1) * stride + (len + 15) / 16 * 16};
+    }
+    // The buffer of values k .. of the rows.
+    __device__ __forceinline__ static __amdgpu_buffer_rsrc_t buffer(const At& t, int k)
+    {
+        const int left = t.size - k;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(t.base + k), 0, left > 0 ? left : 0,
+                                                 0x00020000);
+    }
+    __device__ __forceinline__ void stage(__amdgpu_buffer_rsrc_t from, int i, ROI_LDS uint8_t* dst) const
+    {
+        load_to_lds<false>(from, at, i * (kThreads / 8) * stride,
+                           dst + (i * kThreads + scalar(threadIdx.x >> 6) * 64) * 16);
     }
 };
 
-// A tile's results from a wave's sums: a part of a cut tile as it is, else through LDS
-// (all of which is free) to y.
+// A tile's results from a wave's sums, which become zeros: a part of a cut tile as it
+// is, else 16 tokens at a time through the wave's `mine` of LDS to y.
 template <typename T>
 __device__ __forceinline__ void write_f8_tile(const LinearF8Args& a, const Piece& piece,
-                                              const f32x4 (&acc)[T::kI][T::kJ], ROI_LDS uint8_t* base)
+                                              f32x4 (&acc)[T::kI][T::kJ], ROI_LDS uint8_t* mine)
 {
     using H = Held<T, 16>;
     const int wave = scalar(threadIdx.x >> 6);
@@ -246,43 +259,55 @@ __device__ __forceinline__ void write_f8_tile(const LinearF8Args& a, const Piece
 #pragma unroll
         for (int i = 0; i < T::kI; ++i)
 #pragma unroll
-            for (int j = 0; j < T::kJ; ++j)
+            for (int j = 0; j < T::kJ; ++j) {
                 *reinterpret_cast<f32x4*>(a.partial + H::part_at(piece.part, wave, i, j, 0)) = acc[i][j];
+                acc[i][j] = f32x4{};
+                keep_order();
+            }
         return;
     }
-    // a row of a token's results: 16 kI values of 2 bytes
-    using Lines = RowsOut<T::kI, 8>;
-    ROI_LDS uint8_t* mine = base + wave * (16 * T::kJ * Lines::kRow);
+    f32x4 add[T::kI]; // without a bias -0, which changes nothing
 #pragma unroll
-    for (int i = 0; i < T::kI; ++i) {
-        f32x4 add = {};
-        if (a.bias) {
+    for (int i = 0; i < T::kI; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                add[e] = bf16_bits_to_float(a.bias[least(r0 + 4 * H::quad(i, 0) + e, a.rows - 1)]);
-        }
+        for (int e = 0; e < 4; ++e)
+            add[i][e] = a.bias ? bf16_bits_to_float(a.bias[least(r0 + 4 * H::quad(i, 0) + e, a.rows - 1)]) : -0.0f;
+    using Lines = RowsOut<T::kI, 8>; // of a token: 16 kI values of 2 bytes
 #pragma unroll
-        for (int j = 0; j < T::kJ; ++j) {
-            f32x4 v = acc[i][j];
-            if (a.bias) v += add;
-            *reinterpret_cast<ROI_LDS u32x2*>(Lines::at(mine, H::column(j), H::quad(i, 0))) =
+    for (int j = 0; j < T::kJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < T::kI; ++i) {
+            const f32x4 v = acc[i][j] + add[i];
+            *reinterpret_cast<ROI_LDS u32x2*>(Lines::at(mine, threadIdx.x % 16, H::quad(i, 0))) =
                 u32x2{bf16x2_rne(v[0], v[1]), bf16x2_rne(v[2], v[3])};
+            acc[i][j] = f32x4{};
         }
-    }
-#pragma unroll 2 // code that runs once is fetched once: it is kept short
-    for (int n = 0; n < 16 * T::kJ / Lines::kAtOnce; ++n) {
-        int row, chunk;
-        const Quad v = Lines::get(mine, n, row, chunk);
-        const int t = t0 + row;
-        if (t < a.tokens) store_chunk(a.y + (int64_t)t * a.rows, r0 + chunk * 8, a.rows, v);
+        keep_order();
+#pragma unroll
+        for (int n = 0; n < 16 / Lines::kAtOnce; ++n) {
+            int row, chunk;
+            const Quad v = Lines::get(mine, n, row, chunk);
+            const int t = t0 + 16 * j + row;
+            if (t < a.tokens) store_chunk(a.y + (int64_t)t * a.rows, r0 + chunk * 8, a.rows, v);
+        }
+        keep_order();
     }
 }
 
+// Two operands a step, a word of scales for each of their rows, and 16 tokens of a
+// wave's results.
 template <typename T, int kRing>
-constexpr int f8_lds() { return kRing * 2 * T::kTile * kRowBytes + 2 * 2 * T::kTile * 4; }
+constexpr int f8_lds()
+{
+    return kRing * 2 * T::kTile * (kRowBytes + 4) + T::kWaves * 16 * T::kI * 32;
+}
+// Blocks of a compute unit.
+template <typename T>
+constexpr int f8_blocks() { return T::kWaves == 4 && T::kTile == 128 ? 2 : 1; }
 
 template <typename T, int kRing, int kFormat>
-__global__ __launch_bounds__(T::kThreads, T::kTile == 256 && T::kWaves == 4 ? 1 : 2) void linear_f8_tile_kernel(LinearF8Args a)
+__global__ __launch_bounds__(T::kThreads, f8_blocks<T>() * T::kWaves / 4) void linear_f8_tile_kernel(
+    LinearF8Args a)
 {
     constexpr int kTile = T::kTile, kTileBytes = kTile * kRowBytes;
     constexpr int kI = T::kI, kJ = T::kJ;
@@ -292,165 +317,243 @@ __global__ __launch_bounds__(T::kThreads, T::kTile == 256 && T::kWaves == 4 ? 1 
     ROI_LDS uint8_t* scale_lds = base + kRing * 2 * kTileBytes;
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wave = scalar(threadIdx.x >> 6);
+    ROI_LDS uint8_t* mine = scale_lds + kRing * 2 * kTile * 4 + wave * (16 * kI * 32);
     const int wm = wave / T::kAcross * 16 * kI, wn = wave % T::kAcross * 16 * kJ;
-    const Piece piece = piece_of(a.grid, blockIdx.x);
-    const int r0 = piece.m * kTile, t0 = piece.n * kTile;
+    const uint32_t pieces = a.grid.blocks();
 
-    f32x4 acc[kI][kJ] = {};
     using R = F8Rows<T>;
-    const R wrows(a.w, r0, a.rows, a.cols, a.w_stride), xrows(a.x, t0, a.tokens, a.cols, a.x_stride);
+    const R wrows(a.w_stride), xrows(a.x_stride);
     constexpr int kLoads = R::kLoads;
-    auto w_buffer = [&](int s) { return base + (s & (kRing - 1)) * kTileBytes; };
-    auto x_buffer = [&](int s) { return base + (kRing + (s & (kRing - 1))) * kTileBytes; };
-    auto stage_w = [&](int s, int i) { wrows.stage(i, (piece.first + s) * kRowBytes, w_buffer(s)); };
-    auto stage_x = [&](int s, int i) { xrows.stage(i, (piece.first + s) * kRowBytes, x_buffer(s)); };
-    // quarter n of the loads that step s frees its buffers for: the weight of step
-    // s + kRing and the tokens of the step behind that
-    constexpr int kQuarter = kLoads / 2;
-    auto stage = [&](int s, int n) {
-#pragma unroll
-        for (int i = 0; i < kQuarter; ++i) {
-            if (n < 2)
-                stage_w(s + kRing, n * kQuarter + i);
-            else
-                stage_x(s + 1 + kRing, (n - 2) * kQuarter + i);
-        }
+    // Words of scales: kTile of the weight's rows, then kTile of the tokens'.  With a
+    // thread for each row a load for each operand, else one for both, waves being of
+    // one operand, and those without any bringing the first's again.
+    constexpr bool kApart = T::kThreads == kTile;
+    constexpr int kScaleLoads = kApart ? 2 : 1;
+    const int scale_first = kApart ? wave * 64 : wave * 64 % (2 * kTile);
+    const bool scale_of_w = kApart || scale_first < kTile;
+    // What is loaded next: step S of the sum, `left` steps from the end of its piece.
+    struct Aim {
+        typename R::At w, x;
+        const uint8_t* scales;   // of this wave's operand (kApart: the weight's)
+        const uint8_t* x_scales; // kApart
+        uint32_t scale_at, x_scale_at;
+        int scale_size; // 0 behind the last piece
+        int S, left;
+        uint32_t index;
     };
-    // the words of scales of group q (steps 4 q .. 4 q + 3 of the sum): kTile of the
-    // weight's rows, then kTile of the tokens'; past the last group that one again
-    constexpr int kScaleLoads = (2 * kTile + T::kThreads - 1) / T::kThreads;
-    auto stage_scales = [&](int q) {
-#pragma unroll
-        for (int i = 0; i < kScaleLoads; ++i) {
-            const int at = i * T::kThreads + (int)threadIdx.x; // whole waves on either side
-            if (at >= 2 * kTile) return;
-            const uint8_t* row =
-                at < kTile ? a.ws + (int64_t)(least(r0 + at, a.rows - 1) >> a.w_shift) * a.scales
-                           : a.xs + (int64_t)least(t0 + at - kTile, a.tokens - 1) * a.scales;
-            __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void*)(row + 4 * least(q, a.scales / 4 - 1)),
-                (ROI_LDS void*)(scale_lds + ((q & 1) * 2 * kTile + i * T::kThreads + wave * 64) * 4), 4, 0,
-                0);
+    auto aim_at = [&](Aim& m, uint32_t index) {
+        m.index = index;
+        if (index >= pieces) {
+            m.w.size = m.x.size = m.scale_size = 0;
+            m.left = 0x7FFFFFFF;
+            return;
         }
+        const Piece p = piece_of(a.grid, index);
+        const int r0 = p.m * kTile, t0 = p.n * kTile;
+        m.w = wrows.rows(a.w, r0, a.rows, a.cols);
+        m.x = xrows.rows(a.x, t0, a.tokens, a.cols);
+        // place p of an operand's words is that of row 16 (p % k) + p / k of a wave's 16 k
+        // rows, so that a lane's k words are consecutive
+        auto row_of = [](int p, int k) { return p / (16 * k) * (16 * k) + p % k * 16 + p % (16 * k) / k; };
+        const int place = (scale_first + lane) % kTile;
+        const int at_w = row_of(place, kI), at_x = row_of(place, kJ);
+        const uint8_t* of_w = a.ws + (int64_t)(r0 >> a.w_shift) * a.scales;
+        const uint8_t* of_x = a.xs + (int64_t)t0 * a.scales;
+        const uint32_t w_row = (uint32_t)((least(r0 + at_w, a.rows - 1) >> a.w_shift) - (r0 >> a.w_shift));
+        const uint32_t x_row = (uint32_t)least(at_x, a.tokens - 1 - t0);
+        m.scales = scale_of_w ? of_w : of_x;
+        m.scale_at = (uint32_t)a.scales * (scale_of_w ? w_row : x_row);
+        m.x_scales = of_x;
+        m.x_scale_at = (uint32_t)a.scales * x_row;
+        m.scale_size = 0x7FFFFFFF;
+        m.S = p.first;
+        m.left = p.count;
+    };
+    auto move_on = [&](Aim& m) {
+        if (--m.left == 0)
+            aim_at(m, m.index + gridDim.x);
+        else
+            ++m.S;
+    };
+    // n counts the block's steps over all its pieces
+    auto buffer = [&](int n) { return base + (n & (kRing - 1)) * 2 * kTileBytes; };
+    auto words = [&](int n) { return scale_lds + (n & (kRing - 1)) * 2 * kTile * 4; };
+    auto stage_scales = [&](const Aim& m, int n) {
+        auto bring = [&](const uint8_t* p, uint32_t at, int first) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, m.scale_size, 0x00020000),
+                (ROI_LDS void*)(words(n) + first * 4), 4, (int)at, m.S & ~3, 0, 0);
+        };
+        bring(m.scales, m.scale_at, scale_first);
+        if (kApart) bring(m.x_scales, m.x_scale_at, kTile + scale_first);
     };
     const int from_w = (wm + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
-    const int from_x = (wn + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
-    auto read_w = [&](int s, int i) {
-        ROI_LDS uint8_t* p = w_buffer(s) + i * 16 * kRowBytes;
+    const int from_x = kTileBytes + (wn + (lane & 15)) * kRowBytes + (g ^ (lane & 7)) * 16;
+    auto read_w = [&](int n, int i) {
+        ROI_LDS uint8_t* p = buffer(n) + i * 16 * kRowBytes;
         return joined(lds_read<i32x4>(p + from_w), lds_read<i32x4>(p + (from_w ^ 64)));
     };
-    auto read_x = [&](int s, int j) {
-        ROI_LDS uint8_t* p = x_buffer(s) + j * 16 * kRowBytes;
+    auto read_x = [&](int n, int j) {
+        ROI_LDS uint8_t* p = buffer(n) + j * 16 * kRowBytes;
         return joined(lds_read<i32x4>(p + from_x), lds_read<i32x4>(p + (from_x ^ 64)));
     };
-    int ws[kI], xs[kJ];
-    auto read_scales = [&](int q) {
-        ROI_LDS uint8_t* p = scale_lds + (q & 1) * 2 * kTile * 4 + (lane & 15) * 4;
+    // the words of step n, kI of the weight's and kJ of the tokens' a lane
+    static_assert(kI % 4 == 0 && (kJ == 2 || kJ % 4 == 0), "vectors of words");
+    auto read_words = [&](int n, int (&w_words)[kI], int (&x_words)[kJ]) {
+        ROI_LDS uint8_t* p = words(n) + (wm + (lane & 15) * kI) * 4;
 #pragma unroll
-        for (int i = 0; i < kI; ++i) ws[i] = lds_read<int>(p + (wm + 16 * i) * 4);
+        for (int i = 0; i < kI; i += 4) {
+            const i32x4 v = lds_read<i32x4>(p + 4 * i);
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) xs[j] = lds_read<int>(p + (kTile + wn + 16 * j) * 4);
+            for (int e = 0; e < 4; ++e) w_words[i + e] = v[e];
+        }
+        p = words(n) + (kTile + wn + (lane & 15) * kJ) * 4;
+        if constexpr (kJ == 2) {
+            const i32x2 v = lds_read<i32x2>(p);
+            x_words[0] = v[0];
+            x_words[1] = v[1];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kJ; j += 4) {
+                const i32x4 v = lds_read<i32x4>(p + 4 * j);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x_words[j + e] = v[e];
+            }
+        }
     };
-    static_assert(kI % 4 == 0 && kLoads % 2 == 0, "registers and loads by quarters");
-    i32x8 w[4], now[kJ], next[kJ];
-    const int tail = a.cols % 16;
-    // step s from the tokens in `now`, reading the next step's into `next`.  One step a
-    // turn of the loop, and the tokens moved at its end: with two the compiler holds the
-    // sums twice.
-    auto step = [&](int s) {
-        // Branches stand here only: the compiler moves products past those further on.
-        const int S = piece.first + s;
-        if (s > 0) {
-            if ((S & 3) == 0) {
-                read_scales(S >> 2);
-                stage_scales((S >> 2) + 1);
-            } else {
+
+    f32x4 acc[kI][kJ] = {};
+    int ws[kI], xs[kJ];
+    i32x8 w[4], x[kJ];
+    constexpr int kPairs = kI / 2, kInPair = 2 * kJ;
+    static_assert(kPairs == 2 || kPairs == 4, "where the loads go");
+    // The products of rows 2 p and 2 p + 1, `beside(m)` after the m-th of them.
+    auto pair = [&](int p, auto beside) {
 #pragma unroll
-                for (int i = 0; i < kI; ++i) ws[i] >>= 8;
-#pragma unroll
-                for (int j = 0; j < kJ; ++j) xs[j] >>= 8;
-            }
-        }
-        if (tail && S == a.grid.steps - 1) {
-            // zeros for what the last piece of the rows holds behind their ends: the
-            // tokens' in registers, the weight's in LDS, where its first rows are read
-            // again
-            const int last = a.cols % 128 / 16;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int have = tail - e % 4 * 4; // of this word's bytes
-                const uint32_t keep = g + e / 4 * 4 < last    ? 0xFFFFFFFFu
-                                      : g + e / 4 * 4 > last || have <= 0 ? 0u
-                                      : have >= 4             ? 0xFFFFFFFFu
-                                                              : 0xFFFFFFFFu >> (32 - 8 * have);
-#pragma unroll
-                for (int j = 0; j < kJ; ++j) now[j][e] &= (int)keep;
-            }
-            for (int at = threadIdx.x; at < kTile; at += T::kThreads)
-                cut_piece(w_buffer(s) + at * kRowBytes + (last ^ (at & 7)) * 16, tail);
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            w[0] = read_w(s, 0);
-            w[1] = read_w(s, 1);
-        }
-        constexpr int kAhead = kI - 2; // rows ahead of the barrier
-#pragma unroll
-        for (int i = 0; i < kI; ++i) {
-#pragma unroll
-            for (int j = 0; j < kJ; ++j) {
-                acc[i][j] = multiply_block<kFormat>(w[i % 4], now[j], acc[i][j], ws[i], xs[j]);
-                if (j == 0) {
-                    keep_order();
-                    if (i < kAhead) {
-                        w[(i + 2) % 4] = read_w(s, i + 2);
-#pragma unroll
-                        for (int n = i * kJ / kAhead; n < (i + 1) * kJ / kAhead; ++n)
-                            next[n] = read_x(s + 1, n);
-                        if (i < 2) stage(s - 1, 2 + i);
-                    } else {
-                        w[i - kAhead] = read_w(s + 1, i - kAhead);
-                        stage(s, i - kAhead);
-                    }
-                }
-            }
+        for (int m = 0; m < kInPair; ++m) {
+            const int i = 2 * p + m % 2, j = m / 2;
+            acc[i][j] = multiply_block<kFormat>(w[i % 4], x[j], acc[i][j], ws[i], xs[j]);
             keep_order();
-            if (i == kAhead - 1) {
-                loads_barrier<(kRing - 2) * 2 * kLoads>();
+            beside(m);
+            keep_order();
+        }
+    };
+    // Number of the load that goes beside product m when `count` go beside a pair's, or -1.
+    constexpr auto load_beside = [](int m, int count) {
+        return m % (kInPair / count) == 0 ? m / (kInPair / count) : -1;
+    };
+    // Step n, the loads of step n + kRing as `next` says (`last`: of the step before it).
+    // The loads are spread over the step: more at a time than the vector memory takes
+    // in holds up the wave and its products.  With four pairs the tokens are read, and
+    // their buffer free, past the first.  No branches: the compiler moves products past
+    // those further on.
+    auto step = [&](int n, const Aim& last, const Aim& next, int shift) {
+        constexpr bool kLong = kPairs == 4;
+        constexpr int kBeside = kLong ? kLoads / 2 : kLoads;
+        const __amdgpu_buffer_rsrc_t last_w = R::buffer(last.w, last.S * kRowBytes);
+        const __amdgpu_buffer_rsrc_t next_w = R::buffer(next.w, next.S * kRowBytes);
+        const __amdgpu_buffer_rsrc_t next_x = R::buffer(next.x, next.S * kRowBytes);
+#pragma unroll
+        for (int p = 0; p < kPairs - 1; ++p) {
+            pair(p, [&](int m) {
+                if (m < 2) w[(2 * p + 2 + m) % 4] = read_w(n, 2 * p + 2 + m);
+                const int l = load_beside(m, kBeside);
+                if (l < 0) return;
+                if (p == 0)
+                    wrows.stage(last_w, kLoads - kBeside + l, buffer(n - 1));
+                else
+                    xrows.stage(next_x, (p - 1) * kBeside + l, buffer(n) + kTileBytes);
+            });
+            if (kLong && p == 0) {
+                asm volatile("s_barrier" ::: "memory");
                 keep_order();
             }
         }
+        loads_barrier<(kRing - 2) * (2 * kLoads + kScaleLoads) + (kLong ? kLoads : 0)>();
+        keep_order();
+        int next_ws[kI], next_xs[kJ];
+        pair(kPairs - 1, [&](int m) {
+            constexpr int kHalf = kInPair / 2;
+            if (m < 2) w[m] = read_w(n + 1, m);
+            if (m == 0) read_words(n + 1, next_ws, next_xs);
+            if (m >= kHalf) {
+                xs[m - kHalf] = next_xs[m - kHalf] >> shift;
 #pragma unroll
-        for (int j = 0; j < kJ; ++j) now[j] = next[j];
+                for (int i = (m - kHalf) * kI / kHalf; i < (m + 1 - kHalf) * kI / kHalf; ++i)
+                    if (i < kI - 2) ws[i] = next_ws[i] >> shift;
+            }
+            if (m % 2) x[m / 2] = read_x(n + 1, m / 2);
+            const int l = load_beside(m, kBeside);
+            if (l < 0) return;
+            if (kLong)
+                wrows.stage(next_w, l, buffer(n));
+            else
+                xrows.stage(next_x, l, buffer(n) + kTileBytes);
+        });
+        ws[kI - 2] = next_ws[kI - 2] >> shift;
+        ws[kI - 1] = next_ws[kI - 1] >> shift;
+        stage_scales(next, n);
     };
-    if (piece.count > 0) {
-        stage_scales(piece.first >> 2);
-        stage_scales((piece.first >> 2) + 1);
+
+    Aim next;
+    aim_at(next, blockIdx.x);
+    Piece piece = piece_of(a.grid, blockIdx.x);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) stage_x(0, i);
+    for (int n = 0; n < kRing; ++n) {
+        if (n > 0) move_on(next);
+        const __amdgpu_buffer_rsrc_t wb = R::buffer(next.w, next.S * kRowBytes);
+        const __amdgpu_buffer_rsrc_t xb = R::buffer(next.x, next.S * kRowBytes);
+        stage_scales(next, n);
 #pragma unroll
-        for (int s = 0; s < kRing; ++s) {
+        for (int i = 0; i < kLoads; ++i) xrows.stage(xb, i, buffer(n) + kTileBytes);
+        // the last one's weight is loaded beside the first products
+        const int count = n < kRing - 1 ? kLoads : kPairs == 4 ? kLoads / 2 : 0;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) stage_w(s, i);
-            if (s + 1 == kRing) break;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) stage_x(s + 1, i);
-        }
-        loads_barrier<(kRing - 2) * 2 * kLoads + kLoads>();
-        read_scales(piece.first >> 2);
-#pragma unroll
-        for (int i = 0; i < kI; ++i) ws[i] >>= 8 * (piece.first & 3);
-#pragma unroll
-        for (int j = 0; j < kJ; ++j) xs[j] >>= 8 * (piece.first & 3);
-        w[0] = read_w(0, 0);
-        w[1] = read_w(0, 1);
-#pragma unroll
-        for (int j = 0; j < kJ; ++j) now[j] = read_x(0, j);
-        // every wave has its tokens of step 0: their buffer takes those of step kRing
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        // past the end of the sum or of this part, loads are in bounds or zeros, and unused
-        for (int s = 0; s < piece.count; ++s) step(s);
+        for (int i = 0; i < count; ++i) wrows.stage(wb, i, buffer(n));
     }
-    loads_barrier();
-    write_f8_tile<T>(a, piece, acc, base);
+    // the steps behind the first go on loading
+    loads_barrier<(kRing - 1) * (kScaleLoads + 2 * kLoads) - (kPairs == 4 ? kLoads / 2 : kLoads)>();
+    auto first_operands = [&](int n) {
+        w[0] = read_w(n, 0);
+        w[1] = read_w(n, 1);
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) x[j] = read_x(n, j);
+    };
+    first_operands(0);
+    read_words(0, ws, xs);
+#pragma unroll
+    for (int i = 0; i < kI; ++i) ws[i] >>= (piece.first & 3) * 8;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) xs[j] >>= (piece.first & 3) * 8;
+    const int ragged = a.cols % 128;
+    int n = 0;
+    for (uint32_t index = blockIdx.x;;) {
+        index += gridDim.x;
+        const Piece after = index < pieces ? piece_of(a.grid, index) : Piece{};
+        for (int s = 0; s < piece.count; ++s, ++n) {
+            const Aim last = next;
+            move_on(next);
+            if (ragged && piece.first + s == a.grid.steps - 1) {
+                // zeros behind the rows' ends, and once more what has been read
+                for (int at = threadIdx.x; at < 2 * kTile; at += T::kThreads) {
+                    ROI_LDS uint8_t* row = buffer(n) + at * kRowBytes;
+                    int c = ragged / 16;
+                    if (ragged % 16) {
+                        cut_piece(row + (c ^ (at & 7)) * 16, ragged % 16);
+                        ++c;
+                    }
+                    for (; c < 8; ++c) *reinterpret_cast<ROI_LDS u32x4*>(row + (c ^ (at & 7)) * 16) = u32x4{};
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                first_operands(n);
+            }
+            step(n, last, next, ((s + 1 < piece.count ? piece.first + s + 1 : after.first) & 3) * 8);
+        }
+        write_f8_tile<T>(a, piece, acc, mine);
+        if (index >= pieces) break;
+        piece = after;
+    }
+    loads_wait<0>(); // the loads behind the last piece, into this block's LDS
 }
 
 // The sums of the tiles that were cut: one wave for a quad of results a lane.
@@ -474,7 +577,8 @@ __global__ __launch_bounds__(256) void linear_f8_sum_kernel(LinearF8Args a)
 template <typename T, int kRing, int kFormat>
 void launch_f8_tiles(const LinearF8Args& a, hipStream_t stream)
 {
-    const dim3 grid(a.grid.blocks()), sums(a.grid.rest() * T::kI * T::kJ * T::kWaves / 4);
+    const uint32_t most = (uint32_t)(f8_blocks<T>() * kUnits), blocks = a.grid.blocks();
+    const dim3 grid(blocks < most ? blocks : most), sums(a.grid.rest() * T::kI * T::kJ * T::kWaves / 4);
     hipLaunchKernelGGL((linear_f8_tile_kernel<T, kRing, kFormat>), grid, dim3(T::kThreads),
                        (f8_lds<T, kRing>()), stream, a);
     if (sums.x > 0) hipLaunchKernelGGL((linear_f8_sum_kernel<T>), sums, dim3(256), 0, stream, a);
