@@ -74,6 +74,10 @@ __device__ __forceinline__ i32x8 joined(i32x4 lo, i32x4 hi)
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+// Waits for all LDS reads, known to the compiler: reads that are on their way at only
+// one of a loop's entries would have it wait for all in every turn.
+__device__ __forceinline__ void lds_reads_wait() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+
 // ---------------------------------------------------------------- few tokens
 // A block owns 16 kRow weight rows and up to kTokens tokens (8, or a multiple of
 // 16); its waves share out the sum by steps of 128 values and add up their parts in
@@ -442,21 +446,22 @@ __global__ __launch_bounds__(T::kThreads, f8_blocks<T>() * T::kWaves / 4) void l
     constexpr auto load_beside = [](int m, int count) {
         return m % (kInPair / count) == 0 ? m / (kInPair / count) : -1;
     };
-    // Step n, the loads of step n + kRing as `next` says (`last`: of the step before it).
+    // Step n, the loads of step n + kRing as `next` says, and those of the weight that
+    // step n - 1 has left from `last`, step last_S.  `after`: step n + 1 of the sum.
     // The loads are spread over the step: more at a time than the vector memory takes
     // in holds up the wave and its products.  With four pairs the tokens are read, and
     // their buffer free, past the first.  No branches: the compiler moves products past
     // those further on.
-    auto step = [&](int n, const Aim& last, const Aim& next, int shift) {
+    auto step = [&](int n, const typename R::At& last, int last_S, const Aim& next, int after) {
         constexpr bool kLong = kPairs == 4;
         constexpr int kBeside = kLong ? kLoads / 2 : kLoads;
-        const __amdgpu_buffer_rsrc_t last_w = R::buffer(last.w, last.S * kRowBytes);
-        const __amdgpu_buffer_rsrc_t next_w = R::buffer(next.w, next.S * kRowBytes);
-        const __amdgpu_buffer_rsrc_t next_x = R::buffer(next.x, next.S * kRowBytes);
+        __amdgpu_buffer_rsrc_t last_w, next_w, next_x;
 #pragma unroll
         for (int p = 0; p < kPairs - 1; ++p) {
             pair(p, [&](int m) {
                 if (m < 2) w[(2 * p + 2 + m) % 4] = read_w(n, 2 * p + 2 + m);
+                if (m == 0 && p == 0) last_w = R::buffer(last, last_S * kRowBytes);
+                if (m == 0 && p == 1) next_x = R::buffer(next.x, next.S * kRowBytes);
                 const int l = load_beside(m, kBeside);
                 if (l < 0) return;
                 if (p == 0)
@@ -471,11 +476,14 @@ __global__ __launch_bounds__(T::kThreads, f8_blocks<T>() * T::kWaves / 4) void l
         }
         loads_barrier<(kRing - 2) * (2 * kLoads + kScaleLoads) + (kLong ? kLoads : 0)>();
         keep_order();
-        int next_ws[kI], next_xs[kJ];
+        int next_ws[kI], next_xs[kJ], shift = 0;
         pair(kPairs - 1, [&](int m) {
             constexpr int kHalf = kInPair / 2;
             if (m < 2) w[m] = read_w(n + 1, m);
             if (m == 0) read_words(n + 1, next_ws, next_xs);
+            if (m == 0 && kLong) next_w = R::buffer(next.w, next.S * kRowBytes);
+            if (m == 0 && !kLong) next_x = R::buffer(next.x, next.S * kRowBytes);
+            if (m == kHalf - 1) shift = (after & 3) * 8;
             if (m >= kHalf) {
                 xs[m - kHalf] = next_xs[m - kHalf] >> shift;
 #pragma unroll
@@ -525,29 +533,42 @@ __global__ __launch_bounds__(T::kThreads, f8_blocks<T>() * T::kWaves / 4) void l
     for (int i = 0; i < kI; ++i) ws[i] >>= (piece.first & 3) * 8;
 #pragma unroll
     for (int j = 0; j < kJ; ++j) xs[j] >>= (piece.first & 3) * 8;
+    lds_reads_wait();
     const int ragged = a.cols % 128;
     int n = 0;
     for (uint32_t index = blockIdx.x;;) {
         index += gridDim.x;
         const Piece after = index < pieces ? piece_of(a.grid, index) : Piece{};
-        for (int s = 0; s < piece.count; ++s, ++n) {
-            const Aim last = next;
-            move_on(next);
-            if (ragged && piece.first + s == a.grid.steps - 1) {
-                // zeros behind the rows' ends, and once more what has been read
-                for (int at = threadIdx.x; at < 2 * kTile; at += T::kThreads) {
-                    ROI_LDS uint8_t* row = buffer(n) + at * kRowBytes;
-                    int c = ragged / 16;
-                    if (ragged % 16) {
-                        cut_piece(row + (c ^ (at & 7)) * 16, ragged % 16);
-                        ++c;
+        // `run` steps go on alike: to the end of this piece or of the loads', or to a
+        // ragged step, by themselves
+        int s = 0, run = 0;
+        for (; s < piece.count; ++s, ++n, --run) {
+            const typename R::At last = next.w;
+            const int last_S = next.S;
+            ++next.S;
+            --next.left;
+            if (run == 0) {
+                if (next.left == 0) aim_at(next, next.index + gridDim.x);
+                run = least(piece.count - s, next.left);
+                const int to_ragged = a.grid.steps - 1 - piece.first - s;
+                if (ragged && to_ragged > 0) run = least(run, to_ragged);
+                if (ragged && to_ragged == 0) {
+                    // zeros behind the rows' ends, and once more what has been read
+                    for (int at = threadIdx.x; at < 2 * kTile; at += T::kThreads) {
+                        ROI_LDS uint8_t* row = buffer(n) + at * kRowBytes;
+                        int c = ragged / 16;
+                        if (ragged % 16) {
+                            cut_piece(row + (c ^ (at & 7)) * 16, ragged % 16);
+                            ++c;
+                        }
+                        for (; c < 8; ++c) *reinterpret_cast<ROI_LDS u32x4*>(row + (c ^ (at & 7)) * 16) = u32x4{};
                     }
-                    for (; c < 8; ++c) *reinterpret_cast<ROI_LDS u32x4*>(row + (c ^ (at & 7)) * 16) = u32x4{};
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    first_operands(n);
+                    lds_reads_wait();
                 }
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                first_operands(n);
             }
-            step(n, last, next, ((s + 1 < piece.count ? piece.first + s + 1 : after.first) & 3) * 8);
+            step(n, last, last_S, next, s + 1 < piece.count ? piece.first + s + 1 : after.first);
         }
         write_f8_tile<T>(a, piece, acc, mine);
         if (index >= pieces) break;
