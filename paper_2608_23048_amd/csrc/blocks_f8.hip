@@ -14,40 +14,85 @@
 namespace roi {
 namespace {
 
-// Elements k .. k + 7 of a row of `cols`, zeros past its end.
-template <typename T>
-__device__ __forceinline__ void load_eight_f32(const T* row, int64_t k, int64_t cols, float (&f)[8])
-{
-    struct Eight {
-        uint32_t w[2 * sizeof(T)];
-    } e{};
-    if (k + 8 <= cols) {
-        e = load_any<Eight>(row + k);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < cols)
-                e.w[i * sizeof(T) / 4] |= (uint32_t)row[k + i] << (8 * (i * sizeof(T) % 4));
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
+// kN consecutive elements of a row, as loaded: bf16 two to a word.
+template <typename T, int kN>
+struct Held {
+    uint32_t w[kN * sizeof(T) / 4];
+
+    __device__ __forceinline__ float get(int i) const
+    {
         if constexpr (sizeof(T) == 2)
-            f[i] = __uint_as_float(i & 1 ? e.w[i / 2] & 0xFFFF0000u : e.w[i / 2] << 16);
+            return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
         else
-            f[i] = __uint_as_float(e.w[i]);
+            return __uint_as_float(w[i]);
     }
+};
+// Elements k .. of a row of `cols`, zeros past its end.
+template <bool kStream, typename T, int kN>
+__device__ __forceinline__ Held<T, kN> load_held(const T* row, int64_t k, int64_t cols)
+{
+    using H = Held<T, kN>;
+    if (k + kN <= cols) return kStream ? stream_load_any<H>(row + k) : load_any<H>(row + k);
+    H h{};
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+        if (k + i < cols) h.w[i * sizeof(T) / 4] |= (uint32_t)row[k + i] << (8 * (i * sizeof(T) % 4));
+    return h;
 }
 
-// Bytes k .. k + 7 of a row of `cols`.
-__device__ __forceinline__ void store_eight(uint8_t* row, int64_t k, int64_t cols, uint32_t lo,
+// The largest magnitudes of two values in the halves of a word (bf16), or of one
+// (fp32); infinities and NaN are above every number.
+template <typename T>
+__device__ __forceinline__ uint32_t magnitudes(uint32_t w)
+{
+    return w & (sizeof(T) == 2 ? 0x7FFF7FFFu : 0x7FFFFFFFu);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b)
+{
+    if constexpr (sizeof(T) == 2) {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                      __builtin_bit_cast(u16x2, b)));
+    } else {
+        return most(a, b);
+    }
+}
+// fp32 bits of the larger of what larger() gives.
+template <typename T>
+__device__ __forceinline__ uint32_t larger_half(uint32_t m)
+{
+    return sizeof(T) == 2 ? most(m << 16, m & 0xFFFF0000u) : m;
+}
+// The largest finite magnitude: what larger() passes over where one is not finite.
+template <typename T, int kN>
+__device__ __forceinline__ uint32_t largest_finite(const Held<T, kN>& h)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) m = most(m, finite_bits(h.get(i)));
+    return m;
+}
+
+// Bytes k .. k + 7 (one word: .. k + 3) of a row of `cols`.
+__device__ __forceinline__ void store_bytes(uint8_t* row, int64_t k, int64_t cols, uint32_t lo)
+{
+    if (k + 4 <= cols) {
+        *reinterpret_cast<uint32_t*>(row + k) = lo;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i < cols) row[k + i] = (uint8_t)(lo >> (8 * i));
+    }
+}
+__device__ __forceinline__ void store_bytes(uint8_t* row, int64_t k, int64_t cols, uint32_t lo,
                                             uint32_t hi)
 {
     if (k + 8 <= cols) {
         *reinterpret_cast<u32x2*>(row + k) = u32x2{lo, hi};
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (k + i < cols) row[k + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i % 4)));
+        store_bytes(row, k, cols, lo);
+        if (k + 4 < cols) store_bytes(row, k + 4, cols, hi);
     }
 }
 
@@ -61,23 +106,27 @@ struct QuantizeArgs {
 };
 
 // Blocks of rows: a wave takes kUnits times 512 consecutive values of a row (four
-// blocks, one word of scales), eight values a lane.
+// blocks, one word of scales), 16 bytes a lane and load.
 template <typename T, int kFormat>
 __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, int64_t per_row)
 {
-    constexpr int kUnits = 4;
+    constexpr int kUnits = 4, kN = 16 / sizeof(T), kLoads = 512 / (64 * kN);
     const int lane = threadIdx.x & 63;
     const int64_t units = a.rows * per_row;
     for (int64_t u = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * kUnits; u < units;
          u += (int64_t)gridDim.x * 4 * kUnits) {
-        float f[kUnits][8];
+        Held<T, kN> h[kUnits][kLoads];
         int64_t r = u / per_row, c = u - r * per_row;
         const int64_t r0 = r, c0 = c;
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
-            if (u + i < units)
-                load_eight_f32(static_cast<const T*>(a.x) + r * a.cols, c * 512 + lane * 8, a.cols,
-                               f[i]);
+            if (u + i < units) {
+#pragma unroll
+                for (int l = 0; l < kLoads; ++l) {
+                    const int64_t k = c * 512 + (l * 64 + lane) * kN;
+                    h[i][l] = load_held<true, T, kN>(static_cast<const T*>(a.x) + r * a.cols, k, a.cols);
+                }
+            }
             if (++c == per_row) {
                 c = 0;
                 ++r;
@@ -88,22 +137,37 @@ __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, i
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             if (u + i < units) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) m = most(m, finite_bits(f[i][e]));
-                const int byte = scale_byte<kFormat>(most_of_16(m));
-                const float inv = inverse_scale(byte);
-                const int64_t k = c * 512 + lane * 8;
-                store_eight(a.q + r * a.stride, k, a.cols,
-                            to_f8x4<kFormat>(f[i][0] * inv, f[i][1] * inv, f[i][2] * inv, f[i][3] * inv),
-                            to_f8x4<kFormat>(f[i][4] * inv, f[i][5] * inv, f[i][6] * inv, f[i][7] * inv));
                 uint32_t word = 0;
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    word |= (c * 512 + b * kF8Block < a.cols
-                                 ? (uint32_t)__builtin_amdgcn_readlane(byte, 16 * b)
-                                 : (uint32_t)kNoScale)
-                            << (8 * b);
+                for (int l = 0; l < kLoads; ++l) {
+                    uint32_t m = magnitudes<T>(h[i][l].w[0]);
+#pragma unroll
+                    for (int e = 1; e < 4; ++e) m = larger<T>(m, magnitudes<T>(h[i][l].w[e]));
+                    auto of_block = [](uint32_t v) { return kN == 8 ? most_of_16(v) : most_of_32(v); };
+                    m = of_block(larger_half<T>(m));
+                    if (__builtin_amdgcn_ballot_w64(m >= kInfinity)) m = of_block(largest_finite(h[i][l]));
+                    const int byte = scale_byte<kFormat>(m);
+                    const float inv = inverse_scale(byte);
+                    const int64_t k = c * 512 + (l * 64 + lane) * kN;
+                    uint32_t q[kN / 4];
+#pragma unroll
+                    for (int e = 0; e < kN; e += 4)
+                        q[e / 4] = to_f8x4<kFormat>(h[i][l].get(e) * inv, h[i][l].get(e + 1) * inv,
+                                                    h[i][l].get(e + 2) * inv, h[i][l].get(e + 3) * inv);
+                    if constexpr (kN == 8)
+                        store_bytes(a.q + r * a.stride, k, a.cols, q[0], q[1]);
+                    else
+                        store_bytes(a.q + r * a.stride, k, a.cols, q[0]);
+                    constexpr int kBlocks = kN / 2; // of this load
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) {
+                        const int at = l * kBlocks + b;
+                        word |= (c * 512 + at * kF8Block < a.cols
+                                     ? (uint32_t)__builtin_amdgcn_readlane(byte, 64 / kBlocks * b)
+                                     : (uint32_t)kNoScale)
+                                << (8 * at);
+                    }
+                }
                 if (lane == 0) reinterpret_cast<uint32_t*>(a.scale)[r * per_row + c] = word;
             }
             if (++c == per_row) {
@@ -117,11 +181,13 @@ __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, i
 // A block takes 128 x 128 values; thread (g, c) of 16 x 16 those of rows 8 g .. 8 g + 7
 // and columns 8 c .. 8 c + 7.  The transposed bytes pass LDS: eight rows of a
 // column are a piece of 8 bytes, piece g of column k at place g ^ (k / 8), so that
-// the 16 lanes of equal g cover all banks.
+// the 16 lanes of equal g cover all banks.  The values stay as they were loaded: bf16
+// in half the registers, and so twice the blocks on a compute unit.
 template <typename T, int kFormat, bool kSquare>
 __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, int64_t tiles_c,
                                                                int64_t tiles)
 {
+    constexpr int kWords = 2 * sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t out[128 * 128];
     __shared__ uint32_t part[4][128];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -130,32 +196,47 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t tr = tile / tiles_c, tc = tile - tr * tiles_c;
         const int64_t r0 = tr * 128 + 8 * g, k0 = tc * 128 + 8 * c;
-        float f[8][8];
+        Held<T, 8> h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            h[i] = r0 + i < a.rows ? load_held<true, T, 8>(static_cast<const T*>(a.x) + (r0 + i) * a.cols, k0, a.cols)
+                                   : Held<T, 8>{};
+        uint32_t row_most[8], col_most[kWords];
+#pragma unroll
+        for (int e = 0; e < kWords; ++e) col_most[e] = 0;
+        uint32_t any = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (r0 + i < a.rows) {
-                load_eight_f32(static_cast<const T*>(a.x) + (r0 + i) * a.cols, k0, a.cols, f[i]);
-            } else {
+            uint32_t m = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[i][e] = 0.0f;
+            for (int e = 0; e < kWords; ++e) {
+                const uint32_t b = magnitudes<T>(h[i].w[e]);
+                m = larger<T>(m, b);
+                col_most[e] = larger<T>(col_most[e], b);
             }
+            row_most[i] = larger_half<T>(m);
+            any = most(any, row_most[i]);
         }
-        uint32_t row_most[8], col_most[8] = {};
+        uint32_t col[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            row_most[i] = 0;
+        for (int e = 0; e < 8; ++e)
+            col[e] = sizeof(T) == 2 ? (e & 1 ? col_most[e / 2] & 0xFFFF0000u : col_most[e / 2] << 16)
+                                    : col_most[e % kWords];
+        if (__builtin_amdgcn_ballot_w64(any >= kInfinity)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) row_most[i] = largest_finite(h[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const uint32_t b = finite_bits(f[i][e]);
-                row_most[i] = most(row_most[i], b);
-                col_most[e] = most(col_most[e], b);
+                col[e] = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) col[e] = most(col[e], finite_bits(h[i].get(e)));
             }
         }
         int row_byte[8], col_byte[8];
         if constexpr (kSquare) {
             uint32_t m = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = most(m, col_most[e]);
+            for (int i = 0; i < 8; ++i) m = most(m, row_most[i]);
             m = most_of_32(m);
             m = most(m, (uint32_t)__shfl_xor((int)m, 32));
             if (lane == 0) part[wave][0] = m;
@@ -170,15 +251,15 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
             }
         } else {
 #pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t m = most(col[e], (uint32_t)__shfl_xor((int)col[e], 16));
+                m = most(m, (uint32_t)__shfl_xor((int)m, 32));
+                if (lane < 16) part[wave][8 * c + e] = m;
+            }
+#pragma unroll
             for (int i = 0; i < 8; ++i) {
                 row_byte[i] = scale_byte<kFormat>(most_of_16(row_most[i]));
                 if (c == 0 && r0 + i < a.rows) a.scale[(r0 + i) * scales + tc] = (uint8_t)row_byte[i];
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                uint32_t m = most(col_most[e], (uint32_t)__shfl_xor((int)col_most[e], 16));
-                m = most(m, (uint32_t)__shfl_xor((int)m, 32));
-                if (lane < 16) part[wave][8 * c + e] = m;
             }
             __syncthreads();
 #pragma unroll
@@ -193,17 +274,17 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
         for (int i = 0; i < 8; ++i) {
             const float inv = inverse_scale(row_byte[i]);
             if (r0 + i < a.rows)
-                store_eight(a.q + (r0 + i) * a.stride, k0, a.cols,
-                            to_f8x4<kFormat>(f[i][0] * inv, f[i][1] * inv, f[i][2] * inv, f[i][3] * inv),
-                            to_f8x4<kFormat>(f[i][4] * inv, f[i][5] * inv, f[i][6] * inv, f[i][7] * inv));
+                store_bytes(a.q + (r0 + i) * a.stride, k0, a.cols,
+                            to_f8x4<kFormat>(h[i].get(0) * inv, h[i].get(1) * inv, h[i].get(2) * inv, h[i].get(3) * inv),
+                            to_f8x4<kFormat>(h[i].get(4) * inv, h[i].get(5) * inv, h[i].get(6) * inv, h[i].get(7) * inv));
         }
         if (a.qt) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float inv = inverse_scale(col_byte[e]);
                 const u32x2 v = {
-                    to_f8x4<kFormat>(f[0][e] * inv, f[1][e] * inv, f[2][e] * inv, f[3][e] * inv),
-                    to_f8x4<kFormat>(f[4][e] * inv, f[5][e] * inv, f[6][e] * inv, f[7][e] * inv)};
+                    to_f8x4<kFormat>(h[0].get(e) * inv, h[1].get(e) * inv, h[2].get(e) * inv, h[3].get(e) * inv),
+                    to_f8x4<kFormat>(h[4].get(e) * inv, h[5].get(e) * inv, h[6].get(e) * inv, h[7].get(e) * inv)};
                 *reinterpret_cast<u32x2*>(out + (8 * c + e) * 128 + ((g ^ c) * 8)) = v;
             }
             __syncthreads();
@@ -213,16 +294,14 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
                 const int k = n * 32 + threadIdx.x / 8, p = threadIdx.x % 8, by = k / 8;
                 const u32x4 v = *reinterpret_cast<const u32x4*>(out + k * 128 + (p ^ (by >> 1)) * 16);
                 const u32x4 w = by & 1 ? u32x4{v.z, v.w, v.x, v.y} : v;
-                const int64_t col = tc * 128 + k, r = tr * 128 + 16 * p;
-                if (col < a.cols) {
-                    uint8_t* to = a.qt + col * a.stride_t;
+                const int64_t col_at = tc * 128 + k, r = tr * 128 + 16 * p;
+                if (col_at < a.cols) {
+                    uint8_t* to = a.qt + col_at * a.stride_t;
                     if (r + 16 <= a.rows) {
                         *reinterpret_cast<u32x4*>(to + r) = w;
                     } else {
-                        for (int i = 0; i < 16; ++i)
-                            if (r + i < a.rows)
-                                to[r + i] = (uint8_t)((i < 8 ? (i < 4 ? w.x : w.y) : (i < 12 ? w.z : w.w)) >>
-                                                      (8 * (i % 4)));
+                        store_bytes(to, r, a.rows, w.x, w.y);
+                        store_bytes(to, r + 8, a.rows, w.z, w.w);
                     }
                 }
             }
@@ -243,44 +322,55 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
     }
 }
 
-// One wave per 512 values of a row, eight a lane.
+// One wave per 1024 values of a row; a lane's pieces make 16 bytes of x, so that a
+// wave stores 1024 consecutive bytes at a time, past the caches.
 template <typename T, int kFormat>
 __global__ __launch_bounds__(256) void dequantize_f8_kernel(const uint8_t* q, int64_t stride,
                                                             const uint8_t* scale, T* x, int64_t rows,
                                                             int64_t cols, int64_t per_row, int shift)
 {
+    constexpr int kN = 16 / sizeof(T), kPieces = 16 / kN;
+    struct Piece {
+        uint32_t w[kN / 4];
+    };
     const int lane = threadIdx.x & 63;
-    const int64_t units = rows * per_row;
+    const int64_t units = rows * per_row, scales = (cols + 511) / 512 * 4;
     for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units;
          u += (int64_t)gridDim.x * 4) {
-        const int64_t r = u / per_row, c = u - r * per_row, k = c * 512 + lane * 8;
-        if (k >= cols) continue;
-        const Pair v = k + 8 <= cols ? load_any<Pair>(q + r * stride + k)
-                                     : load_row<Pair>(q + r * stride, k, cols);
-        const float s = scale_value(scale[(r >> shift) * (per_row * 4) + k / kF8Block]);
-        float f[8];
-        float(&lo)[4] = *reinterpret_cast<float(*)[4]>(f);
-        float(&hi)[4] = *reinterpret_cast<float(*)[4]>(f + 4);
-        from_f8x4<kFormat>(v.w[0], lo);
-        from_f8x4<kFormat>(v.w[1], hi);
-        struct Eight {
-            uint32_t w[2 * sizeof(T)];
-        } o;
+        const int64_t r = u / per_row, k0 = (u - r * per_row) * 1024 + lane * kN;
+        const uint8_t* in = q + r * stride;
+        const uint8_t* of_row = scale + (r >> shift) * scales;
+        Piece v[kPieces];
+        float s[kPieces];
 #pragma unroll
-        for (int i = 0; i < (int)(2 * sizeof(T)); ++i) {
-            if constexpr (sizeof(T) == 2)
-                o.w[i] = bf16x2_rne(f[2 * i] * s, f[2 * i + 1] * s);
-            else
-                o.w[i] = __float_as_uint(f[i] * s);
+        for (int j = 0; j < kPieces; ++j) {
+            const int64_t k = k0 + j * 64 * kN;
+            v[j] = k < cols ? load_row<Piece>(in, k, cols) : Piece{};
+            s[j] = k < cols ? scale_value(of_row[k / kF8Block]) : 0.0f;
         }
-        T* out = x + r * cols + k;
-        if (k + 8 <= cols) {
-            store_any(out, o);
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < cols)
-                    out[i] = sizeof(T) == 2 ? (T)(o.w[i / 2] >> (16 * (i % 2))) : (T)o.w[i % (2 * sizeof(T))];
+        for (int j = 0; j < kPieces; ++j) {
+            const int64_t k = k0 + j * 64 * kN;
+            float f[kN];
+#pragma unroll
+            for (int i = 0; i < kN / 4; ++i) from_f8x4<kFormat>(v[j].w[i], *reinterpret_cast<float(*)[4]>(f + 4 * i));
+            Quad o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(T) == 2)
+                    o.w[i] = bf16x2_rne(f[2 * i] * s[j], f[2 * i + 1] * s[j]);
+                else
+                    o.w[i] = __float_as_uint(f[i] * s[j]);
+            }
+            T* out = x + r * cols + k;
+            if (k + kN <= cols) {
+                stream_store_any(out, o);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kN; ++i)
+                    if (k + i < cols)
+                        out[i] = sizeof(T) == 2 ? (T)(o.w[i / 2] >> (16 * (i % 2))) : (T)o.w[i % 4];
+            }
         }
     }
 }
@@ -344,7 +434,7 @@ extern "C" int roi_dequantize_blocks(const uint8_t* q, int64_t q_stride, const u
                                         &todo))
         return st;
     if (!todo) return ok();
-    const int64_t per_row = (cols + 511) / 512;
+    const int64_t per_row = (cols + 1023) / 1024;
     const int64_t blocks = (rows * per_row + 3) / 4;
     const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
     const int shift = square ? 7 : 0;
