@@ -178,35 +178,35 @@ __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, i
     }
 }
 
-// A block takes 128 x 128 values; thread (g, c) of 16 x 16 those of rows 8 g .. 8 g + 7
-// and columns 8 c .. 8 c + 7.  The transposed bytes pass LDS: eight rows of a
-// column are a piece of 8 bytes, piece g of column k at place g ^ (k / 8), so that
-// the 16 lanes of equal g cover all banks.  The values stay as they were loaded: bf16
-// in half the registers, and so twice the blocks on a compute unit.
+// A block takes 128 x 128 values; thread (g, c) of 32 x 16 those of rows 4 g .. 4 g + 3
+// and columns 8 c .. 8 c + 7: few enough registers for four blocks on a compute unit
+// (with twice the rows a thread, and two blocks, 8192 x 18944 took 157 us).  The
+// transposed bytes pass LDS: eight rows of a column are a piece of 8 bytes, piece p of
+// column k at place p ^ (k / 8), so that a wave's writes cover all banks evenly.
 template <typename T, int kFormat, bool kSquare>
-__global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, int64_t tiles_c,
+__global__ __launch_bounds__(512) void quantize_tile_f8_kernel(QuantizeArgs a, int64_t tiles_c,
                                                                int64_t tiles)
 {
     constexpr int kWords = 2 * sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t out[128 * 128];
-    __shared__ uint32_t part[4][128];
+    __shared__ uint32_t part[8][128];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int g = threadIdx.x / 16, c = threadIdx.x % 16;
     const int64_t scales = (a.cols + 511) / 512 * 4, scales_t = (a.rows + 511) / 512 * 4;
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int64_t tr = tile / tiles_c, tc = tile - tr * tiles_c;
-        const int64_t r0 = tr * 128 + 8 * g, k0 = tc * 128 + 8 * c;
-        Held<T, 8> h[8];
+        const int64_t r0 = tr * 128 + 4 * g, k0 = tc * 128 + 8 * c;
+        Held<T, 8> h[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
             h[i] = r0 + i < a.rows ? load_held<true, T, 8>(static_cast<const T*>(a.x) + (r0 + i) * a.cols, k0, a.cols)
                                    : Held<T, 8>{};
-        uint32_t row_most[8], col_most[kWords];
+        uint32_t row_most[4], col_most[kWords];
 #pragma unroll
         for (int e = 0; e < kWords; ++e) col_most[e] = 0;
         uint32_t any = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             uint32_t m = 0;
 #pragma unroll
             for (int e = 0; e < kWords; ++e) {
@@ -224,27 +224,30 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
                                     : col_most[e % kWords];
         if (__builtin_amdgcn_ballot_w64(any >= kInfinity)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) row_most[i] = largest_finite(h[i]);
+            for (int i = 0; i < 4; ++i) row_most[i] = largest_finite(h[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 col[e] = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) col[e] = most(col[e], finite_bits(h[i].get(e)));
+                for (int i = 0; i < 4; ++i) col[e] = most(col[e], finite_bits(h[i].get(e)));
             }
         }
-        int row_byte[8], col_byte[8];
+        int row_byte[4], col_byte[8];
         if constexpr (kSquare) {
             uint32_t m = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = most(m, row_most[i]);
+            for (int i = 0; i < 4; ++i) m = most(m, row_most[i]);
             m = most_of_32(m);
             m = most(m, (uint32_t)__shfl_xor((int)m, 32));
             if (lane == 0) part[wave][0] = m;
             __syncthreads();
-            m = most(most(part[0][0], part[1][0]), most(part[2][0], part[3][0]));
+#pragma unroll
+            for (int v = 0; v < 8; ++v) m = most(m, part[v][0]);
             const int byte = scale_byte<kFormat>(m);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) row_byte[i] = col_byte[i] = byte;
+            for (int i = 0; i < 4; ++i) row_byte[i] = byte;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) col_byte[e] = byte;
             if (threadIdx.x == 0) {
                 a.scale[tr * scales + tc] = (uint8_t)byte;
                 if (a.qt) a.scale_t[tc * scales_t + tr] = (uint8_t)byte;
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
                 if (lane < 16) part[wave][8 * c + e] = m;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 row_byte[i] = scale_byte<kFormat>(most_of_16(row_most[i]));
                 if (c == 0 && r0 + i < a.rows) a.scale[(r0 + i) * scales + tc] = (uint8_t)row_byte[i];
             }
@@ -265,13 +268,15 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int k = 8 * c + e;
-                col_byte[e] = scale_byte<kFormat>(
-                    most(most(part[0][k], part[1][k]), most(part[2][k], part[3][k])));
+                uint32_t m = 0;
+#pragma unroll
+                for (int v = 0; v < 8; ++v) m = most(m, part[v][k]);
+                col_byte[e] = scale_byte<kFormat>(m);
                 if (g == 0 && k0 + e < a.cols) a.scale_t[(k0 + e) * scales_t + tr] = (uint8_t)col_byte[e];
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             const float inv = inverse_scale(row_byte[i]);
             if (r0 + i < a.rows)
                 store_bytes(a.q + (r0 + i) * a.stride, k0, a.cols,
@@ -282,16 +287,14 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float inv = inverse_scale(col_byte[e]);
-                const u32x2 v = {
-                    to_f8x4<kFormat>(h[0].get(e) * inv, h[1].get(e) * inv, h[2].get(e) * inv, h[3].get(e) * inv),
-                    to_f8x4<kFormat>(h[4].get(e) * inv, h[5].get(e) * inv, h[6].get(e) * inv, h[7].get(e) * inv)};
-                *reinterpret_cast<u32x2*>(out + (8 * c + e) * 128 + ((g ^ c) * 8)) = v;
+                *reinterpret_cast<uint32_t*>(out + (8 * c + e) * 128 + (g / 2 ^ c) * 8 + g % 2 * 4) =
+                    to_f8x4<kFormat>(h[0].get(e) * inv, h[1].get(e) * inv, h[2].get(e) * inv, h[3].get(e) * inv);
             }
             __syncthreads();
             // eight lanes a column, 16 rows each: pieces 2 p and 2 p + 1
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const int k = n * 32 + threadIdx.x / 8, p = threadIdx.x % 8, by = k / 8;
+            for (int n = 0; n < 2; ++n) {
+                const int k = n * 64 + threadIdx.x / 8, p = threadIdx.x % 8, by = k / 8;
                 const u32x4 v = *reinterpret_cast<const u32x4*>(out + k * 128 + (p ^ (by >> 1)) * 16);
                 const u32x4 w = by & 1 ? u32x4{v.z, v.w, v.x, v.y} : v;
                 const int64_t col_at = tc * 128 + k, r = tr * 128 + 16 * p;
@@ -310,12 +313,12 @@ __global__ __launch_bounds__(256) void quantize_tile_f8_kernel(QuantizeArgs a, i
         const int64_t last_c = (a.cols + 127) / 128, last_r = (a.rows + 127) / 128;
         if (tc == last_c - 1 && last_c < scales) {
             const int64_t first = kSquare ? tr : tr * 128, end = kSquare ? tr + 1 : a.rows;
-            for (int64_t r = first + threadIdx.x; r < end && r < first + 128; r += 256)
+            for (int64_t r = first + threadIdx.x; r < end && r < first + 128; r += 512)
                 for (int64_t k = last_c; k < scales; ++k) a.scale[r * scales + k] = (uint8_t)kNoScale;
         }
         if (a.qt && tr == last_r - 1 && last_r < scales_t) {
             const int64_t first = kSquare ? tc : tc * 128, end = kSquare ? tc + 1 : a.cols;
-            for (int64_t k = first + threadIdx.x; k < end && k < first + 128; k += 256)
+            for (int64_t k = first + threadIdx.x; k < end && k < first + 128; k += 512)
                 for (int64_t r = last_r; r < scales_t; ++r) a.scale_t[k * scales_t + r] = (uint8_t)kNoScale;
         }
         __syncthreads(); // the next tile's shared values
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(256) void dequantize_f8_kernel(const uint8_t* q, in
     }
 }
 
-constexpr int64_t kMostBlocks = 0xFFFFFF; // of 256 threads: a launch has fewer than 2^32
+constexpr int64_t kMostBlocks = 0x7FFFFF; // of up to 512 threads: a launch has fewer than 2^32
 
 template <typename T, int kFormat>
 void quantize_f8(const QuantizeArgs& a, bool square, hipStream_t stream)
@@ -391,10 +394,10 @@ void quantize_f8(const QuantizeArgs& a, bool square, hipStream_t stream)
     const int64_t tiles_c = (a.cols + 127) / 128, tiles = (a.rows + 127) / 128 * tiles_c;
     const dim3 grid((unsigned)(tiles < kMostBlocks ? tiles : kMostBlocks));
     if (square)
-        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, true>), grid, dim3(256), 0, stream, a,
+        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, true>), grid, dim3(512), 0, stream, a,
                            tiles_c, tiles);
     else
-        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, false>), grid, dim3(256), 0, stream, a,
+        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, false>), grid, dim3(512), 0, stream, a,
                            tiles_c, tiles);
 }
 
