@@ -492,10 +492,19 @@ int roi_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_
  *             left alone); bits 32: not looked at
  *  numel      >= 0, below 2^40 (a tensor of none is skipped)
  *  elem_offset % 4 == 0; only bits 8 use it, as they do seed and step
- *  opt        as in roi_mask_bwd_adamw
+ *  opt        as in roi_mask_bwd_adamw, in 64 bits: each of beta and 1 - beta is
+ *             rounded to fp32 once
  * No output may overlap another tensor's or an input.  State starts as zeros
  * (the scale bytes may be zeros too).
  */
+typedef struct {
+    double lr;
+    double beta1, beta2;
+    double eps;
+    double weight_decay;
+    int64_t t;
+} roi_step_params;
+
 typedef struct {
     float* param;
     const void* grad;
@@ -508,7 +517,7 @@ typedef struct {
 } roi_step_tensor;
 
 int roi_adamw_grouped(const roi_step_tensor* tensors, int count, int grad_dtype, int bits,
-                      uint64_t seed, uint64_t step, const roi_adamw_params* opt,
+                      uint64_t seed, uint64_t step, const roi_step_params* opt,
                       hipStream_t stream);
 
 /*

@@ -44,6 +44,12 @@ class AdamWParams(ctypes.Structure):
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("t", ctypes.c_int64)]
 
 
+class StepParams(ctypes.Structure):
+    """roi_step_params (include/roi.h)."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("t", ctypes.c_int64)]
+
+
 class AdamWTensor(ctypes.Structure):
     """roi_adamw_tensor (include/roi.h)."""
     _fields_ = [("grad_W_masked", ctypes.c_void_p), ("W", ctypes.c_void_p),
@@ -260,7 +266,21 @@ def mask_bwd(grad_W_masked, W, logits, n: int, m: int, tau: float = 1.0, lam: fl
 def adamw_params(lr: float, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.05,
                  t: int = 1) -> AdamWParams:
     """AdamW settings of one step (defaults: the appendix's betas and weight decay)."""
-    return AdamWParams(lr, betas[0], betas[1], eps, weight_decay, t)
+    opt = AdamWParams(lr, betas[0], betas[1], eps, weight_decay, t)
+    opt.betas = (float(betas[0]), float(betas[1]))  # the struct holds them in fp32
+    return opt
+
+
+def _step_params(opt):
+    """opt's fields as they are now, the betas in 64 bits where adamw_params was given
+    them so."""
+    b1, b2 = opt.beta1, opt.beta2
+    g1, g2 = getattr(opt, "betas", (b1, b2))
+    if ctypes.c_float(g1).value == b1:
+        b1 = g1
+    if ctypes.c_float(g2).value == b2:
+        b2 = g2
+    return StepParams(opt.lr, b1, b2, opt.eps, opt.weight_decay, opt.t)
 
 
 def mask_bwd_adamw(grad_W_masked, W, logits, exp_avg, exp_avg_sq, n: int, m: int,
@@ -961,8 +981,9 @@ def adamw_grouped(tensors, opt: AdamWParams, seed: int = 0, step: int = 0, offse
     elif offsets is not None:
         raise ValueError("the plan has its offsets")
     if plan.count:
+        params = _step_params(opt)  # alive during the call
         _call(plan.device, lib().roi_adamw_grouped, plan.address, plan.count, plan.grad_code,
-              plan.bits, seed, step, ctypes.addressof(opt))
+              plan.bits, seed, step, ctypes.addressof(params))
 
 
 def gumbel_noise(count: int, seed: int = 0, step: int = 0, elem_offset: int = 0, device="cuda",

@@ -18,9 +18,11 @@
 namespace roi {
 namespace {
 
-// A launch takes as many pieces (tensors) as 4 KiB of arguments hold; a piece is
-// given blocks by its units of 512 values, a wave each.
-constexpr int kStepPieces = 56;
+// A launch takes as many pieces (tensors) as 4 KiB of arguments hold; a piece is given
+// blocks by its units of 512 values, a wave each.
+constexpr int kStepPieces = 63;
+constexpr int kUnit = 512, kWavesOfBlock = 4;
+constexpr int64_t kMostStepBlocks = 0xFFFFFE; // of a launch
 struct StepPiece {
     float* param;
     const void* grad;
@@ -28,25 +30,31 @@ struct StepPiece {
     void* sq;
     uint8_t* avg_scale;
     uint8_t* sq_scale;
-    int64_t numel;
+    uint64_t first_numel; // the first block in the high 24 bits (all ones: no piece), the values in 40
     uint64_t offset;
+
+    __host__ __device__ int64_t numel() const { return (int64_t)(first_numel & kMaxStepValues - 1); }
+    __host__ __device__ int64_t blocks() const
+    {
+        const int64_t n = (numel() + kUnit * kWavesOfBlock - 1) / (kUnit * kWavesOfBlock);
+        return n < kMostStepBlocks ? n : kMostStepBlocks;
+    }
 };
 struct StepBatch {
-    uint32_t starts[64]; // the first block of each piece, 0xFFFFFFFF behind the last
     StepPiece p[kStepPieces];
     AdamStep adam;
     uint32_t k0, k1, step_lo, step_hi;
 };
 static_assert(sizeof(StepBatch) <= 4096, "kernel arguments");
-constexpr int kUnit = 512, kWavesOfBlock = 4;
 
+// The piece that owns this block: the last that starts at or before it.  A lane looks
+// at a piece each: a search would wait for the arguments' memory at each of its six
+// steps (61 tensors of 5001 values took 5.5 us a launch so).
 __device__ __forceinline__ int find_step_piece(const StepBatch& a, uint32_t block)
 {
-    int i = 0;
-#pragma unroll
-    for (int step = 32; step >= 1; step /= 2)
-        if (block >= a.starts[i + step]) i += step;
-    return i;
+    const int lane = threadIdx.x & 63;
+    const uint32_t first = lane < kStepPieces ? (uint32_t)(a.p[lane].first_numel >> 40) : 0xFFFFFFu;
+    return __builtin_popcountll(__builtin_amdgcn_ballot_w64(first <= block)) - 1;
 }
 
 // Values k .. k + 3 of n; zeros past the end.
@@ -113,16 +121,14 @@ __device__ __forceinline__ int round_by(float t, uint32_t word, int old)
 template <typename G, int kBits>
 __global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
 {
-    const int i = find_step_piece(a, blockIdx.x);
-    const StepPiece& p = a.p[i];
-    const uint32_t first = a.starts[i];
-    const uint32_t last = i + 1 < 64 ? a.starts[i + 1] : 0xFFFFFFFFu;
-    const uint32_t blocks = (last == 0xFFFFFFFFu ? gridDim.x : last) - first;
+    const int i = __builtin_amdgcn_readfirstlane(find_step_piece(a, blockIdx.x));
+    const StepPiece p = a.p[i];
+    const uint32_t first = (uint32_t)(p.first_numel >> 40);
     const int lane = threadIdx.x & 63;
-    const int64_t n = p.numel, units = (n + kUnit - 1) / kUnit;
+    const int64_t n = p.numel(), units = (n + kUnit - 1) / kUnit, blocks = p.blocks();
     const G* grad = static_cast<const G*>(p.grad);
     for (int64_t u = (int64_t)(blockIdx.x - first) * kWavesOfBlock + (threadIdx.x >> 6); u < units;
-         u += (int64_t)blocks * kWavesOfBlock) {
+         u += blocks * kWavesOfBlock) {
         const int64_t k0 = u * kUnit + 4 * lane;
         f32x4 par[2], g[2];
 #pragma unroll
@@ -230,7 +236,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
 using StepFn = void (*)(StepBatch);
 
 int adamw_run(const roi_step_tensor* t, int count, int grad_dtype, int bits, uint64_t seed,
-              uint64_t step, const roi_adamw_params* opt, hipStream_t stream)
+              uint64_t step, const roi_step_params* opt, hipStream_t stream)
 {
     StepBatch b{};
     bool todo;
@@ -242,12 +248,11 @@ int adamw_run(const roi_step_tensor* t, int count, int grad_dtype, int bits, uin
     b.k1 = (uint32_t)(seed >> 32);
     b.step_lo = (uint32_t)step;
     b.step_hi = (uint32_t)(step >> 32);
-    constexpr int64_t kMost = 0xFFFFFF; // blocks of a launch
     int pieces = 0;
     int64_t blocks = 0;
     auto flush = [&]() -> int {
         if (pieces == 0) return ROI_OK;
-        for (int i = pieces; i < 64; ++i) b.starts[i] = 0xFFFFFFFFu;
+        for (int i = pieces; i < kStepPieces; ++i) b.p[i].first_numel = ~(uint64_t)0;
         hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(64 * kWavesOfBlock), 0, stream, b);
         pieces = 0;
         blocks = 0;
@@ -255,15 +260,13 @@ int adamw_run(const roi_step_tensor* t, int count, int grad_dtype, int bits, uin
     };
     for (int i = 0; i < count; ++i) {
         if (t[i].numel == 0) continue;
-        const int64_t units = (t[i].numel + kUnit - 1) / kUnit;
-        int64_t need = (units + kWavesOfBlock - 1) / kWavesOfBlock;
-        if (need > kMost) need = kMost;
-        if (pieces == kStepPieces || blocks + need > kMost)
+        StepPiece p{t[i].param,     t[i].grad,     t[i].exp_avg,          t[i].exp_avg_sq,
+                    t[i].avg_scale, t[i].sq_scale, (uint64_t)t[i].numel, t[i].elem_offset};
+        if (pieces == kStepPieces || blocks + p.blocks() > kMostStepBlocks)
             if (int st = flush()) return st;
-        b.starts[pieces] = (uint32_t)blocks;
-        b.p[pieces++] = StepPiece{t[i].param,     t[i].grad,     t[i].exp_avg, t[i].exp_avg_sq,
-                                  t[i].avg_scale, t[i].sq_scale, t[i].numel,   t[i].elem_offset};
-        blocks += need;
+        p.first_numel |= (uint64_t)blocks << 40;
+        blocks += p.blocks();
+        b.p[pieces++] = p;
     }
     return flush();
 }
@@ -274,7 +277,7 @@ int adamw_run(const roi_step_tensor* t, int count, int grad_dtype, int bits, uin
 using namespace roi;
 
 extern "C" int roi_adamw_grouped(const roi_step_tensor* tensors, int count, int grad_dtype, int bits,
-                                 uint64_t seed, uint64_t step, const roi_adamw_params* opt,
+                                 uint64_t seed, uint64_t step, const roi_step_params* opt,
                                  hipStream_t stream)
 {
     try {

@@ -107,7 +107,7 @@ struct QuantizeArgs {
 
 // Blocks of rows: a wave takes kUnits times 512 consecutive values of a row (four
 // blocks, one word of scales), 16 bytes a lane and load.
-template <typename T, int kFormat>
+template <typename T, int kFormat, bool kStream>
 __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, int64_t per_row)
 {
     constexpr int kUnits = 4, kN = 16 / sizeof(T), kLoads = 512 / (64 * kN);
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, i
 #pragma unroll
                 for (int l = 0; l < kLoads; ++l) {
                     const int64_t k = c * 512 + (l * 64 + lane) * kN;
-                    h[i][l] = load_held<true, T, kN>(static_cast<const T*>(a.x) + r * a.cols, k, a.cols);
+                    h[i][l] = load_held<kStream, T, kN>(static_cast<const T*>(a.x) + r * a.cols, k, a.cols);
                 }
             }
             if (++c == per_row) {
@@ -183,13 +183,14 @@ __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, i
 // (with twice the rows a thread, and two blocks, 8192 x 18944 took 157 us).  The
 // transposed bytes pass LDS: eight rows of a column are a piece of 8 bytes, piece p of
 // column k at place p ^ (k / 8), so that a wave's writes cover all banks evenly.
-template <typename T, int kFormat, bool kSquare>
+template <typename T, int kFormat, bool kSquare, bool kStream>
 __global__ __launch_bounds__(512) void quantize_tile_f8_kernel(QuantizeArgs a, int64_t tiles_c,
                                                                int64_t tiles)
 {
     constexpr int kWords = 2 * sizeof(T);
     __shared__ __attribute__((aligned(16))) uint8_t out[128 * 128];
     __shared__ uint32_t part[8][128];
+    __shared__ __attribute__((aligned(8))) uint8_t of_column[128];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int g = threadIdx.x / 16, c = threadIdx.x % 16;
     const int64_t scales = (a.cols + 511) / 512 * 4, scales_t = (a.rows + 511) / 512 * 4;
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(512) void quantize_tile_f8_kernel(QuantizeArgs a, i
         Held<T, 8> h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            h[i] = r0 + i < a.rows ? load_held<true, T, 8>(static_cast<const T*>(a.x) + (r0 + i) * a.cols, k0, a.cols)
+            h[i] = r0 + i < a.rows ? load_held<kStream, T, 8>(static_cast<const T*>(a.x) + (r0 + i) * a.cols, k0, a.cols)
                                    : Held<T, 8>{};
         uint32_t row_most[4], col_most[kWords];
 #pragma unroll
@@ -237,8 +238,7 @@ __global__ __launch_bounds__(512) void quantize_tile_f8_kernel(QuantizeArgs a, i
             uint32_t m = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) m = most(m, row_most[i]);
-            m = most_of_32(m);
-            m = most(m, (uint32_t)__shfl_xor((int)m, 32));
+            m = most_with_32(most_of_32(m));
             if (lane == 0) part[wave][0] = m;
             __syncthreads();
 #pragma unroll
@@ -255,8 +255,7 @@ __global__ __launch_bounds__(512) void quantize_tile_f8_kernel(QuantizeArgs a, i
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                uint32_t m = most(col[e], (uint32_t)__shfl_xor((int)col[e], 16));
-                m = most(m, (uint32_t)__shfl_xor((int)m, 32));
+                const uint32_t m = most_with_32(most_with_16(col[e]));
                 if (lane < 16) part[wave][8 * c + e] = m;
             }
 #pragma unroll
@@ -265,15 +264,21 @@ __global__ __launch_bounds__(512) void quantize_tile_f8_kernel(QuantizeArgs a, i
                 if (c == 0 && r0 + i < a.rows) a.scale[(r0 + i) * scales + tc] = (uint8_t)row_byte[i];
             }
             __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int k = 8 * c + e;
+            // a column's by one thread: all of a column's threads reading the eight waves'
+            // took 8192 x 18944 from 113 us to 147
+            if (threadIdx.x < 128) {
                 uint32_t m = 0;
 #pragma unroll
-                for (int v = 0; v < 8; ++v) m = most(m, part[v][k]);
-                col_byte[e] = scale_byte<kFormat>(m);
-                if (g == 0 && k0 + e < a.cols) a.scale_t[(k0 + e) * scales_t + tr] = (uint8_t)col_byte[e];
+                for (int v = 0; v < 8; ++v) m = most(m, part[v][threadIdx.x]);
+                const int byte = scale_byte<kFormat>(m);
+                of_column[threadIdx.x] = (uint8_t)byte;
+                const int64_t k = tc * 128 + threadIdx.x;
+                if (k < a.cols) a.scale_t[k * scales_t + tr] = (uint8_t)byte;
             }
+            __syncthreads();
+            const u32x2 bytes = *reinterpret_cast<const u32x2*>(of_column + 8 * c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) col_byte[e] = (e < 4 ? bytes.x : bytes.y) >> (8 * (e % 4)) & 255;
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -380,13 +385,18 @@ __global__ __launch_bounds__(256) void dequantize_f8_kernel(const uint8_t* q, in
 
 constexpr int64_t kMostBlocks = 0x7FFFFF; // of up to 512 threads: a launch has fewer than 2^32
 
-template <typename T, int kFormat>
-void quantize_f8(const QuantizeArgs& a, bool square, hipStream_t stream)
+// Past the caches where x is larger than the 256 MB behind all L2s: 8192 x 18944 (310 MB)
+// takes 132 us so with its transposed copy and 137 through them, 8192 x 3584, which
+// what made it left there, 30 and 26.
+constexpr int64_t kCached = (int64_t)1 << 28;
+
+template <typename T, int kFormat, bool kStream>
+void quantize_f8_as(const QuantizeArgs& a, bool square, hipStream_t stream)
 {
     if (!square && !a.qt) {
         const int64_t per_row = (a.cols + 511) / 512;
         const int64_t blocks = (a.rows * per_row + 15) / 16;
-        hipLaunchKernelGGL((quantize_rows_f8_kernel<T, kFormat>),
+        hipLaunchKernelGGL((quantize_rows_f8_kernel<T, kFormat, kStream>),
                            dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0,
                            stream, a, per_row);
         return;
@@ -394,11 +404,19 @@ void quantize_f8(const QuantizeArgs& a, bool square, hipStream_t stream)
     const int64_t tiles_c = (a.cols + 127) / 128, tiles = (a.rows + 127) / 128 * tiles_c;
     const dim3 grid((unsigned)(tiles < kMostBlocks ? tiles : kMostBlocks));
     if (square)
-        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, true>), grid, dim3(512), 0, stream, a,
-                           tiles_c, tiles);
+        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, true, kStream>), grid, dim3(512), 0,
+                           stream, a, tiles_c, tiles);
     else
-        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, false>), grid, dim3(512), 0, stream, a,
-                           tiles_c, tiles);
+        hipLaunchKernelGGL((quantize_tile_f8_kernel<T, kFormat, false, kStream>), grid, dim3(512), 0,
+                           stream, a, tiles_c, tiles);
+}
+template <typename T, int kFormat>
+void quantize_f8(const QuantizeArgs& a, bool square, hipStream_t stream)
+{
+    if (a.rows * a.cols > kCached / (int64_t)sizeof(T))
+        quantize_f8_as<T, kFormat, true>(a, square, stream);
+    else
+        quantize_f8_as<T, kFormat, false>(a, square, stream);
 }
 
 } // namespace

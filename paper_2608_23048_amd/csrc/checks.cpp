@@ -100,31 +100,40 @@ int check_count(const void* t, int count)
     return ROI_OK;
 }
 
-int check_adamw(const roi_adamw_params* o, AdamStep* st)
+namespace {
+
+// Params: roi_adamw_params or roi_step_params.
+template <typename Params>
+int fold_adamw(const Params* o, AdamStep* st)
 {
     if (!o) return fail(ROI_E_INVAL, "the AdamW parameters must not be NULL");
-    if (!(o->lr >= 0.0f) || !std::isfinite(o->lr))
+    // in fp32, which the step is taken in
+    if (!(o->lr >= 0) || !std::isfinite((float)o->lr))
         return fail(ROI_E_INVAL, "AdamW lr must be finite and >= 0");
-    if (!(o->beta1 >= 0.0f && o->beta1 < 1.0f) || !(o->beta2 >= 0.0f && o->beta2 < 1.0f))
+    if (!(o->beta1 >= 0 && o->beta1 < 1) || !(o->beta2 >= 0 && o->beta2 < 1))
         return fail(ROI_E_INVAL, "AdamW betas must lie in [0, 1)");
-    if (!(o->eps > 0.0f) || !std::isfinite(o->eps))
+    if (!((float)o->eps > 0) || !std::isfinite((float)o->eps))
         return fail(ROI_E_INVAL, "AdamW eps must be finite and > 0");
-    if (!(o->weight_decay >= 0.0f) || !std::isfinite(o->weight_decay))
+    if (!(o->weight_decay >= 0) || !std::isfinite((float)o->weight_decay))
         return fail(ROI_E_INVAL, "AdamW weight_decay must be finite and >= 0");
     if (o->t < 1) return fail(ROI_E_INVAL, "AdamW step count t must be >= 1");
     const double lr = o->lr, b1 = o->beta1, b2 = o->beta2;
     const double bc1 = 1.0 - std::pow(b1, (double)o->t);
     const double bc2 = 1.0 - std::pow(b2, (double)o->t);
     st->decay = (float)(1.0 - lr * (double)o->weight_decay);
-    st->beta1 = o->beta1;
-    st->beta2 = o->beta2;
+    st->beta1 = (float)b1;
+    st->beta2 = (float)b2;
     st->one_m_beta1 = (float)(1.0 - b1);
     st->one_m_beta2 = (float)(1.0 - b2);
     st->step_size = (float)(lr / bc1);
     st->inv_sqrt_bc2 = (float)(1.0 / std::sqrt(bc2));
-    st->eps = o->eps;
+    st->eps = (float)o->eps;
     return ROI_OK;
 }
+
+} // namespace
+
+int check_adamw(const roi_adamw_params* o, AdamStep* st) { return fold_adamw(o, st); }
 
 int validate_fwd(const roi_fwd_tensor* t, int count, int n, int m, float tau, float lambda,
                  int* with_s, int* with_idx)
@@ -651,13 +660,13 @@ int validate_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, i
 }
 
 int validate_step(const roi_step_tensor* t, int count, int grad_dtype, int bits,
-                  const roi_adamw_params* opt, AdamStep* step, bool* todo)
+                  const roi_step_params* opt, AdamStep* step, bool* todo)
 {
     *todo = false;
     if (int st = check_dtype(grad_dtype)) return st;
     if (bits != 8 && bits != 32)
         return fail(ROI_E_INVAL, "the moments' bits must be 8 or 32 (got %d)", bits);
-    if (int st = check_adamw(opt, step)) return st;
+    if (int st = fold_adamw(opt, step)) return st;
     if (int st = check_count(t, count)) return st;
     std::vector<Range> ranges;
     ranges.reserve((size_t)count * 6);

@@ -202,7 +202,7 @@ int validate_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, i
 // are empty.
 constexpr int64_t kMaxStepValues = (int64_t)1 << 40;
 int validate_step(const roi_step_tensor* t, int count, int grad_dtype, int bits,
-                  const roi_adamw_params* opt, AdamStep* step, bool* todo);
+                  const roi_step_params* opt, AdamStep* step, bool* todo);
 
 // Calls launch(first, count, elem0) for consecutive pieces of [0, items) --
 // items of `per_item` elements starting at global element elem_offset -- so

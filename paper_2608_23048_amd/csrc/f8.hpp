@@ -88,11 +88,20 @@ __device__ __forceinline__ uint32_t most_of_16(uint32_t v)
     v = most_with_rotated<2>(v);
     return most_with_rotated<1>(v);
 }
-// And over the 32 lanes of a half wave (lane ^ 16 by swizzle: xor mask in bits 10..).
-__device__ __forceinline__ uint32_t most_of_32(uint32_t v)
+// The larger of this lane's and that of lane ^ 16, and of lane ^ 32: both swap
+// instructions of a value with itself leave it in one result and the other lane's in the
+// other.
+__device__ __forceinline__ uint32_t most_with_16(uint32_t v)
 {
-    v = most_of_16(v);
-    return most(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x401F));
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return most(s[0], s[1]);
 }
+__device__ __forceinline__ uint32_t most_with_32(uint32_t v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return most(s[0], s[1]);
+}
+// The largest over the 32 lanes of a half wave, in all of them.
+__device__ __forceinline__ uint32_t most_of_32(uint32_t v) { return most_with_16(most_of_16(v)); }
 
 } // namespace roi

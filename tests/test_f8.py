@@ -12,6 +12,8 @@ The optimizer's tolerances count its roundings where they are used.
 """
 from __future__ import annotations
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -124,8 +126,7 @@ def step_call(L, bits=8, count=1, grad=1, opt=None, other=None, null=False, **kw
         fields += [b[k] for k in keys]
         count = 2
     arr = roi._descriptors(fields)
-    opt = roi.adamw_params(1e-3) if opt is None else opt
-    import ctypes
+    opt = roi._step_params(roi.adamw_params(1e-3) if opt is None else opt)
     return L.roi_adamw_grouped(None if null else ctypes.addressof(arr), count, grad, bits, 0, 0,
                                ctypes.addressof(opt), None)
 
@@ -629,13 +630,14 @@ def value_of(q, s, n):
 
 def step_ref(p, g, m, v, opt):
     """The step in fp64 from the fp32 constants, with the errors that fp32 may make."""
-    b1, b2 = opt.beta1, opt.beta2
-    o1, o2 = f32(1.0 - b1), f32(1.0 - b2)
+    p64 = roi._step_params(opt)
+    b1, b2 = f32(p64.beta1), f32(p64.beta2)
+    o1, o2 = f32(1.0 - p64.beta1), f32(1.0 - p64.beta2)
     m1 = b1 * m + o1 * g
     v1 = b2 * v + o2 * g * g
     em = 2.0 ** -23 * ((b1 * m).abs() + (o1 * g).abs()) + 2.0 ** -149
     root = v1.sqrt()
-    c1, c2 = 1 - opt.beta1 ** opt.t, 1 - opt.beta2 ** opt.t
+    c1, c2 = 1 - p64.beta1 ** opt.t, 1 - p64.beta2 ** opt.t
     den = root / c2 ** 0.5 + opt.eps
     up = opt.lr / c1 * m1 / den
     p1 = p * (1 - opt.lr * opt.weight_decay) - up
@@ -725,11 +727,12 @@ def test_step_in_32_bits(grad_dtype):
 
 @pytest.mark.gpu
 def test_step_is_the_fused_one():
-    """On the gradient that the sampler's backward writes, the step gives the fused call's state."""
+    """On the gradient that the sampler's backward writes, the step gives the fused call's
+    state, with betas that fp32 holds (that call takes them so)."""
     from paper_2608_23048_amd import workloads as wl
     W, phi, G = wl.small_case(64, 128, 5, device=torch.device("cuda"))
     m, v = torch.rand_like(phi) * 1e-4, torch.rand_like(phi) * 1e-8
-    opt = roi.adamw_params(**OPT)
+    opt = roi.adamw_params(2.0 ** -9, (0.875, 0.9375), 2.0 ** -26, 0.0625, t=3)
     a = [t.clone() for t in (phi, m, v)]
     d = torch.empty_like(phi)
     roi.mask_bwd_adamw(G, W, *a, 2, 4, 0.5, 1.0, 1, 2, opt=opt, grad_out=d)
@@ -874,6 +877,18 @@ def test_step_refusals():
         with pytest.raises(kind):
             call()
     roi.adamw_grouped([], opt)
+
+
+def test_settings_of_a_step():
+    """Betas as they were given, unless the struct's were changed since."""
+    opt = roi.adamw_params(1e-3, (0.9, 0.95), t=2)
+    s = roi._step_params(opt)
+    assert (s.beta1, s.beta2, s.t) == (0.9, 0.95, 2)
+    opt.beta1, opt.t, opt.lr = 0.5, 3, 0.25
+    s = roi._step_params(opt)
+    assert (s.beta1, s.beta2, s.t, s.lr) == (0.5, 0.95, 3, 0.25)
+    plain = roi.AdamWParams(0.25, 0.9, 0.95, 1e-8, 0.0, 1)
+    assert roi._step_params(plain).beta1 == f32(0.9)
 
 
 # ------------------------------------------------------------- a training step
