@@ -43,6 +43,7 @@ struct StepPiece {
 struct StepBatch {
     StepPiece p[kStepPieces];
     AdamStep adam;
+    float beta1_rest, one_m_beta1_rest; // what adam.beta1 and one_m_beta1 lack
     uint32_t k0, k1, step_lo, step_hi;
 };
 static_assert(sizeof(StepBatch) <= 4096, "kernel arguments");
@@ -118,6 +119,17 @@ __device__ __forceinline__ int round_by(float t, uint32_t word, int old)
     return __builtin_amdgcn_cvt_sr_fp8_f32(t, (int)word, old, kByte);
 }
 
+// m' = beta1 m + (1 - beta1) g to half a rounding: a value's error is what turns its
+// 8-bit neighbours about.  The product's remainder and the sum's, and what the factors
+// lost to fp32, are added last.
+__device__ __forceinline__ float mixed(const StepBatch& a, float m, float g)
+{
+    const float p = a.adam.one_m_beta1 * g;
+    const float sum = __builtin_fmaf(a.adam.beta1, m, p);
+    const float rest = __builtin_fmaf(a.adam.beta1, m, p - sum) + __builtin_fmaf(a.adam.one_m_beta1, g, -p);
+    return sum + __builtin_fmaf(a.beta1_rest, m, __builtin_fmaf(a.one_m_beta1_rest, g, rest));
+}
+
 template <typename G, int kBits>
 __global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
 {
@@ -180,23 +192,36 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
                 from_f8x4<ROI_E4M3>(mq[j], m);
                 from_f8x4<ROI_E4M3>(rq[j], r);
                 const float m_scale = scale_value(ms[j]), r_scale = scale_value(rs[j]);
-                uint32_t m_most = 0, r_most = 0;
+                uint32_t m_most = 0, r_most = 0; // what is not finite above every number
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float root = r[e] * r_scale;
-                    m[e] = __builtin_fmaf(a.adam.beta1, m[e] * m_scale, a.adam.one_m_beta1 * g[j][e]);
+                    m[e] = mixed(a, m[e] * m_scale, g[j][e]);
                     const float v = __builtin_fmaf(a.adam.beta2, root * root,
                                                    a.adam.one_m_beta2 * (g[j][e] * g[j][e]));
                     r[e] = __builtin_amdgcn_sqrtf(v);
                     const float den = __builtin_fmaf(r[e], a.adam.inv_sqrt_bc2, a.adam.eps);
                     par[j][e] = __builtin_fmaf(-a.adam.step_size * m[e], __builtin_amdgcn_rcpf(den),
                                                par[j][e] * a.adam.decay);
-                    m_most = most(m_most, finite_bits(m[e]));
-                    r_most = most(r_most, finite_bits(r[e]));
+                    m_most = most(m_most, __float_as_uint(m[e]) & 0x7FFFFFFFu);
+                    r_most = most(r_most, __float_as_uint(r[e]));
                 }
                 store_four(p.param, k0 + 256 * j, n, par[j]);
-                ms[j] = scale_byte<ROI_E4M3>(most_of_32(m_most));
-                rs[j] = scale_byte<ROI_E4M3>(most_of_32(r_most));
+                m_most = most_of_32(m_most);
+                r_most = most_of_32(r_most);
+                const bool finite = __builtin_amdgcn_ballot_w64(most(m_most, r_most) >= kInfinity) == 0;
+                if (!finite) {
+                    m_most = r_most = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        m_most = most(m_most, finite_bits(m[e]));
+                        r_most = most(r_most, finite_bits(r[e]));
+                    }
+                    m_most = most_of_32(m_most);
+                    r_most = most_of_32(r_most);
+                }
+                ms[j] = scale_byte<ROI_E4M3>(m_most);
+                rs[j] = scale_byte<ROI_E4M3>(r_most);
                 const float m_inv = inverse_scale(ms[j]), r_inv = inverse_scale(rs[j]);
                 const uint64_t block = (p.offset + (uint64_t)(k0 + 256 * j)) >> 2;
                 const uint4 word = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), a.step_lo,
@@ -217,10 +242,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
                 ro = round_by<1>(s[1], bits[1], ro);
                 ro = round_by<2>(s[2], bits[2], ro);
                 ro = round_by<3>(s[3], bits[3], ro);
+                if (!finite) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                  for (int e = 0; e < 4; ++e) {
                     if (!(__builtin_fabsf(m[e]) < __builtin_inff())) mo = (mo & ~(255 << (8 * e))) | 127 << (8 * e);
                     if (!(r[e] < __builtin_inff())) ro = (ro & ~(255 << (8 * e))) | 127 << (8 * e);
+                  }
                 }
                 store_four(avg, k0 + 256 * j, n, (uint32_t)mo);
                 store_four(sq, k0 + 256 * j, n, (uint32_t)ro);
@@ -244,6 +271,8 @@ int adamw_run(const roi_step_tensor* t, int count, int grad_dtype, int bits, uin
     if (!todo) return ok();
     const StepFn fn = bits == 8 ? (grad_dtype == ROI_FP32 ? adamw_kernel<float, 8> : adamw_kernel<uint16_t, 8>)
                                 : (grad_dtype == ROI_FP32 ? adamw_kernel<float, 32> : adamw_kernel<uint16_t, 32>);
+    b.beta1_rest = (float)(opt->beta1 - (double)b.adam.beta1);
+    b.one_m_beta1_rest = (float)(1.0 - opt->beta1 - (double)b.adam.one_m_beta1);
     b.k0 = (uint32_t)seed;
     b.k1 = (uint32_t)(seed >> 32);
     b.step_lo = (uint32_t)step;
