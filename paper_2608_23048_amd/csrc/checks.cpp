@@ -576,21 +576,80 @@ int check_f8_sizes(int64_t rows, int64_t cols)
 
 } // namespace
 
+namespace {
+
+// The 8-bit floats' tiles, which a block goes through without a pause: microseconds of
+// a step of `blocks` tiles at a time (the clock falls as units fill), of a tile's results
+// beside the next one's steps, and of the launch with its first loads and last
+// results.  Fitted to 32 products of 33 to 18944 tokens, each in whole tiles of both
+// sizes and in all numbers of parts; expected within 8 % of 1024 x 18944 x 3584 (256-tiles
+// in four parts 75.8 us, whole 84.7, 128-tiles 91) and of 256 x 3584 x 3584 (128-tiles 17.4,
+// 256-tiles in eight parts 24.5, the streaming kernel 16).
+double f8_step_us(int tile, int64_t blocks)
+{
+    const double b = (double)blocks / (double)kUnits;
+    if (tile == 256) return 1.05 + 0.40 * b;
+    return b <= 1 ? 0.40 + 0.12 * b : 0.92 + 0.18 * (b - 1);
+}
+constexpr double kF8Launch[2] = {10, 5.5}, kF8Result[2] = {4, 0.8}, kF8SumUs = 4;
+constexpr double kF8PartBytesPerUs = 4.5e6; // as kPartBytesPerUs
+
+// One tile size: the last round's tiles are cut as in cut_tiles.
+Cut cut_f8(int64_t m, int64_t n, int64_t k, int tile)
+{
+    Cut c{};
+    c.tile = tile;
+    c.tm = (m + tile - 1) / tile;
+    c.tn = (n + tile - 1) / tile;
+    c.steps = (k + 127) / 128;
+    const int64_t tiles = c.tm * c.tn, slots = kUnits * (tile == 256 ? 1 : 2), rest = tiles % slots;
+    const int small = tile == 128;
+    const double rounds = (double)(tiles / slots) * ((double)c.steps * f8_step_us(tile, slots) + kF8Result[small]) +
+                          kF8Launch[small];
+    c.full = tiles;
+    c.splits = 1;
+    c.us = rounds + (rest ? (double)c.steps * f8_step_us(tile, rest) : 0);
+    const int64_t most = rest ? std::min(std::min(slots / rest, c.steps / 2), kMostSplits) : 0;
+    for (int64_t splits = 2; splits <= most; ++splits) {
+        const int64_t bytes = rest * splits * tile * tile * 4;
+        const double us = rounds + (double)((c.steps + splits - 1) / splits) * f8_step_us(tile, rest * splits) +
+                          (double)bytes / kF8PartBytesPerUs + kF8SumUs + kSumPartUs * (double)splits;
+        if (us < c.us) {
+            c.us = us;
+            c.full = tiles - rest;
+            c.splits = splits;
+            c.bytes = bytes;
+        }
+    }
+    // blocks are counted in 32 bits
+    c.fits = c.full + rest * c.splits < ((int64_t)1 << 31);
+    return c;
+}
+
+// The streaming kernel's expected time, as few_us: 64 tokens through 3584 x 3584 take
+// 6.7 us so and 14.2 in tiles, 128 through 18944 x 3584 44 and 18.
+double f8_few_us(int64_t tokens, int64_t rows, int64_t cols)
+{
+    const int64_t groups = (tokens + 31) / 32;
+    const double blocks = (double)((rows + 31) / 32) * (double)groups;
+    const double weight = (double)rows * (double)cols;
+    return 2.2 + blocks * 1.2 / 512 + weight / 5.0e6 + (double)(groups - 1) * weight / 9.5e6;
+}
+
+} // namespace
+
 LinearPlan plan_linear_f8(int64_t tokens, int64_t rows, int64_t cols)
 {
     LinearPlan p{};
     p.few = tokens <= 32 || cols == 0;
     if (p.few) return p;
     p.row = cols;
-    p.cut = cut_product(rows, tokens, cols, 128, kF8Cost);
-    double tiles_us = p.cut.us;
+    const Cut big = cut_f8(rows, tokens, cols, 256), small = cut_f8(rows, tokens, cols, 128);
+    p.cut = small.us < big.us && small.fits ? small : big;
     // few tiles: their steps may be less work than reading the weight
-    if (tokens <= 128)
-        tiles_us += std::max(0.0, (double)rows * (double)cols / 5.0e6 -
-                                      (double)(p.cut.steps / p.cut.splits) * kF8Cost.step128);
-    p.bytes = p.cut.bytes;
-    p.few = tokens <= 1024 && few_us(tokens, rows, cols / 16 * 16, false) < tiles_us;
-    if (p.few) p.bytes = 0;
+    const double weight_us = (double)rows * (double)cols / 5.0e6;
+    p.few = tokens <= 1024 && f8_few_us(tokens, rows, cols) < std::max(p.cut.us, weight_us);
+    if (!p.few) p.bytes = p.cut.bytes;
     return p;
 }
 

@@ -184,7 +184,6 @@ int validate_grad_i8(const uint16_t* grad_y, const int8_t* q, const float* scale
 constexpr int64_t kMaxStride = kMaxLinearDim;
 // A product's way: with few tokens the kernel that streams the weight past them
 // (no workspace), else tiles, the parts of cut ones in the workspace.
-constexpr TileCost kF8Cost = {1.36, 9, 0.39, 0.80, 5.5};
 LinearPlan plan_linear_f8(int64_t tokens, int64_t rows, int64_t cols);
 int validate_quantize_f8(const void* x, int dtype, int64_t rows, int64_t cols, bool square, int format,
                          const uint8_t* q, int64_t q_stride, const uint8_t* scale, const uint8_t* qt,
