@@ -960,8 +960,16 @@ class AdamWPlan:
 
 def adamw_plan(tensors, offsets=None) -> AdamWPlan:
     """Checks adamw_grouped's list of tensors once and keeps it: what a training loop
-    whose gradients stay in place passes to each step instead of the list."""
-    return AdamWPlan(tensors, offsets)
+    whose gradients stay in place passes to each step instead of the list.  It steps the
+    memory that they had then: a tensor given new memory (``p.data = ...``, a gradient
+    set to None) needs a new plan."""
+    plan = AdamWPlan(tensors, offsets)
+
+    def alias(t):  # keeps the memory that the descriptors point into
+        return t.detach() if isinstance(t, _torch.Tensor) else tuple(map(alias, t))
+
+    plan.tensors = [tuple(map(alias, t)) for t in plan.tensors]
+    return plan
 
 
 def adamw_grouped(tensors, opt: AdamWParams, seed: int = 0, step: int = 0, offsets=None):

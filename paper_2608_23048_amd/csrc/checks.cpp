@@ -642,14 +642,19 @@ LinearPlan plan_linear_f8(int64_t tokens, int64_t rows, int64_t cols)
 {
     LinearPlan p{};
     p.few = tokens <= 32 || cols == 0;
-    if (p.few) return p;
-    p.row = cols;
-    const Cut big = cut_f8(rows, tokens, cols, 256), small = cut_f8(rows, tokens, cols, 128);
-    p.cut = small.us < big.us && small.fits ? small : big;
-    // few tiles: their steps may be less work than reading the weight
-    const double weight_us = (double)rows * (double)cols / 5.0e6;
-    p.few = tokens <= 1024 && f8_few_us(tokens, rows, cols) < std::max(p.cut.us, weight_us);
-    if (!p.few) p.bytes = p.cut.bytes;
+    if (!p.few) {
+        const Cut big = cut_f8(rows, tokens, cols, 256), small = cut_f8(rows, tokens, cols, 128);
+        p.cut = small.us < big.us && small.fits ? small : big;
+        // few tiles: their steps may be less work than reading the weight
+        const double weight_us = (double)rows * (double)cols / 5.0e6;
+        p.few = tokens <= 1024 && f8_few_us(tokens, rows, cols) < std::max(p.cut.us, weight_us);
+    }
+    if (p.few) {
+        p.cut = Cut{};
+        // blocks of 256 threads, a launch having fewer than 2^32
+        p.cut.fits = (rows + 15) / 16 * ((tokens + 31) / 32) < (1 << 24);
+    }
+    p.bytes = p.cut.bytes;
     return p;
 }
 

@@ -610,7 +610,7 @@ void launch_f8_few_as(LinearF8Args a, hipStream_t stream)
 {
     const int64_t tm = ((int64_t)a.rows + 16 * kRow - 1) / (16 * kRow);
     const int64_t tn = ((int64_t)a.tokens + kTokens - 1) / kTokens;
-    a.grid.tm = (uint32_t)tm; // few tokens and fewer than 2^22 rows: a launch has room
+    a.grid.tm = (uint32_t)tm;
     hipLaunchKernelGGL((linear_f8_few_kernel<kRow, kTokens, kDepth, kFormat>), dim3((unsigned)(tm * tn)),
                        dim3(256), 0, stream, a);
 }
@@ -647,8 +647,7 @@ void launch_f8(LinearF8Args a, const LinearPlan& plan, void* workspace, hipStrea
 
 int check_f8_fits(const LinearPlan& plan)
 {
-    return plan.few || plan.cut.fits ? ROI_OK
-                                     : fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
+    return plan.cut.fits ? ROI_OK : fail(ROI_E_UNSUPPORTED, "y has too many elements for one call");
 }
 
 } // namespace
