@@ -4,7 +4,8 @@
 // E from the largest finite magnitude of 128 (or 128 x 128) values, q = x 2^(127 - E)
 // rounded by the conversion instruction (to nearest, ties to even): some ten
 // instructions a value.  Bound by HBM: a value is read once (2 or 4 bytes) and
-// written once a copy (1 byte).
+// written once a copy (1 byte).  8192 x 18944 in bf16: blocks of rows 70 to 89 us (6.6
+// to 5.2 TB/s), restored in 66, with the transposed copy 129 to 136, square 118 to 129.
 #include <hip/hip_runtime.h>
 
 #include "f8.hpp"
