@@ -493,7 +493,8 @@ int roi_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_
  *  numel      >= 0, below 2^40 (a tensor of none is skipped)
  *  elem_offset % 4 == 0; only bits 8 use it, as they do seed and step
  *  opt        as in roi_mask_bwd_adamw, in 64 bits: each of beta and 1 - beta is
- *             rounded to fp32 once.  It is read during the call, as `tensors` are: a
+ *             rounded to fp32 once; eps is at least 2^-126, and second moments
+ *             below that may be taken for 0.  It is read during the call, as `tensors` are: a
  *             captured call replays with the settings, seed and step it was given
  * No output may overlap another tensor's or an input.  State starts as zeros
  * (the scale bytes may be zeros too).

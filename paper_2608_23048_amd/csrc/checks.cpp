@@ -2,6 +2,7 @@
 #include "checks.hpp"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -731,6 +732,8 @@ int validate_step(const roi_step_tensor* t, int count, int grad_dtype, int bits,
     if (bits != 8 && bits != 32)
         return fail(ROI_E_INVAL, "the moments' bits must be 8 or 32 (got %d)", bits);
     if (int st = fold_adamw(opt, step)) return st;
+    if (step->eps < FLT_MIN) // whose reciprocal the step multiplies with
+        return fail(ROI_E_INVAL, "AdamW eps must be at least 2^-126");
     if (int st = check_count(t, count)) return st;
     std::vector<Range> ranges;
     ranges.reserve((size_t)count * 6);

@@ -137,6 +137,8 @@ def step_call(L, bits=8, count=1, grad=1, opt=None, other=None, null=False, **kw
     (dict(opt=roi.adamw_params(-1.0)), roi.ROI_E_INVAL),
     (dict(opt=roi.adamw_params(1e-3, t=0)), roi.ROI_E_INVAL),
     (dict(opt=roi.adamw_params(1e-3, eps=0.0)), roi.ROI_E_INVAL),
+    (dict(opt=roi.adamw_params(1e-3, eps=1e-39)), roi.ROI_E_INVAL),
+    (dict(opt=roi.adamw_params(1e-3, eps=1e-39), bits=32), roi.ROI_E_INVAL),
     (dict(opt=roi.adamw_params(1e-3, betas=(1.0, 0.5))), roi.ROI_E_INVAL),
     (dict(numel=-1), roi.ROI_E_INVAL), (dict(numel=1 << 40), roi.ROI_E_UNSUPPORTED),
     (dict(off=2), roi.ROI_E_INVAL), (dict(off=(1 << 64) - 8), roi.ROI_E_INVAL),
@@ -847,6 +849,16 @@ def test_step_past_32_bits():
            tuple(t.view(torch.uint8)[k:].view(t.dtype) for t, k in zip(r, (at, at // 128))))
     check_step8(1030, tail[0], tail[1].bfloat16().float(), tail[2], tail[3], got, opt, 5, 6, offset + at)
     assert not p[:at].any()
+
+
+@pytest.mark.gpu
+def test_smallest_eps():
+    """No gradient and no moments: the update is 0 / eps."""
+    for bits in (8, 32):
+        p = torch.ones(300, device="cuda")
+        roi.adamw_grouped([(p, torch.zeros_like(p), *roi.adamw_moments(p, bits))],
+                          roi.adamw_params(0.5, eps=2.0 ** -126, weight_decay=0.0))
+        assert bool((p == 1).all())
 
 
 @pytest.mark.gpu

@@ -206,6 +206,29 @@ def test_streams_of_every_way_at_once():
         assert torch.equal(y, want[n])
 
 
+def far_apart(q, stride):
+    """q in rows `stride` bytes apart, NaN between them."""
+    room = torch.full((q.shape[0], stride), 0x7F, dtype=torch.uint8, device="cuda")
+    room[:, : q.shape[1]] = q.view(torch.uint8)
+    return room.view(q.dtype)[:, : q.shape[1]]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,rows,cols,x_stride,w_stride,way", [
+    (70000, 33000, 200, 65536, 131072, "256"),     # y past 2^31 values, both operands past 2^32 bytes
+    (5, 1100000, 100, 1 << 22, 4096, "few"),       # the weight past 2^32 bytes
+    (1500, 1600, 256, 1 << 22, 1 << 22, "128"),    # the widest strides
+    (776, 14425, 663, 1 << 22, 1 << 20, "256"),
+])
+def test_products_past_32_bits(tokens, rows, cols, x_stride, w_stride, way):
+    xq, xs, wq, ws = operands(tokens, rows, cols, E4, False, 8)
+    y = roi.linear_f8(far_apart(xq, x_stride), xs, far_apart(wq, w_stride), ws)
+    at = [t for t in (0, 1, 255, 256, 32767, 32768, 65074, 65075, 65076, 65535, 65536, tokens - 2, tokens - 1)
+          if t < tokens]
+    x, w = values(xq, xs, False)[at], values(wq, ws, False).t().contiguous()
+    assert same(y[at], nearest(torch.mm(x, w)))
+
+
 @pytest.mark.gpu
 def test_product_without_a_sum():
     """No columns: the bias, or zeros; more blocks than a launch takes are refused."""
