@@ -395,9 +395,9 @@ int roi_linear_i8_grad_input(const uint16_t* grad_y, const int8_t* wq, const flo
  *
  * Layout
  *  - q: bytes, rows q_stride bytes apart, a multiple of 16 and at least the row;
- *    what lies between a row's end and the next row is left alone.  The products
- *    read whole 16-byte pieces, so that the bytes behind a row's end up to the
- *    piece's are read, and not used.
+ *    what lies between a row's end and the next row is left alone.  Rows are read
+ *    in whole pieces of up to 16 bytes, so that the bytes behind a row's end up
+ *    to the next multiple of 16 are read, and not used.
  *  - scale: bytes E, a row of them for each row (or 128 rows) of the tensor, each
  *    of roi_block_scales(cols) bytes: whole 32-bit words, 127 behind the last
  *    block's.  Aligned to 4 bytes, so that a batch may be cut at any token whose

@@ -114,22 +114,22 @@ struct QuantizeArgs {
     int64_t rows, cols, stride, stride_t;
 };
 
-// Blocks of rows: a wave takes kUnits times 512 consecutive values of a row (four
+// Blocks of rows: a wave takes kOfWave times 512 consecutive values of a row (four
 // blocks, one word of scales), 16 bytes a lane and load.  Its results are read soon
 // (past the caches, 8192 x 18944 and its restoring take 149 us instead of 143.5).
-template <typename T, int kFormat, bool kStream>
+template <typename T, int kFormat, bool kStream, int kOfWave>
 __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, int64_t per_row)
 {
-    constexpr int kUnits = 4, kN = 16 / sizeof(T), kLoads = 512 / (64 * kN);
+    constexpr int kN = 16 / sizeof(T), kLoads = 512 / (64 * kN);
     const int lane = threadIdx.x & 63;
     const int64_t units = a.rows * per_row;
-    for (int64_t u = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * kUnits; u < units;
-         u += (int64_t)gridDim.x * 4 * kUnits) {
-        Held<T, kN> h[kUnits][kLoads];
+    for (int64_t u = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * kOfWave; u < units;
+         u += (int64_t)gridDim.x * 4 * kOfWave) {
+        Held<T, kN> h[kOfWave][kLoads];
         int64_t r = u / per_row, c = u - r * per_row;
         const int64_t r0 = r, c0 = c;
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
+        for (int i = 0; i < kOfWave; ++i) {
             if (u + i < units) {
 #pragma unroll
                 for (int l = 0; l < kLoads; ++l) {
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(256) void quantize_rows_f8_kernel(QuantizeArgs a, i
         r = r0;
         c = c0;
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
+        for (int i = 0; i < kOfWave; ++i) {
             if (u + i < units) {
                 uint32_t word = 0;
 #pragma unroll
@@ -342,14 +342,15 @@ __global__ __launch_bounds__(512) void quantize_tile_f8_kernel(QuantizeArgs a, i
     }
 }
 
-// One wave per 1024 values of a row; a lane's pieces make 16 bytes of x, so that a
-// wave stores 1024 consecutive bytes at a time, past the caches.
-template <typename T, int kFormat>
+// One wave per kPieces times 1024 bytes of a row of x, which it stores 1024 consecutive
+// bytes at a time, past the caches: a lane's piece of q makes 16.  Pieces are read
+// whole, past a row's end too.
+template <typename T, int kFormat, int kPieces>
 __global__ __launch_bounds__(256) void dequantize_f8_kernel(const uint8_t* q, int64_t stride,
                                                             const uint8_t* scale, T* x, int64_t rows,
                                                             int64_t cols, int64_t per_row, int shift)
 {
-    constexpr int kN = 16 / sizeof(T), kPieces = 16 / kN;
+    constexpr int kN = 16 / sizeof(T);
     struct Piece {
         uint32_t w[kN / 4];
     };
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(256) void dequantize_f8_kernel(const uint8_t* q, in
     const int64_t units = rows * per_row, scales = (cols + 511) / 512 * 4;
     for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units;
          u += (int64_t)gridDim.x * 4) {
-        const int64_t r = u / per_row, k0 = (u - r * per_row) * 1024 + lane * kN;
+        const int64_t r = u / per_row, k0 = (u - r * per_row) * (64 * kN * kPieces) + lane * kN;
         const uint8_t* in = q + r * stride;
         const uint8_t* of_row = scale + (r >> shift) * scales;
         Piece v[kPieces];
@@ -365,7 +366,7 @@ __global__ __launch_bounds__(256) void dequantize_f8_kernel(const uint8_t* q, in
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             const int64_t k = k0 + j * 64 * kN;
-            v[j] = k < cols ? load_row<Piece>(in, k, cols) : Piece{};
+            v[j] = k < cols ? load_any<Piece>(in + k) : Piece{};
             s[j] = k < cols ? scale_value(of_row[k / kF8Block]) : 0.0f;
         }
 #pragma unroll
@@ -402,16 +403,25 @@ constexpr int64_t kMostBlocks = 0x7FFFFF; // of up to 512 threads: a launch has 
 // what made it left there, 30 and 26.
 constexpr int64_t kCached = (int64_t)1 << 28;
 
+// A wave of blocks of rows takes one unit where all are on the chip at once (1024 x 3584
+// in bf16: 4.0 us, with two 4.2, with four 4.6; 333 x 896: 2.6, 3.3, 4.6), else two
+// (8192 x 3584: 15.8 us, with one 16.4, with four 16.7), in bf16 from memory four
+// (8192 x 18944: 71.7, with two 74, with one 83; fp32: 120, 117, 119).
 template <typename T, int kFormat, bool kStream>
 void quantize_f8_as(const QuantizeArgs& a, bool square, hipStream_t stream)
 {
     if (!square && !a.qt) {
-        const int64_t per_row = (a.cols + 511) / 512;
-        const int64_t blocks = (a.rows * per_row + 15) / 16;
-        hipLaunchKernelGGL((quantize_rows_f8_kernel<T, kFormat, kStream>),
-                           dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0,
-                           stream, a, per_row);
-        return;
+        const int64_t per_row = (a.cols + 511) / 512, units = a.rows * per_row;
+        auto go = [&](auto kernel, int64_t of_block) {
+            const int64_t blocks = (units + of_block - 1) / of_block;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)),
+                               dim3(256), 0, stream, a, per_row);
+        };
+        constexpr int kMany = kStream && sizeof(T) == 2 ? 4 : 2;
+        if constexpr (!kStream) { // else they are 131072 and more
+            if (units <= kUnits * 32) return go(quantize_rows_f8_kernel<T, kFormat, kStream, 1>, 4);
+        }
+        return go(quantize_rows_f8_kernel<T, kFormat, kStream, kMany>, 4 * kMany);
     }
     const int64_t tiles_c = (a.cols + 127) / 128, tiles = (a.rows + 127) / 128 * tiles_c;
     const dim3 grid((unsigned)(tiles < kMostBlocks ? tiles : kMostBlocks));
@@ -467,19 +477,27 @@ extern "C" int roi_dequantize_blocks(const uint8_t* q, int64_t q_stride, const u
                                         &todo))
         return st;
     if (!todo) return ok();
-    const int64_t per_row = (cols + 1023) / 1024;
-    const int64_t blocks = (rows * per_row + 3) / 4;
-    const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
     const int shift = square ? 7 : 0;
-    auto go = [&](auto kernel, auto* out) {
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, q, q_stride, scale, out, rows, cols,
-                           per_row, shift);
+    auto go = [&](auto* out, auto one, auto more, int pieces) {
+        // a piece a wave where these are few (fp32, 2048 x 3584: 6.1 us, with four 7.4; 16 x
+        // 18944: 2.4, 3.0), else 1024 values (2048 x 18944 in bf16: 18.6 us, with one 19.4)
+        const int64_t of_piece = 1024 / (int64_t)sizeof(*out);
+        const bool few = rows * ((cols + of_piece - 1) / of_piece) <= kUnits * 128;
+        const int64_t of_wave = few ? of_piece : of_piece * pieces;
+        const int64_t per_row = (cols + of_wave - 1) / of_wave, blocks = (rows * per_row + 3) / 4;
+        const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
+        hipLaunchKernelGGL(few ? one : more, grid, dim3(256), 0, stream, q, q_stride, scale, out, rows,
+                           cols, per_row, shift);
     };
+    auto to_bf16 = [&](auto one, auto more) { go(static_cast<uint16_t*>(x), one, more, 2); };
+    auto to_fp32 = [&](auto one, auto more) { go(static_cast<uint32_t*>(x), one, more, 4); };
     if (dtype == ROI_BF16)
-        format == ROI_E4M3 ? go(dequantize_f8_kernel<uint16_t, ROI_E4M3>, static_cast<uint16_t*>(x))
-                           : go(dequantize_f8_kernel<uint16_t, ROI_E5M2>, static_cast<uint16_t*>(x));
+        format == ROI_E4M3
+            ? to_bf16(dequantize_f8_kernel<uint16_t, ROI_E4M3, 1>, dequantize_f8_kernel<uint16_t, ROI_E4M3, 2>)
+            : to_bf16(dequantize_f8_kernel<uint16_t, ROI_E5M2, 1>, dequantize_f8_kernel<uint16_t, ROI_E5M2, 2>);
     else
-        format == ROI_E4M3 ? go(dequantize_f8_kernel<uint32_t, ROI_E4M3>, static_cast<uint32_t*>(x))
-                           : go(dequantize_f8_kernel<uint32_t, ROI_E5M2>, static_cast<uint32_t*>(x));
+        format == ROI_E4M3
+            ? to_fp32(dequantize_f8_kernel<uint32_t, ROI_E4M3, 1>, dequantize_f8_kernel<uint32_t, ROI_E4M3, 4>)
+            : to_fp32(dequantize_f8_kernel<uint32_t, ROI_E5M2, 1>, dequantize_f8_kernel<uint32_t, ROI_E5M2, 4>);
     return launch_status("roi_dequantize_blocks");
 }
