@@ -2,7 +2,7 @@
 //
 // With 8 bits a value moves 16 bytes (param 4 + 4, grad 4, moments 2 x (1 + 1)) and
 // 4 / 128 of scales instead of 28; both forms are bound by HBM (358 million values in
-// 8 bits take 908 us, 6.3 TB/s; 802816 in 32 bits 4.6, 4.9 TB/s).  A half wave holds
+// 8 bits take 955 us, 6.0 TB/s; 802816 in 32 bits 4.5, 5.0 TB/s).  A half wave holds
 // a block of 128 consecutive values, four a lane, so that the block's largest
 // moments take five cross-lane steps and a lane's four noise words one Philox
 // call.  The moments are rounded by the stochastic conversion instruction: as
@@ -21,7 +21,7 @@ namespace {
 
 // A launch takes as many pieces (tensors) as 4 KiB of arguments hold; a piece is given
 // blocks by its units of 512 values, a wave each.
-constexpr int kStepPieces = 63;
+constexpr int kStepPieces = 62;
 constexpr int kUnit = 512, kWavesOfBlock = 4;
 constexpr int64_t kMostStepBlocks = 0xFFFFFE; // of a launch
 struct StepPiece {
@@ -44,6 +44,7 @@ struct StepPiece {
 struct StepBatch {
     StepPiece p[kStepPieces];
     AdamStep adam;
+    double beta1, beta2;
     float beta1_rest, one_m_beta1_rest; // what adam.beta1 and one_m_beta1 lack
     uint32_t k0, k1, step_lo, step_hi;
 };
@@ -120,19 +121,57 @@ __device__ __forceinline__ int round_by(float t, uint32_t word, int old)
     return __builtin_amdgcn_cvt_sr_fp8_f32(t, (int)word, old, kByte);
 }
 
-// m' = beta1 m + (1 - beta1) g to half a rounding: a value's error is what turns its
-// 8-bit neighbours about.  The product's remainder and the sum's, and what the factors
-// lost to fp32, are added last.
+// m' = beta1 m + (1 - beta1) g to a rounding of its own, also where the two cancel: what
+// the products and their sum leave out, and what the factors lost to fp32, is added last.
 __device__ __forceinline__ float mixed(const StepBatch& a, float m, float g)
 {
-    const float p = a.adam.one_m_beta1 * g;
-    const float sum = __builtin_fmaf(a.adam.beta1, m, p);
-    const float rest = __builtin_fmaf(a.adam.beta1, m, p - sum) + __builtin_fmaf(a.adam.one_m_beta1, g, -p);
+    const float p = a.adam.one_m_beta1 * g, q = a.adam.beta1 * m, sum = q + p, of_p = sum - q;
+    const float rest = __builtin_fmaf(a.adam.beta1, m, -q) + __builtin_fmaf(a.adam.one_m_beta1, g, -p) +
+                       ((q - (sum - of_p)) + (p - of_p));
     return sum + __builtin_fmaf(a.beta1_rest, m, __builtin_fmaf(a.one_m_beta1_rest, g, rest));
 }
 
+// Whether fp32 bits of t, with an error of up to 4 of them, and the 20 bits that are
+// added leave the rounding open: the sum's low bits are near 0 (an e4m3 step is 2^20 of
+// t's bits from 2^-6 on, below it 2^-9).
+__device__ __forceinline__ bool undecided(float t, uint32_t chance)
+{
+    const uint32_t low = t < 0x1p-6f ? (uint32_t)(t * 0x1p29f) : __float_as_uint(t);
+    return ((low + chance + 4) & 0xFFFFF) < 8;
+}
+// Whether so near a largest magnitude's fraction is to 3/4 (scale_byte).
+__device__ __forceinline__ bool undecided_scale(uint32_t largest)
+{
+    return ((largest + 0x1FFFFFu + 4) & 0x7FFFFFu) < 8;
+}
+// E of a block (the largest over its 32 lanes) from four magnitudes a lane in 64 bits.
+__device__ __forceinline__ int wide_scale(const double (&x)[4])
+{
+    uint32_t most_e = 1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x[e]);
+        const int of = (int)((b + ((1ull << 50) - 1)) >> 52) - 1023 + 127 - kF8Top<ROI_E4M3>;
+        most_e = most(most_e, (uint32_t)(of > 1 ? of : 1));
+    }
+    return (int)most_of_32(most_e);
+}
+// floor(t / u + chance) u of t = x 2^(127 - scale).
+__device__ __forceinline__ float wide_round(double x, int scale, double chance)
+{
+    const double t = x * __builtin_bit_cast(double, (uint64_t)(1023 + 127 - scale) << 52);
+    const int power = (int)(__builtin_bit_cast(uint64_t, t) >> 52);
+    const int step = (power > 1023 - 6 ? power : 1023 - 6) - 3; // u = 2^(step - 1023)
+    return (float)(__builtin_floor(t * __builtin_bit_cast(double, (uint64_t)(2046 - step) << 52) + chance) *
+                   __builtin_bit_cast(double, (uint64_t)step << 52));
+}
+
+// In 8 bits the stored moments are those of 64-bit arithmetic: a rounding that fp32 leaves
+// open is done again in 64 bits, by one wave in some 200.  Without that 358 million
+// values took 911 us, and some 300 moments came out on the other side.  Its registers
+// leave five waves on a SIMD; four take 1093 us, eight with some in memory 2057.
 template <typename G, int kBits>
-__global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
+__global__ __launch_bounds__(256, kBits == 8 ? 5 : 8) void adamw_kernel(StepBatch a)
 {
     const int i = __builtin_amdgcn_readfirstlane(find_step_piece(a, blockIdx.x));
     const StepPiece p = a.p[i];
@@ -192,7 +231,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
                 float m[4], r[4];
                 from_f8x4<ROI_E4M3>(mq[j], m);
                 from_f8x4<ROI_E4M3>(rq[j], r);
-                const float m_scale = scale_value(ms[j]), r_scale = scale_value(rs[j]);
+                const int old_ms = ms[j], old_rs = rs[j];
+                const float m_scale = scale_value(old_ms), r_scale = scale_value(old_rs);
                 uint32_t m_most = 0, r_most = 0; // what is not finite above every number
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -245,10 +285,44 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepBatch a)
                 ro = round_by<3>(s[3], bits[3], ro);
                 if (!finite) {
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) {
-                    if (!(__builtin_fabsf(m[e]) < __builtin_inff())) mo = (mo & ~(255 << (8 * e))) | 127 << (8 * e);
-                    if (!(r[e] < __builtin_inff())) ro = (ro & ~(255 << (8 * e))) | 127 << (8 * e);
-                  }
+                    for (int e = 0; e < 4; ++e) {
+                        if (!(__builtin_fabsf(m[e]) < __builtin_inff())) mo = (mo & ~(255 << (8 * e))) | 127 << (8 * e);
+                        if (!(r[e] < __builtin_inff())) ro = (ro & ~(255 << (8 * e))) | 127 << (8 * e);
+                    }
+                } else {
+                    bool near = undecided_scale(m_most) || undecided_scale(r_most);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        near |= undecided(__builtin_fabsf(t[e]), bits[e] << 20 >> 12) || undecided(s[e], bits[e] >> 12);
+                    if (__builtin_amdgcn_ballot_w64(near)) {
+                        // one in some 200: again in 64 bits, which decide
+                        double x[4];
+                        float f[4], old[4];
+                        from_f8x4<ROI_E4M3>(mq[j], old);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[e] = __builtin_fabs(a.beta1 * (double)(old[e] * scale_value(old_ms)) +
+                                                  (1.0 - a.beta1) * (double)g[j][e]);
+                        ms[j] = wide_scale(x);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) // of the sign that it has in 32 bits
+                            f[e] = __builtin_copysignf(
+                                wide_round(x[e], ms[j], (double)(bits[e] & 4095) * 0x1p-12), m[e]);
+                        mo = (int)to_f8x4<ROI_E4M3>(f[0], f[1], f[2], f[3]);
+                        from_f8x4<ROI_E4M3>(rq[j], old);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const double root = (double)(old[e] * scale_value(old_rs)), g_e = (double)g[j][e];
+                            x[e] = __builtin_sqrt(a.beta2 * (root * root) + (1.0 - a.beta2) * (g_e * g_e));
+                        }
+                        rs[j] = wide_scale(x);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            f[e] = wide_round(x[e], rs[j], (double)(bits[e] >> 12) * 0x1p-20);
+                            if (r[e] > 0.0f && f[e] < 0x1p-9f) f[e] = 0x1p-9f;
+                        }
+                        ro = (int)to_f8x4<ROI_E4M3>(f[0], f[1], f[2], f[3]);
+                    }
                 }
                 store_four(avg, k0 + 256 * j, n, (uint32_t)mo);
                 store_four(sq, k0 + 256 * j, n, (uint32_t)ro);
@@ -273,6 +347,8 @@ int adamw_run(const roi_step_tensor* t, int count, int grad_dtype, int bits, uin
     const StepFn fn = bits == 8 ? (grad_dtype == ROI_FP32 ? adamw_kernel<float, 8> : adamw_kernel<uint16_t, 8>)
                                 : (grad_dtype == ROI_FP32 ? adamw_kernel<float, 32> : adamw_kernel<uint16_t, 32>);
     b.beta1_rest = (float)(opt->beta1 - (double)b.adam.beta1);
+    b.beta1 = opt->beta1;
+    b.beta2 = opt->beta2;
     b.one_m_beta1_rest = (float)(1.0 - opt->beta1 - (double)b.adam.one_m_beta1);
     b.k0 = (uint32_t)seed;
     b.k1 = (uint32_t)(seed >> 32);

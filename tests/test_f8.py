@@ -801,6 +801,38 @@ def test_moments_are_kept_in_the_mean():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("t,betas", [(100, (0.9, 0.95)), (1, (0.9, 0.999)), (7, (0.0, 0.5))])
+def test_moments_are_those_of_64_bits(t, betas):
+    """Every byte: what fp32 leaves open is decided in 64 bits, by the same operations as
+    here (0.9 m + 0.1 g can lie on a boundary exactly, but for their roundings)."""
+    n = 1 << 21
+    g = torch.Generator(device="cuda").manual_seed(t)
+    normal = lambda: torch.randn(n, generator=g, device="cuda")
+    wide = torch.exp(2 * normal())
+    p, grad = normal(), normal() * wide * 1e-3
+    m = roi.quantize_blocks(normal() * wide * 3e-4)
+    r = roi.quantize_blocks(normal().abs() * wide * 1e-3)
+    power = lambda e: ((e.long() + 1023) << 52).view(torch.float64)
+    held = lambda q, s: q.double() * power(s.view(torch.uint8).long() - 127).repeat_interleave(128)[:n]
+    b1, b2 = betas
+    m1 = b1 * held(*m) + (1 - b1) * grad.double()
+    r1 = (b2 * held(*r) ** 2 + (1 - b2) * grad.double() ** 2).sqrt()
+    word = roi.gumbel_noise(n, 7, 3, 0, want_gumbel=False)[0].long() & 0xFFFFFFFF
+    roi.adamw_grouped([(p, grad, m, r)], roi.adamw_params(1e-3, betas, t=t), seed=7, step=3)
+    for x, chance, (q, s) in ((m1, (word % 4096).double() / 4096, m),
+                              (r1, (word // 4096).double() / 2 ** 20, r)):
+        most = x.abs().view(-1, 128).amax(1).view(torch.int64)
+        e = ((most + 2 ** 50 - 1) >> 52) - 1023 + 127 - 8  # one more where the fraction is over 3/4
+        assert torch.equal(s.view(torch.uint8).long(), e.clamp_min(1))
+        v = x.abs() * power(127 - e.clamp_min(1)).repeat_interleave(128)
+        u = power(((v.view(torch.int64) >> 52) - 1023).clamp_min(-6) - 3)
+        want = torch.floor(v / u + chance) * u
+        if x is r1:
+            want = torch.where(x > 0, want.clamp_min(2.0 ** -9), want)
+        assert torch.equal(q.double(), torch.copysign(want, x))
+
+
+@pytest.mark.gpu
 def test_step_from_zeros_and_what_is_not_finite():
     n = 1000
     g = torch.randn(n, generator=torch.Generator().manual_seed(2)).cuda()
