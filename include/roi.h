@@ -472,8 +472,8 @@ int roi_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_
  * bits 8: m and the root of v, each in e4m3 [numel] with a scale byte for each
  * 128 consecutive values (the format above, a tensor being one row):
  *   m = exp_avg 2^(avg_scale - 127), v = (exp_avg_sq 2^(sq_scale - 127))^2.
- * param's step is taken in fp32.  m' and sqrt(v'), as 64 bits give them, are stored
- * with new scales, rounded
+ * param's step is taken in fp32.  m' and sqrt(v') are stored with new scales as 64
+ * bits give them (as fp32 does where one of 256 neighbours is not finite), rounded
  * up or down with the chance that their distance says, so that they are kept
  * in the mean (rounding to nearest would hold v where a step changes its root by
  * less than half of an e4m3 step, 3 to 6 %).  The chance's bits are those of the
