@@ -1,0 +1,209 @@
+"""The quantizer of blocks and its restoring on each kernel that their calls can take
+(the choice is by sizes alone, blocks_f8.hip) and past 32 bits.  References are plain torch on the GPU, from the definition: the bytes are those
+of the format's nearest value after an exact scaling, and restoring is exact but for
+bf16's subnormals.
+"""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import paper_2608_23048_amd as roi
+
+E4, E5, E8 = torch.float8_e4m3fn, torch.float8_e5m2, torch.float8_e8m0fnu
+TOP = {E4: 8, E5: 15}
+
+
+def blocks(n):
+    return (n + 127) // 128
+
+
+def power(e):
+    """2^e in 64 bits, exactly."""
+    return (e.long() + 1023 << 52).view(torch.float64)
+
+
+def spread(v, rows, cols, square):
+    """The blocks' values at each of their elements."""
+    v = v.repeat_interleave(128, 1)[:, :cols]
+    return v.repeat_interleave(128, 0)[:rows] if square else v
+
+
+def quantized(x, dtype, square):
+    """(q, E [.., blocks of a row]) of x."""
+    rows, cols = x.shape
+    a = x.float().abs()
+    a = torch.nn.functional.pad(torch.where(torch.isfinite(a), a, torch.zeros_like(a)),
+                                (0, -cols % 128, 0, -rows % 128 if square else 0))
+    high = 128 if square else 1
+    most = a.view(a.shape[0] // high, high, blocks(cols), 128).amax(dim=(1, 3))
+    half, exponent = torch.frexp(most.double())  # half in [1/2, 1)
+    e = exponent + 126 + (half * 2 > 1.75).int() - TOP[dtype]
+    e = torch.where(most > 0, e, torch.ones_like(e)).clamp_min(1)
+    return (x.float() * spread(power(127 - e).float(), rows, cols, square)).to(dtype), e
+
+
+def restored(q, e, square, dtype):
+    """e: scale bytes, with 255 a NaN."""
+    r, c = q.shape
+    scale = torch.where(e == 255, torch.full((), float("nan"), dtype=torch.float64, device=e.device),
+                        power(e.long() - 127))
+    return (q.double() * spread(scale, r, c, square)).float().to(dtype)
+
+
+def kept(e, cols):
+    """Scale bytes as they are kept."""
+    room = torch.full((e.shape[0], roi.block_scales(cols)), 127, dtype=torch.uint8, device=e.device)
+    room[:, : e.shape[1]] = e.to(torch.uint8)
+    return room
+
+
+def same_f8(got, want):
+    """Equal bytes, any NaN for a NaN."""
+    nan = torch.isnan(want.float())
+    assert torch.equal(torch.isnan(got.float()), nan)
+    b = [t.contiguous().view(torch.uint8).masked_fill(nan, 0) for t in (got, want)]
+    assert torch.equal(*b)
+
+
+def same_bits(got, want):
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(got), nan)
+    kind = torch.int16 if got.dtype is torch.bfloat16 else torch.int32
+    b = [t.contiguous().view(kind).masked_fill(nan, 0) for t in (got, want)]
+    assert torch.equal(*b)
+
+
+def values(rows, cols, given, seed):
+    """Many magnitudes, rows and blocks of zeros, and what is not finite."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g, device="cuda")
+    x *= torch.exp(4 * torch.randn(rows, 1, generator=g, device="cuda"))
+    x[rows // 2, cols // 2 :] = 0
+    x[0, : cols // 3] = 0
+    for k, v in enumerate((float("nan"), float("inf"), float("-inf"), 2.0 ** -149, 2.0 ** -133, 3.3e38)):
+        x[(rows - 1) * k // 5, (cols - 1) * (5 - k) // 5] = v
+    return x.to(given)
+
+
+# (rows, cols, given): a wave takes one, two or four times 512 values by their number and by
+# whether x is past 256 MB (there also the tiles' loads are others); the number of its
+# shares is odd here, and no row ends with a share
+QUANTIZED = [
+    (333, 1001, torch.bfloat16), (333, 1001, torch.float32),      # one, all at once
+    (1701, 3301, torch.bfloat16), (1701, 3301, torch.float32),    # two
+    (8211, 8203, torch.float32),                                  # two, past 256 MB
+    (11603, 11591, torch.bfloat16),                               # four, past 256 MB
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [E4, E5])
+@pytest.mark.parametrize("rows,cols,given", QUANTIZED)
+def test_quantizer_each_way(rows, cols, given, dtype):
+    x = values(rows, cols, given, rows)
+    for square in (False, True):
+        want, e = quantized(x, dtype, square)
+        q, s = roi.quantize_blocks(x, square=square, dtype=dtype)
+        same_f8(q, want)
+        assert torch.equal(s.view(torch.uint8), kept(e, cols))
+        del q, s
+        q, s, qt, st = roi.quantize_blocks(x, square=square, transposed=True, dtype=dtype)
+        same_f8(q, want)
+        assert torch.equal(s.view(torch.uint8), kept(e, cols))
+        del q, s, want, e
+        want, e = quantized(x.t().contiguous(), dtype, square)
+        same_f8(qt, want)
+        assert torch.equal(st.view(torch.uint8), kept(e, rows))
+        del qt, st, want, e
+
+
+# a wave takes one piece of a row, or 1024 values where the pieces (512 values into bf16,
+# 256 into fp32) are more than 32768
+RESTORED = [(77, 4865), (3001, 6001), (40000, 300), (40, 700001)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("square", [False, True])
+@pytest.mark.parametrize("dtype", [E4, E5])
+@pytest.mark.parametrize("rows,cols", RESTORED)
+def test_restoring_each_way(rows, cols, dtype, square):
+    """Every byte and every scale, NaN between the rows, outputs between marked values."""
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    room = torch.full((rows, (cols + 15) // 16 * 16 + 16), 0x7F, dtype=torch.uint8, device="cuda")
+    room[:, :cols] = torch.randint(0, 256, (rows, cols), generator=g, device="cuda", dtype=torch.uint8)
+    q = room.view(dtype)[:, :cols]
+    e = torch.randint(0, 256, (blocks(rows) if square else rows, blocks(cols)), generator=g, device="cuda")
+    s = kept(e, cols).view(E8)
+    for given in (torch.bfloat16, torch.float32):
+        flat = torch.full((rows * cols + 64,), 9.0, dtype=given, device="cuda")
+        out = flat[32 : 32 + rows * cols].view(rows, cols)
+        assert roi.dequantize_blocks(q, s, out=out) is out
+        same_bits(out, restored(q, e, square, given))
+        assert bool((flat[:32] == 9).all()) and bool((flat[32 + rows * cols :] == 9).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("given", [torch.bfloat16, torch.float32])
+def test_restoring_past_32_bits(given):
+    """2^32 values and more, of which fp32 takes 2^34 bytes: quantized, then all restored."""
+    rows, cols = 66000, 65544
+    x = torch.zeros(rows, cols, dtype=given, device="cuda")
+    at = [0, 1, 32767, 65529, 65536, 65999]
+    some = values(len(at), cols, given, 1)
+    x[at] = some
+    q, s = roi.quantize_blocks(x)
+    want, e = quantized(some, E4, False)
+    same_f8(q.view(torch.uint8)[at].view(E4), want)
+    assert torch.equal(s.view(torch.uint8)[at], kept(e, cols))
+    x.fill_(7)
+    assert roi.dequantize_blocks(q, s, out=x) is x
+    same_bits(x[at], restored(want, e, False, given))
+    x[at] = 0
+    assert not any(bool(part.any()) for part in x.split(6000))
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_launch_has_blocks():
+    """A value a row: blocks take a second turn, in the quantizer and in restoring."""
+    rows = (1 << 28) + 77
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(rows, 1, generator=g, device="cuda", dtype=torch.bfloat16)
+    q, s = roi.quantize_blocks(x, dtype=E5)
+    back = torch.zeros_like(x)
+    roi.dequantize_blocks(q, s, out=back)
+    for first in range(0, rows, 1 << 22):
+        part = slice(first, first + (1 << 22))
+        want, e = quantized(x[part], E5, False)
+        same_f8(q[part], want)
+        assert torch.equal(s.view(torch.uint8)[part], kept(e, 1))
+        same_bits(back[part], restored(want, e, False, torch.bfloat16))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("square", [False, True])
+def test_more_tiles_than_a_launch_has_blocks(square):
+    rows = (1 << 30) + 300
+    x = torch.zeros(rows, 1, dtype=torch.bfloat16, device="cuda")
+    first = [0, 1 << 29, (1 << 30) - 1024]  # whole tiles from here on; the second turn's are last
+    for n, at in enumerate(first):
+        x[at : at + 1324] = values(1, 1324, torch.bfloat16, n).t()
+    q, s, qt, st = roi.quantize_blocks(x, square=square, transposed=True)
+    assert qt.shape == (1, rows)
+    for at in first:
+        part = x[at : at + 1324]
+        want, e = quantized(part, E4, square)
+        same_f8(q[at : at + 1324], want)
+        of = slice(at // 128, at // 128 + blocks(1324)) if square else slice(at, at + 1324)
+        assert torch.equal(s.view(torch.uint8)[of], kept(e, 1))
+        want, e = quantized(part.t().contiguous(), E4, square)
+        same_f8(qt[:, at : at + 1324], want)
+        of = st.view(torch.uint8)[:, at // 128 : at // 128 + blocks(1324)]
+        assert torch.equal(of, e.to(torch.uint8))
+        q[at : at + 1324].view(torch.uint8).zero_()
+        qt[:, at : at + 1324].view(torch.uint8).zero_()
+    for part in qt[0].view(torch.uint8).split(1 << 28):
+        assert not bool(part.any())
+    for part in q.view(torch.uint8).split(1 << 26):
+        assert not bool(part.any())
+    assert bool((st.view(torch.uint8)[:, blocks(rows) :] == 127).all())
