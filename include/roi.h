@@ -427,9 +427,9 @@ int roi_quantize_blocks(const void* x, int dtype, int64_t rows, int64_t cols, in
                         int64_t qt_stride, uint8_t* scale_t, hipStream_t stream);
 /*
  * roi_dequantize_blocks -- x = q 2^(E - 127) in fp32 (exact), rounded to nearest
- * where x is bf16 (exact too, but for subnormals).  Of a block with a value within
- * 1/32 of 2^128 that value is an infinity.  Arguments as above, q and scale read,
- * x written.
+ * where x is bf16 (exact too, but for subnormals).  A value that was within 1/32
+ * (e4m3) or 1/16 (e5m2) of 2^128 is rounded up to it and comes back as an infinity.
+ * Arguments as above, q and scale read, x written.
  */
 int roi_dequantize_blocks(const uint8_t* q, int64_t q_stride, const uint8_t* scale, int64_t rows,
                           int64_t cols, int square, int format, void* x, int dtype,

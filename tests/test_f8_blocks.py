@@ -1,5 +1,6 @@
 """The quantizer of blocks and its restoring on each kernel that their calls can take
-(the choice is by sizes alone, blocks_f8.hip) and past 32 bits.  References are plain torch on the GPU, from the definition: the bytes are those
+(the choice is by sizes alone, blocks_f8.hip), past 32 bits, and at the end of fp32's
+range.  References are plain torch on the GPU, from the definition: the bytes are those
 of the format's nearest value after an exact scaling, and restoring is exact but for
 bf16's subnormals.
 """
@@ -207,3 +208,24 @@ def test_more_tiles_than_a_launch_has_blocks(square):
     for part in q.view(torch.uint8).split(1 << 26):
         assert not bool(part.any())
     assert bool((st.view(torch.uint8)[:, blocks(rows) :] == 127).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("given", [torch.bfloat16, torch.float32])
+def test_restoring_at_the_end_of_the_range(given):
+    """2^128 is an infinity: what a block's last step below it rounds up to it, that is within
+    1/32 of it in e4m3 (a step of 1/16) and within 1/16 in e5m2 (1/8), comes back as one; a
+    tie goes up, whose last bit is even."""
+    for dtype, edge in ((E4, 31.0 / 32), (E5, 15.0 / 16)):
+        below = edge - 2.0 ** (-8 if given is torch.bfloat16 else -24)
+        whole = torch.tensor([edge, below, 0.94, 0.99, 0.9, 0.875], dtype=torch.float64) * 2.0 ** 64
+        x = (whole * 2.0 ** 64).to(given)
+        x = torch.cat([x, -x])[:, None].expand(-1, 128).contiguous().cuda()
+        q, s = roi.quantize_blocks(x, dtype=dtype)
+        back = roi.dequantize_blocks(q, s, dtype=given)
+        past = x.float().abs().double() >= edge * 2.0 ** 128
+        assert torch.equal(torch.isinf(back), past) and past[:, 0].tolist()[:2] == [True, False]
+        step = 2.0 ** (124 if dtype is E4 else 125)
+        want = (torch.round(x.double() / step) * step).to(given)
+        assert torch.equal(back[~past], want[~past])
+        assert torch.equal(torch.sign(back), torch.sign(x))
