@@ -473,11 +473,10 @@ int roi_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_
  * 128 consecutive values (the format above, a tensor being one row):
  *   m = exp_avg 2^(avg_scale - 127), v = (exp_avg_sq 2^(sq_scale - 127))^2.
  * param's step is taken in fp32.  m' and sqrt(v') are stored with new scales as 64
- * bits give them (as fp32 does where one of 256 neighbours is not finite), rounded
- * up or down with the chance that their distance says, so that they are kept
- * in the mean (rounding to nearest would hold v where a step changes its root by
- * less than half of an e4m3 step, 3 to 6 %).  The chance's bits are those of the
- * noise word x of global element e = elem_offset + i (conventions above): with
+ * bits give them, rounded up or down with the chance that their distance says, so
+ * that they are kept in the mean (rounding to nearest would hold v where a step
+ * changes its root by less than half of an e4m3 step, 3 to 6 %).  The chance's bits
+ * are those of the noise word x of global element e = elem_offset + i (conventions above): with
  * t = |value| 2^(127 - E) and u the spacing of e4m3 values at t (2^-9 below
  * 2^-6), the stored value is floor(t / u + b) u, b = (x >> 12) 2^-20 for the
  * root and (x mod 2^12) 2^-12 for m.  A root above 0 is stored as 2^-9 at least:
@@ -494,8 +493,9 @@ int roi_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_
  *  numel      >= 0, below 2^40 (a tensor of none is skipped)
  *  elem_offset % 4 == 0; only bits 8 use it, as they do seed and step
  *  opt        as in roi_mask_bwd_adamw, in 64 bits: each of beta and 1 - beta is
- *             rounded to fp32 once; eps is at least 2^-126, and second moments
- *             below that may be taken for 0.  It is read during the call, as `tensors` are: a
+ *             rounded to fp32 once; eps is at least 2^-126.  Second moments below
+ *             2^-120, and first moments of a block with none above 2^-110, may be
+ *             those of fp32, or 0.  It is read during the call, as `tensors` are: a
  *             captured call replays with the settings, seed and step it was given
  * No output may overlap another tensor's or an input.  State starts as zeros
  * (the scale bytes may be zeros too).

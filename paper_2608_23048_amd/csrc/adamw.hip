@@ -144,6 +144,25 @@ __device__ __forceinline__ bool undecided_scale(uint32_t largest)
 {
     return ((largest + 0x1FFFFFu + 4) & 0x7FFFFFu) < 8;
 }
+// Four elements' new moments (m, r: old values in, new m and root out) and parameters in fp32.
+__device__ __forceinline__ void step_four(const StepBatch& a, float m_scale, float r_scale, f32x4 g,
+                                          f32x4& par, float (&m)[4], float (&r)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float root = r[e] * r_scale;
+        m[e] = mixed(a, m[e] * m_scale, g[e]);
+        const float v = __builtin_fmaf(a.adam.beta2, root * root, a.adam.one_m_beta2 * (g[e] * g[e]));
+        r[e] = __builtin_amdgcn_sqrtf(v);
+        const float den = __builtin_fmaf(r[e], a.adam.inv_sqrt_bc2, a.adam.eps);
+        par[e] = __builtin_fmaf(-a.adam.step_size * m[e], __builtin_amdgcn_rcpf(den), par[e] * a.adam.decay);
+    }
+}
+__device__ __forceinline__ uint4 words_of_four(const StepBatch& a, uint64_t element)
+{
+    const uint64_t block = element >> 2;
+    return philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), a.step_lo, a.step_hi, a.k0, a.k1);
+}
 // E of a block (the largest over its 32 lanes) from four magnitudes a lane in 64 bits.
 __device__ __forceinline__ int wide_scale(const double (&x)[4])
 {
@@ -166,10 +185,100 @@ __device__ __forceinline__ float wide_round(double x, int scale, double chance)
                    __builtin_bit_cast(double, (uint64_t)step << 52));
 }
 
+// The moments of four elements, m and r in 32 bits, again in 64, which decide: their bytes
+// and their blocks' scales.  kFinite: in 32 bits all of the wave's are finite.  Squares of
+// what fp32 holds are finite in 64 bits; what is not finite there is stored as NaN.
+template <bool kFinite>
+__device__ __forceinline__ void moments_again(const StepBatch& a, uint32_t mq, uint32_t rq, int old_ms,
+                                              int old_rs, f32x4 g, const float (&m)[4],
+                                              const float (&r)[4], const uint32_t (&bits)[4], int& mo,
+                                              int& ro, int& ms, int& rs)
+{
+    auto value = [](float q, int scale) { return (double)(q * scale_value(scale)); };
+    // takes what is not finite out of x; NaN bytes in its places
+    auto take_out = [](double(&x)[4]) {
+        int nan = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (!kFinite && !(x[e] < __builtin_inf())) {
+                x[e] = 0.0;
+                nan |= 127 << (8 * e);
+            }
+        return nan;
+    };
+    double x[4];
+    float f[4], old[4], sign[4];
+    from_f8x4<ROI_E4M3>(mq, old);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = a.beta1 * value(old[e], old_ms) + (1.0 - a.beta1) * (double)g[e];
+        // of the sign that it has in 32 bits, if it has a value there
+        if (kFinite || __builtin_fabsf(m[e]) < __builtin_inff())
+            sign[e] = m[e];
+        else
+            sign[e] = __builtin_fabs(x[e]) < __builtin_inf() ? (float)x[e] : 0.0f;
+        x[e] = __builtin_fabs(x[e]);
+    }
+    int nan = take_out(x);
+    ms = wide_scale(x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        f[e] = __builtin_copysignf(wide_round(x[e], ms, (double)(bits[e] & 4095) * 0x1p-12), sign[e]);
+    mo = (int)to_f8x4<ROI_E4M3>(f[0], f[1], f[2], f[3]) | nan;
+    from_f8x4<ROI_E4M3>(rq, old);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const double root = value(old[e], old_rs), g_e = (double)g[e];
+        x[e] = __builtin_sqrt(a.beta2 * (root * root) + (1.0 - a.beta2) * (g_e * g_e));
+    }
+    nan = take_out(x);
+    rs = wide_scale(x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[e] = wide_round(x[e], rs, (double)(bits[e] >> 12) * 0x1p-20);
+        const bool above = kFinite || r[e] < __builtin_inff() ? r[e] > 0.0f : x[e] > 0.0;
+        if (above && f[e] < 0x1p-9f) f[e] = 0x1p-9f;
+    }
+    ro = (int)to_f8x4<ROI_E4M3>(f[0], f[1], f[2], f[3]) | nan;
+}
+
+// Values k .. k + 3 of a lane whose wave has some that are not finite in fp32, from memory:
+// what is finite in 64 bits is stored as any other value, whatever its neighbours are.
+template <typename G>
+__device__ __forceinline__ void step_not_finite(const StepBatch& a, const StepPiece& p, int64_t k,
+                                                int64_t n, int64_t block, bool live)
+{
+    uint8_t* avg = static_cast<uint8_t*>(p.avg);
+    uint8_t* sq = static_cast<uint8_t*>(p.sq);
+    const f32x4 g = load_four(static_cast<const G*>(p.grad), k, n);
+    f32x4 par = load_four(p.param, k, n);
+    const uint32_t mq = load_four(avg, k, n), rq = load_four(sq, k, n);
+    int ms = live ? p.avg_scale[block] : 1, rs = live ? p.sq_scale[block] : 1;
+    const float m_scale = scale_value(ms), r_scale = scale_value(rs);
+    float m[4], r[4];
+    from_f8x4<ROI_E4M3>(mq, m);
+    from_f8x4<ROI_E4M3>(rq, r);
+    step_four(a, m_scale, r_scale, g, par, m, r);
+    store_four(p.param, k, n, par);
+    const uint4 word = words_of_four(a, p.offset + (uint64_t)k);
+    const uint32_t bits[4] = {word.x, word.y, word.z, word.w};
+    int mo, ro;
+    moments_again<false>(a, mq, rq, ms, rs, g, m, r, bits, mo, ro, ms, rs);
+    store_four(avg, k, n, (uint32_t)mo);
+    store_four(sq, k, n, (uint32_t)ro);
+    if ((threadIdx.x & 31) == 0 && live) {
+        p.avg_scale[block] = (uint8_t)ms;
+        p.sq_scale[block] = (uint8_t)rs;
+    }
+}
+
 // In 8 bits the stored moments are those of 64-bit arithmetic: a rounding that fp32 leaves
-// open is done again in 64 bits, by one wave in some 200.  Without that 358 million
-// values took 911 us, and some 300 moments came out on the other side.  Its registers
-// leave five waves on a SIMD; four take 1093 us, eight with some in memory 2057.
+// open is done again in 64 bits, by one wave in some 200 (of moments that are 0, one in 16:
+// every 4096th has chance 0).  Without that 358 million values took 911 us, and some 300
+// moments came out on the other side.  What is not finite waits until the others of a
+// turn are stored: beside them it took registers and scalar registers (985 to 1019 us, so
+// 962).  Five waves fit on a SIMD; four take 1093 us, six 1112, eight with some
+// registers in memory 2057.
 template <typename G, int kBits>
 __global__ __launch_bounds__(256, kBits == 8 ? 5 : 8) void adamw_kernel(StepBatch a)
 {
@@ -218,6 +327,7 @@ __global__ __launch_bounds__(256, kBits == 8 ? 5 : 8) void adamw_kernel(StepBatc
             int ms[2], rs[2];
             const int64_t block0 = u * 4 + lane / 32; // of 128 values
             const int64_t held = (n + kF8Block - 1) / kF8Block;
+            int later = 0;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 mq[j] = load_four(avg, k0 + 256 * j, n);
@@ -233,40 +343,25 @@ __global__ __launch_bounds__(256, kBits == 8 ? 5 : 8) void adamw_kernel(StepBatc
                 from_f8x4<ROI_E4M3>(rq[j], r);
                 const int old_ms = ms[j], old_rs = rs[j];
                 const float m_scale = scale_value(old_ms), r_scale = scale_value(old_rs);
+                step_four(a, m_scale, r_scale, g[j], par[j], m, r);
                 uint32_t m_most = 0, r_most = 0; // what is not finite above every number
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float root = r[e] * r_scale;
-                    m[e] = mixed(a, m[e] * m_scale, g[j][e]);
-                    const float v = __builtin_fmaf(a.adam.beta2, root * root,
-                                                   a.adam.one_m_beta2 * (g[j][e] * g[j][e]));
-                    r[e] = __builtin_amdgcn_sqrtf(v);
-                    const float den = __builtin_fmaf(r[e], a.adam.inv_sqrt_bc2, a.adam.eps);
-                    par[j][e] = __builtin_fmaf(-a.adam.step_size * m[e], __builtin_amdgcn_rcpf(den),
-                                               par[j][e] * a.adam.decay);
                     m_most = most(m_most, __float_as_uint(m[e]) & 0x7FFFFFFFu);
                     r_most = most(r_most, __float_as_uint(r[e]));
+                }
+                const bool finite = __builtin_amdgcn_ballot_w64(most(m_most, r_most) >= kInfinity) == 0;
+                if (__builtin_expect(!finite, 0)) {
+                    later |= 1 << j;
+                    continue;
                 }
                 store_four(p.param, k0 + 256 * j, n, par[j]);
                 m_most = most_of_32(m_most);
                 r_most = most_of_32(r_most);
-                const bool finite = __builtin_amdgcn_ballot_w64(most(m_most, r_most) >= kInfinity) == 0;
-                if (!finite) {
-                    m_most = r_most = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        m_most = most(m_most, finite_bits(m[e]));
-                        r_most = most(r_most, finite_bits(r[e]));
-                    }
-                    m_most = most_of_32(m_most);
-                    r_most = most_of_32(r_most);
-                }
                 ms[j] = scale_byte<ROI_E4M3>(m_most);
                 rs[j] = scale_byte<ROI_E4M3>(r_most);
                 const float m_inv = inverse_scale(ms[j]), r_inv = inverse_scale(rs[j]);
-                const uint64_t block = (p.offset + (uint64_t)(k0 + 256 * j)) >> 2;
-                const uint4 word = philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), a.step_lo,
-                                                 a.step_hi, a.k0, a.k1);
+                const uint4 word = words_of_four(a, p.offset + (uint64_t)(k0 + 256 * j));
                 const uint32_t bits[4] = {word.x, word.y, word.z, word.w};
                 float t[4], s[4];
 #pragma unroll
@@ -283,53 +378,24 @@ __global__ __launch_bounds__(256, kBits == 8 ? 5 : 8) void adamw_kernel(StepBatc
                 ro = round_by<1>(s[1], bits[1], ro);
                 ro = round_by<2>(s[2], bits[2], ro);
                 ro = round_by<3>(s[3], bits[3], ro);
-                if (!finite) {
+                bool near = undecided_scale(m_most) || undecided_scale(r_most);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (!(__builtin_fabsf(m[e]) < __builtin_inff())) mo = (mo & ~(255 << (8 * e))) | 127 << (8 * e);
-                        if (!(r[e] < __builtin_inff())) ro = (ro & ~(255 << (8 * e))) | 127 << (8 * e);
-                    }
-                } else {
-                    bool near = undecided_scale(m_most) || undecided_scale(r_most);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        near |= undecided(__builtin_fabsf(t[e]), bits[e] << 20 >> 12) || undecided(s[e], bits[e] >> 12);
-                    if (__builtin_amdgcn_ballot_w64(near)) {
-                        // one in some 200: again in 64 bits, which decide
-                        double x[4];
-                        float f[4], old[4];
-                        from_f8x4<ROI_E4M3>(mq[j], old);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[e] = __builtin_fabs(a.beta1 * (double)(old[e] * scale_value(old_ms)) +
-                                                  (1.0 - a.beta1) * (double)g[j][e]);
-                        ms[j] = wide_scale(x);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) // of the sign that it has in 32 bits
-                            f[e] = __builtin_copysignf(
-                                wide_round(x[e], ms[j], (double)(bits[e] & 4095) * 0x1p-12), m[e]);
-                        mo = (int)to_f8x4<ROI_E4M3>(f[0], f[1], f[2], f[3]);
-                        from_f8x4<ROI_E4M3>(rq[j], old);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const double root = (double)(old[e] * scale_value(old_rs)), g_e = (double)g[j][e];
-                            x[e] = __builtin_sqrt(a.beta2 * (root * root) + (1.0 - a.beta2) * (g_e * g_e));
-                        }
-                        rs[j] = wide_scale(x);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            f[e] = wide_round(x[e], rs[j], (double)(bits[e] >> 12) * 0x1p-20);
-                            if (r[e] > 0.0f && f[e] < 0x1p-9f) f[e] = 0x1p-9f;
-                        }
-                        ro = (int)to_f8x4<ROI_E4M3>(f[0], f[1], f[2], f[3]);
-                    }
-                }
+                for (int e = 0; e < 4; ++e)
+                    near |= undecided(__builtin_fabsf(t[e]), bits[e] << 20 >> 12) || undecided(s[e], bits[e] >> 12);
+                if (__builtin_amdgcn_ballot_w64(near)) // one in some 200
+                    moments_again<true>(a, mq[j], rq[j], old_ms, old_rs, g[j], m, r, bits, mo, ro, ms[j], rs[j]);
                 store_four(avg, k0 + 256 * j, n, (uint32_t)mo);
                 store_four(sq, k0 + 256 * j, n, (uint32_t)ro);
                 if (lane % 32 == 0 && block0 + 2 * j < held) {
                     p.avg_scale[block0 + 2 * j] = (uint8_t)ms[j];
                     p.sq_scale[block0 + 2 * j] = (uint8_t)rs[j];
                 }
+            }
+            if (__builtin_expect(later, 0)) {
+#pragma unroll 1
+                for (int j = 0; j < 2; ++j)
+                    if (later >> j & 1)
+                        step_not_finite<G>(a, p, k0 + 256 * j, n, block0 + 2 * j, block0 + 2 * j < held);
             }
         }
     }
