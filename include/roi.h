@@ -468,16 +468,18 @@ int roi_linear_f8(const uint8_t* xq, int64_t x_stride, const uint8_t* xs, int x_
  * gradient does not come from one call of the item sampler's backward (summed
  * over micro-batches, the categorical sampler's) and for other parameters.
  *
- * bits 32: exp_avg = m and exp_avg_sq = v, fp32 [numel].
+ * bits 32: exp_avg = m and exp_avg_sq = v, fp32 [numel]; v' past fp32's largest
+ * number, as |grad| above 2^64 makes it, is an infinity.
  * bits 8: m and the root of v, each in e4m3 [numel] with a scale byte for each
- * 128 consecutive values (the format above, a tensor being one row):
+ * 128 consecutive values (the format above, a tensor being one row), for all finite
+ * gradients:
  *   m = exp_avg 2^(avg_scale - 127), v = (exp_avg_sq 2^(sq_scale - 127))^2.
  * param's step is taken in fp32.  m' and sqrt(v') are stored with new scales as 64
  * bits give them, rounded up or down with the chance that their distance says, so
  * that they are kept in the mean (rounding to nearest would hold v where a step
  * changes its root by less than half of an e4m3 step, 3 to 6 %).  The chance's bits
- * are those of the noise word x of global element e = elem_offset + i (conventions above): with
- * t = |value| 2^(127 - E) and u the spacing of e4m3 values at t (2^-9 below
+ * are those of the noise word x of global element e = elem_offset + i (conventions
+ * above): with t = |value| 2^(127 - E) and u the spacing of e4m3 values at t (2^-9 below
  * 2^-6), the stored value is floor(t / u + b) u, b = (x >> 12) 2^-20 for the
  * root and (x mod 2^12) 2^-12 for m.  A root above 0 is stored as 2^-9 at least:
  * m is not divided by eps alone.  A NaN or an infinity is stored as NaN and

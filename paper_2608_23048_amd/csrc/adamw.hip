@@ -187,14 +187,17 @@ __device__ __forceinline__ float wide_round(double x, int scale, double chance)
 
 // The moments of four elements, m and r in 32 bits, again in 64, which decide: their bytes
 // and their blocks' scales.  kFinite: in 32 bits all of the wave's are finite.  Squares of
-// what fp32 holds are finite in 64 bits; what is not finite there is stored as NaN.
+// what fp32 holds are finite in 64 bits, and so is an old moment that is held as 2^128 (a
+// largest one may be rounded up to it); what is not finite there is stored as NaN.
 template <bool kFinite>
 __device__ __forceinline__ void moments_again(const StepBatch& a, uint32_t mq, uint32_t rq, int old_ms,
                                               int old_rs, f32x4 g, const float (&m)[4],
                                               const float (&r)[4], const uint32_t (&bits)[4], int& mo,
                                               int& ro, int& ms, int& rs)
 {
-    auto value = [](float q, int scale) { return (double)(q * scale_value(scale)); };
+    auto value = [](float q, int scale) {
+        return kFinite ? (double)(q * scale_value(scale)) : (double)q * (double)scale_value(scale);
+    };
     // takes what is not finite out of x; NaN bytes in its places
     auto take_out = [](double(&x)[4]) {
         int nan = 0;
@@ -244,21 +247,39 @@ __device__ __forceinline__ void moments_again(const StepBatch& a, uint32_t mq, u
 
 // Values k .. k + 3 of a lane whose wave has some that are not finite in fp32, from memory:
 // what is finite in 64 bits is stored as any other value, whatever its neighbours are.
+// Where g or the old root passes 2^64 its square is an infinity, and where an old moment is
+// held as 2^128 that is: the parameter's step is taken on 2^-75 of them.
 template <typename G>
 __device__ __forceinline__ void step_not_finite(const StepBatch& a, const StepPiece& p, int64_t k,
                                                 int64_t n, int64_t block, bool live)
 {
     uint8_t* avg = static_cast<uint8_t*>(p.avg);
     uint8_t* sq = static_cast<uint8_t*>(p.sq);
-    const f32x4 g = load_four(static_cast<const G*>(p.grad), k, n);
-    f32x4 par = load_four(p.param, k, n);
+    const f32x4 g = load_four(static_cast<const G*>(p.grad), k, n), was = load_four(p.param, k, n);
     const uint32_t mq = load_four(avg, k, n), rq = load_four(sq, k, n);
     int ms = live ? p.avg_scale[block] : 1, rs = live ? p.sq_scale[block] : 1;
     const float m_scale = scale_value(ms), r_scale = scale_value(rs);
-    float m[4], r[4];
-    from_f8x4<ROI_E4M3>(mq, m);
-    from_f8x4<ROI_E4M3>(rq, r);
+    float m[4], r[4], old_m[4], old_r[4];
+    from_f8x4<ROI_E4M3>(mq, old_m);
+    from_f8x4<ROI_E4M3>(rq, old_r);
+    f32x4 par = was;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        m[e] = old_m[e];
+        r[e] = old_r[e];
+    }
     step_four(a, m_scale, r_scale, g, par, m, r);
+    constexpr float kBy = 0x1p-75f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (__builtin_fabsf(m[e]) < __builtin_inff() && r[e] < __builtin_inff()) continue;
+        const float ge = g[e] * kBy, root = old_r[e] * (r_scale * kBy);
+        const float v = __builtin_fmaf(a.adam.beta2, root * root, a.adam.one_m_beta2 * (ge * ge));
+        const float re = r[e] < __builtin_inff() ? r[e] * kBy : __builtin_amdgcn_sqrtf(v);
+        const float me = __builtin_fmaf(a.adam.beta1, old_m[e] * (m_scale * kBy), a.adam.one_m_beta1 * ge);
+        const float den = __builtin_fmaf(re, a.adam.inv_sqrt_bc2, a.adam.eps * kBy);
+        par[e] = __builtin_fmaf(-a.adam.step_size * me, __builtin_amdgcn_rcpf(den), was[e] * a.adam.decay);
+    }
     store_four(p.param, k, n, par);
     const uint4 word = words_of_four(a, p.offset + (uint64_t)k);
     const uint32_t bits[4] = {word.x, word.y, word.z, word.w};

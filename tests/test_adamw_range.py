@@ -1,8 +1,9 @@
-"""adamw_grouped in 8 bits with elements that are not finite among others.
+"""adamw_grouped in 8 bits over the whole of fp32's range: gradients whose squares fp32 does
+not hold, moments next to 2^128, and elements that are not finite among others.
 
 The stored moments are compared byte for byte with 64-bit arithmetic: m' and sqrt(v') as
 products and sums of doubles, then floor(t / u + chance) u with the chance of the
-element's noise word.
+element's noise word.  The parameter's tolerance is test_f8's, of a step in fp32.
 """
 from __future__ import annotations
 
@@ -10,6 +11,7 @@ import pytest
 import torch
 
 import paper_2608_23048_amd as roi
+from tests.test_f8 import step_ref
 
 SEED, STEP = 7, 3
 
@@ -67,6 +69,52 @@ def state(n, seed, size=1e-3):
     wide = torch.exp(2 * normal())
     return (normal(), normal() * wide * size, roi.quantize_blocks(normal() * wide * 0.3 * size),
             roi.quantize_blocks(normal().abs() * wide * size))
+
+
+def check(p, grad, m, r, opt, betas):
+    """One step in place; the parameter and both moments are right."""
+    want = stepped(grad.float(), m, r, betas)
+    h = [held(*m).cpu(), held(*r).cpu()]
+    p1, _, _, ep, _ = step_ref(p.double().cpu(), grad.double().cpu(), h[0], h[1] * h[1], opt)
+    roi.adamw_grouped([(p, grad, m, r)], opt, seed=SEED, step=STEP)
+    same_moments((m, r), want)
+    ok = torch.isfinite(p1)
+    assert bool(((p.double().cpu() - p1).abs() <= ep)[ok].all())
+    assert not torch.isfinite(p.cpu()[~ok]).any()
+
+
+HUGE = [1e20, -3e38, 1.9e19, 5e19, 1.8e19, -1.85e19, 3.4e38, 2.0 ** 64, -2.0 ** 127]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("betas", [(0.9, 0.95), (0.0, 0.0), (0.9, 0.999)])
+def test_gradients_whose_squares_pass_fp32(betas, dtype):
+    n = 128 * 41 + 77
+    p, grad, m, r = state(n, 5)
+    for i, v in enumerate(HUGE):  # some alone in their 256 elements, some together
+        grad[i * 397 + i] = v
+        grad[3840 + 7 * i] = -v
+    grad = grad.clamp(-3.38e38, 3.38e38).to(dtype)
+    for t in range(1, 4):
+        check(p, grad, m, r, roi.adamw_params(1e-3, betas, t=t), betas)
+        assert bool(torch.isfinite(p).all())
+        grad = grad * 0 if t == 1 else torch.randn_like(p).to(dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("betas", [(0.9, 0.95), (0.5, 0.0), (0.0, 0.999)])
+def test_moments_next_to_2_128(betas):
+    """Both moments of some elements are held as 2^128, which fp32 has not."""
+    n = 1000
+    p, grad, m, r = state(n, 6, 1e33)
+    top = torch.zeros(n, device="cuda")
+    top[::51] = 3.4e38
+    m, r = roi.quantize_blocks(top), roi.quantize_blocks(top)
+    assert float(held(*m).max()) == float(held(*r).max()) == 2.0 ** 128
+    for t in range(1, 4):
+        check(p, grad, m, r, roi.adamw_params(1e-3, betas, t=t), betas)
+        assert bool(torch.isfinite(p).all())
 
 
 @pytest.mark.gpu
