@@ -980,7 +980,8 @@ def adamw_grouped(tensors, opt: AdamWParams, seed: int = 0, step: int = 0, offse
     (adamw_moments; about half the memory traffic and a quarter of the memory).  The
     8-bit moments are rounded by the noise of (seed, step, offsets[i] + element):
     use a seed of its own and the step's number; offsets are multiples of 4 and
-    default to the running sum of the sizes, each rounded up to one."""
+    default to the running sum of the sizes, each rounded up to one.  A list is checked
+    in every call, some 3 us a tensor on the host."""
     if opt is None:
         raise ValueError("opt (AdamWParams) is required")
     plan = tensors

@@ -2,7 +2,7 @@
 //
 // With 8 bits a value moves 16 bytes (param 4 + 4, grad 4, moments 2 x (1 + 1)) and
 // 4 / 128 of scales instead of 28; both forms are bound by HBM (358 million values in
-// 8 bits take 955 us, 6.0 TB/s; 802816 in 32 bits 4.5, 5.0 TB/s).  A half wave holds
+// 8 bits take 962 us, 6.0 TB/s; 802816 in 32 bits 4.5, 5.0 TB/s).  A half wave holds
 // a block of 128 consecutive values, four a lane, so that the block's largest
 // moments take five cross-lane steps and a lane's four noise words one Philox
 // call.  The moments are rounded by the stochastic conversion instruction: as

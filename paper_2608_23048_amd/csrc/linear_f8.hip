@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256) void linear_f8_few_kernel(LinearF8Args a)
 // LDS is read half as much again (the product below: 529 us, with four waves 491, and
 // without a pause between tiles 437).  128-tiles share a compute unit two by two, or have
 // eight waves and four buffers where each has one to itself.  8192 tokens through
-// 18944 x 3584 take 424 to 449 us, as the clock has it (2.5 to 2.6 PFLOP/s; the matrix
+// 18944 x 3584 take 424 to 462 us, as the clock has it (2.4 to 2.6 PFLOP/s; the matrix
 // cores are busy for 65 % of the time at 2.05 GHz): bound by their issue and their power.
 
 // Rows of an operand that a thread brings to LDS, where place j ^ (row & 7) of a row
